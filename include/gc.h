@@ -20,6 +20,8 @@
  *   gc_kv_restore_q8        in the cache tier
  *   gc_kv_append            new tokens' K,V -> pool slots after each
  *                           request's cached prefix                (stitch)
+ *   gc_kv_append_rope       the same with the position rotation of q and k
+ *                           on the way
  *   gc_prefix_prefill_attn  causal GQA attention of the new tokens over
  *                           the pool through a block table         (prefill)
  *   gc_paged_decode_attn    the same for one new token per request,
@@ -316,6 +318,53 @@ GC_API gc_status gc_kv_append(gc_kv_pool* pool, const void* k_new, const void* v
                        const int32_t* block_table, const int32_t* seq_lens, cudaStream_t stream,
                        int32_t layer, const int32_t* cu_new_lens, int32_t batch,
                        int32_t max_blocks_per_seq, int32_t total_new_tokens);
+
+/* gc_kv_append_rope flag */
+#define GC_ROPE_INTERLEAVED 1u /* pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
+
+/* gc_kv_append with the position rotation of q and k on the way: what a
+ * layer's projections give goes into the cache and to the attention calls in
+ * one pass (Sec. 2.2: the new tokens' KV is stitched after the cached one;
+ * cached keys are kept rotated, so a hit reuses them as they are).  New token
+ * t < n_b of request b has the slot s = seq_lens[b] + t, the position
+ * p = positions ? positions[cu_new_lens[b]+t] : s, and for every head and
+ * i < rot_dim/2, with (x, y) the head's columns (i, i + rot_dim/2), or
+ * (2i, 2i+1) with GC_ROPE_INTERLEAVED,
+ *     x' = x cos_sin[p][0][i] - y cos_sin[p][1][i]
+ *     y' = y cos_sin[p][0][i] + x cos_sin[p][1][i]
+ * in binary32, rounded once to bf16; columns from rot_dim on are copied.
+ *     q_out[cu_new_lens[b]+t][h]  <- q' (every q head)
+ *     pool[layer][0][slot s of request b][g] <- k',  [1] <- v as it is
+ *   q, k_new, v_new  bf16, device: [T_new] tokens of Hq (k, v: Hkv) heads of d
+ *              columns, dense within a token; q_stride, k_stride, v_stride
+ *              elements from one token to the next (multiples of 8), so that
+ *              the three may be parts of one projection's rows.
+ *   num_q_heads Hq, a multiple of Hkv, or 0: only k and v are written (q and
+ *              q_out are not looked at).
+ *   q_out      [T_new][Hq][d] bf16, dense; q itself if q is dense.  Other
+ *              overlaps of outputs with inputs are not supported.
+ *   cos_sin    binary32, device: [n_positions][2][rot_dim/2], cosines then
+ *              sines of each position's angles (any scaling of the
+ *              frequencies is in the table).
+ *   rot_dim    rotated columns of a head: a multiple of 16, 16 to d.
+ *   positions  int32 [T_new], device, or NULL.  Given, a token's position
+ *              need not be its slot: tokens behind a shared prefix, whose own
+ *              pages begin at slot 0 (gc_shared_prefix_decode_attn).
+ *   block_table, seq_lens, cu_new_lens, total_new_tokens  as gc_kv_append.
+ * A token without a request, or whose position is outside [0, n_positions),
+ * is skipped; one whose page is outside its block table or the pool has its
+ * q written and its K and V skipped; both are recorded as
+ * GC_ERR_OUT_OF_RANGE.
+ * Errors: GC_ERR_INVALID_ARG, GC_ERR_OUT_OF_RANGE (layer),
+ * GC_ERR_UNSUPPORTED ((Hq + 2 Hkv) * d >= 2^30), GC_ERR_CUDA. */
+GC_API gc_status gc_kv_append_rope(gc_kv_pool* pool, const void* q, int64_t q_stride, void* q_out,
+                                   const void* k_new, int64_t k_stride, const void* v_new,
+                                   int64_t v_stride, const int32_t* block_table,
+                                   const int32_t* seq_lens, cudaStream_t stream, int32_t layer,
+                                   const int32_t* cu_new_lens, int32_t batch,
+                                   int32_t max_blocks_per_seq, int32_t total_new_tokens,
+                                   int32_t num_q_heads, const float* cos_sin, int32_t n_positions,
+                                   int32_t rot_dim, const int32_t* positions, uint32_t flags);
 
 /* Prefill of the new tokens over [cached prefix ++ new tokens] (Sec. 2.2:
  * the cached and new tokens' KV are processed together; Sec. 2.1: prefill).

@@ -33,13 +33,14 @@ GC_SAVE_VECTOR = 2
 GC_RESTORE_LAYER_MAJOR = 4
 GC_SAVE_LAYER_MAJOR = 4
 GC_STAGE_Q8 = 8
+GC_ROPE_INTERLEAVED = 1
 
 EXPORTED = (
     "gc_kv_pool_bytes", "gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
     "gc_kv_pool_check", "gc_kv_restore", "gc_kv_save", "gc_kv_restore_layers",
     "gc_kv_save_layers", "gc_kv_stage_layers", "gc_kv_q8_chunk_bytes", "gc_kv_save_q8",
     "gc_kv_restore_q8",
-    "gc_kv_append", "gc_prefix_prefill_attn",
+    "gc_kv_append", "gc_kv_append_rope", "gc_prefix_prefill_attn",
     "gc_prefix_prefill_attn_simt", "gc_prefix_prefill_attn_noalloc",
     "gc_prefix_prefill_attn_q8", "gc_paged_decode_attn_q8",
     "gc_paged_decode_workspace_bytes", "gc_paged_decode_attn", "gc_selftest_wait_timeout",
@@ -92,6 +93,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.gc_kv_save_q8.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, u32]
         lib.gc_kv_restore_q8.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, u32]
         lib.gc_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32]
+        i64 = ctypes.c_int64
+        lib.gc_kv_append_rope.argtypes = [vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, i32, vp,
+                                          i32, i32, i32, i32, vp, i32, i32, vp, u32]
         attn = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, ctypes.c_float, i32]
         lib.gc_prefix_prefill_attn.argtypes = attn
         lib.gc_prefix_prefill_attn_simt.argtypes = attn
@@ -108,7 +112,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         for f in ("gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
                   "gc_kv_pool_check", "gc_kv_restore", "gc_kv_save", "gc_kv_restore_layers",
                   "gc_kv_save_layers", "gc_kv_stage_layers", "gc_kv_save_q8", "gc_kv_restore_q8",
-                  "gc_kv_append",
+                  "gc_kv_append", "gc_kv_append_rope",
                   "gc_prefix_prefill_attn", "gc_prefix_prefill_attn_simt",
                   "gc_prefix_prefill_attn_noalloc", "gc_prefix_prefill_attn_q8",
                   "gc_paged_decode_attn", "gc_paged_decode_attn_q8"):
@@ -247,6 +251,20 @@ def gc_kv_append(pool, k_new, v_new, block_table, seq_lens, stream, layer: int, 
     _check(load().gc_kv_append(pool, _addr(k_new), _addr(v_new), _addr(block_table),
                                _addr(seq_lens), _stream(stream), layer, _addr(cu_new_lens), batch,
                                max_blocks_per_seq, total_new_tokens), "gc_kv_append")
+
+
+def gc_kv_append_rope(pool, q, q_stride: int, q_out, k_new, k_stride: int, v_new, v_stride: int,
+                      block_table, seq_lens, stream, layer: int, cu_new_lens, batch: int,
+                      max_blocks_per_seq: int, total_new_tokens: int, num_q_heads: int, cos_sin,
+                      n_positions: int, rot_dim: int, positions=None, flags: int = 0) -> None:
+    """gc_kv_append with the position rotation of q and k on the way; strides
+    are elements between tokens, positions None: they are the slots."""
+    _check(load().gc_kv_append_rope(pool, _addr(q), q_stride, _addr(q_out), _addr(k_new), k_stride,
+                                    _addr(v_new), v_stride, _addr(block_table), _addr(seq_lens),
+                                    _stream(stream), layer, _addr(cu_new_lens), batch,
+                                    max_blocks_per_seq, total_new_tokens, num_q_heads,
+                                    _addr(cos_sin), n_positions, rot_dim, _addr(positions), flags),
+           "gc_kv_append_rope")
 
 
 def gc_prefix_prefill_attn(q, pool, block_table, prefix_lens, new_lens, out, stream, layer: int,

@@ -516,6 +516,61 @@ gc_status gc_kv_append(gc_kv_pool* pool, const void* k_new, const void* v_new,
                            max_blocks_per_seq, layer, total_new_tokens, stream);
 }
 
+gc_status gc_kv_append_rope(gc_kv_pool* pool, const void* q, int64_t q_stride, void* q_out,
+                            const void* k_new, int64_t k_stride, const void* v_new,
+                            int64_t v_stride, const int32_t* block_table, const int32_t* seq_lens,
+                            cudaStream_t stream, int32_t layer, const int32_t* cu_new_lens,
+                            int32_t batch, int32_t max_blocks_per_seq, int32_t total_new_tokens,
+                            int32_t num_q_heads, const float* cos_sin, int32_t n_positions,
+                            int32_t rot_dim, const int32_t* positions, uint32_t flags) {
+  Range range_("gc_kv_append_rope");
+  g_msg[0] = 0;
+  const char* who = "gc_kv_append_rope";
+  if (!pool) return fail(GC_ERR_INVALID_ARG, "%s: pool is NULL", who);
+  if (batch < 0 || total_new_tokens < 0 || max_blocks_per_seq < 0 || n_positions < 0)
+    return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (flags & ~GC_ROPE_INTERLEAVED)
+    return fail(GC_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
+  if (layer < 0 || layer >= pool->cfg.num_layers)
+    return fail(GC_ERR_OUT_OF_RANGE, "%s: layer %d outside [0, %d)", who, layer,
+                pool->cfg.num_layers);
+  const int hkv = pool->cfg.num_kv_heads, d = pool->cfg.head_dim;
+  if (num_q_heads < 0 || num_q_heads % hkv)
+    return fail(GC_ERR_INVALID_ARG, "%s: num_q_heads %d not a multiple of num_kv_heads %d", who,
+                num_q_heads, hkv);
+  if (rot_dim < 16 || rot_dim > d || rot_dim % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: rot_dim %d not a multiple of 16 in [16, %d]", who,
+                rot_dim, d);
+  // units of 16 elements of a token are numbered with 32-bit ints
+  if ((static_cast<int64_t>(num_q_heads) + 2 * static_cast<int64_t>(hkv)) * d >= (1ll << 30))
+    return fail(GC_ERR_UNSUPPORTED, "%s: %d q heads and %d kv heads", who, num_q_heads, hkv);
+  const int64_t kv_row = static_cast<int64_t>(hkv) * d, q_row = static_cast<int64_t>(num_q_heads) * d;
+  if (k_stride < kv_row || v_stride < kv_row || q_stride < q_row)
+    return fail(GC_ERR_INVALID_ARG, "%s: a token stride is shorter than the token's heads", who);
+  if ((k_stride | v_stride | (num_q_heads ? q_stride : 0)) % 8)
+    return fail(GC_ERR_INVALID_ARG, "%s: token strides must be multiples of 8 elements", who);
+  if (batch == 0 || total_new_tokens == 0) return GC_OK;
+  if (!k_new || !v_new || !block_table || !seq_lens || !cu_new_lens || !cos_sin ||
+      (num_q_heads && (!q || !q_out)))
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
+  if (max_blocks_per_seq == 0) return fail(GC_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
+  if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new) |
+       reinterpret_cast<uintptr_t>(cos_sin) |
+       (num_q_heads ? reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) : 0)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q / q_out / k_new / v_new / cos_sin not 16-byte aligned",
+                who);
+  // in place only row by row: each thread has read what it writes, and nobody else reads it
+  if (num_q_heads && q == q_out && q_stride != q_row)
+    return fail(GC_ERR_INVALID_ARG, "%s: q_out may be q only if q's tokens are dense", who);
+  return gc::launch_append_rope(
+      pool,
+      gc::RopeArgs{q, q_out, k_new, v_new, q_stride, k_stride, v_stride, block_table, seq_lens,
+                   cu_new_lens, cos_sin, positions, batch, max_blocks_per_seq, layer,
+                   total_new_tokens, num_q_heads, n_positions, rot_dim,
+                   (flags & GC_ROPE_INTERLEAVED) != 0},
+      stream);
+}
+
 static gc_status attn_common(const char* who, const void* q, const gc_kv_pool* pool,
                              const int32_t* block_table, const int32_t* prefix_lens,
                              const int32_t* new_lens, void* out, int32_t layer,

@@ -156,6 +156,22 @@ gc_status launch_append(const gc_kv_pool* pool, const void* k_new, const void* v
                         const int32_t* cu_new_lens, int32_t batch, int32_t max_blocks,
                         int32_t layer, int32_t total_new_tokens, cudaStream_t stream);
 
+struct RopeArgs {
+  const void* q;  // nullptr with num_q_heads 0: K and V only
+  void* q_out;
+  const void* k_new;
+  const void* v_new;
+  int64_t q_stride, k_stride, v_stride;  // elements between tokens
+  const int32_t* block_table;
+  const int32_t* prefix_lens;
+  const int32_t* cu_new_lens;
+  const float* cos_sin;  // [n_positions][2][rot_dim / 2]
+  const int32_t* positions;
+  int32_t batch, max_blocks, layer, total_new_tokens, num_q_heads, n_positions, rot_dim;
+  bool interleaved;
+};
+gc_status launch_append_rope(const gc_kv_pool* pool, const RopeArgs& a, cudaStream_t stream);
+
 struct AttnArgs {
   const void* q;
   void* out;
