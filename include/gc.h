@@ -26,6 +26,10 @@
  *                           the pool through a block table         (prefill)
  *   gc_paged_decode_attn    the same for one new token per request,
  *                           split over key ranges                  (decode)
+ *   gc_paged_cross_attn     attention to cached states of another sequence
+ *                           (an encoder's), all of them seen by every row
+ *   gc_shared_prefix_decode_attn  decode of requests that share a cached
+ *                           prefix, which is read once for all of them
  *
  * Conventions for every call
  *  - All device work is ordered on the caller's stream; no call synchronises
@@ -565,6 +569,94 @@ GC_API gc_status gc_paged_decode_attn_q8(const void* q, const gc_kv_pool* pool,
                                          void* workspace, size_t workspace_bytes,
                                          const void* q8_image, const int32_t* q8_table,
                                          int32_t n_image_blocks, uint32_t flags);
+
+/* Cross attention over the paged cache: every new token of request b sees all
+ * kv_lens[b] cached states of another sequence, e.g. an encoder's, whose K and
+ * V are a context that does not change while it is kept (the cached context KV
+ * of Sec. 2.2, restored instead of computed again).  For request b, q head h,
+ * new row i < n_b and g = h / (Hq/Hkv):
+ *     out[cu_new_lens[b]+i][h] = sum_{j < kv_lens[b]} softmax_j(
+ *             softmax_scale * q[cu_new_lens[b]+i][h] . k_j) v_j
+ * with k_j, v_j read from pool[layer] through block_table[b].  A request
+ * without states (kv_lens[b] = 0) gets zeros.  For one new token per request
+ * and no request without states this is also gc_paged_decode_attn over the
+ * states' block table.
+ *   q, out      [T_new][Hq][d] bf16, device; fp32 accumulation, P rounded to
+ *               bf16 before the PV product, out rounded to nearest even.
+ *   kv_lens, new_lens  int32 [batch], device.  cu_new_lens int32 [batch+1],
+ *               device, consistent with new_lens.  The number of states has
+ *               nothing to do with the number of new tokens.
+ *   total_new_tokens  T_new = cu_new_lens[batch], passed from the host; it
+ *               bounds every q / out row access.
+ *   num_q_heads, block_table  as gc_prefix_prefill_attn.
+ *   workspace   device scratch of gc_paged_cross_workspace_bytes(pool, batch,
+ *               max_blocks_per_seq, num_q_heads, total_new_tokens) bytes (0:
+ *               NULL is fine), 16-byte aligned, owned by the caller, not used
+ *               after the stream passes the call; no initial contents needed.
+ *               Calls sharing a workspace must not overlap on the GPU.
+ * A request whose length is outside [0, max_blocks_per_seq*ps], or whose rows
+ * would pass T_new, is skipped (its rows are not written); a bad page leaves
+ * its request's output unspecified; both are recorded as
+ * GC_ERR_OUT_OF_RANGE.
+ * Errors: GC_ERR_INVALID_ARG (null, unaligned, workspace too small),
+ * GC_ERR_OUT_OF_RANGE (layer), GC_ERR_UNSUPPORTED (head grouping, batch >
+ * 8192, sizes past 32-bit numbering), GC_ERR_CUDA. */
+GC_API size_t gc_paged_cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                             int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                             int32_t total_new_tokens);
+GC_API gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool,
+                                     const int32_t* block_table, const int32_t* kv_lens,
+                                     const int32_t* new_lens, void* out, cudaStream_t stream,
+                                     int32_t layer, const int32_t* cu_new_lens, int32_t batch,
+                                     int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                     float softmax_scale, int32_t total_new_tokens,
+                                     void* workspace, size_t workspace_bytes);
+
+/* Decode attention of requests whose contexts begin with the same cached
+ * pages (Sec. 2.2: cached context is reused across requests; a system prompt
+ * or a document that many ask about is reused by several at once): each
+ * group's shared prefix is read once for all of its requests, each request's
+ * own tokens after it once, and the two are joined in fp32.  For request b of
+ * group s (cu_requests[s] <= b < cu_requests[s+1]), q head h and
+ * g = h / (Hq/Hkv):
+ *     out[b][h] = sum_j softmax_j(softmax_scale * q[b][h] . k_j) v_j
+ * over the shared_lens[s] keys read through shared_table[s] and the
+ * seq_lens[b] keys read through block_table[b].  Equals gc_paged_decode_attn
+ * with both page lists in one table (where the shared length is a multiple of
+ * the page size), to the attention tolerance.  The new token's K/V must
+ * already be in the request's own pages (gc_kv_append, or gc_kv_append_rope
+ * with its position given, with seq_lens[b] - 1 as the offset).
+ *   q, out        [batch][Hq][d] bf16, device.
+ *   shared_table  int32 [num_groups][max_shared_blocks], device.
+ *   shared_lens   int32 [num_groups], device: 0 (no prefix) or more; the last
+ *                 shared page may be partly filled.
+ *   cu_requests   int32 [num_groups+1], device: first request of each group
+ *                 (0 first, batch last; a group may be empty).
+ *   block_table   int32 [batch][max_blocks_per_seq], device: own pages.
+ *   seq_lens      int32 [batch], device: own tokens, the new one included.  0
+ *                 is valid; a request without any key gets zeros.
+ *   workspace     device scratch of gc_shared_prefix_decode_workspace_bytes
+ *                 bytes for the same arguments, with the rules of
+ *                 gc_paged_decode_attn's.
+ * A request without a group, or with an own or shared length outside its
+ * table's capacity, is skipped (its rows are not written); a bad page leaves
+ * the outputs of those who read it unspecified; both are recorded as
+ * GC_ERR_OUT_OF_RANGE.  Calls on one pool must not overlap on the GPU with
+ * each other or with the other attention calls.
+ * Errors: GC_ERR_INVALID_ARG (null, unaligned, workspace too small),
+ * GC_ERR_OUT_OF_RANGE (layer), GC_ERR_UNSUPPORTED (head grouping, batch or
+ * num_groups > 8192, sizes past 32-bit numbering), GC_ERR_CUDA. */
+GC_API size_t gc_shared_prefix_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                                      int32_t num_groups,
+                                                      int32_t max_shared_blocks,
+                                                      int32_t max_blocks_per_seq,
+                                                      int32_t num_q_heads);
+GC_API gc_status gc_shared_prefix_decode_attn(
+    const void* q, const gc_kv_pool* pool, const int32_t* shared_table,
+    const int32_t* shared_lens, const int32_t* cu_requests, int32_t num_groups,
+    int32_t max_shared_blocks, const int32_t* block_table, const int32_t* seq_lens, void* out,
+    cudaStream_t stream, int32_t layer, int32_t batch, int32_t max_blocks_per_seq,
+    int32_t num_q_heads, float softmax_scale, void* workspace, size_t workspace_bytes);
 
 /* Test hook, not part of the method (the paper has no counterpart): launches
  * one thread that waits on a device barrier nobody arrives at, with the same

@@ -44,6 +44,8 @@ EXPORTED = (
     "gc_prefix_prefill_attn_simt", "gc_prefix_prefill_attn_noalloc",
     "gc_prefix_prefill_attn_q8", "gc_paged_decode_attn_q8",
     "gc_paged_decode_workspace_bytes", "gc_paged_decode_attn", "gc_selftest_wait_timeout",
+    "gc_paged_cross_workspace_bytes", "gc_paged_cross_attn",
+    "gc_shared_prefix_decode_workspace_bytes", "gc_shared_prefix_decode_attn",
     "gc_last_error",
     "gc_status_string",
 )
@@ -109,13 +111,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                              ctypes.c_float, vp, ctypes.c_size_t]
         lib.gc_paged_decode_attn_q8.argtypes = lib.gc_paged_decode_attn.argtypes + [vp, vp, i32,
                                                                                   u32]
+        lib.gc_paged_cross_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+        lib.gc_paged_cross_workspace_bytes.restype = sz
+        lib.gc_paged_cross_attn.argtypes = attn + [vp, sz]
+        lib.gc_shared_prefix_decode_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
+        lib.gc_shared_prefix_decode_workspace_bytes.restype = sz
+        lib.gc_shared_prefix_decode_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp,
+                                                     i32, i32, i32, i32, ctypes.c_float, vp, sz]
         for f in ("gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
                   "gc_kv_pool_check", "gc_kv_restore", "gc_kv_save", "gc_kv_restore_layers",
                   "gc_kv_save_layers", "gc_kv_stage_layers", "gc_kv_save_q8", "gc_kv_restore_q8",
                   "gc_kv_append", "gc_kv_append_rope",
                   "gc_prefix_prefill_attn", "gc_prefix_prefill_attn_simt",
                   "gc_prefix_prefill_attn_noalloc", "gc_prefix_prefill_attn_q8",
-                  "gc_paged_decode_attn", "gc_paged_decode_attn_q8"):
+                  "gc_paged_decode_attn", "gc_paged_decode_attn_q8", "gc_paged_cross_attn",
+                  "gc_shared_prefix_decode_attn"):
             getattr(lib, f).restype = ctypes.c_int
         lib.gc_last_error.argtypes = []
         lib.gc_last_error.restype = ctypes.c_char_p
@@ -392,6 +402,46 @@ def gc_paged_decode_attn_q8(q, pool, block_table, seq_lens, out, stream, layer: 
                                           _addr(workspace), workspace_bytes, _addr(q8_image),
                                           _addr(q8_table), n_image_blocks, flags),
            "gc_paged_decode_attn_q8")
+
+
+def gc_paged_cross_workspace_bytes(pool, batch: int, max_blocks_per_seq: int, num_q_heads: int,
+                                   total_new_tokens: int) -> int:
+    return int(load().gc_paged_cross_workspace_bytes(pool, batch, max_blocks_per_seq, num_q_heads,
+                                                     total_new_tokens))
+
+
+def gc_paged_cross_attn(q, pool, block_table, kv_lens, new_lens, out, stream, layer: int,
+                        cu_new_lens, batch: int, max_blocks_per_seq: int, num_q_heads: int,
+                        softmax_scale: float, total_new_tokens: int, workspace=None,
+                        workspace_bytes: int = 0) -> None:
+    """Every new token of a request over all of the request's cached states."""
+    _check(load().gc_paged_cross_attn(_addr(q), pool, _addr(block_table), _addr(kv_lens),
+                                      _addr(new_lens), _addr(out), _stream(stream), layer,
+                                      _addr(cu_new_lens), batch, max_blocks_per_seq, num_q_heads,
+                                      softmax_scale, total_new_tokens, _addr(workspace),
+                                      workspace_bytes),
+           "gc_paged_cross_attn")
+
+
+def gc_shared_prefix_decode_workspace_bytes(pool, batch: int, num_groups: int,
+                                            max_shared_blocks: int, max_blocks_per_seq: int,
+                                            num_q_heads: int) -> int:
+    return int(load().gc_shared_prefix_decode_workspace_bytes(
+        pool, batch, num_groups, max_shared_blocks, max_blocks_per_seq, num_q_heads))
+
+
+def gc_shared_prefix_decode_attn(q, pool, shared_table, shared_lens, cu_requests, num_groups: int,
+                                 max_shared_blocks: int, block_table, seq_lens, out, stream,
+                                 layer: int, batch: int, max_blocks_per_seq: int,
+                                 num_q_heads: int, softmax_scale: float, workspace=None,
+                                 workspace_bytes: int = 0) -> None:
+    """Decode of groups of requests whose contexts begin with the same cached
+    pages: a group's shared pages, then each request's own."""
+    _check(load().gc_shared_prefix_decode_attn(
+        _addr(q), pool, _addr(shared_table), _addr(shared_lens), _addr(cu_requests), num_groups,
+        max_shared_blocks, _addr(block_table), _addr(seq_lens), _addr(out), _stream(stream), layer,
+        batch, max_blocks_per_seq, num_q_heads, softmax_scale, _addr(workspace), workspace_bytes),
+        "gc_shared_prefix_decode_attn")
 
 
 def gc_selftest_wait_timeout(pool, stream=None) -> None:

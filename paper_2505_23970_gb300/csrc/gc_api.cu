@@ -771,6 +771,106 @@ gc_status gc_paged_decode_attn_q8(const void* q, const gc_kv_pool* pool,
   return gc::launch_decode(pool, a, stream, &q8);
 }
 
+static gc_status span_common(const char* who, const gc_kv_pool* pool, int32_t layer, int32_t batch,
+                             int32_t max_blocks_per_seq, int32_t num_q_heads,
+                             float softmax_scale) {
+  if (!pool) return fail(GC_ERR_INVALID_ARG, "%s: pool is NULL", who);
+  if (batch < 0 || max_blocks_per_seq < 0) return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (layer < 0 || layer >= pool->cfg.num_layers)
+    return fail(GC_ERR_OUT_OF_RANGE, "%s: layer %d outside [0, %d)", who, layer,
+                pool->cfg.num_layers);
+  const int hkv = pool->cfg.num_kv_heads;
+  if (num_q_heads <= 0 || num_q_heads % hkv)
+    return fail(GC_ERR_INVALID_ARG, "%s: num_q_heads %d not a multiple of num_kv_heads %d", who,
+                num_q_heads, hkv);
+  const int G = num_q_heads / hkv;
+  if (G != 1 && G != 2 && G != 4 && G != 8 && G != 16)
+    return fail(GC_ERR_UNSUPPORTED, "%s: q heads per kv head %d not in {1,2,4,8,16}", who, G);
+  if (!(softmax_scale > 0.0f) || softmax_scale == __builtin_inff())
+    return fail(GC_ERR_INVALID_ARG, "%s: softmax_scale must be positive and finite", who);
+  if (batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", who, batch);
+  // positions in a block table are 32-bit ints
+  if (static_cast<int64_t>(max_blocks_per_seq) * pool->cfg.page_size > 2147483647LL)
+    return fail(GC_ERR_UNSUPPORTED, "%s: block table of %d pages", who, max_blocks_per_seq);
+  return GC_OK;
+}
+
+size_t gc_paged_cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                      int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                      int32_t total_new_tokens) {
+  return 0;
+}
+
+gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool, const int32_t* block_table,
+                              const int32_t* kv_lens, const int32_t* new_lens, void* out,
+                              cudaStream_t stream, int32_t layer, const int32_t* cu_new_lens,
+                              int32_t batch, int32_t max_blocks_per_seq, int32_t num_q_heads,
+                              float softmax_scale, int32_t total_new_tokens, void* workspace,
+                              size_t workspace_bytes) {
+  Range range_("gc_paged_cross_attn");
+  g_msg[0] = 0;
+  const char* who = "gc_paged_cross_attn";
+  const gc_status s =
+      span_common(who, pool, layer, batch, max_blocks_per_seq, num_q_heads, softmax_scale);
+  if (s != GC_OK) return s;
+  if (total_new_tokens < 0) return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (batch == 0 || total_new_tokens == 0) return GC_OK;
+  if (!q || !out || !block_table || !kv_lens || !new_lens || !cu_new_lens)
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
+  if (max_blocks_per_seq == 0) return fail(GC_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) |
+       reinterpret_cast<uintptr_t>(workspace)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q / out / workspace not 16-byte aligned", who);
+  return gc::launch_cross(
+      pool,
+      gc::SpanArgs{q, out, block_table, kv_lens, new_lens, nullptr, nullptr, cu_new_lens,
+                   total_new_tokens, batch, 0, max_blocks_per_seq, 0, layer, num_q_heads,
+                   softmax_scale, workspace, workspace_bytes},
+      stream);
+}
+
+size_t gc_shared_prefix_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                               int32_t num_groups, int32_t max_shared_blocks,
+                                               int32_t max_blocks_per_seq, int32_t num_q_heads) {
+  return 0;
+}
+
+gc_status gc_shared_prefix_decode_attn(const void* q, const gc_kv_pool* pool,
+                                       const int32_t* shared_table, const int32_t* shared_lens,
+                                       const int32_t* cu_requests, int32_t num_groups,
+                                       int32_t max_shared_blocks, const int32_t* block_table,
+                                       const int32_t* seq_lens, void* out, cudaStream_t stream,
+                                       int32_t layer, int32_t batch, int32_t max_blocks_per_seq,
+                                       int32_t num_q_heads, float softmax_scale, void* workspace,
+                                       size_t workspace_bytes) {
+  Range range_("gc_shared_prefix_decode_attn");
+  g_msg[0] = 0;
+  const char* who = "gc_shared_prefix_decode_attn";
+  const gc_status s =
+      span_common(who, pool, layer, batch, max_blocks_per_seq, num_q_heads, softmax_scale);
+  if (s != GC_OK) return s;
+  if (num_groups < 0 || max_shared_blocks < 0)
+    return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (num_groups > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: %d groups > 8192", who, num_groups);
+  if (static_cast<int64_t>(max_shared_blocks) * pool->cfg.page_size > 2147483647LL)
+    return fail(GC_ERR_UNSUPPORTED, "%s: shared block table of %d pages", who, max_shared_blocks);
+  if (batch == 0) return GC_OK;
+  if (num_groups == 0) return fail(GC_ERR_INVALID_ARG, "%s: num_groups is 0", who);
+  if (!q || !out || !shared_table || !shared_lens || !cu_requests || !block_table || !seq_lens)
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
+  if (max_shared_blocks == 0 || max_blocks_per_seq == 0)
+    return fail(GC_ERR_INVALID_ARG, "%s: max_shared_blocks / max_blocks_per_seq is 0", who);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) |
+       reinterpret_cast<uintptr_t>(workspace)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q / out / workspace not 16-byte aligned", who);
+  return gc::launch_shared_decode(
+      pool,
+      gc::SpanArgs{q, out, block_table, seq_lens, nullptr, shared_table, shared_lens, cu_requests,
+                   batch, batch, num_groups, max_blocks_per_seq, max_shared_blocks, layer,
+                   num_q_heads, softmax_scale, workspace, workspace_bytes},
+      stream);
+}
+
 gc_status gc_selftest_wait_timeout(gc_kv_pool* pool, cudaStream_t stream) {
   g_msg[0] = 0;
   if (!pool) return fail(GC_ERR_INVALID_ARG, "gc_selftest_wait_timeout: pool is NULL");

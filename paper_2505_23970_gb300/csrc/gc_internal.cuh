@@ -282,4 +282,24 @@ size_t decode_share_workspace_bytes(const gc_kv_pool* pool);
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
                               int32_t num_q_heads);
 
+// Attention in which every row sees all keys: cross attention (rows are new
+// tokens, `start` the requests' first ones) and decode behind a shared prefix
+// (rows are requests, `start` the groups' first ones).
+struct SpanArgs {
+  const void* q;
+  void* out;
+  const int32_t* block_table;
+  const int32_t* lens;
+  const int32_t* new_lens;      // cross
+  const int32_t* shared_table;  // shared
+  const int32_t* shared_lens;
+  const int32_t* start;
+  int32_t rows, batch, groups, max_blocks, max_shared_blocks, layer, num_q_heads;
+  float softmax_scale;
+  void* workspace;
+  size_t workspace_bytes;
+};
+gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream);
+gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream);
+
 }  // namespace gc
