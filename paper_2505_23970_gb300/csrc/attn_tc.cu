@@ -55,9 +55,11 @@
 //    status word.
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
+#include "span.cuh"
 
 namespace gc {
 namespace {
@@ -119,6 +121,7 @@ struct Geom {
   int32_t q8_n_blocks, q8_layer_major, L;
   uint32_t q8_hdr, q8_chunk;  // scale header and whole chunk (one block, layer, plane), bytes
   UnpackedGeom unpacked;  // pages dequantised beforehand (Pages::kUnpacked)
+  SpanGeom span;          // kSpan
 };
 
 struct Barriers {
@@ -130,6 +133,7 @@ struct Barriers {
   int item_slot[2];
   uint32_t tmem_base;
   int abort_flag;
+  int part_steps;  // kSpan: steps of a part of an item's keys
   int p0_steps;  // P tiles tile 0's softmax has published so far (pacing hint)
 };
 
@@ -143,13 +147,26 @@ struct Item {
   int tok0[2], nt_i[2], nt;
   bool valid[2];
 };
+struct SpanItem : Item {
+  int j0;      // first K/V step of the item's part
+  bool piece;  // the result goes to the workspace
+};
+template <bool kSpan>
+using ItemOf = std::conditional_t<kSpan, SpanItem, Item>;
+__device__ __forceinline__ int first_key(const Item&, int j) { return j * kTileN; }
+__device__ __forceinline__ int first_key(const SpanItem& w, int j) { return (w.j0 + j) * kTileN; }
 
 // item_start[p] = first item of the p-th request in work order; the request
 // itself is order[p] when the batch was sorted (order != nullptr), else p.
+// kSpan: prefix_lens has the numbers of keys, every row sees all of its request's, or of
+// a part of them; items are numbered by kv head, part and pair of tiles (the tiles that
+// read the same keys run at the same time).
+template <bool kSpan>
 __device__ __forceinline__ bool decode_item(int it, const int* item_start, const Geom& geo,
-                                            const int32_t* prefix_lens,
+                                            int part_steps, const int32_t* prefix_lens,
                                             const int32_t* new_lens,
-                                            const int32_t* cu_new_lens, Item& w) {
+                                            const int32_t* cu_new_lens,
+                                            ItemOf<kSpan>& w) {
   int lo = 0, hi = geo.batch;  // last b with item_start[b] <= it
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -160,6 +177,28 @@ __device__ __forceinline__ bool decode_item(int it, const int* item_start, const
                                        : lo;
   w.b = b;
   const int local = it - item_start[lo];
+  if constexpr (kSpan) {
+    const SpanRequest r =
+        span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
+    const int steps = span_steps(r.T), tiles = span_tiles(r.n, geo.G);
+    const int parts = span_parts(steps, part_steps);
+    const int head_part = local / tiles, pair = local - head_part * tiles;
+    w.g = head_part / parts;
+    w.j0 = (head_part - w.g * parts) * part_steps;
+    w.T = r.T;
+    w.n = r.n;
+    w.cu = r.cu;
+    w.nt = min(part_steps, steps - w.j0);
+    w.piece = geo.span.shared || parts > 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r0 = (pair * 2 + i) * kTileM;
+      w.valid[i] = r0 < r.n * geo.G;
+      w.tok0[i] = r0 / geo.G;
+      w.nt_i[i] = w.valid[i] ? w.nt : 0;
+    }
+    return true;
+  }
   const int pairs = (item_start[lo + 1] - item_start[lo]) / geo.Hkv;
   const int pair = pairs - 1 - local / geo.Hkv;  // later rows (more keys) first
   w.g = local % geo.Hkv;
@@ -327,10 +366,10 @@ __device__ void converter(uint8_t* smem_kv, Barriers& bar, Q8State& q8, const Ge
 }
 
 // ------------------------------------------------------------------ roles
-template <int D, Pages kPages>
+template <int D, Pages kPages, bool kSpan>
 __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8State* q8,
                          const int* item_start, int total_items, const Geom& geo,
-                         const CUtensorMap* map_q, const CUtensorMap* map_kv,
+                         int part_steps, const CUtensorMap* map_q, const CUtensorMap* map_kv,
                          const CUtensorMap* map_img,
                          const int32_t* block_table,
                          const int32_t* prefix_lens,
@@ -352,8 +391,8 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
   for (uint32_t k = 0; ok; ++k) {
     const int it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
     if (!ok || it < 0) break;
-    Item w;
-    decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
+    ItemOf<kSpan> w;
+    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
     // ---- Q tiles
     ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
     if (!ok) break;
@@ -393,7 +432,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
     };
     auto load_raw = [&](int j) -> Raw {
       Raw r{-2, -1};
-      const int key0 = j * kTileN;
+      const int key0 = first_key(w, j);
       const int nkeys = min(kTileN, w.T - key0);
       const int npages = (nkeys + geo.ps - 1) >> geo.ps_shift;
       const int blk0 = key0 >> geo.ps_shift;
@@ -409,7 +448,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
       Lookup l{r.page, -1, 0.f, 0.f};
       if (kPages == Pages::kUnpacked && r.page != -2)
         l.page = unpacked_or_pool_page(geo.unpacked, r.page, r.ib,
-                                       bt_row + ((j * kTileN) >> geo.ps_shift) + lane,
+                                       bt_row + (first_key(w, j) >> geo.ps_shift) + lane,
                                        geo.num_pages);
       if (kQ8 && r.ib >= 0) {
         l.page = -2;
@@ -428,7 +467,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
     Lookup next = resolve(load_raw(0), 0);
     Raw raw2 = load_raw(1);
     for (int j = 0; ok && j < w.nt; ++j) {
-      const int key0 = j * kTileN;
+      const int key0 = first_key(w, j);
       const int nkeys = min(kTileN, w.T - key0);
       Lookup cur = next;
       next = resolve(raw2, j + 1);
@@ -547,10 +586,10 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
 // read by the softmax; it is issued before PV_i(j), and the next scores are
 // there when the softmax has published P_i(j) (a batch of 12 requests with 32/8
 // heads of 64: 158 -> 125 us; 2 x (16000 + 1024) tokens 486 -> 349 us).
-template <int D>
+template <int D, bool kSpan>
 __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, uint32_t tmem,
                            const int* item_start, int total_items, const Geom& geo,
-                           const int32_t* prefix_lens,
+                           int part_steps, const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens) {
   using C = Cfg<D>;
@@ -568,8 +607,8 @@ __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& b
     if (!ok) break;
     mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
-    Item w;
-    decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
+    ItemOf<kSpan> w;
+    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -746,9 +785,9 @@ __device__ __forceinline__ bool tile_exp_after(const uint32_t (&sr)[4][32], uint
   return true;
 }
 
-template <int D, int i>
+template <int D, int i, bool kSpan>
 __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
-                           int total_items, const Geom& geo,
+                           int total_items, const Geom& geo, int part_steps,
                            const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens,
@@ -771,8 +810,8 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
-    Item w;
-    decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
+    ItemOf<kSpan> w;
+    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -788,7 +827,7 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     };
     const int tok = w.tok0[i] + r / geo.G;
     const bool row_valid = tok < w.n;
-    const int kmax = row_valid ? w.P + tok : w.T - 1;  // last visible key
+    const int kmax = row_valid && !kSpan ? w.P + tok : w.T - 1;  // last visible key
     float m_run = -INFINITY, l = 0.f;
     for (int j = 0; j < w.nt_i[i]; ++j) {
       ok = mbar_wait(&bar.s_full[i], s_count & 1, abortp);
@@ -807,7 +846,7 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
       for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sr[c]);
       tmem_wait_ld();
       if (C::kOwnP) arrive_warp(&bar.s_free[i]);  // the next S may be computed
-      const int key0 = j * kTileN;
+      const int key0 = first_key(w, j);
       if (key0 + kTileN - 1 > kmax) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -861,6 +900,26 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     if (rel) release(w.nt_i[i] - 1, 1);
     tc_fence_after();
     const int h = w.g * geo.G + r % geo.G;
+    bool piece = false;
+    if constexpr (kSpan) piece = w.piece;
+    if (kSpan && piece) {
+      const int64_t row = static_cast<int64_t>(it) * geo.span.stride + i * kTileM + r;
+      if (row_valid) geo.span.ml[row] = make_float2(m_run, l);
+      uint4* dst = reinterpret_cast<uint4*>(geo.span.o + row * D);
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tmem_ld32(tO + c * 32, o);
+        tmem_wait_ld();
+        if (row_valid) {
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            dst[c * 8 + v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+        }
+      }
+      tc_fence_before();
+      continue;
+    }
     const float inv_l = 1.f / l;
     uint4* orow = reinterpret_cast<uint4*>(
         out + (static_cast<int64_t>(w.cu + tok) * geo.Hq + h) * D);
@@ -885,7 +944,7 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
   }
 }
 
-template <int D, Pages kPages>
+template <int D, Pages kPages, bool kSpan = false>
 __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThreads, 1)
     attn_tc_kernel(const __grid_constant__ CUtensorMap map_q,
                    const __grid_constant__ CUtensorMap map_kv,
@@ -907,6 +966,8 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   Q8State* q8 = kQ8 ? reinterpret_cast<Q8State*>(
                           (reinterpret_cast<uintptr_t>(order + kSortMax) + 7) & ~uintptr_t(7))
                     : nullptr;
+  // kSpan, shared: first item of each group, where that is not its place in work order
+  int* first_of = reinterpret_cast<int*>(order + kSortMax);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -946,7 +1007,9 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   dependent_begin();
   if (geo.batch <= kSortMax) {
     // rank requests by total length, longest first (ties by index)
-    auto total_len = [&](int b) { return ld_plain(prefix_lens + b) + ld_plain(new_lens + b); };
+    auto total_len = [&](int b) {
+      return ld_plain(prefix_lens + b) + (kSpan ? 0 : ld_plain(new_lens + b));
+    };
     for (int b = threadIdx.x; b < geo.batch; b += blockDim.x) {
       const int tb = total_len(b);
       int rank = 0;
@@ -959,13 +1022,26 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   }
   __syncthreads();
   if (warp == 2) {
+    auto request = [&](int b) {
+      return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
+    };
+    int steps = 0;
+    if (kSpan) {
+      steps = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                        geo.span.pieces > 0 && (geo.span.shared || geo.batch <= kSortMax), request);
+      if (lane == 0) bar.part_steps = steps;
+    }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
     for (int b0 = 0; b0 < geo.batch; b0 += 32) {
       const int p = b0 + lane;
       const int b = p < geo.batch ? (geo.batch <= kSortMax ? order[p] : p) : p;
       int cnt = 0;
-      if (p < geo.batch) {
+      if (kSpan && p < geo.batch) {
+        const SpanRequest r = request(b);
+        if (r.bad) record_error(status, GC_ERR_OUT_OF_RANGE);
+        if (r.n > 0) cnt = geo.Hkv * span_tiles(r.n, geo.G) * span_parts(span_steps(r.T), steps);
+      } else if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
         const bool sane = n >= 0 && P >= 0 && cu >= 0 && cu + n <= geo.total_new;
@@ -979,6 +1055,8 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
         if (lane >= o) incl += y;
       }
       if (p < geo.batch) item_start[p] = running + incl - cnt;
+      if (kSpan && geo.span.shared && p < geo.batch && geo.batch <= kSortMax)
+        first_of[b] = running + incl - cnt;
       running += __shfl_sync(0xffffffffu, incl, 31);
     }
     if (lane == 0) item_start[geo.batch] = running;
@@ -987,18 +1065,29 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
-  const int total_items = item_start[geo.batch];
+  int total_items = item_start[geo.batch];
+  bool fits = true;
+  int part_steps = 0;
+  if (kSpan) {
+    part_steps = bar.part_steps;
+    // (groups that overlap could be more items than the workspace has pieces)
+    fits = !geo.span.shared || total_items <= geo.span.pieces;
+    if (!fits) {
+      total_items = 0;
+      if (threadIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+    }
+  }
 
   if (warp < 4) {
     regs_dec<kQ8 ? kRegsProducerQ8 : kRegsProducer>();
     if (warp == 0) {
-      producer<D, kPages>(smem_q, smem_kv, bar, q8, item_start, total_items, geo, &map_q, &map_kv,
-                          &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
+      producer<D, kPages, kSpan>(smem_q, smem_kv, bar, q8, item_start, total_items, geo,
+                          part_steps, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
                           work_counter);
     } else if (warp == 1 || warp == 2) {
       if (lane == 0)
-        mma_issuer<D>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
-                      prefix_lens, new_lens, cu_new_lens);
+        mma_issuer<D, kSpan>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
+                      part_steps, prefix_lens, new_lens, cu_new_lens);
       __syncwarp();
     }
   } else if (kQ8 && warp >= kThreads / 32) {
@@ -1006,12 +1095,23 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     converter<D>(smem_kv, bar, *q8, geo);
   } else {
     regs_inc<kQ8 ? kRegsSoftmaxQ8 : kRegsSoftmax>();
+    if (kSpan) {
+      const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
+      const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
+      if (geo.span.shared)
+        span_priors(geo.span, geo.batch, geo.G, geo.total_new, part_steps, !fits,
+                    geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me,
+                    all);
+      else
+        span_empty_and_cut(geo.span, geo.batch, geo.Hq, D, geo.total_new, part_steps, item_start,
+                           order, prefix_lens, new_lens, cu_new_lens, out, me, all);
+    }
     if (warp < 8)
-      softmax_wg<D, 0>(bar, tmem, item_start, total_items, geo, prefix_lens, new_lens,
-                       cu_new_lens, out);
+      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, part_steps, prefix_lens,
+                              new_lens, cu_new_lens, out);
     else
-      softmax_wg<D, 1>(bar, tmem, item_start, total_items, geo, prefix_lens, new_lens,
-                       cu_new_lens, out);
+      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, part_steps, prefix_lens,
+                              new_lens, cu_new_lens, out);
   }
   tc_fence_before();
   __syncthreads();
@@ -1063,12 +1163,12 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 template <int D>
 gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                  int* work_counter, const Q8Pages* q8 = nullptr,
-                 const UnpackedPages* unpacked = nullptr) {
+                 const UnpackedPages* unpacked = nullptr, const SpanGeom* span = nullptr) {
   using C = Cfg<D>;
   gc_status bound = check_item_bound(pool, a, pool->num_sms);
   if (bound != GC_OK) return bound;
   auto enc = encode_fn();
-  if (!enc) return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: cuTensorMapEncodeTiled unavailable");
+  if (!enc) return fail(GC_ERR_CUDA, "%s: cuTensorMapEncodeTiled unavailable", a.who);
   const auto& cfg = pool->cfg;
   Geom geo;
   geo.batch = a.batch;
@@ -1100,7 +1200,7 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   const uint64_t pool_rows = static_cast<uint64_t>(cfg.num_layers) * 2 * cfg.num_pages *
                              cfg.num_kv_heads * cfg.page_size;
   if (pool_rows >= (1ull << 31))
-    return fail(GC_ERR_UNSUPPORTED, "gc_prefix_prefill_attn: pool has %llu rows (limit 2^31)",
+    return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
                 static_cast<unsigned long long>(pool_rows));
   CUtensorMap map_q, map_kv;
   {
@@ -1114,7 +1214,7 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                      strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS)
-      return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: q tensor map (CUresult %d)", (int)r);
+      return fail(GC_ERR_CUDA, "%s: q tensor map (CUresult %d)", a.who, (int)r);
   }
   // The rows of the pool, or of unpacked image pages, one box per page and half.
   auto encode_rows = [&](const void* base, uint64_t rows, CUtensorMap* map) {
@@ -1132,7 +1232,7 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
     r = encode_rows(unpacked->data, 2ull * unpacked->pages * cfg.num_kv_heads * cfg.page_size,
                     &map_img);
   if (r != CUDA_SUCCESS)
-    return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: K/V tensor map (CUresult %d)", (int)r);
+    return fail(GC_ERR_CUDA, "%s: K/V tensor map (CUresult %d)", a.who, (int)r);
   // 8-bit image: its code rows (d bytes each; Hkv*ps rows per chunk after the
   // scale header) as a 3-D map, box = one page of one kv head
   if (q8) {
@@ -1153,16 +1253,20 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   }
   const size_t smem = 1024 + 2 * C::kTileBytes + C::kStages * C::kTileBytes + sizeof(Barriers) +
                       (static_cast<size_t>(a.batch) + 1) * sizeof(int) +
-                      kSortMax * sizeof(int16_t) + (q8 ? sizeof(Q8State) + 8 : 0);
+                      kSortMax * sizeof(int16_t) + (q8 ? sizeof(Q8State) + 8 : 0) +
+                      (span && span->shared ? kSortMax * sizeof(int) : 0);
   // (at d = 128 only the image variant is used: see below)
   constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
   constexpr Pages kUnpacked = D == 128 ? Pages::kImage : Pages::kUnpacked;
-  auto kernel = q8         ? attn_tc_kernel<D, Pages::kImage>
+  // (and nothing is cut there)
+  constexpr bool kSpan = D == 64;
+  auto kernel = span       ? attn_tc_kernel<D, kPool, kSpan>
+                : q8       ? attn_tc_kernel<D, Pages::kImage>
                 : unpacked ? attn_tc_kernel<D, kUnpacked>
                            : attn_tc_kernel<D, kPool>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(smem));
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: smem attribute");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   // items beyond one per CTA are claimed from a counter; a call that cannot
   // have any needs no counter, and only as many CTAs as it can have items
   const long long most_items =
@@ -1170,14 +1274,23 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
       ((static_cast<long long>(a.total_new_tokens) * geo.G + (2 * kTileM - 1ll) * a.batch) /
        (2 * kTileM));
   geo.more_items = most_items > pool->num_sms;
+  long long ctas = geo.more_items ? pool->num_sms : most_items;
+  geo.span = SpanGeom{};
+  if (span) {
+    // (an item may be cut into as many parts as the block tables have steps for)
+    geo.span = *span;
+    geo.span.workers = pool->num_sms;
+    const long long steps = static_cast<long long>(a.max_blocks) * cfg.page_size / kTileN + 1;
+    if (span->pieces > 0) ctas = min(static_cast<long long>(pool->num_sms), most_items * steps);
+  }
   if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: clearing the work counter");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   e = launch_dependent(kernel,
-                       geo.more_items ? pool->num_sms : static_cast<unsigned>(most_items),
+                       static_cast<unsigned>(ctas),
                        q8 ? kThreadsQ8 : kThreads, smem, stream, map_q, map_kv, map_img,
                        a.block_table, a.prefix_lens, a.new_lens, a.cu_new_lens,
                        static_cast<__nv_bfloat16*>(a.out), geo, pool->status, work_counter);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: launch");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
 }
 
@@ -1224,6 +1337,11 @@ bool converts_in_kernel(const gc_kv_pool* pool, const AttnArgs& a) {
   // items per request and kv head, on average
   const long long items = (rows + 2ll * kTileM * a.batch - 1) / (2ll * kTileM * a.batch);
   return items <= (pool->cfg.head_dim == 128 ? 1 : 3) && 2 * heads * items >= 3ll * pool->num_sms;
+}
+
+gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
+                              const SpanGeom& span) {
+  return launch<64>(pool, a, stream, pool->work_counter, nullptr, nullptr, &span);
 }
 
 gc_status launch_attn_tc_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pages& q8,

@@ -58,6 +58,7 @@
 
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
+#include "span.cuh"
 
 namespace gc {
 namespace {
@@ -99,6 +100,7 @@ struct Geom2 {
   int32_t more_items;  // there may be more items than pairs
   float scale_log2;
   UnpackedGeom unpacked;  // kImg
+  SpanGeom span;          // kSpan
 };
 
 // A CTA's place: its pair's part of the keys (split of splits; 0 of 1 when the
@@ -106,6 +108,7 @@ struct Geom2 {
 // cluster.
 struct Place {
   uint32_t parity, lead, split, splits;
+  int part_steps;  // kSpan: steps of a part of an item's keys
 };
 
 struct Bars2 {
@@ -124,7 +127,8 @@ struct Bars2 {
   uint64_t item_full[2];      // work-item ring, written by the even CTA's K producer
   uint64_t item_empty[2];     // even CTA: item slot read by every consumer of both CTAs
   uint64_t drain;             // even CTA: both issuers' last commits
-  int item_msg[2][8];         // a claimed item, decoded: it, b, tile, g, P, n, cu (it < 0: end)
+  int item_msg[2][8];         // a claimed item, decoded (item_message; it < 0: end)
+  int part_steps;             // kSpan: steps of a part
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -140,15 +144,24 @@ struct Item2 {
   int b, g, P, n, cu, T;
   int tok0;      // first token of this CTA's 128 rows
   int j0, nt;    // this pair's K/V steps: [j0, j0 + nt)
+  bool piece;    // kSpan: the result goes to the workspace
   bool read;     // the whole message has been read (always true, but only known then)
 };
+
+// kSpan: the rows of an item see all keys of their request, or of a part of them (an
+// item of work order p is, in this order, a kv head, a part and a tile: the tiles that
+// read the same keys run at the same time).  P is then the number of keys, T, and the
+// message has the part as well.
+template <bool kSpan>
+constexpr int kMessageWords = kSpan ? 8 : 7;
 
 // Which request, kv head and 256-row tile item `it` is (item_start: first
 // item of each request in work order, then the order itself when the batch
 // was ranked), with the request's lengths: the message the even CTA's
 // producer sends to every role of both CTAs.
+template <bool kSpan>
 __device__ __forceinline__ void item_message(int it, const int* item_start, const Geom2& geo,
-                                             const int32_t* prefix_lens,
+                                             const Place& at, const int32_t* prefix_lens,
                                              const int32_t* new_lens,
                                              const int32_t* cu_new_lens, int* m) {
   int lo = 0, hi = geo.batch;  // last p with item_start[p] <= it
@@ -160,9 +173,23 @@ __device__ __forceinline__ void item_message(int it, const int* item_start, cons
                     reinterpret_cast<const int16_t*>(item_start + geo.batch + 1)[lo])
                                        : lo;
   const int local = it - item_start[lo];
-  const int tiles = (item_start[lo + 1] - item_start[lo]) / geo.Hkv;
   m[0] = it;
   m[1] = b;
+  if (kSpan) {
+    const SpanRequest r =
+        span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
+    const int tiles = span_tiles(r.n, geo.G);
+    const int parts = span_parts(span_steps(r.T), at.part_steps);
+    const int head_part = local / tiles;
+    m[2] = local - head_part * tiles;
+    m[3] = head_part / parts;
+    m[7] = head_part - m[3] * parts;
+    m[4] = r.T;
+    m[5] = r.n;
+    m[6] = r.cu;
+    return;
+  }
+  const int tiles = (item_start[lo + 1] - item_start[lo]) / geo.Hkv;
   m[4] = ld_plain(prefix_lens + b);
   m[5] = ld_plain(new_lens + b);
   // later rows (more keys) first; the kv heads of a tile together, or where a
@@ -191,6 +218,7 @@ __device__ __forceinline__ void item_read_warp(const Item2& w, uint32_t item_emp
 }
 
 // The quantities a role derives from an item message.
+template <bool kSpan>
 __device__ __forceinline__ void item_from_message(const int* m, const Geom2& geo, const Place& at,
                                                   Item2& w) {
   w.read = (m[1] | m[2] | m[3] | m[4] | m[5] | m[6]) >= 0;
@@ -199,10 +227,19 @@ __device__ __forceinline__ void item_from_message(const int* m, const Geom2& geo
   w.P = m[4];
   w.n = m[5];
   w.cu = m[6];
-  w.T = w.P + w.n;
-  const int rows = w.n << geo.g_shift;
   const int r0 = m[2] * 2 * kRows;
   w.tok0 = (r0 + static_cast<int>(at.parity) * kRows) >> geo.g_shift;
+  if (kSpan) {
+    w.read = w.read && m[7] >= 0;
+    w.T = m[4];
+    const int all = span_steps(w.T);
+    w.j0 = m[7] * at.part_steps;
+    w.nt = min(at.part_steps, all - w.j0);
+    w.piece = geo.span.shared || all > at.part_steps;
+    return;
+  }
+  w.T = w.P + w.n;
+  const int rows = w.n << geo.g_shift;
   const int r_last = min(r0 + 2 * kRows - 1, rows - 1);  // last valid row of the item
   const int kend = w.P + (r_last >> geo.g_shift) + 1;     // keys [0, kend) reach some row
   const int nt = (kend + kKeys - 1) >> 7;
@@ -218,6 +255,7 @@ __device__ __forceinline__ void item_from_message(const int* m, const Geom2& geo
 // Read item k of the ring (every consumer thread); the caller releases the
 // slot with one arrival per consumer warp on the even CTA's item_empty.
 // Returns the item number, -1 at the end.
+template <bool kSpan>
 __device__ __forceinline__ int read_item2(Bars2& bar, uint32_t k, const Geom2& geo,
                                           const Place& at, Item2& w, volatile int* abortp,
                                           bool& ok) {
@@ -225,18 +263,19 @@ __device__ __forceinline__ int read_item2(Bars2& bar, uint32_t k, const Geom2& g
   ok = mbar_wait_cluster(&bar.item_full[k & 1], (k >> 1) & 1, abortp);
   if (!ok) return -1;
   const volatile int* m = bar.item_msg[k & 1];
-  int mm[7];
+  int mm[kMessageWords<kSpan>];
 #pragma unroll
-  for (int i = 0; i < 7; ++i) mm[i] = m[i];
-  if (mm[0] >= 0) item_from_message(mm, geo, at, w);
+  for (int i = 0; i < kMessageWords<kSpan>; ++i) mm[i] = m[i];
+  if (mm[0] >= 0) item_from_message<kSpan>(mm, geo, at, w);
   return mm[0];
 }
 
 // The same for a whole warp (every lane reads the item; the lanes agree).
+template <bool kSpan>
 __device__ __forceinline__ int read_item2_warp(Bars2& bar, uint32_t k, const Geom2& geo,
                                                const Place& at, Item2& w, volatile int* abortp,
                                                bool& ok) {
-  const int it = read_item2(bar, k, geo, at, w, abortp, ok);
+  const int it = read_item2<kSpan>(bar, k, geo, at, w, abortp, ok);
   ok = __all_sync(0xffffffffu, ok);
   return it;
 }
@@ -299,7 +338,7 @@ struct Producer {
   }
 };
 
-template <bool kIsK, bool kImg>
+template <bool kIsK, bool kImg, bool kSpan>
 __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, Bars2& bar,
                           const Remote& rm, const int* item_start, int total_items,
                           const Geom2& geo, const CUtensorMap* map_q, const CUtensorMap* map_kv,
@@ -329,7 +368,7 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
       // claim the next item and send it, decoded, to every role of both CTAs
       ok = pr.wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1);
       if (!ok) break;
-      int m[7];
+      int m[kMessageWords<kSpan>];
       if (lane == 0) {
         // a cluster's first item is the one of its own number; the counter hands
         // out the rest.  Without one there are no more unless new_lens sums up to
@@ -340,15 +379,15 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
                  : static_cast<int>(blockIdx.x / (2 * at.splits)) + static_cast<int>(k) * clusters;
         if (it >= total_items) it = -1;
         if (it >= 0) {
-          item_message(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, m);
+          item_message<kSpan>(it, item_start, geo, at, prefix_lens, new_lens, cu_new_lens, m);
           if (at.splits > 1) {  // fewer steps than pairs: some pairs have none
-            item_from_message(m, geo, at, w);
+            item_from_message<kSpan>(m, geo, at, w);
             if (w.nt == 0) it = -1;
           }
         }
         m[0] = it;
 #pragma unroll
-        for (int i = 0; i < 7; ++i) {
+        for (int i = 0; i < kMessageWords<kSpan>; ++i) {
           bar.item_msg[s][i] = m[i];
           st_cluster_u32(rm.item_msg + 32 * s + 4 * i, static_cast<uint32_t>(m[i]));
           if (it < 0) break;
@@ -367,12 +406,12 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       const volatile int* mv = bar.item_msg[s];
-      int mm[7];
+      int mm[kMessageWords<kSpan>];
 #pragma unroll
-      for (int i = 0; i < 7; ++i) mm[i] = mv[i];
+      for (int i = 0; i < kMessageWords<kSpan>; ++i) mm[i] = mv[i];
       it = mm[0];
       if (it < 0) break;
-      item_from_message(mm, geo, at, w);
+      item_from_message<kSpan>(mm, geo, at, w);
       if (!claims) item_read_warp(w, rm.item_empty + 8 * s);
     }
     if (kIsK) {
@@ -488,6 +527,7 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
 // reader), so S runs up to two steps ahead of the softmax and the softmax
 // never waits for a P buffer.  Frees the Q buffer by a commit after the
 // item's last S product (the softmax frees the K slots).
+template <bool kSpan>
 __device__ void s_issuer2(const Place& at, uint8_t* smem_q, uint8_t* smem_k, Bars2& bar,
                           const Remote& rm, uint32_t tmem, const Geom2& geo) {
   const uint16_t both = static_cast<uint16_t>(0x3u << at.lead);  // this pair's CTAs
@@ -497,7 +537,7 @@ __device__ void s_issuer2(const Place& at, uint8_t* smem_q, uint8_t* smem_k, Bar
   bool ok = true;
   for (uint32_t k = 0; ok; ++k) {
     Item2 w;
-    const int it = read_item2(bar, k, geo, at, w, abortp, ok);
+    const int it = read_item2<kSpan>(bar, k, geo, at, w, abortp, ok);
     if (!ok) break;
     if (it < 0) break;
     item_read(w, rm.item_empty + 8 * (k & 1));
@@ -540,6 +580,7 @@ __device__ void s_issuer2(const Place& at, uint8_t* smem_q, uint8_t* smem_k, Bar
 // in; an item's first product (which overwrites O) also waits until the
 // previous item's epilogue has read O.  Its commits tell both CTAs when the
 // S buffer and the V slot have been read.
+template <bool kSpan>
 __device__ void pv_issuer2(const Place& at, uint8_t* smem_v, Bars2& bar, const Remote& rm,
                            uint32_t tmem, const Geom2& geo) {
   const uint16_t both = static_cast<uint16_t>(0x3u << at.lead);  // this pair's CTAs
@@ -549,7 +590,7 @@ __device__ void pv_issuer2(const Place& at, uint8_t* smem_v, Bars2& bar, const R
   bool ok = true;
   for (uint32_t k = 0; ok; ++k) {
     Item2 w;
-    const int it = read_item2(bar, k, geo, at, w, abortp, ok);
+    const int it = read_item2<kSpan>(bar, k, geo, at, w, abortp, ok);
     if (!ok) break;
     if (it < 0) break;
     item_read(w, rm.item_empty + 8 * (k & 1));
@@ -616,7 +657,9 @@ __device__ __forceinline__ float key15_to_f32(uint32_t k15) {
 
 // kSplit: this pair has part of the item's keys; O stays in tensor memory and
 // the row's reference max and sum go to `part` (merge2 combines the pairs).
-template <bool kSplit>
+// kSpan: every row sees all keys of the item, and a piece's O, maxima and sums go to
+// the workspace.
+template <bool kSplit, bool kSpan>
 __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Remote& rm,
                           uint32_t tmem, uint16_t* xch, const Geom2& geo, __nv_bfloat16* out,
                           float2* part) {
@@ -669,7 +712,7 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
   float2 fin = make_float2(-INFINITY, 0.f);  // kSplit: no keys so far
   Item2 w;
   auto next_item = [&](uint32_t k) -> int {
-    const int it = read_item2_warp(bar, k, geo, at, w, abortp, ok);
+    const int it = read_item2_warp<kSpan>(bar, k, geo, at, w, abortp, ok);
     if (ok && it >= 0) item_read_warp(w, rm.item_empty + 8 * (k & 1));
     return it;
   };
@@ -677,7 +720,7 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
   for (uint32_t k = 0; ok && it >= 0; ++k) {
     const int tok = w.tok0 + (r >> geo.g_shift);
     const bool row_valid = tok < w.n;
-    const int kmax = row_valid ? w.P + tok : w.T - 1;  // last visible key
+    const int kmax = row_valid && !kSpan ? w.P + tok : w.T - 1;  // last visible key
     float m_run = -INFINITY, l = 0.f;
     const float sl2 = geo.scale_log2;
     for (int j = 0; j < w.nt; ++j, ++u) {
@@ -792,6 +835,9 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
     // the row (token, head) of out that lane / 8 of this warp's first store belongs to
     const uint32_t out_row = static_cast<uint32_t>(w.cu + w.tok0) * geo.Hq + w.g * geo.G;
     const int left = w.n - w.tok0;  // tokens from this CTA's first row on
+    const bool piece = kSpan && w.piece;
+    const int64_t piece_row = kSpan ? static_cast<int64_t>(it) * geo.span.stride +
+                                          static_cast<int>(at.parity) * kRows + quad * 32 : 0;
     // (the next item is read while the last PV product runs)
     it = next_item(k + 1);
     if (!ok) break;
@@ -817,6 +863,33 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive_remote(rm.o_free);
+    if (piece) {
+      // 32 columns at a time through the warp's 4 KB, so that a store covers four
+      // whole 128-byte row parts here too
+      if (hw == 0 && row_valid) geo.span.ml[piece_row + lane] = make_float2(m_run, l_row);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          *reinterpret_cast<uint4*>(mine + lane * 128 + ((c ^ (lane & 7)) << 4)) =
+              make_uint4(o[half][4 * c], o[half][4 * c + 1], o[half][4 * c + 2], o[half][4 * c + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const int wrow = 4 * c + (lane >> 3);
+          const uint4 v = *reinterpret_cast<const uint4*>(
+              mine + wrow * 128 + (((lane & 7) ^ (wrow & 7)) << 4));
+          if ((quad * 32 + wrow) >> geo.g_shift < left)
+            *reinterpret_cast<uint4*>(geo.span.o + (piece_row + wrow) * kD + hw * 64 + half * 32 +
+                                      (lane & 7) * 4) = v;
+        }
+        __syncwarp();
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar.q_empty[k & 1]);
+      continue;
+    }
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
       const uint32_t* x = &o[c >> 2][8 * (c & 3)];
@@ -934,7 +1007,7 @@ __device__ void merge2_store(const Place& at, const uint8_t* smem, const Item2& 
 }
 
 // ------------------------------------------------------------------- kernel
-template <bool kSplit, bool kImg>
+template <bool kSplit, bool kImg, bool kSpan>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_tc2_kernel(const __grid_constant__ CUtensorMap map_q,
                     const __grid_constant__ CUtensorMap map_k,
@@ -957,10 +1030,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   int16_t* order = reinterpret_cast<int16_t*>(item_start + geo.batch + 1);
   // half-row softmax exchange words [2 buffers][2 halves][128 rows]
   uint16_t* xch = reinterpret_cast<uint16_t*>(order + (geo.batch <= kSortMax ? kSortMax : 0));
+  // kSpan, shared: first item of each group, where that is not its place in work order
+  int* first_of = reinterpret_cast<int*>(xch + 2 * 2 * kRows);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   Place at{rank & 1u, rank & ~1u, kSplit ? rank >> 1 : 0u,
-           kSplit ? cluster_nctarank() >> 1 : 1u};
+           kSplit ? cluster_nctarank() >> 1 : 1u, 0};
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -1002,11 +1077,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   dependent_begin();
   if (geo.batch <= kSortMax) {
     // rank requests by total length, longest first (ties by index)
+    // (kSpan: prefix_lens has the numbers of keys)
+    auto length = [&](int b) {
+      return ld_plain(prefix_lens + b) + (kSpan ? 0 : ld_plain(new_lens + b));
+    };
     for (int b = threadIdx.x; b < geo.batch; b += kThreads) {
-      const int tb = ld_plain(prefix_lens + b) + ld_plain(new_lens + b);
+      const int tb = length(b);
       int rk = 0;
       for (int o = 0; o < geo.batch; ++o) {
-        const int to = ld_plain(prefix_lens + o) + ld_plain(new_lens + o);
+        const int to = length(o);
         rk += (to > tb) || (to == tb && o < b);
       }
       order[rk] = static_cast<int16_t>(b);
@@ -1014,13 +1093,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   if (warp == 2) {
+    auto request = [&](int b) {
+      return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
+    };
+    if (kSpan) {
+      at.part_steps = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                                geo.span.pieces > 0 && (geo.span.shared || geo.batch <= kSortMax),
+                                request);
+      if (lane == 0) bar.part_steps = at.part_steps;
+    }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
     for (int b0 = 0; b0 < geo.batch; b0 += 32) {
       const int p = b0 + lane;
       const int b = p < geo.batch ? (geo.batch <= kSortMax ? order[p] : p) : p;
       int cnt = 0;
-      if (p < geo.batch) {
+      if (kSpan && p < geo.batch) {
+        const SpanRequest r = request(b);
+        if (r.bad && at.parity == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+        if (r.n > 0)
+          cnt = geo.Hkv * span_tiles(r.n, geo.G) * span_parts(span_steps(r.T), at.part_steps);
+      } else if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
         const bool sane = n >= 0 && P >= 0 && cu >= 0 && cu + n <= geo.total_new;
@@ -1034,6 +1127,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane >= o) incl += y;
       }
       if (p < geo.batch) item_start[p] = running + incl - cnt;
+      if (kSpan && geo.span.shared && p < geo.batch && geo.batch <= kSortMax)
+        first_of[b] = running + incl - cnt;
       running += __shfl_sync(0xffffffffu, incl, 31);
     }
     if (lane == 0) item_start[geo.batch] = running;
@@ -1056,7 +1151,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
-  const int total_items = item_start[geo.batch];
+  int total_items = item_start[geo.batch];
+  bool fits = true;
+  if (kSpan) {
+    at.part_steps = bar.part_steps;
+    // (groups that overlap could be more items than the workspace has pieces)
+    fits = !geo.span.shared || total_items <= geo.span.pieces;
+    if (!fits) {
+      total_items = 0;
+      if (threadIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+    }
+  }
   // each cluster has one item; should there be more (see producer2), every pair takes
   // whole ones
   if (kSplit && total_items > static_cast<int>(gridDim.x / (2 * at.splits)))
@@ -1064,21 +1169,32 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   float2* part = reinterpret_cast<float2*>(smem_k);  // splits: free once the roles are done
   if (warp == 0) {
-    producer2<true, kImg>(at, smem_q, smem_k, bar, rm, item_start, total_items, geo, &map_q,
+    producer2<true, kImg, kSpan>(at, smem_q, smem_k, bar, rm, item_start, total_items, geo, &map_q,
                     &map_k, &map_img_k, block_table, prefix_lens, new_lens, cu_new_lens, status,
                     work_counter);
   } else if (warp == 1) {
-    if (at.parity == 0 && lane == 0) s_issuer2(at, smem_q, smem_k, bar, rm, tmem, geo);
+    if (at.parity == 0 && lane == 0) s_issuer2<kSpan>(at, smem_q, smem_k, bar, rm, tmem, geo);
     __syncwarp();
   } else if (warp == 2) {
-    if (at.parity == 0 && lane == 0) pv_issuer2(at, smem_v, bar, rm, tmem, geo);
+    if (at.parity == 0 && lane == 0) pv_issuer2<kSpan>(at, smem_v, bar, rm, tmem, geo);
     __syncwarp();
   } else if (warp == 3) {
-    producer2<false, kImg>(at, smem_q, smem_v, bar, rm, item_start, total_items, geo, &map_q,
+    producer2<false, kImg, kSpan>(at, smem_q, smem_v, bar, rm, item_start, total_items, geo, &map_q,
                      &map_v, &map_img_v, block_table, prefix_lens, new_lens, cu_new_lens, status,
                      work_counter);
   } else if (warp >= 4) {
-    softmax2h<kSplit>(at, smem_q, bar, rm, tmem, xch, geo, out, part);
+    if (kSpan) {
+      const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
+      const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
+      if (geo.span.shared)
+        span_priors(geo.span, geo.batch, geo.G, geo.total_new, at.part_steps,
+                    !fits, geo.batch <= kSortMax ? first_of : item_start, prefix_lens,
+                    cu_new_lens, me, all);
+      else
+        span_empty_and_cut(geo.span, geo.batch, geo.Hq, kD, geo.total_new, at.part_steps,
+                           item_start, order, prefix_lens, new_lens, cu_new_lens, out, me, all);
+    }
+    softmax2h<kSplit, kSpan>(at, smem_q, bar, rm, tmem, xch, geo, out, part);
   }
   // a CTA that gave up tells its peer, so that the peer's roles leave their
   // loops instead of waiting for arrivals that will not come
@@ -1096,10 +1212,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     cluster_sync();
     if (warp >= 4 && it < total_items) {
-      int m[7];
+      int m[kMessageWords<kSpan>];
       Item2 w;
-      item_message(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, m);
-      item_from_message(m, geo, at, w);
+      item_message<kSpan>(it, item_start, geo, at, prefix_lens, new_lens, cu_new_lens, m);
+      item_from_message<kSpan>(m, geo, at, w);
       merge2_store(at, smem_q, w, geo, out);
     }
   }
@@ -1123,8 +1239,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn2() {
   return fn;
 }
 
-size_t smem_bytes2(int batch) {
-  return 1024 + 2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
+size_t smem_bytes2(int batch, bool shared = false) {
+  return (shared && batch <= kSortMax ? kSortMax * sizeof(int) : 0) + 1024 + 2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
          (static_cast<size_t>(batch) + 1) * sizeof(int) +
          (batch <= kSortMax ? kSortMax * sizeof(int16_t) : 0) + 2 * 2 * kRows * sizeof(uint16_t);
 }
@@ -1136,11 +1252,12 @@ namespace {
 constexpr int kMaxSplits = 8;  // pairs of the largest cluster (16 CTAs)
 
 // Kernel attributes of a launch (per context, so set on every call).
-using Kernel2 = decltype(&attn_tc2_kernel<false, false>);
+using Kernel2 = decltype(&attn_tc2_kernel<false, false, false>);
 
 Kernel2 kernel2(int splits, bool img) {
-  if (img) return splits > 1 ? attn_tc2_kernel<true, true> : attn_tc2_kernel<false, true>;
-  return splits > 1 ? attn_tc2_kernel<true, false> : attn_tc2_kernel<false, false>;
+  if (img)
+    return splits > 1 ? attn_tc2_kernel<true, true, false> : attn_tc2_kernel<false, true, false>;
+  return splits > 1 ? attn_tc2_kernel<true, false, false> : attn_tc2_kernel<false, false, false>;
 }
 
 cudaError_t prepare_kernel(Kernel2 kernel, int splits, size_t smem) {
@@ -1207,11 +1324,11 @@ int splits_of(const gc_kv_pool* pool, long long items, long long steps, size_t s
 }  // namespace
 
 gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                          int* work_counter, const UnpackedPages* unpacked) {
+                          int* work_counter, const UnpackedPages* unpacked, const SpanGeom* span) {
   const auto& cfg = pool->cfg;
   if (cfg.head_dim != kD)
-    return fail(GC_ERR_UNSUPPORTED, "gc_prefix_prefill_attn: pair kernel needs head_dim 128");
-  const size_t smem = smem_bytes2(a.batch);
+    return fail(GC_ERR_UNSUPPORTED, "%s: pair kernel needs head_dim 128", a.who);
+  const size_t smem = smem_bytes2(a.batch, span && span->shared);
   // at most this many items, of at most this many 128-key steps
   const long long G = a.num_q_heads / cfg.num_kv_heads;
   const long long most_items =
@@ -1220,14 +1337,14 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
        (2 * kRows));
   const long long most_steps =
       static_cast<long long>(a.max_blocks) * cfg.page_size / kKeys + 1;
-  const int splits = splits_of(pool, most_items, most_steps, smem);
+  const int splits = span ? 1 : splits_of(pool, most_items, most_steps, smem);
   const int pairs = splits > 1 ? static_cast<int>(most_items) : clusters_that_fit(pool, 1, smem);
   if (pairs <= 0)
-    return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: no CTA pair fits on the device");
+    return fail(GC_ERR_CUDA, "%s: no CTA pair fits on the device", a.who);
   gc_status bound = check_item_bound(pool, a, 2 * pairs);
   if (bound != GC_OK) return bound;
   auto enc = encode_fn2();
-  if (!enc) return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: cuTensorMapEncodeTiled unavailable");
+  if (!enc) return fail(GC_ERR_CUDA, "%s: cuTensorMapEncodeTiled unavailable", a.who);
   Geom2 geo;
   geo.batch = a.batch;
   geo.Hq = a.num_q_heads;
@@ -1253,7 +1370,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   const uint64_t pool_rows = static_cast<uint64_t>(cfg.num_layers) * 2 * cfg.num_pages *
                              cfg.num_kv_heads * cfg.page_size;
   if (pool_rows >= (1ull << 31))
-    return fail(GC_ERR_UNSUPPORTED, "gc_prefix_prefill_attn: pool has %llu rows (limit 2^31)",
+    return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
                 static_cast<unsigned long long>(pool_rows));
   CUtensorMap map_q, map_k, map_v;
   {
@@ -1268,7 +1385,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
                      strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS)
-      return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: q tensor map (CUresult %d)", (int)r);
+      return fail(GC_ERR_CUDA, "%s: q tensor map (CUresult %d)", a.who, (int)r);
   }
   // The rows of the pool, or of unpacked image pages, as the producers read them.
   auto encode_rows = [&](const void* base, uint64_t rows, CUtensorMap* k, CUtensorMap* v) {
@@ -1299,7 +1416,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
                     2ull * unpacked->pages * cfg.num_kv_heads * cfg.page_size, &map_img_k,
                     &map_img_v);
   if (r != CUDA_SUCCESS)
-    return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn: K/V tensor map (CUresult %d)", (int)r);
+    return fail(GC_ERR_CUDA, "%s: K/V tensor map (CUresult %d)", a.who, (int)r);
   geo.unpacked = unpacked ? UnpackedGeom{unpacked->table, unpacked->pages, unpacked->image_blocks,
                                          unpacked->by_position ? 1 : 0}
                           : UnpackedGeom{};
@@ -1308,13 +1425,22 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   // A call that cannot have more needs no counter, so nothing clears it, and
   // only as many clusters as it can have items are launched.
   geo.more_items = most_items > pairs;
-  const Kernel2 kernel = kernel2(splits, unpacked != nullptr);
+  long long clusters = geo.more_items ? pairs : most_items;
+  geo.span = SpanGeom{};
+  if (span) {
+    // (an item may be cut into as many parts as the block tables have steps for)
+    geo.span = *span;
+    geo.span.workers = pairs;
+    if (span->pieces > 0) clusters = min(static_cast<long long>(pairs), most_items * most_steps);
+  }
+  const Kernel2 kernel = span ? attn_tc2_kernel<false, false, true>
+                              : kernel2(splits, unpacked != nullptr);
   cudaError_t e = prepare_kernel(kernel, splits, smem);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: kernel attributes");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: clearing the work counter");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(2 * splits * (geo.more_items ? pairs : static_cast<int>(most_items)));
+  lc.gridDim = dim3(static_cast<unsigned>(2 * splits * clusters));
   lc.blockDim = dim3(kThreads);
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
@@ -1330,7 +1456,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   e = cudaLaunchKernelEx(&lc, kernel, map_q, map_k, map_v, map_img_k, map_img_v, a.block_table,
                          a.prefix_lens, a.new_lens, a.cu_new_lens,
                          static_cast<__nv_bfloat16*>(a.out), geo, pool->status, work_counter);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_prefix_prefill_attn: launch");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
 }
 

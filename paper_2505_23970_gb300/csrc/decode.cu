@@ -115,11 +115,11 @@ size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max
 }
 
 gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
-                        const Q8Pages* q8) {
-  if (a.batch > 8192) return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn: batch %d > 8192", a.batch);
+                        const Q8Pages* q8, const SpanGeom* span) {
+  if (a.batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", a.who, a.batch);
   const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
   if (cap > 2147483647LL)
-    return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn: %lld-token block table",
+    return fail(GC_ERR_UNSUPPORTED, "%s: %lld-token block table", a.who,
                 static_cast<long long>(cap));
   const bool shares = decode_shares(pool, a.num_q_heads);
   DecodeSplit sp = {};
@@ -132,31 +132,31 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
   }
   if (need > 0 && (a.workspace == nullptr || a.workspace_bytes < need))
     return fail(GC_ERR_INVALID_ARG,
-                "gc_paged_decode_attn: workspace of %zu bytes needed "
+                "%s: workspace of %zu bytes needed "
                 "(gc_paged_decode_workspace_bytes), got %zu",
-                need, a.workspace_bytes);
+                a.who, need, a.workspace_bytes);
   // the work is numbered with 32-bit ints: 128-key tiles (decode_units adds to them
   // only what still fits) or key ranges
   const int64_t tiles = (cap + kTileKeys - 1) / kTileKeys;
   const long long units = static_cast<long long>(a.batch) * pool->cfg.num_kv_heads *
                           (shares ? tiles : static_cast<int64_t>(sp.splits));
   if (units + 2LL * pool->num_sms > 2147483647LL)
-    return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn: %lld work items", units);
+    return fail(GC_ERR_UNSUPPORTED, "%s: %lld work items", a.who, units);
   const uint64_t pool_rows = static_cast<uint64_t>(pool->cfg.num_layers) * 2 *
                              pool->cfg.num_pages * pool->cfg.num_kv_heads * pool->cfg.page_size;
   if (pool_rows >= (1ull << 31))
-    return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn: pool has %llu rows (limit 2^31)",
+    return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
                 static_cast<unsigned long long>(pool_rows));
   if (q8 && static_cast<uint64_t>(q8->n_blocks) * pool->cfg.num_layers * 2 >= (1ull << 31))
     return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn_q8: image of %d blocks", q8->n_blocks);
-  const gc_status st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8);
+  const gc_status st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8, span);
   if (st != GC_OK || shares || sp.splits <= 1) return st;
   const cudaError_t e = launch_dependent(
       decode_merge_kernel<64>,
       static_cast<unsigned>(a.batch) * static_cast<unsigned>(a.num_q_heads), 64, 0, stream,
       static_cast<const float*>(a.workspace), a.seq_lens, a.batch, a.num_q_heads, sp.splits,
       static_cast<int32_t>(cap), sp.split_tiles, static_cast<__nv_bfloat16*>(a.out));
-  if (e != cudaSuccess) return cuda_fail(e, "gc_paged_decode_attn: merge kernel launch");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
 }
 

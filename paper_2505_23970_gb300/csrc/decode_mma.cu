@@ -55,6 +55,7 @@
 #include "decode_units.h"
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
+#include "span.cuh"
 
 namespace gc {
 namespace {
@@ -79,6 +80,7 @@ struct DecGeom {
   const int32_t* q8_table;   // >= 0: the image block holding the page
   int32_t q8_n_blocks, q8_layer_major;
   uint32_t q8_hdr, q8_chunk;
+  SpanGeom span;  // kJoin: the shared prefixes' pieces
 };
 
 // Threads and resident CTAs of a variant: NT tiles of 8 heads, d columns.  The
@@ -289,6 +291,43 @@ struct Acc {
       }
   }
 
+  // kJoin: start from the request's part of its group's shared prefix, as if its keys
+  // had been taken before.  (The sum goes to one of the lanes that share a head.)
+  __device__ __forceinline__ void join(const SpanGeom& sp, int b, int g, int G) {
+    const int4 pr = ld_plain(sp.prior + b);  // SpanPrior
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    if (pr.z <= 0) return;
+    first = false;
+    const int64_t row0 = (pr.x + static_cast<int64_t>(g) * pr.z * pr.y) * sp.stride + pr.w;
+    const int64_t step = static_cast<int64_t>(pr.y) * sp.stride;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int h = 8 * t + 2 * c + x;
+        if (h >= G) continue;
+        const float2* ml = sp.ml + row0 + h;
+        const float* op = sp.o + (row0 + h) * D + r * (D / 8);
+        float M = -INFINITY, L = 0.f;
+        for (int s = 0; s < pr.z; ++s) M = fmaxf(M, ld_plain(ml + s * step).x);
+        for (int s = 0; s < pr.z; ++s) {
+          const float2 y = ld_plain(ml + s * step);
+          const float f = y.x == -INFINITY ? 0.f : ex2_approx(y.x - M);
+          L = fmaf(y.y, f, L);
+#pragma unroll
+          for (int i = 0; i < D / 16; i += 2) {
+            const float4 v = ld_plain(reinterpret_cast<const float4*>(op + s * step * D + 2 * i));
+            o[t][i][x] = fmaf(v.x, f, o[t][i][x]);
+            o[t][i][x + 2] = fmaf(v.y, f, o[t][i][x + 2]);
+            o[t][i + 1][x] = fmaf(v.z, f, o[t][i + 1][x]);
+            o[t][i + 1][x + 2] = fmaf(v.w, f, o[t][i + 1][x + 2]);
+          }
+        }
+        m[t][x] = M;
+        l[t][x] = r == 0 ? L : 0.f;
+      }
+  }
+
   // S^T of a group
   template <int E>
   __device__ __forceinline__ void scores(const Keys<D, E>& f, uint64_t sk2, float (&s)[NT][4]) {
@@ -424,6 +463,12 @@ __device__ __forceinline__ Where look_up(const DecGeom& geo, const DecPiece& w, 
 //     out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  M = max_s m_s,
 // four columns of one head per thread at a time.  The partials come from other
 // SMs, so they are read through L2.
+// 1 / sum; a request behind a shared prefix may have no key at all: its row is 0.
+template <bool kJoin>
+__device__ __forceinline__ float inverse(float l) {
+  return kJoin && l == 0.f ? 0.f : 1.f / l;
+}
+
 template <int D, int NT>
 __device__ void merge_shares(const float* part_o, const float2* part_ml, int c0, int c1,
                              int first_slot, int G, __nv_bfloat16* out_g) {
@@ -477,7 +522,9 @@ __device__ __forceinline__ void prefetch_l2(uint64_t at) {
 }
 
 // ------------------------------------------------------------------- kernel
-template <int D, int NT, bool kQ8>
+// kJoin: seq_lens counts the keys after a shared prefix whose results are in pieces
+// (span.cuh); a request may then have no keys of its own.
+template <int D, int NT, bool kQ8, bool kJoin>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     decode_mma_kernel(const __nv_bfloat16* q, const int32_t* block_table,
                       const int32_t* seq_lens, __nv_bfloat16* out,
@@ -504,13 +551,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     int most = 0, n = 0;
     for (int b = threadIdx.x; b < geo.batch; b += S::kThreads) {
       const int T = ld_plain(seq_lens + b);
-      if (T < 1 || T > cap) {
+      const bool bad = T < (kJoin ? 0 : 1) || T > cap ||
+                       (kJoin && ld_plain(geo.span.prior + b).z < 0);
+      if (bad) {
         if (blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
       } else {
         most = max(most, T);
         ++n;
       }
-      start[b] = T < 1 || T > cap ? 0 : T;
+      // (kJoin: without own keys, the work of one)
+      start[b] = bad ? 0 : kJoin ? max(T, 1) : T;
     }
     most = __reduce_max_sync(0xffffffffu, most);
     n = __reduce_add_sync(0xffffffffu, n);
@@ -609,6 +659,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     acc.reset();
     const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq + w.g * geo.G;
     acc.load_q(q + head0 * D, geo.G);
+    if (kJoin && w.k0 == 0 && first == 0) acc.join(geo.span, w.b, w.g, geo.G);
     Where nxt{0, 0.f, 0.f};
     if (key_of(32) < k1)
       nxt = look_up<D, kQ8>(geo, w, key_of(32 + lane), pool_k, block_table, status);
@@ -703,7 +754,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
         for (int x = 0; x < 2; ++x) {
           const int h = 8 * t + 2 * (lane & 3) + x;
           if (h >= geo.G) continue;
-          const float inv = 1.f / acc.l[t][x];
+          const float inv = inverse<kJoin>(acc.l[t][x]);
           uint4* dst = reinterpret_cast<uint4*>(out + (head0 + h) * D + (lane >> 2) * (D / 8));
 #pragma unroll
           for (int v = 0; v < D / 64; ++v) {
@@ -766,7 +817,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
         o.y += v.y;
       }
       if (w.part < 0) {
-        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) = pack_bf16x2(o.x / L, o.y / L);
+        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) =
+            kJoin && L == 0.f ? 0u : pack_bf16x2(o.x / L, o.y / L);
       } else {
         *reinterpret_cast<float2*>(ws + (part0 + h * part_step) * D + d) = o;
         if (d == 0) part_ml[part0 + h * part_step] = make_float2(M, L);
@@ -803,35 +855,35 @@ size_t smem_bytes(int batch) {
          (static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 
-template <int D, int NT, bool kQ8>
+template <int D, int NT, bool kQ8, bool kJoin>
 gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo, int grid,
                  cudaStream_t stream) {
   using S = Shape<D, NT>;
   const size_t smem = smem_bytes<D, NT>(a.batch);
-  auto kernel = decode_mma_kernel<D, NT, kQ8>;
+  auto kernel = decode_mma_kernel<D, NT, kQ8, kJoin>;
   cudaError_t e = cudaSuccess;
   // a block gets 48 KB without asking, its static words (well below 1 KB) included
   if (smem > 47 * 1024)
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(smem));
-  if (e != cudaSuccess) return cuda_fail(e, "gc_paged_decode_attn: smem attribute");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   e = launch_dependent(kernel, grid, S::kThreads, smem, stream,
                        static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.seq_lens,
                        static_cast<__nv_bfloat16*>(a.out), static_cast<float*>(a.workspace), geo,
                        pool->status, pool->merge_counters);
-  if (e != cudaSuccess) return cuda_fail(e, "gc_paged_decode_attn: launch");
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
 }
 
-template <int D, bool kQ8>
+template <int D, bool kQ8, bool kJoin>
 gc_status launch_heads(const gc_kv_pool* pool, const DecodeArgs& a, DecGeom geo, int max_ranges,
                        cudaStream_t stream) {
   const bool narrow = geo.G <= 8;
   const int ctas = narrow ? Shape<D, 1>::kCtas : Shape<D, 2>::kCtas;
   int grid = min(ctas * pool->num_sms, kMergeCounters);
   if (geo.range_tiles) grid = min(grid, max_ranges);
-  return narrow ? launch<D, 1, kQ8>(pool, a, geo, grid, stream)
-                : launch<D, 2, kQ8>(pool, a, geo, grid, stream);
+  return narrow ? launch<D, 1, kQ8, kJoin>(pool, a, geo, grid, stream)
+                : launch<D, 2, kQ8, kJoin>(pool, a, geo, grid, stream);
 }
 
 }  // namespace
@@ -844,7 +896,7 @@ size_t decode_share_workspace_bytes(const gc_kv_pool* pool) {
 }
 
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
-                            cudaStream_t stream, const Q8Pages* q8) {
+                            cudaStream_t stream, const Q8Pages* q8, const SpanGeom* span) {
   const auto& cfg = pool->cfg;
   DecGeom geo;
   geo.batch = a.batch;
@@ -867,6 +919,7 @@ gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const D
   geo.q8_layer_major = q8 && q8->layer_major ? 1 : 0;
   geo.q8_hdr = static_cast<uint32_t>(q8_header_bytes(cfg));
   geo.q8_chunk = static_cast<uint32_t>(q8_chunk_bytes(cfg));
+  geo.span = span ? *span : SpanGeom{};
   geo.range_tiles = split ? split->split_tiles : 0;
   geo.max_splits = split ? split->splits : 1;
   const DecodeUnits units = decode_units(static_cast<int64_t>(a.batch) * cfg.num_kv_heads,
@@ -878,10 +931,12 @@ gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const D
       split ? static_cast<long long>(a.batch) * cfg.num_kv_heads * split->splits : 0;
   const int max_ranges = static_cast<int>(ranges < kMergeCounters ? ranges : kMergeCounters);
   if (cfg.head_dim == 128)
-    return q8 ? launch_heads<128, true>(pool, a, geo, max_ranges, stream)
-              : launch_heads<128, false>(pool, a, geo, max_ranges, stream);
-  return q8 ? launch_heads<64, true>(pool, a, geo, max_ranges, stream)
-            : launch_heads<64, false>(pool, a, geo, max_ranges, stream);
+    return span ? launch_heads<128, false, true>(pool, a, geo, max_ranges, stream)
+           : q8 ? launch_heads<128, true, false>(pool, a, geo, max_ranges, stream)
+                : launch_heads<128, false, false>(pool, a, geo, max_ranges, stream);
+  return span ? launch_heads<64, false, true>(pool, a, geo, max_ranges, stream)
+         : q8 ? launch_heads<64, true, false>(pool, a, geo, max_ranges, stream)
+              : launch_heads<64, false, false>(pool, a, geo, max_ranges, stream);
 }
 
 }  // namespace gc

@@ -798,7 +798,10 @@ static gc_status span_common(const char* who, const gc_kv_pool* pool, int32_t la
 size_t gc_paged_cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
                                       int32_t max_blocks_per_seq, int32_t num_q_heads,
                                       int32_t total_new_tokens) {
-  return 0;
+  if (!pool || batch <= 0 || max_blocks_per_seq <= 0 || num_q_heads <= 0 || total_new_tokens <= 0 ||
+      num_q_heads % pool->cfg.num_kv_heads)
+    return 0;
+  return gc::cross_workspace_bytes(pool, batch, max_blocks_per_seq, num_q_heads, total_new_tokens);
 }
 
 gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool, const int32_t* block_table,
@@ -832,7 +835,11 @@ gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool, const int32
 size_t gc_shared_prefix_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
                                                int32_t num_groups, int32_t max_shared_blocks,
                                                int32_t max_blocks_per_seq, int32_t num_q_heads) {
-  return 0;
+  if (!pool || batch <= 0 || num_groups <= 0 || max_shared_blocks <= 0 ||
+      max_blocks_per_seq <= 0 || num_q_heads <= 0 || num_q_heads % pool->cfg.num_kv_heads)
+    return 0;
+  return gc::shared_decode_workspace_bytes(pool, batch, num_groups, max_shared_blocks,
+                                           max_blocks_per_seq, num_q_heads);
 }
 
 gc_status gc_shared_prefix_decode_attn(const void* q, const gc_kv_pool* pool,

@@ -181,6 +181,7 @@ struct AttnArgs {
   const int32_t* cu_new_lens;
   int32_t batch, max_blocks, layer, num_q_heads, total_new_tokens;
   float softmax_scale;
+  const char* who = "gc_prefix_prefill_attn";  // for messages
 };
 
 gc_status launch_attn_simt(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream);
@@ -243,8 +244,15 @@ gc_status launch_unpack_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pa
 // head_dim 128 prefill on CTA pairs (attn_tc2.cu), work items claimed from
 // `work_counter` (zeroed by the launch if it is needed); pages that `unpacked`
 // maps are read from there instead of the pool.
+// With `span`, every row sees all keys of its request (or group) and prefix_lens has
+// their numbers (span.cuh).
+struct SpanGeom;
 gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                          int* work_counter, const UnpackedPages* unpacked = nullptr);
+                          int* work_counter, const UnpackedPages* unpacked = nullptr,
+                          const SpanGeom* span = nullptr);
+// The same at head_dim 64, on single SMs.
+gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
+                              const SpanGeom& span);
 // Host-side bound of the attention kernels' 32-bit work numbering (items and
 // q rows of one call, with a margin of two claims per CTA of `grid`):
 // GC_ERR_UNSUPPORTED before anything is launched when a call could pass it.
@@ -260,6 +268,7 @@ struct DecodeArgs {
   float softmax_scale;
   void* workspace;
   size_t workspace_bytes;
+  const char* who = "gc_paged_decode_attn";  // for messages
 };
 struct DecodeSplit {
   int32_t splits, split_tiles;  // key ranges per request (at most), their 128-key tiles
@@ -269,14 +278,16 @@ DecodeSplit decode_split(const gc_kv_pool* pool, int32_t batch, int32_t max_bloc
                          int32_t num_q_heads);
 // With q8, the pages that q8->table maps (>= 0) are read from the 8-bit
 // image instead of the pool.
+// With span, the requests' keys come after shared prefixes whose pieces it names
+// (span.cuh).
 gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
-                        const Q8Pages* q8 = nullptr);
+                        const Q8Pages* q8 = nullptr, const SpanGeom* span = nullptr);
 // The decode kernel (decode_mma.cu).  split: key ranges with partials for the
 // merge kernel (head_dim 64); nullptr: equal shares, merged in the kernel
 // (head_dim 128).  With q8, the pages that q8->table maps (>= 0) are read from
 // the 8-bit image instead of the pool.
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
-                            cudaStream_t stream, const Q8Pages* q8);
+                            cudaStream_t stream, const Q8Pages* q8, const SpanGeom* span);
 size_t decode_share_workspace_bytes(const gc_kv_pool* pool);
 // Workspace bytes of a decode call on either path.
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
@@ -299,6 +310,11 @@ struct SpanArgs {
   void* workspace;
   size_t workspace_bytes;
 };
+size_t cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
+                             int32_t num_q_heads, int32_t total_new_tokens);
+size_t shared_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t groups,
+                                     int32_t max_shared_blocks, int32_t max_blocks,
+                                     int32_t num_q_heads);
 gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream);
 gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream);
 

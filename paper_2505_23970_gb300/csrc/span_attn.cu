@@ -1,141 +1,164 @@
-// Attention in which every row sees all keys of one or two page lists: cross
-// attention (a request's new tokens over its cached states of another sequence)
-// and decode behind a shared prefix (a request's one new token over its group's
-// shared pages, then its own).  One warp per (row, q head), fp32 throughout,
-// running maximum and sum over the keys read through the block tables.
+// Cross attention and decode behind a shared prefix on the tensor-core kernels.
+//
+// Both are attention whose rows see all keys of a page list: a request's new tokens
+// over its cached states, or all requests of a group (one token each) over the group's
+// shared pages.  The kernels of the prefill attention take them (attn_tc2.cu at
+// head_dim 128, attn_tc.cu at 64) without the causal limit, cut where the items alone
+// would leave SMs idle (span.cuh); the rows of a group's requests lie next to each
+// other, so the shared keys are read once for 256 of them.  Cross attention joins the
+// pieces of cut requests here.  Decode behind a shared prefix leaves every piece to the
+// decode kernel (decode_mma.cu), which starts each request from them and goes on over
+// its own keys.
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
+#include "span.cuh"
 
 namespace gc {
 namespace {
 
-using ptx::ex2_approx;
-
-struct SpanGeom {
-  int32_t Hq, Hkv, G, ps_shift, num_pages, layer, rows;
-  int32_t count[2], width[2];  // table rows and columns: [0] requests, [1] groups
-  float scale_log2;
-};
-
+// Joins the pieces of the requests that were cut: a warp's unit is one row of a
+// (request, kv head, tile), its columns spread over the lanes.
 template <int D>
-struct RowState {
-  static constexpr int E = D / 32;  // columns per lane
-  float q[E], o[E], m, l;
-};
-
-// Keys [0, n) of table row `row`.  False if a page is bad (its keys are left out).
-template <int D>
-__device__ bool add_keys(RowState<D>& r, const uint8_t* pool, const int32_t* table, int64_t row,
-                         int width, int n, int g, const SpanGeom& geo) {
-  constexpr int E = RowState<D>::E;
-  const int lane = threadIdx.x & 31, ps = 1 << geo.ps_shift;
-  const int64_t plane = static_cast<int64_t>(geo.num_pages) * geo.Hkv * ps * D;
-  const __nv_bfloat16* k =
-      reinterpret_cast<const __nv_bfloat16*>(pool) + static_cast<int64_t>(geo.layer) * 2 * plane;
-  bool good = true;
-  for (int j = 0; j < n; ++j) {
-    const int page = ld_plain(table + row * width + (j >> geo.ps_shift));
-    if (page < 0 || page >= geo.num_pages) {
-      good = false;
-      continue;
-    }
-    const int64_t at = ((static_cast<int64_t>(page) * geo.Hkv + g) * ps + (j & (ps - 1))) * D + lane * E;
-    float s = 0.f;
-    for (int e = 0; e < E; ++e) s += r.q[e] * __bfloat162float(k[at + e]);
-    for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-    const float m = fmaxf(r.m, s);
-    const float f = r.m == -INFINITY ? 0.f : ex2_approx(r.m - m), p = ex2_approx(s - m);
-    r.m = m;
-    r.l = r.l * f + p;
-    for (int e = 0; e < E; ++e) r.o[e] = r.o[e] * f + p * __bfloat162float(k[plane + at + e]);
-  }
-  return good;
-}
-
-__device__ int last_start(const int32_t* start, int count, int t) {
-  int lo = 0, hi = count;  // the last row whose start is <= t
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (ld_plain(start + mid) <= t) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-// kShared: a row is a request, start[] the groups' first requests; otherwise a row
-// is a new token, start[] the requests' first tokens.
-template <int D, bool kShared>
-__global__ void __launch_bounds__(128)
-    span_attn_kernel(const __nv_bfloat16* q, const uint8_t* pool, const int32_t* table,
-                     const int32_t* lens, const int32_t* shared_table, const int32_t* shared_lens,
-                     const int32_t* start, __nv_bfloat16* out, SpanGeom geo, int32_t* status) {
+__global__ void __launch_bounds__(256)
+    span_join_kernel(SpanGeom sp, const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
+                     __nv_bfloat16* out, int Hq, int Hkv, int G, int total_new) {
   dependent_begin();
-  constexpr int E = RowState<D>::E;
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  if (unit >= static_cast<int64_t>(geo.rows) * geo.Hq) return;
-  const int t = static_cast<int>(unit / geo.Hq), h = static_cast<int>(unit % geo.Hq);
-  const int count = geo.count[kShared ? 1 : 0];
-  const int s = last_start(start, count, t);
-  const int begin = ld_plain(start + s), end = ld_plain(start + s + 1);
-  bool good = begin >= 0 && t >= begin && t < end && end <= geo.rows;
-  const int b = kShared ? t : s;
-  const int n = good ? ld_plain(lens + b) : 0;
-  const int S = good && kShared ? ld_plain(shared_lens + s) : 0;
-  good = good && n >= 0 && S >= 0 && n <= static_cast<int64_t>(geo.width[0]) << geo.ps_shift &&
-         (!kShared || S <= static_cast<int64_t>(geo.width[1]) << geo.ps_shift);
-  if (good) {
-    RowState<D> r;
-    for (int e = 0; e < E; ++e) {
-      r.q[e] = __bfloat162float(q[unit * D + lane * E + e]) * geo.scale_log2;
-      r.o[e] = 0.f;
+  constexpr int kLanes = D / 4;  // four columns each
+  constexpr int kRowsPerBlock = 256 / kLanes;
+  constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of a tile
+  const int cuts = ld_plain(sp.cut), part_steps = ld_plain(sp.cut + 1);
+  if (cuts == 0) return;
+  // items are numbered by request, head, part and tile; here by request, tile and head
+  // in the place of the first part, so a unit's number is at most its item's
+  const int64_t units = static_cast<int64_t>(ld_plain(sp.cut + kCutFirst + cuts)) * kChunks;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int it = static_cast<int>(u / kChunks), chunk = static_cast<int>(u % kChunks);
+    int lo = 0, hi = cuts;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (ld_plain(sp.cut + kCutFirst + mid) <= it) lo = mid; else hi = mid;
     }
-    r.m = -INFINITY;
-    r.l = 0.f;
-    if (kShared) good = add_keys<D>(r, pool, shared_table, s, geo.width[1], S, h / geo.G, geo);
-    good &= add_keys<D>(r, pool, table, b, geo.width[0], n, h / geo.G, geo);
-    const float inv = r.l > 0.f ? 1.f / r.l : 0.f;  // no key: 0
-    for (int e = 0; e < E; ++e) out[unit * D + lane * E + e] = __float2bfloat16_rn(r.o[e] * inv);
+    const int first = ld_plain(sp.cut + kCutFirst + lo);
+    const SpanRequest r =
+        span_request(sp, ld_plain(sp.cut + kCutOrder + lo), total_new, lens, new_lens, cu);
+    if (r.n == 0) continue;
+    const int tiles = span_tiles(r.n, G), parts = span_parts(span_steps(r.T), part_steps);
+    const int local = it - first;
+    if (local >= Hkv * tiles) continue;
+    const int g = local / tiles, tile = local - g * tiles;
+    const int row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
+    const int at = tile * kSpanRows + row;  // q row of the request and kv head
+    if (at >= r.n * G) continue;
+    const int c = static_cast<int>(threadIdx.x) % kLanes;
+    const int64_t piece0 = first + static_cast<int64_t>(g) * parts * tiles + tile;
+    float M = -INFINITY, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < parts; s0 += 8) {
+      float2 ml[8];
+      float4 o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool in = s0 + k < parts;
+        const int64_t x = (piece0 + static_cast<int64_t>(s0 + k) * tiles) * sp.stride + row;
+        ml[k] = in ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
+        o[k] = in ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
+                  : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) Mn = fmaxf(Mn, ml[k].x);
+      const float f = M == -INFINITY ? 0.f : ptx::ex2_approx(M - Mn);
+      L *= f;
+      acc.x *= f;
+      acc.y *= f;
+      acc.z *= f;
+      acc.w *= f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float w = ml[k].x == -INFINITY ? 0.f : ptx::ex2_approx(ml[k].x - Mn);
+        L = fmaf(ml[k].y, w, L);
+        acc.x = fmaf(o[k].x, w, acc.x);
+        acc.y = fmaf(o[k].y, w, acc.y);
+        acc.z = fmaf(o[k].z, w, acc.z);
+        acc.w = fmaf(o[k].w, w, acc.w);
+      }
+      M = Mn;
+    }
+    const int64_t dst = (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c;
+    *reinterpret_cast<uint2*>(out + dst) = make_uint2(ptx::pack_bf16x2(acc.x / L, acc.y / L),
+                                                      ptx::pack_bf16x2(acc.z / L, acc.w / L));
   }
-  if (!good && lane == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
 }
 
-template <bool kShared>
-gc_status launch(const gc_kv_pool* pool, const SpanArgs& a, const char* who, cudaStream_t stream) {
-  const auto& cfg = pool->cfg;
-  SpanGeom geo;
-  geo.Hq = a.num_q_heads;
-  geo.Hkv = cfg.num_kv_heads;
-  geo.G = geo.Hq / geo.Hkv;
-  int s = 0;
-  while ((1 << s) < cfg.page_size) ++s;
-  geo.ps_shift = s;
-  geo.num_pages = cfg.num_pages;
-  geo.layer = a.layer;
-  geo.rows = a.rows;
-  geo.count[0] = a.batch;
-  geo.count[1] = a.groups;
-  geo.width[0] = a.max_blocks;
-  geo.width[1] = a.max_shared_blocks;
-  geo.scale_log2 = a.softmax_scale * 1.4426950408889634f;
-  const int64_t grid = (static_cast<int64_t>(a.rows) * geo.Hq + 3) / 4;
-  if (grid > 2147483647LL) return fail(GC_ERR_UNSUPPORTED, "%s: %d rows", who, a.rows);
-  const auto kernel = cfg.head_dim == 128 ? span_attn_kernel<128, kShared> : span_attn_kernel<64, kShared>;
-  const cudaError_t e = launch_dependent(
-      kernel, static_cast<unsigned>(grid), 128, 0, stream, static_cast<const __nv_bfloat16*>(a.q),
-      pool->data, a.block_table, a.lens, a.shared_table, a.shared_lens, a.start,
-      static_cast<__nv_bfloat16*>(a.out), geo, pool->status);
-  if (e != cudaSuccess) return cuda_fail(e, who);
-  return GC_OK;
+gc_status launch_items(const gc_kv_pool* pool, const AttnArgs& a, const SpanGeom& span,
+                       cudaStream_t stream) {
+  return pool->cfg.head_dim == 128
+             ? launch_attn_tc2(pool, a, stream, pool->work_counter, nullptr, &span)
+             : launch_attn_tc_span(pool, a, stream, span);
+}
+
+gc_status check_space(const char* who, size_t need, const void* workspace, size_t bytes) {
+  if (need == 0 || (workspace && bytes >= need)) return GC_OK;
+  return fail(GC_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, got %zu", who, need,
+              workspace ? bytes : 0);
 }
 
 }  // namespace
 
+size_t cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
+                             int32_t num_q_heads, int32_t total_new_tokens) {
+  return span_space(pool, total_new_tokens, batch, max_blocks, num_q_heads, false).end;
+}
+
 gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream) {
-  return launch<false>(pool, a, "gc_paged_cross_attn", stream);
+  const char* who = "gc_paged_cross_attn";
+  const auto& cfg = pool->cfg;
+  const SpanSpace space = span_space(pool, a.rows, a.batch, a.max_blocks, a.num_q_heads, false);
+  gc_status st = check_space(who, space.end, a.workspace, a.workspace_bytes);
+  if (st != GC_OK) return st;
+  const SpanGeom span = span_geom(space, static_cast<int64_t>(a.max_blocks) * cfg.page_size, false,
+                                  a.workspace);
+  const AttnArgs args{a.q, a.out, a.block_table, a.lens, a.new_lens, a.start, a.batch,
+                      a.max_blocks, a.layer, a.num_q_heads, a.rows, a.softmax_scale, who};
+  st = launch_items(pool, args, span, stream);
+  if (st != GC_OK || span.pieces == 0) return st;
+  const auto join = cfg.head_dim == 128 ? span_join_kernel<128> : span_join_kernel<64>;
+  const cudaError_t e = launch_dependent(
+      join, static_cast<unsigned>(4 * pool->num_sms), 256, 0, stream, span, a.lens, a.new_lens,
+      a.start, static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, cfg.num_kv_heads,
+      a.num_q_heads / cfg.num_kv_heads, a.rows);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return GC_OK;
+}
+
+size_t shared_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t groups,
+                                     int32_t max_shared_blocks, int32_t max_blocks,
+                                     int32_t num_q_heads) {
+  return span_space(pool, batch, groups, max_shared_blocks, num_q_heads, true).end +
+         decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
 }
 
 gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream) {
-  return launch<true>(pool, a, "gc_shared_prefix_decode_attn", stream);
+  const char* who = "gc_shared_prefix_decode_attn";
+  const auto& cfg = pool->cfg;
+  const SpanSpace space =
+      span_space(pool, a.batch, a.groups, a.max_shared_blocks, a.num_q_heads, true);
+  gc_status st = check_space(who,
+                             space.end + decode_workspace_bytes(pool, a.batch, a.max_blocks,
+                                                                a.num_q_heads),
+                             a.workspace, a.workspace_bytes);
+  if (st != GC_OK) return st;
+  const SpanGeom span = span_geom(
+      space, static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size, true, a.workspace);
+  const AttnArgs args{a.q, a.out, a.shared_table, a.shared_lens, nullptr, a.start, a.groups,
+                      a.max_shared_blocks, a.layer, a.num_q_heads, a.batch, a.softmax_scale, who};
+  st = launch_items(pool, args, span, stream);
+  if (st != GC_OK) return st;
+  const DecodeArgs own{a.q, a.out, a.block_table, a.lens, a.batch, a.max_blocks, a.layer,
+                       a.num_q_heads, a.softmax_scale,
+                       static_cast<uint8_t*>(a.workspace) + space.end,
+                       a.workspace_bytes - space.end, who};
+  return launch_decode(pool, own, stream, nullptr, &span);
 }
 
 }  // namespace gc
