@@ -33,13 +33,14 @@ __device__ __forceinline__ int request_splits(int T, int cap, int split_tiles) {
   return (tiles + split_tiles - 1) / split_tiles;
 }
 
-template <int D>
+// kParts: the sums and M go to `own` as they are.
+template <int D, bool kParts>
 __global__ void __launch_bounds__(D) decode_merge_kernel(const float* ws,
                                                          const int32_t* seq_lens,
                                                          int32_t batch, int32_t Hq,
                                                          int32_t max_splits, int32_t cap,
                                                          int32_t split_tiles,
-                                                         __nv_bfloat16* out) {
+                                                         __nv_bfloat16* out, DecodeParts own) {
   // launched as a programmatic dependent of the decode kernel: the
   // blocks may be resident before it ends, so wait for its results here
   dependent_begin();
@@ -74,6 +75,11 @@ __global__ void __launch_bounds__(D) decode_merge_kernel(const float* ws,
       acc = fmaf(os[t], f, acc);
       L = fmaf(mls[t].y, f, L);
     }
+  }
+  if (kParts) {
+    own.o[head * D + d] = acc;
+    if (d == 0) own.ml[head] = make_float2(M, L);
+    return;
   }
   out[head * D + d] = __float2bfloat16_rn(acc / L);
 }
@@ -115,7 +121,7 @@ size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max
 }
 
 gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
-                        const Q8Pages* q8, const SpanGeom* span) {
+                        const Q8Pages* q8) {
   if (a.batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", a.who, a.batch);
   const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
   if (cap > 2147483647LL)
@@ -149,13 +155,13 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
                 static_cast<unsigned long long>(pool_rows));
   if (q8 && static_cast<uint64_t>(q8->n_blocks) * pool->cfg.num_layers * 2 >= (1ull << 31))
     return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn_q8: image of %d blocks", q8->n_blocks);
-  const gc_status st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8, span);
+  const gc_status st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8);
   if (st != GC_OK || shares || sp.splits <= 1) return st;
   const cudaError_t e = launch_dependent(
-      decode_merge_kernel<64>,
+      a.own.o ? decode_merge_kernel<64, true> : decode_merge_kernel<64, false>,
       static_cast<unsigned>(a.batch) * static_cast<unsigned>(a.num_q_heads), 64, 0, stream,
       static_cast<const float*>(a.workspace), a.seq_lens, a.batch, a.num_q_heads, sp.splits,
-      static_cast<int32_t>(cap), sp.split_tiles, static_cast<__nv_bfloat16*>(a.out));
+      static_cast<int32_t>(cap), sp.split_tiles, static_cast<__nv_bfloat16*>(a.out), a.own);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
 }

@@ -55,7 +55,6 @@
 #include "decode_units.h"
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
-#include "span.cuh"
 
 namespace gc {
 namespace {
@@ -80,7 +79,7 @@ struct DecGeom {
   const int32_t* q8_table;   // >= 0: the image block holding the page
   int32_t q8_n_blocks, q8_layer_major;
   uint32_t q8_hdr, q8_chunk;
-  SpanGeom span;  // kJoin: the shared prefixes' pieces
+  DecodeParts own;  // kParts
 };
 
 // Threads and resident CTAs of a variant: NT tiles of 8 heads, d columns.  The
@@ -291,43 +290,6 @@ struct Acc {
       }
   }
 
-  // kJoin: start from the request's part of its group's shared prefix, as if its keys
-  // had been taken before.  (The sum goes to one of the lanes that share a head.)
-  __device__ __forceinline__ void join(const SpanGeom& sp, int b, int g, int G) {
-    const int4 pr = ld_plain(sp.prior + b);  // SpanPrior
-    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    if (pr.z <= 0) return;
-    first = false;
-    const int64_t row0 = (pr.x + static_cast<int64_t>(g) * pr.z * pr.y) * sp.stride + pr.w;
-    const int64_t step = static_cast<int64_t>(pr.y) * sp.stride;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int h = 8 * t + 2 * c + x;
-        if (h >= G) continue;
-        const float2* ml = sp.ml + row0 + h;
-        const float* op = sp.o + (row0 + h) * D + r * (D / 8);
-        float M = -INFINITY, L = 0.f;
-        for (int s = 0; s < pr.z; ++s) M = fmaxf(M, ld_plain(ml + s * step).x);
-        for (int s = 0; s < pr.z; ++s) {
-          const float2 y = ld_plain(ml + s * step);
-          const float f = y.x == -INFINITY ? 0.f : ex2_approx(y.x - M);
-          L = fmaf(y.y, f, L);
-#pragma unroll
-          for (int i = 0; i < D / 16; i += 2) {
-            const float4 v = ld_plain(reinterpret_cast<const float4*>(op + s * step * D + 2 * i));
-            o[t][i][x] = fmaf(v.x, f, o[t][i][x]);
-            o[t][i][x + 2] = fmaf(v.y, f, o[t][i][x + 2]);
-            o[t][i + 1][x] = fmaf(v.z, f, o[t][i + 1][x]);
-            o[t][i + 1][x + 2] = fmaf(v.w, f, o[t][i + 1][x + 2]);
-          }
-        }
-        m[t][x] = M;
-        l[t][x] = r == 0 ? L : 0.f;
-      }
-  }
-
   // S^T of a group
   template <int E>
   __device__ __forceinline__ void scores(const Keys<D, E>& f, uint64_t sk2, float (&s)[NT][4]) {
@@ -462,16 +424,11 @@ __device__ __forceinline__ Where look_up(const DecGeom& geo, const DecPiece& w, 
 // pair starts c0's share, slot 0 of the others):
 //     out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  M = max_s m_s,
 // four columns of one head per thread at a time.  The partials come from other
-// SMs, so they are read through L2.
-// 1 / sum; a request behind a shared prefix may have no key at all: its row is 0.
-template <bool kJoin>
-__device__ __forceinline__ float inverse(float l) {
-  return kJoin && l == 0.f ? 0.f : 1.f / l;
-}
-
-template <int D, int NT>
+// SMs, so they are read through L2.  kParts: the sums and M go to own_o and own_ml.
+template <int D, int NT, bool kParts>
 __device__ void merge_shares(const float* part_o, const float2* part_ml, int c0, int c1,
-                             int first_slot, int G, __nv_bfloat16* out_g) {
+                             int first_slot, int G, __nv_bfloat16* out_g, float* own_o,
+                             float2* own_ml) {
   using S = Shape<D, NT>;
   for (int x = threadIdx.x; x < G * (D / 4); x += S::kThreads) {
     const int h = x / (D / 4), d4 = x % (D / 4);
@@ -510,6 +467,11 @@ __device__ void merge_shares(const float* part_o, const float2* part_ml, int c0,
       }
       M = Mn;
     }
+    if constexpr (kParts) {
+      *reinterpret_cast<float4*>(own_o + h * D + 4 * d4) = acc;
+      if (d4 == 0) own_ml[h] = make_float2(M, L);
+      continue;
+    }
     uint2 pk;
     pk.x = pack_bf16x2(acc.x / L, acc.y / L);
     pk.y = pack_bf16x2(acc.z / L, acc.w / L);
@@ -522,9 +484,9 @@ __device__ __forceinline__ void prefetch_l2(uint64_t at) {
 }
 
 // ------------------------------------------------------------------- kernel
-// kJoin: seq_lens counts the keys after a shared prefix whose results are in pieces
-// (span.cuh); a request may then have no keys of its own.
-template <int D, int NT, bool kQ8, bool kJoin>
+// kParts: the keys are a part of each request's (those after a shared prefix), and the
+// results go to geo.own; a request may have none of them.
+template <int D, int NT, bool kQ8, bool kParts>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     decode_mma_kernel(const __nv_bfloat16* q, const int32_t* block_table,
                       const int32_t* seq_lens, __nv_bfloat16* out,
@@ -551,16 +513,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     int most = 0, n = 0;
     for (int b = threadIdx.x; b < geo.batch; b += S::kThreads) {
       const int T = ld_plain(seq_lens + b);
-      const bool bad = T < (kJoin ? 0 : 1) || T > cap ||
-                       (kJoin && ld_plain(geo.span.prior + b).z < 0);
-      if (bad) {
-        if (blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+      if (T < 1 || T > cap) {
+        if (blockIdx.x == 0 && !(kParts && T == 0)) record_error(status, GC_ERR_OUT_OF_RANGE);
       } else {
         most = max(most, T);
         ++n;
       }
-      // (kJoin: without own keys, the work of one)
-      start[b] = bad ? 0 : kJoin ? max(T, 1) : T;
+      start[b] = T < 1 || T > cap ? 0 : T;
     }
     most = __reduce_max_sync(0xffffffffu, most);
     n = __reduce_add_sync(0xffffffffu, n);
@@ -659,7 +618,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     acc.reset();
     const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq + w.g * geo.G;
     acc.load_q(q + head0 * D, geo.G);
-    if (kJoin && w.k0 == 0 && first == 0) acc.join(geo.span, w.b, w.g, geo.G);
     Where nxt{0, 0.f, 0.f};
     if (key_of(32) < k1)
       nxt = look_up<D, kQ8>(geo, w, key_of(32 + lane), pool_k, block_table, status);
@@ -754,7 +712,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
         for (int x = 0; x < 2; ++x) {
           const int h = 8 * t + 2 * (lane & 3) + x;
           if (h >= geo.G) continue;
-          const float inv = inverse<kJoin>(acc.l[t][x]);
+          if constexpr (kParts) {
+            float4* dst = reinterpret_cast<float4*>(geo.own.o + (head0 + h) * D +
+                                                    (lane >> 2) * (D / 8));
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v)
+              dst[v] = make_float4(acc.o[t][2 * v][x], acc.o[t][2 * v][x + 2],
+                                   acc.o[t][2 * v + 1][x], acc.o[t][2 * v + 1][x + 2]);
+            if (lane < 4) geo.own.ml[head0 + h] = make_float2(acc.m[t][x], acc.l[t][x]);
+            continue;
+          }
+          const float inv = 1.f / acc.l[t][x];
           uint4* dst = reinterpret_cast<uint4*>(out + (head0 + h) * D + (lane >> 2) * (D / 8));
 #pragma unroll
           for (int v = 0; v < D / 64; ++v) {
@@ -816,9 +784,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
         o.x += v.x;
         o.y += v.y;
       }
+      if constexpr (kParts) {
+        if (w.part < 0) {
+          *reinterpret_cast<float2*>(geo.own.o + (head0 + h) * D + d) = o;
+          if (d == 0) geo.own.ml[head0 + h] = make_float2(M, L);
+          continue;
+        }
+      }
       if (w.part < 0) {
-        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) =
-            kJoin && L == 0.f ? 0u : pack_bf16x2(o.x / L, o.y / L);
+        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) = pack_bf16x2(o.x / L, o.y / L);
       } else {
         *reinterpret_cast<float2*>(ws + (part0 + h * part_step) * D + d) = o;
         if (d == 0) part_ml[part0 + h * part_step] = make_float2(M, L);
@@ -841,8 +815,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
       }
       __syncthreads();
       if (merge_flag)
-        merge_shares<D, NT>(ws, part_ml, c0, c1, c0 * per >= pair0 ? 0 : 1, geo.G,
-                            out + head0 * D);
+        merge_shares<D, NT, kParts>(ws, part_ml, c0, c1, c0 * per >= pair0 ? 0 : 1, geo.G,
+                                    out + head0 * D, kParts ? geo.own.o + head0 * D : nullptr,
+                                    kParts ? geo.own.ml + head0 : nullptr);
     }
     __syncthreads();  // the merge buffers are free again
   }
@@ -855,12 +830,12 @@ size_t smem_bytes(int batch) {
          (static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 
-template <int D, int NT, bool kQ8, bool kJoin>
+template <int D, int NT, bool kQ8, bool kParts>
 gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo, int grid,
                  cudaStream_t stream) {
   using S = Shape<D, NT>;
   const size_t smem = smem_bytes<D, NT>(a.batch);
-  auto kernel = decode_mma_kernel<D, NT, kQ8, kJoin>;
+  auto kernel = decode_mma_kernel<D, NT, kQ8, kParts>;
   cudaError_t e = cudaSuccess;
   // a block gets 48 KB without asking, its static words (well below 1 KB) included
   if (smem > 47 * 1024)
@@ -875,15 +850,15 @@ gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo
   return GC_OK;
 }
 
-template <int D, bool kQ8, bool kJoin>
+template <int D, bool kQ8, bool kParts>
 gc_status launch_heads(const gc_kv_pool* pool, const DecodeArgs& a, DecGeom geo, int max_ranges,
                        cudaStream_t stream) {
   const bool narrow = geo.G <= 8;
   const int ctas = narrow ? Shape<D, 1>::kCtas : Shape<D, 2>::kCtas;
   int grid = min(ctas * pool->num_sms, kMergeCounters);
   if (geo.range_tiles) grid = min(grid, max_ranges);
-  return narrow ? launch<D, 1, kQ8, kJoin>(pool, a, geo, grid, stream)
-                : launch<D, 2, kQ8, kJoin>(pool, a, geo, grid, stream);
+  return narrow ? launch<D, 1, kQ8, kParts>(pool, a, geo, grid, stream)
+                : launch<D, 2, kQ8, kParts>(pool, a, geo, grid, stream);
 }
 
 }  // namespace
@@ -896,7 +871,7 @@ size_t decode_share_workspace_bytes(const gc_kv_pool* pool) {
 }
 
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
-                            cudaStream_t stream, const Q8Pages* q8, const SpanGeom* span) {
+                            cudaStream_t stream, const Q8Pages* q8) {
   const auto& cfg = pool->cfg;
   DecGeom geo;
   geo.batch = a.batch;
@@ -919,7 +894,7 @@ gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const D
   geo.q8_layer_major = q8 && q8->layer_major ? 1 : 0;
   geo.q8_hdr = static_cast<uint32_t>(q8_header_bytes(cfg));
   geo.q8_chunk = static_cast<uint32_t>(q8_chunk_bytes(cfg));
-  geo.span = span ? *span : SpanGeom{};
+  geo.own = a.own;
   geo.range_tiles = split ? split->split_tiles : 0;
   geo.max_splits = split ? split->splits : 1;
   const DecodeUnits units = decode_units(static_cast<int64_t>(a.batch) * cfg.num_kv_heads,
@@ -931,12 +906,12 @@ gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const D
       split ? static_cast<long long>(a.batch) * cfg.num_kv_heads * split->splits : 0;
   const int max_ranges = static_cast<int>(ranges < kMergeCounters ? ranges : kMergeCounters);
   if (cfg.head_dim == 128)
-    return span ? launch_heads<128, false, true>(pool, a, geo, max_ranges, stream)
-           : q8 ? launch_heads<128, true, false>(pool, a, geo, max_ranges, stream)
-                : launch_heads<128, false, false>(pool, a, geo, max_ranges, stream);
-  return span ? launch_heads<64, false, true>(pool, a, geo, max_ranges, stream)
-         : q8 ? launch_heads<64, true, false>(pool, a, geo, max_ranges, stream)
-              : launch_heads<64, false, false>(pool, a, geo, max_ranges, stream);
+    return a.own.o ? launch_heads<128, false, true>(pool, a, geo, max_ranges, stream)
+           : q8    ? launch_heads<128, true, false>(pool, a, geo, max_ranges, stream)
+                   : launch_heads<128, false, false>(pool, a, geo, max_ranges, stream);
+  return a.own.o ? launch_heads<64, false, true>(pool, a, geo, max_ranges, stream)
+         : q8    ? launch_heads<64, true, false>(pool, a, geo, max_ranges, stream)
+                 : launch_heads<64, false, false>(pool, a, geo, max_ranges, stream);
 }
 
 }  // namespace gc

@@ -259,6 +259,12 @@ gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStr
 gc_status check_item_bound(const gc_kv_pool* pool, const AttnArgs& a, int grid);
 
 // Paged decode attention (one new token per request), split-KV.
+// Results over a part of each request's keys, per [request][q head]: O unscaled [d],
+// reference maximum in log2 units and sum.  (Not written for a request without keys.)
+struct DecodeParts {
+  float* o;
+  float2* ml;
+};
 struct DecodeArgs {
   const void* q;
   void* out;
@@ -269,6 +275,7 @@ struct DecodeArgs {
   void* workspace;
   size_t workspace_bytes;
   const char* who = "gc_paged_decode_attn";  // for messages
+  DecodeParts own = {nullptr, nullptr};      // given: the results go there instead of to out
 };
 struct DecodeSplit {
   int32_t splits, split_tiles;  // key ranges per request (at most), their 128-key tiles
@@ -278,16 +285,14 @@ DecodeSplit decode_split(const gc_kv_pool* pool, int32_t batch, int32_t max_bloc
                          int32_t num_q_heads);
 // With q8, the pages that q8->table maps (>= 0) are read from the 8-bit
 // image instead of the pool.
-// With span, the requests' keys come after shared prefixes whose pieces it names
-// (span.cuh).
 gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
-                        const Q8Pages* q8 = nullptr, const SpanGeom* span = nullptr);
+                        const Q8Pages* q8 = nullptr);
 // The decode kernel (decode_mma.cu).  split: key ranges with partials for the
 // merge kernel (head_dim 64); nullptr: equal shares, merged in the kernel
 // (head_dim 128).  With q8, the pages that q8->table maps (>= 0) are read from
 // the 8-bit image instead of the pool.
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
-                            cudaStream_t stream, const Q8Pages* q8, const SpanGeom* span);
+                            cudaStream_t stream, const Q8Pages* q8);
 size_t decode_share_workspace_bytes(const gc_kv_pool* pool);
 // Workspace bytes of a decode call on either path.
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,

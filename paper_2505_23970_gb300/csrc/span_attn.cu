@@ -5,10 +5,9 @@
 // shared pages.  The kernels of the prefill attention take them (attn_tc2.cu at
 // head_dim 128, attn_tc.cu at 64) without the causal limit, cut where the items alone
 // would leave SMs idle (span.cuh); the rows of a group's requests lie next to each
-// other, so the shared keys are read once for 256 of them.  Cross attention joins the
-// pieces of cut requests here.  Decode behind a shared prefix leaves every piece to the
-// decode kernel (decode_mma.cu), which starts each request from them and goes on over
-// its own keys.
+// other, so the shared keys are read once for 256 of them.  The pieces of cut requests are
+// joined here, those of a shared prefix with what the decode kernel (decode_mma.cu)
+// has for the request's own keys.
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
 #include "span.cuh"
@@ -16,8 +15,67 @@
 namespace gc {
 namespace {
 
-// Joins the pieces of the requests that were cut: a warp's unit is one row of a
-// (request, kv head, tile), its columns spread over the lanes.
+// One row's join over its pieces and, last, another part (m, l, o): four columns of a
+// row per thread, eight pieces' loads in flight.
+struct Join {
+  float M = -INFINITY, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+
+  // piece rows x0, x0 + step, ...
+  template <int D>
+  __device__ __forceinline__ void pieces(const SpanGeom& sp, int64_t x0, int64_t step, int parts,
+                                         int c) {
+    constexpr int kBatch = 8;
+    for (int s0 = 0; s0 < parts; s0 += kBatch) {
+      float2 ml[kBatch];
+      float4 o[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const bool in = s0 + k < parts;
+        const int64_t x = x0 + (s0 + k) * step;
+        ml[k] = in ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
+        o[k] = in ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
+                  : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) Mn = fmaxf(Mn, ml[k].x);
+      rescale(Mn);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) add(ml[k], o[k]);
+    }
+  }
+  __device__ __forceinline__ void part(const float2& ml, const float4& o) {
+    rescale(fmaxf(M, ml.x));
+    add(ml, o);
+  }
+  __device__ __forceinline__ uint2 rounded() const {
+    const float inv = L == 0.f ? 0.f : 1.f / L;  // (no key at all)
+    return make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv),
+                      ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
+  }
+
+ private:
+  __device__ __forceinline__ void rescale(float Mn) {
+    const float f = M == -INFINITY ? 0.f : ptx::ex2_approx(M - Mn);
+    L *= f;
+    acc.x *= f;
+    acc.y *= f;
+    acc.z *= f;
+    acc.w *= f;
+    M = Mn;
+  }
+  __device__ __forceinline__ void add(const float2& ml, const float4& o) {
+    const float w = ml.x == -INFINITY ? 0.f : ptx::ex2_approx(ml.x - M);
+    L = fmaf(ml.y, w, L);
+    acc.x = fmaf(o.x, w, acc.x);
+    acc.y = fmaf(o.y, w, acc.y);
+    acc.z = fmaf(o.z, w, acc.z);
+    acc.w = fmaf(o.w, w, acc.w);
+  }
+};
+
+// Cross attention: the rows of the requests that were cut.
 template <int D>
 __global__ void __launch_bounds__(256)
     span_join_kernel(SpanGeom sp, const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
@@ -28,7 +86,7 @@ __global__ void __launch_bounds__(256)
   constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of a tile
   const int cuts = ld_plain(sp.cut), part_steps = ld_plain(sp.cut + 1);
   if (cuts == 0) return;
-  // items are numbered by request, head, part and tile; here by request, tile and head
+  // items are numbered by request, head, part and tile; here by request, head and tile
   // in the place of the first part, so a unit's number is at most its item's
   const int64_t units = static_cast<int64_t>(ld_plain(sp.cut + kCutFirst + cuts)) * kChunks;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -51,43 +109,39 @@ __global__ void __launch_bounds__(256)
     if (at >= r.n * G) continue;
     const int c = static_cast<int>(threadIdx.x) % kLanes;
     const int64_t piece0 = first + static_cast<int64_t>(g) * parts * tiles + tile;
-    float M = -INFINITY, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < parts; s0 += 8) {
-      float2 ml[8];
-      float4 o[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const bool in = s0 + k < parts;
-        const int64_t x = (piece0 + static_cast<int64_t>(s0 + k) * tiles) * sp.stride + row;
-        ml[k] = in ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
-        o[k] = in ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
-                  : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      float Mn = M;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) Mn = fmaxf(Mn, ml[k].x);
-      const float f = M == -INFINITY ? 0.f : ptx::ex2_approx(M - Mn);
-      L *= f;
-      acc.x *= f;
-      acc.y *= f;
-      acc.z *= f;
-      acc.w *= f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float w = ml[k].x == -INFINITY ? 0.f : ptx::ex2_approx(ml[k].x - Mn);
-        L = fmaf(ml[k].y, w, L);
-        acc.x = fmaf(o[k].x, w, acc.x);
-        acc.y = fmaf(o[k].y, w, acc.y);
-        acc.z = fmaf(o[k].z, w, acc.z);
-        acc.w = fmaf(o[k].w, w, acc.w);
-      }
-      M = Mn;
-    }
-    const int64_t dst = (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c;
-    *reinterpret_cast<uint2*>(out + dst) = make_uint2(ptx::pack_bf16x2(acc.x / L, acc.y / L),
-                                                      ptx::pack_bf16x2(acc.z / L, acc.w / L));
+    Join j;
+    j.pieces<D>(sp, piece0 * sp.stride + row, static_cast<int64_t>(tiles) * sp.stride, parts, c);
+    *reinterpret_cast<uint2*>(
+        out + (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c) =
+        j.rounded();
   }
+}
+
+// Decode behind a shared prefix: every row of a request that is not skipped.
+template <int D>
+__global__ void __launch_bounds__(256)
+    shared_join_kernel(SpanGeom sp, const int32_t* own_lens, int own_cap, DecodeParts own,
+                       __nv_bfloat16* out, int Hq, int G, int64_t rows, int32_t* status) {
+  dependent_begin();
+  constexpr int kLanes = D / 4;
+  const int c = static_cast<int>(threadIdx.x) % kLanes;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
+  if (row >= rows) return;
+  const int b = static_cast<int>(row / Hq), h = static_cast<int>(row - static_cast<int64_t>(b) * Hq);
+  const int T = ld_plain(own_lens + b);
+  const int4 p = ld_plain(sp.prior + b);  // SpanPrior
+  if (p.z < 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+  if (T < 0 || T > own_cap || p.z < 0) return;
+  const float2 ml = T > 0 ? ld_plain(own.ml + row) : make_float2(-INFINITY, 0.f);
+  const float4 o = T > 0 ? ld_plain(reinterpret_cast<const float4*>(own.o + row * D) + c)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
+  const int g = h / G;
+  const int64_t piece0 = p.x + static_cast<int64_t>(g) * p.z * p.y;
+  Join j;
+  j.pieces<D>(sp, piece0 * sp.stride + p.w + (h - g * G), static_cast<int64_t>(p.y) * sp.stride,
+              p.z, c);
+  j.part(ml, o);
+  *reinterpret_cast<uint2*>(out + row * D + 4 * c) = j.rounded();
 }
 
 gc_status launch_items(const gc_kv_pool* pool, const AttnArgs& a, const SpanGeom& span,
@@ -131,34 +185,61 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
   return GC_OK;
 }
 
+// A shared call's workspace: the prefixes' pieces, the own parts, then the decode
+// kernel's.
+struct SharedSpace {
+  SpanSpace span;
+  size_t ml, o, decode, end;
+};
+static SharedSpace shared_space(const gc_kv_pool* pool, int32_t batch, int32_t groups,
+                                int32_t max_shared_blocks, int32_t max_blocks,
+                                int32_t num_q_heads) {
+  SharedSpace s;
+  s.span = span_space(pool, batch, groups, max_shared_blocks, num_q_heads, true);
+  const size_t rows = static_cast<size_t>(batch) * num_q_heads;
+  s.ml = s.span.end;
+  s.o = s.ml + (rows * sizeof(float2) + 255) / 256 * 256;
+  s.decode = s.o + rows * pool->cfg.head_dim * sizeof(float);  // (rows of 256 bytes or more)
+  s.end = s.decode + decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
+  return s;
+}
+
 size_t shared_decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t groups,
                                      int32_t max_shared_blocks, int32_t max_blocks,
                                      int32_t num_q_heads) {
-  return span_space(pool, batch, groups, max_shared_blocks, num_q_heads, true).end +
-         decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
+  return shared_space(pool, batch, groups, max_shared_blocks, max_blocks, num_q_heads).end;
 }
 
 gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream) {
   const char* who = "gc_shared_prefix_decode_attn";
   const auto& cfg = pool->cfg;
-  const SpanSpace space =
-      span_space(pool, a.batch, a.groups, a.max_shared_blocks, a.num_q_heads, true);
-  gc_status st = check_space(who,
-                             space.end + decode_workspace_bytes(pool, a.batch, a.max_blocks,
-                                                                a.num_q_heads),
-                             a.workspace, a.workspace_bytes);
+  const SharedSpace space =
+      shared_space(pool, a.batch, a.groups, a.max_shared_blocks, a.max_blocks, a.num_q_heads);
+  gc_status st = check_space(who, space.end, a.workspace, a.workspace_bytes);
   if (st != GC_OK) return st;
+  uint8_t* w = static_cast<uint8_t*>(a.workspace);
   const SpanGeom span = span_geom(
-      space, static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size, true, a.workspace);
+      space.span, static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size, true, w);
+  DecodeArgs own{a.q, a.out, a.block_table, a.lens, a.batch, a.max_blocks, a.layer, a.num_q_heads,
+                 a.softmax_scale, w + space.decode, space.end - space.decode, who,
+                 DecodeParts{reinterpret_cast<float*>(w + space.o),
+                             reinterpret_cast<float2*>(w + space.ml)}};
+  st = launch_decode(pool, own, stream);
+  if (st != GC_OK) return st;
   const AttnArgs args{a.q, a.out, a.shared_table, a.shared_lens, nullptr, a.start, a.groups,
                       a.max_shared_blocks, a.layer, a.num_q_heads, a.batch, a.softmax_scale, who};
   st = launch_items(pool, args, span, stream);
   if (st != GC_OK) return st;
-  const DecodeArgs own{a.q, a.out, a.block_table, a.lens, a.batch, a.max_blocks, a.layer,
-                       a.num_q_heads, a.softmax_scale,
-                       static_cast<uint8_t*>(a.workspace) + space.end,
-                       a.workspace_bytes - space.end, who};
-  return launch_decode(pool, own, stream, nullptr, &span);
+  const int64_t rows = static_cast<int64_t>(a.batch) * a.num_q_heads;
+  const int per_block = 256 / (cfg.head_dim / 4);
+  const auto join = cfg.head_dim == 128 ? shared_join_kernel<128> : shared_join_kernel<64>;
+  const cudaError_t e = launch_dependent(
+      join, static_cast<unsigned>((rows + per_block - 1) / per_block), 256, 0, stream, span, a.lens,
+      static_cast<int>(static_cast<int64_t>(a.max_blocks) * cfg.page_size), own.own,
+      static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, a.num_q_heads / cfg.num_kv_heads, rows,
+      pool->status);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return GC_OK;
 }
 
 }  // namespace gc
