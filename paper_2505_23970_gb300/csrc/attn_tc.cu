@@ -72,6 +72,7 @@ constexpr int kThreadsQ8 = 512;
 // Batches up to this size are numbered longest request first (ranked in
 // shared memory by every CTA); larger batches keep the given order.
 constexpr int kSortMax = 512;
+constexpr int kOwnBytes = 72 * 1024;  // kOwn: shared memory of a group that decodes own keys
 constexpr int kRegsProducer = 88;   // warps 0-3 after setmaxnreg.dec
 constexpr int kRegsSoftmax = 208;   // warps 4-11 after setmaxnreg.inc
 static_assert(128 * kRegsProducer + 256 * kRegsSoftmax <= kThreads * 168,
@@ -122,6 +123,7 @@ struct Geom {
   uint32_t q8_hdr, q8_chunk;  // scale header and whole chunk (one block, layer, plane), bytes
   UnpackedGeom unpacked;  // pages dequantised beforehand (Pages::kUnpacked)
   SpanGeom span;          // kSpan
+  OwnDecode own;          // kOwn
 };
 
 struct Barriers {
@@ -133,7 +135,7 @@ struct Barriers {
   int item_slot[2];
   uint32_t tmem_base;
   int abort_flag;
-  int part_steps;  // kSpan: steps of a part of an item's keys
+  int share, workers;  // kSpan: units of a share (0: whole items), workers that have one
   int p0_steps;  // P tiles tile 0's softmax has published so far (pacing hint)
 };
 
@@ -148,8 +150,9 @@ struct Item {
   bool valid[2];
 };
 struct SpanItem : Item {
-  int j0;      // first K/V step of the item's part
-  bool piece;  // the result goes to the workspace
+  int j0;    // first K/V step of the piece
+  int slot;  // the piece's, -1 for a whole item
+  int next;  // unit after it
 };
 template <bool kSpan>
 using ItemOf = std::conditional_t<kSpan, SpanItem, Item>;
@@ -159,14 +162,39 @@ __device__ __forceinline__ int first_key(const SpanItem& w, int j) { return (w.j
 // item_start[p] = first item of the p-th request in work order; the request
 // itself is order[p] when the batch was sorted (order != nullptr), else p.
 // kSpan: prefix_lens has the numbers of keys, every row sees all of its request's, or of
-// a part of them; items are numbered by kv head, part and pair of tiles (the tiles that
-// read the same keys run at the same time).
+// a piece's range of steps; `it` is then a unit of this CTA's share, if share != 0.
 template <bool kSpan>
 __device__ __forceinline__ bool decode_item(int it, const int* item_start, const Geom& geo,
-                                            int part_steps, const int32_t* prefix_lens,
+                                            int share, const int32_t* prefix_lens,
                                             const int32_t* new_lens,
                                             const int32_t* cu_new_lens,
                                             ItemOf<kSpan>& w) {
+  if constexpr (kSpan) {
+    const int worker = static_cast<int>(blockIdx.x);
+    const SpanPiece r = span_piece(
+        it, share, worker, share ? min(item_start[geo.batch], (worker + 1) * share) : 0, geo.batch,
+        item_start, reinterpret_cast<const int16_t*>(item_start + geo.batch + 1), geo.Hkv, geo.G,
+        [&](int b) {
+          return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
+        });
+    w.b = r.b;
+    w.g = r.g;
+    w.j0 = r.j0;
+    w.T = r.T;
+    w.n = r.n;
+    w.cu = r.cu;
+    w.nt = r.nt;
+    w.slot = r.slot;
+    w.next = r.next;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r0 = (r.tile * 2 + i) * kTileM;
+      w.valid[i] = r0 < r.n * geo.G;
+      w.tok0[i] = r0 / geo.G;
+      w.nt_i[i] = w.valid[i] ? w.nt : 0;
+    }
+    return true;
+  }
   int lo = 0, hi = geo.batch;  // last b with item_start[b] <= it
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -177,28 +205,6 @@ __device__ __forceinline__ bool decode_item(int it, const int* item_start, const
                                        : lo;
   w.b = b;
   const int local = it - item_start[lo];
-  if constexpr (kSpan) {
-    const SpanRequest r =
-        span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
-    const int steps = span_steps(r.T), tiles = span_tiles(r.n, geo.G);
-    const int parts = span_parts(steps, part_steps);
-    const int head_part = local / tiles, pair = local - head_part * tiles;
-    w.g = head_part / parts;
-    w.j0 = (head_part - w.g * parts) * part_steps;
-    w.T = r.T;
-    w.n = r.n;
-    w.cu = r.cu;
-    w.nt = min(part_steps, steps - w.j0);
-    w.piece = geo.span.shared || parts > 1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r0 = (pair * 2 + i) * kTileM;
-      w.valid[i] = r0 < r.n * geo.G;
-      w.tok0[i] = r0 / geo.G;
-      w.nt_i[i] = w.valid[i] ? w.nt : 0;
-    }
-    return true;
-  }
   const int pairs = (item_start[lo + 1] - item_start[lo]) / geo.Hkv;
   const int pair = pairs - 1 - local / geo.Hkv;  // later rows (more keys) first
   w.g = local % geo.Hkv;
@@ -242,6 +248,33 @@ __device__ __forceinline__ int claim_item(Barriers& bar, uint32_t k, int* work_c
     mbar_arrive(&bar.item_full[s]);
   }
   return __shfl_sync(0xffffffffu, it, 0);
+}
+
+// The same for the next piece of this CTA's share, from `unit` on; the item is decoded
+// here because a share may end in front of an item's first step.
+template <int D, bool kSpan>
+__device__ __forceinline__ int claim_piece(Barriers& bar, uint32_t k, int& unit,
+                                           const int* item_start, const Geom& geo, int share,
+                                           const int32_t* prefix_lens, const int32_t* new_lens,
+                                           const int32_t* cu_new_lens, ItemOf<kSpan>& w,
+                                           volatile int* abortp, bool& ok) {
+  const int s = k & 1;
+  ok = mbar_wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1, abortp);
+  ok = __all_sync(0xffffffffu, ok);
+  int it = -1;
+  const int end = min(item_start[geo.batch], (static_cast<int>(blockIdx.x) + 1) * share);
+  if constexpr (kSpan) {
+    if (unit < end) {
+      decode_item<kSpan>(unit, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
+      if (w.nt > 0) it = unit;
+      unit = w.next;
+    }
+  }
+  if ((threadIdx.x & 31) == 0 && ok) {
+    bar.item_slot[s] = it;
+    mbar_arrive(&bar.item_full[s]);
+  }
+  return it;
 }
 
 // Read item k of the ring (all consumer threads); the caller releases the
@@ -369,7 +402,7 @@ __device__ void converter(uint8_t* smem_kv, Barriers& bar, Q8State& q8, const Ge
 template <int D, Pages kPages, bool kSpan>
 __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8State* q8,
                          const int* item_start, int total_items, const Geom& geo,
-                         int part_steps, const CUtensorMap* map_q, const CUtensorMap* map_kv,
+                         int share, const CUtensorMap* map_q, const CUtensorMap* map_kv,
                          const CUtensorMap* map_img,
                          const int32_t* block_table,
                          const int32_t* prefix_lens,
@@ -385,14 +418,23 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
   uint32_t armed8 = 0, armed8_par = 0;  // the same for the code copies of image pages
   int armed_q = -1, armed_vfix = -1;
   bool ok = true;
+  int unit = 0;  // kSpan, shares: this CTA's next
+  if (kSpan && share)
+    unit = static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * share,
+                                static_cast<int64_t>(total_items)));
   const uint32_t box_bytes = static_cast<uint32_t>(geo.ps) * 128;  // one page, one column block
   const uint32_t page_codes = static_cast<uint32_t>(geo.ps) * D;   // one page of 8-bit codes
 
   for (uint32_t k = 0; ok; ++k) {
-    const int it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
-    if (!ok || it < 0) break;
     ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
+    int it;
+    if (kSpan && share)
+      it = claim_piece<D, kSpan>(bar, k, unit, item_start, geo, share, prefix_lens, new_lens,
+                                 cu_new_lens, w, abortp, ok);
+    else
+      it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
+    if (!ok || it < 0) break;
+    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
     // ---- Q tiles
     ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
     if (!ok) break;
@@ -589,7 +631,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
 template <int D, bool kSpan>
 __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, uint32_t tmem,
                            const int* item_start, int total_items, const Geom& geo,
-                           int part_steps, const int32_t* prefix_lens,
+                           int share, const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens) {
   using C = Cfg<D>;
@@ -608,7 +650,7 @@ __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& b
     mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
     ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
+    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -787,7 +829,7 @@ __device__ __forceinline__ bool tile_exp_after(const uint32_t (&sr)[4][32], uint
 
 template <int D, int i, bool kSpan>
 __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
-                           int total_items, const Geom& geo, int part_steps,
+                           int total_items, const Geom& geo, int share,
                            const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens,
@@ -811,7 +853,7 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     if ((threadIdx.x & 31) == 0) mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
     ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, part_steps, prefix_lens, new_lens, cu_new_lens, w);
+    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -900,12 +942,14 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     if (rel) release(w.nt_i[i] - 1, 1);
     tc_fence_after();
     const int h = w.g * geo.G + r % geo.G;
-    bool piece = false;
-    if constexpr (kSpan) piece = w.piece;
-    if (kSpan && piece) {
-      const int64_t row = static_cast<int64_t>(it) * geo.span.stride + i * kTileM + r;
-      if (row_valid) geo.span.ml[row] = make_float2(m_run, l);
-      uint4* dst = reinterpret_cast<uint4*>(geo.span.o + row * D);
+    int slot = -1;
+    if constexpr (kSpan) slot = w.slot;
+    if (kSpan && (slot >= 0 || geo.span.shared)) {
+      // a piece's rows lie in its slot, a shared prefix's whole items' as in out
+      const int64_t row = slot >= 0 ? static_cast<int64_t>(slot) * geo.span.stride + i * kTileM + r
+                                    : static_cast<int64_t>(w.cu + tok) * geo.Hq + h;
+      if (row_valid) (slot >= 0 ? geo.span.ml : geo.span.whole.ml)[row] = make_float2(m_run, l);
+      uint4* dst = reinterpret_cast<uint4*>((slot >= 0 ? geo.span.o : geo.span.whole.o) + row * D);
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t o[32];
@@ -944,7 +988,9 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
   }
 }
 
-template <int D, Pages kPages, bool kSpan = false>
+// kOwn: some of the CTAs decode the requests' own keys (span.cuh), with NT tiles of 8
+// heads.
+template <int D, Pages kPages, bool kSpan = false, int kOwn = 0>
 __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThreads, 1)
     attn_tc_kernel(const __grid_constant__ CUtensorMap map_q,
                    const __grid_constant__ CUtensorMap map_kv,
@@ -966,7 +1012,8 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   Q8State* q8 = kQ8 ? reinterpret_cast<Q8State*>(
                           (reinterpret_cast<uintptr_t>(order + kSortMax) + 7) & ~uintptr_t(7))
                     : nullptr;
-  // kSpan, shared: first item of each group, where that is not its place in work order
+  // kSpan, shared: first unit or item of each group, where that is not its place in work
+  // order
   int* first_of = reinterpret_cast<int*>(order + kSortMax);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -1025,11 +1072,15 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     auto request = [&](int b) {
       return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
     };
-    int steps = 0;
+    int share = 0;
     if (kSpan) {
-      steps = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                        geo.span.pieces > 0 && (geo.span.shared || geo.batch <= kSortMax), request);
-      if (lane == 0) bar.part_steps = steps;
+      const SpanPlan plan = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                                      kOwn ? &geo.own : nullptr, 1, request);
+      share = plan.share;
+      if (lane == 0) {
+        bar.share = plan.share;
+        bar.workers = plan.workers;
+      }
     }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
@@ -1040,7 +1091,8 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       if (kSpan && p < geo.batch) {
         const SpanRequest r = request(b);
         if (r.bad) record_error(status, GC_ERR_OUT_OF_RANGE);
-        if (r.n > 0) cnt = geo.Hkv * span_tiles(r.n, geo.G) * span_parts(span_steps(r.T), steps);
+        const int steps = r.n > 0 ? span_steps(r.T) : 0;
+        if (steps > 0) cnt = geo.Hkv * span_tiles(r.n, geo.G) * (share ? steps + kSpanLead : 1);
       } else if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
@@ -1065,29 +1117,39 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
-  int total_items = item_start[geo.batch];
-  bool fits = true;
-  int part_steps = 0;
-  if (kSpan) {
-    part_steps = bar.part_steps;
-    // (groups that overlap could be more items than the workspace has pieces)
-    fits = !geo.span.shared || total_items <= geo.span.pieces;
-    if (!fits) {
-      total_items = 0;
-      if (threadIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    }
-  }
+  const int total_items = item_start[geo.batch];  // (shares: units)
+  const int share = kSpan ? bar.share : 0;
 
-  if (warp < 4) {
+  if (kSpan && warp >= 4) {
+    const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
+    const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
+    span_write_plan(geo.span, geo.batch, share, item_start, order, me, all);
+    if (geo.span.shared)
+      span_priors(geo.span, geo.batch, geo.G, geo.total_new,
+                  geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me, all);
+    else
+      span_zeros(geo.span, geo.batch, geo.Hq, D, geo.total_new, prefix_lens, new_lens,
+                 cu_new_lens, out, me, all);
+  }
+  if (kOwn && static_cast<int>(blockIdx.x) >= bar.workers) {
+    if constexpr (kOwn > 0) {
+      using S = dec::SharedShape<D, kOwn>;
+      const int first = bar.workers, group = S::group();
+      dec::decode_cta<S, D, kOwn, false, true>(
+          smem_q + group * kOwnBytes, 2 * (static_cast<int>(blockIdx.x) - first) + group,
+          2 * (static_cast<int>(gridDim.x) - first), geo.own.q, geo.own.block_table, geo.own.lens,
+          out, geo.own.workspace, geo.own.geo, status, geo.own.merge_counters);
+    }
+  } else if (warp < 4) {
     regs_dec<kQ8 ? kRegsProducerQ8 : kRegsProducer>();
     if (warp == 0) {
       producer<D, kPages, kSpan>(smem_q, smem_kv, bar, q8, item_start, total_items, geo,
-                          part_steps, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
+                          share, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
                           work_counter);
     } else if (warp == 1 || warp == 2) {
       if (lane == 0)
         mma_issuer<D, kSpan>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
-                      part_steps, prefix_lens, new_lens, cu_new_lens);
+                      share, prefix_lens, new_lens, cu_new_lens);
       __syncwarp();
     }
   } else if (kQ8 && warp >= kThreads / 32) {
@@ -1095,22 +1157,11 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     converter<D>(smem_kv, bar, *q8, geo);
   } else {
     regs_inc<kQ8 ? kRegsSoftmaxQ8 : kRegsSoftmax>();
-    if (kSpan) {
-      const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
-      const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
-      if (geo.span.shared)
-        span_priors(geo.span, geo.batch, geo.G, geo.total_new, part_steps, !fits,
-                    geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me,
-                    all);
-      else
-        span_empty_and_cut(geo.span, geo.batch, geo.Hq, D, geo.total_new, part_steps, item_start,
-                           order, prefix_lens, new_lens, cu_new_lens, out, me, all);
-    }
     if (warp < 8)
-      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, part_steps, prefix_lens,
+      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, share, prefix_lens,
                               new_lens, cu_new_lens, out);
     else
-      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, part_steps, prefix_lens,
+      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, share, prefix_lens,
                               new_lens, cu_new_lens, out);
   }
   tc_fence_before();
@@ -1163,7 +1214,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 template <int D>
 gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                  int* work_counter, const Q8Pages* q8 = nullptr,
-                 const UnpackedPages* unpacked = nullptr, const SpanGeom* span = nullptr) {
+                 const UnpackedPages* unpacked = nullptr, const SpanGeom* span = nullptr,
+                 const OwnDecode* own = nullptr) {
   using C = Cfg<D>;
   gc_status bound = check_item_bound(pool, a, pool->num_sms);
   if (bound != GC_OK) return bound;
@@ -1255,12 +1307,15 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                       (static_cast<size_t>(a.batch) + 1) * sizeof(int) +
                       kSortMax * sizeof(int16_t) + (q8 ? sizeof(Q8State) + 8 : 0) +
                       (span && span->shared ? kSortMax * sizeof(int) : 0);
+  static_assert(2 * kOwnBytes <= (2 + C::kStages) * C::kTileBytes, "own keys: shared memory");
   // (at d = 128 only the image variant is used: see below)
   constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
   constexpr Pages kUnpacked = D == 128 ? Pages::kImage : Pages::kUnpacked;
   // (and nothing is cut there)
   constexpr bool kSpan = D == 64;
-  auto kernel = span       ? attn_tc_kernel<D, kPool, kSpan>
+  auto kernel = own && geo.G > 8 ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 2 : 0>
+                : own      ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 1 : 0>
+                : span     ? attn_tc_kernel<D, kPool, kSpan>
                 : q8       ? attn_tc_kernel<D, Pages::kImage>
                 : unpacked ? attn_tc_kernel<D, kUnpacked>
                            : attn_tc_kernel<D, kPool>;
@@ -1273,15 +1328,17 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
       static_cast<long long>(geo.Hkv) *
       ((static_cast<long long>(a.total_new_tokens) * geo.G + (2 * kTileM - 1ll) * a.batch) /
        (2 * kTileM));
-  geo.more_items = most_items > pool->num_sms;
+  geo.more_items = most_items > pool->num_sms && !own;
   long long ctas = geo.more_items ? pool->num_sms : most_items;
   geo.span = SpanGeom{};
+  geo.own = own ? *own : OwnDecode{};
   if (span) {
-    // (an item may be cut into as many parts as the block tables have steps for)
+    // (items may be cut into as many pieces as the block tables have steps for)
     geo.span = *span;
-    geo.span.workers = pool->num_sms;
     const long long steps = static_cast<long long>(a.max_blocks) * cfg.page_size / kTileN + 1;
-    if (span->pieces > 0) ctas = min(static_cast<long long>(pool->num_sms), most_items * steps);
+    if (span->cuts) ctas = min(static_cast<long long>(pool->num_sms), most_items * steps);
+    if (own) ctas = pool->num_sms;
+    geo.span.workers = static_cast<int32_t>(ctas);
   }
   if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
@@ -1340,8 +1397,8 @@ bool converts_in_kernel(const gc_kv_pool* pool, const AttnArgs& a) {
 }
 
 gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                              const SpanGeom& span) {
-  return launch<64>(pool, a, stream, pool->work_counter, nullptr, nullptr, &span);
+                              const SpanGeom& span, const OwnDecode* own) {
+  return launch<64>(pool, a, stream, pool->work_counter, nullptr, nullptr, &span, own);
 }
 
 gc_status launch_attn_tc_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pages& q8,

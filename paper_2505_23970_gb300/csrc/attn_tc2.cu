@@ -76,6 +76,7 @@ constexpr int kRing = 4;              // slots of 16 KB in each of the K and V r
 constexpr int kSlotBytes = 16384;
 constexpr int kQBytes = kRows * kD * 2;  // 32 KB: two 64-column blocks of 128 rows
 constexpr int kSortMax = 512;
+constexpr int kOwnBytes = 64 * 1024;  // kOwn: shared memory of a group that decodes own keys
 // Requests of more keys x kv heads than this (64 MB of K and V, half of the L2) have
 // their items numbered head by head: with a tile's heads together the pairs at work
 // read all heads at once, 12.2 GB of DRAM for two requests of 131072 + 2048 tokens
@@ -101,6 +102,7 @@ struct Geom2 {
   float scale_log2;
   UnpackedGeom unpacked;  // kImg
   SpanGeom span;          // kSpan
+  OwnDecode own;          // kOwn
 };
 
 // A CTA's place: its pair's part of the keys (split of splits; 0 of 1 when the
@@ -108,8 +110,10 @@ struct Geom2 {
 // cluster.
 struct Place {
   uint32_t parity, lead, split, splits;
-  int part_steps;  // kSpan: steps of a part of an item's keys
+  int share;  // kSpan: units of a share, 0: whole items (span.cuh)
 };
+
+constexpr int kMessage = 12;  // ints of an item message, at most
 
 struct Bars2 {
   uint64_t q_full[2];         // even CTA: both Q halves landed (2 arrivals + both copies' bytes)
@@ -127,8 +131,8 @@ struct Bars2 {
   uint64_t item_full[2];      // work-item ring, written by the even CTA's K producer
   uint64_t item_empty[2];     // even CTA: item slot read by every consumer of both CTAs
   uint64_t drain;             // even CTA: both issuers' last commits
-  int item_msg[2][8];         // a claimed item, decoded (item_message; it < 0: end)
-  int part_steps;             // kSpan: steps of a part
+  int item_msg[2][kMessage];  // a claimed item, decoded (item_message; it < 0: end)
+  int share, workers;         // kSpan: units of a share, workers that have one
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -144,24 +148,22 @@ struct Item2 {
   int b, g, P, n, cu, T;
   int tok0;      // first token of this CTA's 128 rows
   int j0, nt;    // this pair's K/V steps: [j0, j0 + nt)
-  bool piece;    // kSpan: the result goes to the workspace
+  int slot;      // kSpan: the piece's, -1 for a whole item
   bool read;     // the whole message has been read (always true, but only known then)
 };
 
-// kSpan: the rows of an item see all keys of their request, or of a part of them (an
-// item of work order p is, in this order, a kv head, a part and a tile: the tiles that
-// read the same keys run at the same time).  P is then the number of keys, T, and the
-// message has the part as well.
+// kSpan: the rows of an item see all keys of their request, or (a piece) of a range of
+// steps; P is then the number of keys, T, and the message has the range and the piece's
+// slot as well.
 template <bool kSpan>
-constexpr int kMessageWords = kSpan ? 8 : 7;
+constexpr int kMessageWords = kSpan ? 10 : 7;
 
 // Which request, kv head and 256-row tile item `it` is (item_start: first
 // item of each request in work order, then the order itself when the batch
 // was ranked), with the request's lengths: the message the even CTA's
 // producer sends to every role of both CTAs.
-template <bool kSpan>
 __device__ __forceinline__ void item_message(int it, const int* item_start, const Geom2& geo,
-                                             const Place& at, const int32_t* prefix_lens,
+                                             const int32_t* prefix_lens,
                                              const int32_t* new_lens,
                                              const int32_t* cu_new_lens, int* m) {
   int lo = 0, hi = geo.batch;  // last p with item_start[p] <= it
@@ -175,20 +177,6 @@ __device__ __forceinline__ void item_message(int it, const int* item_start, cons
   const int local = it - item_start[lo];
   m[0] = it;
   m[1] = b;
-  if (kSpan) {
-    const SpanRequest r =
-        span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
-    const int tiles = span_tiles(r.n, geo.G);
-    const int parts = span_parts(span_steps(r.T), at.part_steps);
-    const int head_part = local / tiles;
-    m[2] = local - head_part * tiles;
-    m[3] = head_part / parts;
-    m[7] = head_part - m[3] * parts;
-    m[4] = r.T;
-    m[5] = r.n;
-    m[6] = r.cu;
-    return;
-  }
   const int tiles = (item_start[lo + 1] - item_start[lo]) / geo.Hkv;
   m[4] = ld_plain(prefix_lens + b);
   m[5] = ld_plain(new_lens + b);
@@ -200,6 +188,29 @@ __device__ __forceinline__ void item_message(int it, const int* item_start, cons
   m[2] = tiles - 1 - (by_head ? local - head * tiles : by_tile);
   m[3] = by_head ? head : local - by_tile * geo.Hkv;
   m[6] = ld_plain(cu_new_lens + b);
+}
+
+// kSpan: the message of the piece at unit (or of item) u; returns the unit after it, and
+// m[0] < 0 if there is none.
+__device__ __forceinline__ int span_message(int u, int end, const int* start, const Geom2& geo,
+                                            const Place& at, int worker, const int32_t* lens,
+                                            const int32_t* new_lens, const int32_t* cu, int* m) {
+  const SpanPiece w = span_piece(
+      u, at.share, worker, end, geo.batch, start,
+      reinterpret_cast<const int16_t*>(start + geo.batch + 1), geo.Hkv, geo.G, [&](int b) {
+        return span_request(geo.span, b, geo.total_new, lens, new_lens, cu);
+      });
+  m[0] = w.nt > 0 ? u : -1;
+  m[1] = w.b;
+  m[2] = w.tile;
+  m[3] = w.g;
+  m[4] = w.T;
+  m[5] = w.n;
+  m[6] = w.cu;
+  m[7] = w.j0;
+  m[8] = w.nt;
+  m[9] = w.slot + 1;
+  return w.next;
 }
 
 // Every consumer releases an item slot once it has the message: item_read by a
@@ -230,12 +241,11 @@ __device__ __forceinline__ void item_from_message(const int* m, const Geom2& geo
   const int r0 = m[2] * 2 * kRows;
   w.tok0 = (r0 + static_cast<int>(at.parity) * kRows) >> geo.g_shift;
   if (kSpan) {
-    w.read = w.read && m[7] >= 0;
+    w.read = w.read && (m[7] | m[8] | m[9]) >= 0;
     w.T = m[4];
-    const int all = span_steps(w.T);
-    w.j0 = m[7] * at.part_steps;
-    w.nt = min(at.part_steps, all - w.j0);
-    w.piece = geo.span.shared || all > at.part_steps;
+    w.j0 = m[7];
+    w.nt = m[8];
+    w.slot = m[9] - 1;
     return;
   }
   w.T = w.P + w.n;
@@ -360,6 +370,14 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
   const uint32_t rank = at.parity;
   const bool claims = kIsK && rank == 0;  // the even CTA's K producer claims the items
 
+  // kSpan, shares: this worker's units that are left
+  const int worker = static_cast<int>(blockIdx.x / 2);
+  int unit = 0, unit_end = 0;
+  if (kSpan && at.share) {
+    unit = static_cast<int>(min(static_cast<int64_t>(worker) * at.share,
+                                static_cast<int64_t>(total_items)));
+    unit_end = min(total_items, unit + at.share);
+  }
   for (uint32_t k = 0; ok; ++k) {
     const int s = k & 1;
     int it = -1;
@@ -377,9 +395,14 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
         it = k > 0 && geo.more_items
                  ? clusters + atomicAdd(work_counter, 1)
                  : static_cast<int>(blockIdx.x / (2 * at.splits)) + static_cast<int>(k) * clusters;
+        if (kSpan && at.share) it = unit < unit_end ? unit : total_items;
         if (it >= total_items) it = -1;
-        if (it >= 0) {
-          item_message<kSpan>(it, item_start, geo, at, prefix_lens, new_lens, cu_new_lens, m);
+        if (kSpan && it >= 0) {
+          unit = span_message(it, unit_end, item_start, geo, at, worker, prefix_lens, new_lens,
+                              cu_new_lens, m);
+          it = m[0];
+        } else if (it >= 0) {
+          item_message(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, m);
           if (at.splits > 1) {  // fewer steps than pairs: some pairs have none
             item_from_message<kSpan>(m, geo, at, w);
             if (w.nt == 0) it = -1;
@@ -389,7 +412,7 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
 #pragma unroll
         for (int i = 0; i < kMessageWords<kSpan>; ++i) {
           bar.item_msg[s][i] = m[i];
-          st_cluster_u32(rm.item_msg + 32 * s + 4 * i, static_cast<uint32_t>(m[i]));
+          st_cluster_u32(rm.item_msg + 4 * (kMessage * s + i), static_cast<uint32_t>(m[i]));
           if (it < 0) break;
         }
         mbar_arrive(&bar.item_full[s]);
@@ -835,9 +858,8 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
     // the row (token, head) of out that lane / 8 of this warp's first store belongs to
     const uint32_t out_row = static_cast<uint32_t>(w.cu + w.tok0) * geo.Hq + w.g * geo.G;
     const int left = w.n - w.tok0;  // tokens from this CTA's first row on
-    const bool piece = kSpan && w.piece;
-    const int64_t piece_row = kSpan ? static_cast<int64_t>(it) * geo.span.stride +
-                                          static_cast<int>(at.parity) * kRows + quad * 32 : 0;
+    // kSpan: a piece's rows lie in its slot, a shared prefix's whole items' as in out
+    const int slot = kSpan ? w.slot : -1;
     // (the next item is read while the last PV product runs)
     it = next_item(k + 1);
     if (!ok) break;
@@ -863,10 +885,19 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive_remote(rm.o_free);
-    if (piece) {
+    if (kSpan && (slot >= 0 || geo.span.shared)) {
       // 32 columns at a time through the warp's 4 KB, so that a store covers four
       // whole 128-byte row parts here too
-      if (hw == 0 && row_valid) geo.span.ml[piece_row + lane] = make_float2(m_run, l_row);
+      float* po = slot >= 0 ? geo.span.o : geo.span.whole.o;
+      float2* pml = slot >= 0 ? geo.span.ml : geo.span.whole.ml;
+      auto row_of = [&](int wrow) -> int64_t {
+        const int row = quad * 32 + wrow;
+        return slot >= 0 ? static_cast<int64_t>(slot) * geo.span.stride +
+                               static_cast<int>(at.parity) * kRows + row
+                         : static_cast<int64_t>(out_row + (row >> geo.g_shift) * geo.Hq +
+                                                (row & (geo.G - 1)));
+      };
+      if (hw == 0 && row_valid) pml[row_of(lane)] = make_float2(m_run, l_row);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -880,7 +911,7 @@ __device__ void softmax2h(const Place& at, uint8_t* smem_q, Bars2& bar, const Re
           const uint4 v = *reinterpret_cast<const uint4*>(
               mine + wrow * 128 + (((lane & 7) ^ (wrow & 7)) << 4));
           if ((quad * 32 + wrow) >> geo.g_shift < left)
-            *reinterpret_cast<uint4*>(geo.span.o + (piece_row + wrow) * kD + hw * 64 + half * 32 +
+            *reinterpret_cast<uint4*>(po + row_of(wrow) * kD + hw * 64 + half * 32 +
                                       (lane & 7) * 4) = v;
         }
         __syncwarp();
@@ -1007,7 +1038,8 @@ __device__ void merge2_store(const Place& at, const uint8_t* smem, const Item2& 
 }
 
 // ------------------------------------------------------------------- kernel
-template <bool kSplit, bool kImg, bool kSpan>
+// kOwn: some of the CTAs decode the requests' own keys (span.cuh).
+template <bool kSplit, bool kImg, bool kSpan, bool kOwn = false>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_tc2_kernel(const __grid_constant__ CUtensorMap map_q,
                     const __grid_constant__ CUtensorMap map_k,
@@ -1030,7 +1062,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   int16_t* order = reinterpret_cast<int16_t*>(item_start + geo.batch + 1);
   // half-row softmax exchange words [2 buffers][2 halves][128 rows]
   uint16_t* xch = reinterpret_cast<uint16_t*>(order + (geo.batch <= kSortMax ? kSortMax : 0));
-  // kSpan, shared: first item of each group, where that is not its place in work order
+  // kSpan, shared: first unit or item of each group, where that is not its place in work
+  // order
   int* first_of = reinterpret_cast<int*>(xch + 2 * 2 * kRows);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
@@ -1097,10 +1130,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
     };
     if (kSpan) {
-      at.part_steps = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                                geo.span.pieces > 0 && (geo.span.shared || geo.batch <= kSortMax),
-                                request);
-      if (lane == 0) bar.part_steps = at.part_steps;
+      const SpanPlan plan = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                                      kOwn ? &geo.own : nullptr, 2, request);
+      at.share = plan.share;
+      if (lane == 0) {
+        bar.share = plan.share;
+        bar.workers = plan.workers;
+      }
     }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
@@ -1111,8 +1147,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (kSpan && p < geo.batch) {
         const SpanRequest r = request(b);
         if (r.bad && at.parity == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-        if (r.n > 0)
-          cnt = geo.Hkv * span_tiles(r.n, geo.G) * span_parts(span_steps(r.T), at.part_steps);
+        const int steps = r.n > 0 ? span_steps(r.T) : 0;
+        if (steps > 0)
+          cnt = geo.Hkv * span_tiles(r.n, geo.G) * (at.share ? steps + kSpanLead : 1);
       } else if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
@@ -1151,24 +1188,36 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
-  int total_items = item_start[geo.batch];
-  bool fits = true;
-  if (kSpan) {
-    at.part_steps = bar.part_steps;
-    // (groups that overlap could be more items than the workspace has pieces)
-    fits = !geo.span.shared || total_items <= geo.span.pieces;
-    if (!fits) {
-      total_items = 0;
-      if (threadIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    }
-  }
+  const int total_items = item_start[geo.batch];  // (shares: units)
+  if (kSpan) at.share = bar.share;
   // each cluster has one item; should there be more (see producer2), every pair takes
   // whole ones
   if (kSplit && total_items > static_cast<int>(gridDim.x / (2 * at.splits)))
     at.split = 0, at.splits = 1;
 
+  const bool own_cta = kOwn && static_cast<int>(blockIdx.x / 2) >= bar.workers;
+  if (kSpan && warp >= 4) {
+    const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
+    const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
+    span_write_plan(geo.span, geo.batch, at.share, item_start, order, me, all);
+    if (geo.span.shared)
+      span_priors(geo.span, geo.batch, geo.G, geo.total_new,
+                  geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me, all);
+    else
+      span_zeros(geo.span, geo.batch, geo.Hq, kD, geo.total_new, prefix_lens, new_lens,
+                 cu_new_lens, out, me, all);
+  }
   float2* part = reinterpret_cast<float2*>(smem_k);  // splits: free once the roles are done
-  if (warp == 0) {
+  if (own_cta) {
+    if constexpr (kOwn) {
+      using S = dec::SharedShape<kD, 1>;
+      const int first = 2 * bar.workers, group = S::group();
+      dec::decode_cta<S, kD, 1, false, true>(
+          smem_q + group * kOwnBytes, 2 * (static_cast<int>(blockIdx.x) - first) + group,
+          2 * (static_cast<int>(gridDim.x) - first), geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo, status,
+          geo.own.merge_counters);
+    }
+  } else if (warp == 0) {
     producer2<true, kImg, kSpan>(at, smem_q, smem_k, bar, rm, item_start, total_items, geo, &map_q,
                     &map_k, &map_img_k, block_table, prefix_lens, new_lens, cu_new_lens, status,
                     work_counter);
@@ -1183,17 +1232,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                      &map_v, &map_img_v, block_table, prefix_lens, new_lens, cu_new_lens, status,
                      work_counter);
   } else if (warp >= 4) {
-    if (kSpan) {
-      const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
-      const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
-      if (geo.span.shared)
-        span_priors(geo.span, geo.batch, geo.G, geo.total_new, at.part_steps,
-                    !fits, geo.batch <= kSortMax ? first_of : item_start, prefix_lens,
-                    cu_new_lens, me, all);
-      else
-        span_empty_and_cut(geo.span, geo.batch, geo.Hq, kD, geo.total_new, at.part_steps,
-                           item_start, order, prefix_lens, new_lens, cu_new_lens, out, me, all);
-    }
     softmax2h<kSplit, kSpan>(at, smem_q, bar, rm, tmem, xch, geo, out, part);
   }
   // a CTA that gave up tells its peer, so that the peer's roles leave their
@@ -1214,7 +1252,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp >= 4 && it < total_items) {
       int m[kMessageWords<kSpan>];
       Item2 w;
-      item_message<kSpan>(it, item_start, geo, at, prefix_lens, new_lens, cu_new_lens, m);
+      item_message(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, m);
       item_from_message<kSpan>(m, geo, at, w);
       merge2_store(at, smem_q, w, geo, out);
     }
@@ -1324,11 +1362,13 @@ int splits_of(const gc_kv_pool* pool, long long items, long long steps, size_t s
 }  // namespace
 
 gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                          int* work_counter, const UnpackedPages* unpacked, const SpanGeom* span) {
+                          int* work_counter, const UnpackedPages* unpacked, const SpanGeom* span,
+                          const OwnDecode* own) {
   const auto& cfg = pool->cfg;
   if (cfg.head_dim != kD)
     return fail(GC_ERR_UNSUPPORTED, "%s: pair kernel needs head_dim 128", a.who);
   const size_t smem = smem_bytes2(a.batch, span && span->shared);
+  static_assert(2 * kOwnBytes <= 2 * kQBytes + 2 * kRing * kSlotBytes, "own keys: shared memory");
   // at most this many items, of at most this many 128-key steps
   const long long G = a.num_q_heads / cfg.num_kv_heads;
   const long long most_items =
@@ -1424,17 +1464,20 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   // control block, or the static scratch of the allocation-free entry point).
   // A call that cannot have more needs no counter, so nothing clears it, and
   // only as many clusters as it can have items are launched.
-  geo.more_items = most_items > pairs;
+  geo.more_items = most_items > pairs && !own;
   long long clusters = geo.more_items ? pairs : most_items;
   geo.span = SpanGeom{};
+  geo.own = own ? *own : OwnDecode{};
   if (span) {
-    // (an item may be cut into as many parts as the block tables have steps for)
+    // (items may be cut into as many pieces as the block tables have steps for)
     geo.span = *span;
-    geo.span.workers = pairs;
-    if (span->pieces > 0) clusters = min(static_cast<long long>(pairs), most_items * most_steps);
+    if (span->cuts) clusters = min(static_cast<long long>(pairs), most_items * most_steps);
+    if (own) clusters = pairs;
+    geo.span.workers = static_cast<int32_t>(clusters);
   }
-  const Kernel2 kernel = span ? attn_tc2_kernel<false, false, true>
-                              : kernel2(splits, unpacked != nullptr);
+  const Kernel2 kernel = own    ? attn_tc2_kernel<false, false, true, true>
+                         : span ? attn_tc2_kernel<false, false, true>
+                                : kernel2(splits, unpacked != nullptr);
   cudaError_t e = prepare_kernel(kernel, splits, smem);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);

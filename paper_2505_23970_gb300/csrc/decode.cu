@@ -120,13 +120,25 @@ size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max
   return decode_split(pool, batch, max_blocks, num_q_heads).workspace_bytes;
 }
 
-gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
-                        const Q8Pages* q8) {
+gc_status check_decode(const gc_kv_pool* pool, const DecodeArgs& a) {
   if (a.batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", a.who, a.batch);
   const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
   if (cap > 2147483647LL)
     return fail(GC_ERR_UNSUPPORTED, "%s: %lld-token block table", a.who,
                 static_cast<long long>(cap));
+  const uint64_t pool_rows = static_cast<uint64_t>(pool->cfg.num_layers) * 2 *
+                             pool->cfg.num_pages * pool->cfg.num_kv_heads * pool->cfg.page_size;
+  if (pool_rows >= (1ull << 31))
+    return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
+                static_cast<unsigned long long>(pool_rows));
+  return GC_OK;
+}
+
+gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_t stream,
+                        const Q8Pages* q8) {
+  gc_status st = check_decode(pool, a);
+  if (st != GC_OK) return st;
+  const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
   const bool shares = decode_shares(pool, a.num_q_heads);
   DecodeSplit sp = {};
   size_t need;
@@ -148,14 +160,9 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
                           (shares ? tiles : static_cast<int64_t>(sp.splits));
   if (units + 2LL * pool->num_sms > 2147483647LL)
     return fail(GC_ERR_UNSUPPORTED, "%s: %lld work items", a.who, units);
-  const uint64_t pool_rows = static_cast<uint64_t>(pool->cfg.num_layers) * 2 *
-                             pool->cfg.num_pages * pool->cfg.num_kv_heads * pool->cfg.page_size;
-  if (pool_rows >= (1ull << 31))
-    return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
-                static_cast<unsigned long long>(pool_rows));
   if (q8 && static_cast<uint64_t>(q8->n_blocks) * pool->cfg.num_layers * 2 >= (1ull << 31))
     return fail(GC_ERR_UNSUPPORTED, "gc_paged_decode_attn_q8: image of %d blocks", q8->n_blocks);
-  const gc_status st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8);
+  st = launch_decode_mma(pool, a, shares ? nullptr : &sp, stream, q8);
   if (st != GC_OK || shares || sp.splits <= 1) return st;
   const cudaError_t e = launch_dependent(
       a.own.o ? decode_merge_kernel<64, true> : decode_merge_kernel<64, false>,

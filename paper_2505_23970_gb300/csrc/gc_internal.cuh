@@ -246,13 +246,15 @@ gc_status launch_unpack_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pa
 // maps are read from there instead of the pool.
 // With `span`, every row sees all keys of its request (or group) and prefix_lens has
 // their numbers (span.cuh).
+// With `own` too (a shared prefix), some of the CTAs decode the requests' own keys.
 struct SpanGeom;
+struct OwnDecode;
 gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                           int* work_counter, const UnpackedPages* unpacked = nullptr,
-                          const SpanGeom* span = nullptr);
+                          const SpanGeom* span = nullptr, const OwnDecode* own = nullptr);
 // The same at head_dim 64, on single SMs.
 gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                              const SpanGeom& span);
+                              const SpanGeom& span, const OwnDecode* own);
 // Host-side bound of the attention kernels' 32-bit work numbering (items and
 // q rows of one call, with a margin of two claims per CTA of `grid`):
 // GC_ERR_UNSUPPORTED before anything is launched when a call could pass it.
@@ -294,6 +296,8 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
                             cudaStream_t stream, const Q8Pages* q8);
 size_t decode_share_workspace_bytes(const gc_kv_pool* pool);
+// Limits of a decode call's sizes, GC_OK if they are kept.
+gc_status check_decode(const gc_kv_pool* pool, const DecodeArgs& a);
 // Workspace bytes of a decode call on either path.
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
                               int32_t num_q_heads);

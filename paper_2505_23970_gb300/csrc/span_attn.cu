@@ -21,21 +21,21 @@ struct Join {
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  // piece rows x0, x0 + step, ...
+  // row `row` of the slots of a cut item
   template <int D>
-  __device__ __forceinline__ void pieces(const SpanGeom& sp, int64_t x0, int64_t step, int parts,
-                                         int c) {
+  __device__ __forceinline__ void pieces(const SpanGeom& sp, const SpanCut& cut, int row, int c) {
     constexpr int kBatch = 8;
-    for (int s0 = 0; s0 < parts; s0 += kBatch) {
+    for (int s0 = cut.c0; s0 <= cut.c1; s0 += kBatch) {
       float2 ml[kBatch];
       float4 o[kBatch];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        const bool in = s0 + k < parts;
-        const int64_t x = x0 + (s0 + k) * step;
-        ml[k] = in ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
-        o[k] = in ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
-                  : make_float4(0.f, 0.f, 0.f, 0.f);
+        const int s = s0 + k;
+        const int64_t x =
+            static_cast<int64_t>(2 * s + (s == cut.c0 ? cut.first : 0)) * sp.stride + row;
+        ml[k] = s <= cut.c1 ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
+        o[k] = s <= cut.c1 ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
       }
       float Mn = M;
 #pragma unroll
@@ -75,46 +75,42 @@ struct Join {
   }
 };
 
-// Cross attention: the rows of the requests that were cut.
+// Cross attention: the rows of the items that were cut.  Every cut item has one share in
+// which it begins and which it is the last of: block (share, row chunk).
 template <int D>
 __global__ void __launch_bounds__(256)
-    span_join_kernel(SpanGeom sp, const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
-                     __nv_bfloat16* out, int Hq, int Hkv, int G, int total_new) {
+    cross_join_kernel(SpanGeom sp, const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
+                      __nv_bfloat16* out, int Hq, int G, int total_new) {
   dependent_begin();
   constexpr int kLanes = D / 4;  // four columns each
   constexpr int kRowsPerBlock = 256 / kLanes;
-  constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of a tile
-  const int cuts = ld_plain(sp.cut), part_steps = ld_plain(sp.cut + 1);
-  if (cuts == 0) return;
-  // items are numbered by request, head, part and tile; here by request, head and tile
-  // in the place of the first part, so a unit's number is at most its item's
-  const int64_t units = static_cast<int64_t>(ld_plain(sp.cut + kCutFirst + cuts)) * kChunks;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int it = static_cast<int>(u / kChunks), chunk = static_cast<int>(u % kChunks);
-    int lo = 0, hi = cuts;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (ld_plain(sp.cut + kCutFirst + mid) <= it) lo = mid; else hi = mid;
-    }
-    const int first = ld_plain(sp.cut + kCutFirst + lo);
-    const SpanRequest r =
-        span_request(sp, ld_plain(sp.cut + kCutOrder + lo), total_new, lens, new_lens, cu);
-    if (r.n == 0) continue;
-    const int tiles = span_tiles(r.n, G), parts = span_parts(span_steps(r.T), part_steps);
-    const int local = it - first;
-    if (local >= Hkv * tiles) continue;
-    const int g = local / tiles, tile = local - g * tiles;
-    const int row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
-    const int at = tile * kSpanRows + row;  // q row of the request and kv head
-    if (at >= r.n * G) continue;
-    const int c = static_cast<int>(threadIdx.x) % kLanes;
-    const int64_t piece0 = first + static_cast<int64_t>(g) * parts * tiles + tile;
-    Join j;
-    j.pieces<D>(sp, piece0 * sp.stride + row, static_cast<int64_t>(tiles) * sp.stride, parts, c);
-    *reinterpret_cast<uint2*>(
-        out + (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c) =
-        j.rounded();
+  constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of an item
+  const int share = ld_plain(sp.plan), units = ld_plain(sp.plan + 1);
+  const int c0 = static_cast<int>(blockIdx.x) / kChunks, chunk = static_cast<int>(blockIdx.x) % kChunks;
+  const int64_t end = (static_cast<int64_t>(c0) + 1) * share;
+  if (share == 0 || end >= units) return;
+  const int* start = sp.plan + kPlanStart;
+  int lo = 0, hi = ld_plain(sp.plan + 2);  // the last request whose first unit is <= end
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (ld_plain(start + mid) <= end) lo = mid; else hi = mid;
   }
+  const SpanRequest r =
+      span_request(sp, ld_plain(sp.plan + kPlanOrder + lo), total_new, lens, new_lens, cu);
+  const int steps = span_steps(r.T), per = steps + kSpanLead, tiles = span_tiles(r.n, G);
+  const int local = static_cast<int>(end) - ld_plain(start + lo), item = local / per;
+  const int u0 = static_cast<int>(end) - (local - item * per);
+  const SpanCut cut = span_cut(u0, steps, share);
+  if (cut.c0 != c0 || cut.c1 == c0) return;
+  const int g = item / tiles, tile = item - g * tiles;
+  const int row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
+  const int at = tile * kSpanRows + row;  // q row of the request and kv head
+  if (at >= r.n * G) return;
+  const int c = static_cast<int>(threadIdx.x) % kLanes;
+  Join j;
+  j.pieces<D>(sp, cut, row, c);
+  *reinterpret_cast<uint2*>(
+      out + (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c) = j.rounded();
 }
 
 // Decode behind a shared prefix: every row of a request that is not skipped.
@@ -128,27 +124,39 @@ __global__ void __launch_bounds__(256)
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
   if (row >= rows) return;
   const int b = static_cast<int>(row / Hq), h = static_cast<int>(row - static_cast<int64_t>(b) * Hq);
-  const int T = ld_plain(own_lens + b);
+  const int T = ld_plain(own_lens + b), share = ld_plain(sp.plan);
   const int4 p = ld_plain(sp.prior + b);  // SpanPrior
   if (p.z < 0) record_error(status, GC_ERR_OUT_OF_RANGE);
   if (T < 0 || T > own_cap || p.z < 0) return;
-  const float2 ml = T > 0 ? ld_plain(own.ml + row) : make_float2(-INFINITY, 0.f);
-  const float4 o = T > 0 ? ld_plain(reinterpret_cast<const float4*>(own.o + row * D) + c)
-                         : make_float4(0.f, 0.f, 0.f, 0.f);
-  const int g = h / G;
-  const int64_t piece0 = p.x + static_cast<int64_t>(g) * p.z * p.y;
+  auto load = [&](const DecodeParts& parts, bool any, float2& ml, float4& o) {
+    ml = any ? ld_plain(parts.ml + row) : make_float2(-INFINITY, 0.f);
+    o = any ? ld_plain(reinterpret_cast<const float4*>(parts.o + row * D) + c)
+            : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  float2 ml;
+  float4 o;
+  load(own, T > 0, ml, o);
   Join j;
-  j.pieces<D>(sp, piece0 * sp.stride + p.w + (h - g * G), static_cast<int64_t>(p.y) * sp.stride,
-              p.z, c);
+  SpanCut cut{0, 0, 0};
+  const int g = h / G;
+  if (share && p.z > 0) cut = span_cut(p.x + g * p.y, p.z, share);
+  if (cut.c1 > cut.c0) {
+    j.pieces<D>(sp, cut, p.w + (h - g * G), c);
+  } else {
+    float2 sml;
+    float4 so;
+    load(sp.whole, p.z > 0, sml, so);
+    j.part(sml, so);
+  }
   j.part(ml, o);
   *reinterpret_cast<uint2*>(out + row * D + 4 * c) = j.rounded();
 }
 
 gc_status launch_items(const gc_kv_pool* pool, const AttnArgs& a, const SpanGeom& span,
-                       cudaStream_t stream) {
+                       cudaStream_t stream, const OwnDecode* own = nullptr) {
   return pool->cfg.head_dim == 128
-             ? launch_attn_tc2(pool, a, stream, pool->work_counter, nullptr, &span)
-             : launch_attn_tc_span(pool, a, stream, span);
+             ? launch_attn_tc2(pool, a, stream, pool->work_counter, nullptr, &span, own)
+             : launch_attn_tc_span(pool, a, stream, span, own);
 }
 
 gc_status check_space(const char* who, size_t need, const void* workspace, size_t bytes) {
@@ -175,14 +183,30 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
   const AttnArgs args{a.q, a.out, a.block_table, a.lens, a.new_lens, a.start, a.batch,
                       a.max_blocks, a.layer, a.num_q_heads, a.rows, a.softmax_scale, who};
   st = launch_items(pool, args, span, stream);
-  if (st != GC_OK || span.pieces == 0) return st;
-  const auto join = cfg.head_dim == 128 ? span_join_kernel<128> : span_join_kernel<64>;
+  if (st != GC_OK || !span.cuts) return st;
+  // (one block per share and 1024 / d rows)
+  const int chunks = kSpanRows / (1024 / cfg.head_dim);
+  const auto join = cfg.head_dim == 128 ? cross_join_kernel<128> : cross_join_kernel<64>;
   const cudaError_t e = launch_dependent(
-      join, static_cast<unsigned>(4 * pool->num_sms), 256, 0, stream, span, a.lens, a.new_lens,
-      a.start, static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, cfg.num_kv_heads,
+      join, static_cast<unsigned>(space.slots / 2 * chunks), 256, 0, stream, span, a.lens,
+      a.new_lens, a.start, static_cast<__nv_bfloat16*>(a.out), a.num_q_heads,
       a.num_q_heads / cfg.num_kv_heads, a.rows);
   if (e != cudaSuccess) return cuda_fail(e, who);
   return GC_OK;
+}
+
+// One kernel for both sides of a call, unless the own keys' side needs more registers
+// than the span kernel's threads have (16 heads of 128), or the units could not be
+// numbered.  Otherwise a kernel each.
+static bool decodes_in_kernel(const gc_kv_pool* pool, const SpanArgs& a) {
+  const auto& cfg = pool->cfg;
+  const int64_t G = a.num_q_heads / cfg.num_kv_heads;
+  const int64_t items = cfg.num_kv_heads * (a.batch * G / kSpanRows + a.groups);
+  const int64_t steps = static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size / 128 + 1;
+  const int64_t own = static_cast<int64_t>(a.batch) * cfg.num_kv_heads *
+                      (static_cast<int64_t>(a.max_blocks) * cfg.page_size / 128 + 1);
+  return own + 2 * kMergeCounters < 2147483647LL && (cfg.head_dim == 64 || G <= 8) && a.groups <= kSpanRequests &&
+         items * (steps + kSpanLead) < (1ll << 30) - pool->num_sms;
 }
 
 // A shared call's workspace: the prefixes' pieces, the own parts, then the decode
@@ -200,7 +224,9 @@ static SharedSpace shared_space(const gc_kv_pool* pool, int32_t batch, int32_t g
   s.ml = s.span.end;
   s.o = s.ml + (rows * sizeof(float2) + 255) / 256 * 256;
   s.decode = s.o + rows * pool->cfg.head_dim * sizeof(float);  // (rows of 256 bytes or more)
-  s.end = s.decode + decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
+  const size_t shares = decode_share_workspace_bytes(pool);  // (in the span kernel)
+  const size_t alone = decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
+  s.end = s.decode + (shares > alone ? shares : alone);
   return s;
 }
 
@@ -224,11 +250,19 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
                  a.softmax_scale, w + space.decode, space.end - space.decode, who,
                  DecodeParts{reinterpret_cast<float*>(w + space.o),
                              reinterpret_cast<float2*>(w + space.ml)}};
-  st = launch_decode(pool, own, stream);
-  if (st != GC_OK) return st;
   const AttnArgs args{a.q, a.out, a.shared_table, a.shared_lens, nullptr, a.start, a.groups,
                       a.max_shared_blocks, a.layer, a.num_q_heads, a.batch, a.softmax_scale, who};
-  st = launch_items(pool, args, span, stream);
+  if (decodes_in_kernel(pool, a)) {
+    st = check_decode(pool, own);
+    if (st != GC_OK) return st;
+    const OwnDecode with{static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.lens,
+                         static_cast<float*>(own.workspace), pool->merge_counters,
+                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 15 : 5};
+    st = launch_items(pool, args, span, stream, &with);
+  } else {
+    st = launch_decode(pool, own, stream);
+    if (st == GC_OK) st = launch_items(pool, args, span, stream);
+  }
   if (st != GC_OK) return st;
   const int64_t rows = static_cast<int64_t>(a.batch) * a.num_q_heads;
   const int per_block = 256 / (cfg.head_dim / 4);
