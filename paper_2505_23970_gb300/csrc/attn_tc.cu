@@ -133,9 +133,11 @@ struct Barriers {
   uint64_t s_free[2];  // d = 64: S_i has been read by its softmax
   uint64_t item_full[2], item_empty[2];  // work-item ring, producer -> other roles
   int item_slot[2];
+  unsigned long long own_keys;  // kOwn: their sum
   uint32_t tmem_base;
   int abort_flag;
-  int share, workers;  // kSpan: units of a share (0: whole items), workers that have one
+  SpanDeal deal;  // kSpan: how the work is dealt out
+  int workers;    // kSpan: workers that have a share
   int p0_steps;  // P tiles tile 0's softmax has published so far (pacing hint)
 };
 
@@ -159,24 +161,31 @@ using ItemOf = std::conditional_t<kSpan, SpanItem, Item>;
 __device__ __forceinline__ int first_key(const Item&, int j) { return j * kTileN; }
 __device__ __forceinline__ int first_key(const SpanItem& w, int j) { return (w.j0 + j) * kTileN; }
 
+// kSpan: what follows the order in shared memory: first unit or item of each group (shared
+// prefixes), then the requests (SpanRequests).
+__device__ __forceinline__ int* span_first_of(const int* item_start, int batch) {
+  return const_cast<int*>(item_start + batch + 1 + kSortMax / 2);
+}
+__device__ __forceinline__ int* span_held(const int* item_start, int batch) {
+  return span_first_of(item_start, batch) + kSortMax;
+}
+
 // item_start[p] = first item of the p-th request in work order; the request
 // itself is order[p] when the batch was sorted (order != nullptr), else p.
 // kSpan: prefix_lens has the numbers of keys, every row sees all of its request's, or of
-// a piece's range of steps; `it` is then a unit of this CTA's share, if share != 0.
+// a piece's range of steps; `it` is then a unit of this CTA's share, if there are shares.
 template <bool kSpan>
 __device__ __forceinline__ bool decode_item(int it, const int* item_start, const Geom& geo,
-                                            int share, const int32_t* prefix_lens,
+                                            SpanDeal deal, const int32_t* prefix_lens,
                                             const int32_t* new_lens,
                                             const int32_t* cu_new_lens,
                                             ItemOf<kSpan>& w) {
   if constexpr (kSpan) {
     const int worker = static_cast<int>(blockIdx.x);
+    int* held = span_held(item_start, geo.batch);
     const SpanPiece r = span_piece(
-        it, share, worker, share ? min(item_start[geo.batch], (worker + 1) * share) : 0, geo.batch,
-        item_start, reinterpret_cast<const int16_t*>(item_start + geo.batch + 1), geo.Hkv, geo.G,
-        [&](int b) {
-          return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
-        });
+        it, deal, worker, geo.batch, item_start, reinterpret_cast<const int16_t*>(item_start + geo.batch + 1), geo.Hkv, geo.G,
+        SpanRequests{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch, geo.total_new, held});
     w.b = r.b;
     w.g = r.g;
     w.j0 = r.j0;
@@ -254,7 +263,7 @@ __device__ __forceinline__ int claim_item(Barriers& bar, uint32_t k, int* work_c
 // here because a share may end in front of an item's first step.
 template <int D, bool kSpan>
 __device__ __forceinline__ int claim_piece(Barriers& bar, uint32_t k, int& unit,
-                                           const int* item_start, const Geom& geo, int share,
+                                           const int* item_start, const Geom& geo, SpanDeal deal,
                                            const int32_t* prefix_lens, const int32_t* new_lens,
                                            const int32_t* cu_new_lens, ItemOf<kSpan>& w,
                                            volatile int* abortp, bool& ok) {
@@ -262,10 +271,11 @@ __device__ __forceinline__ int claim_piece(Barriers& bar, uint32_t k, int& unit,
   ok = mbar_wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1, abortp);
   ok = __all_sync(0xffffffffu, ok);
   int it = -1;
-  const int end = min(item_start[geo.batch], (static_cast<int>(blockIdx.x) + 1) * share);
+  int first, end;
+  span_share(deal, static_cast<int>(blockIdx.x), item_start[geo.batch], first, end);
   if constexpr (kSpan) {
     if (unit < end) {
-      decode_item<kSpan>(unit, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
+      decode_item<kSpan>(unit, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
       if (w.nt > 0) it = unit;
       unit = w.next;
     }
@@ -402,7 +412,7 @@ __device__ void converter(uint8_t* smem_kv, Barriers& bar, Q8State& q8, const Ge
 template <int D, Pages kPages, bool kSpan>
 __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8State* q8,
                          const int* item_start, int total_items, const Geom& geo,
-                         int share, const CUtensorMap* map_q, const CUtensorMap* map_kv,
+                         SpanDeal deal, const CUtensorMap* map_q, const CUtensorMap* map_kv,
                          const CUtensorMap* map_img,
                          const int32_t* block_table,
                          const int32_t* prefix_lens,
@@ -419,22 +429,23 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
   int armed_q = -1, armed_vfix = -1;
   bool ok = true;
   int unit = 0;  // kSpan, shares: this CTA's next
-  if (kSpan && share)
-    unit = static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * share,
-                                static_cast<int64_t>(total_items)));
+  if (kSpan && deal.share) {
+    int end;
+    span_share(deal, static_cast<int>(blockIdx.x), total_items, unit, end);
+  }
   const uint32_t box_bytes = static_cast<uint32_t>(geo.ps) * 128;  // one page, one column block
   const uint32_t page_codes = static_cast<uint32_t>(geo.ps) * D;   // one page of 8-bit codes
 
   for (uint32_t k = 0; ok; ++k) {
     ItemOf<kSpan> w;
     int it;
-    if (kSpan && share)
-      it = claim_piece<D, kSpan>(bar, k, unit, item_start, geo, share, prefix_lens, new_lens,
+    if (kSpan && deal.share)
+      it = claim_piece<D, kSpan>(bar, k, unit, item_start, geo, deal, prefix_lens, new_lens,
                                  cu_new_lens, w, abortp, ok);
     else
       it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
     if (!ok || it < 0) break;
-    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
+    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
     // ---- Q tiles
     ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
     if (!ok) break;
@@ -631,7 +642,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
 template <int D, bool kSpan>
 __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, uint32_t tmem,
                            const int* item_start, int total_items, const Geom& geo,
-                           int share, const int32_t* prefix_lens,
+                           SpanDeal deal, const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens) {
   using C = Cfg<D>;
@@ -650,7 +661,7 @@ __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& b
     mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
     ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
+    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -829,7 +840,7 @@ __device__ __forceinline__ bool tile_exp_after(const uint32_t (&sr)[4][32], uint
 
 template <int D, int i, bool kSpan>
 __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
-                           int total_items, const Geom& geo, int share,
+                           int total_items, const Geom& geo, SpanDeal deal,
                            const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens,
@@ -853,7 +864,7 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
     if ((threadIdx.x & 31) == 0) mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
     ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, share, prefix_lens, new_lens, cu_new_lens, w);
+    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -1014,7 +1025,9 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
                     : nullptr;
   // kSpan, shared: first unit or item of each group, where that is not its place in work
   // order
-  int* first_of = reinterpret_cast<int*>(order + kSortMax);
+  int* first_of = span_first_of(item_start, geo.batch);
+  const SpanRequests request{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch,
+                             geo.total_new, span_held(item_start, geo.batch)};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -1038,9 +1051,11 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       mbar_init(&bar.item_empty[s], kItemConsumers);
     }
     bar.abort_flag = 0;
+    bar.own_keys = 0;
     bar.p0_steps = 0;
     fence_barrier_init();
   }
+  if (kOwn) __syncthreads();  // (the sum of own keys begins at 0)
   if (warp == 0 && lane == 0) {
     prefetch_tensormap(&map_q);
     prefetch_tensormap(&map_kv);
@@ -1052,10 +1067,15 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   }
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
+  if (kSpan) {
+    if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+    if (kOwn) span_own_keys(geo.own, kThreads, &bar.own_keys);
+    __syncthreads();
+  }
   if (geo.batch <= kSortMax) {
     // rank requests by total length, longest first (ties by index)
     auto total_len = [&](int b) {
-      return ld_plain(prefix_lens + b) + (kSpan ? 0 : ld_plain(new_lens + b));
+      return kSpan ? request.held[b] : ld_plain(prefix_lens + b) + ld_plain(new_lens + b);
     };
     for (int b = threadIdx.x; b < geo.batch; b += blockDim.x) {
       const int tb = total_len(b);
@@ -1069,31 +1089,26 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   }
   __syncthreads();
   if (warp == 2) {
-    auto request = [&](int b) {
-      return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
-    };
-    int share = 0;
     if (kSpan) {
-      const SpanPlan plan = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                                      kOwn ? &geo.own : nullptr, 1, request);
-      share = plan.share;
+      int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
+      if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      const SpanPlan plan =
+          span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                    kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 1,
+                    item_start, order, request);
+      if (plan.deal.share) span_scan(plan.deal, geo.Hkv, geo.G, order, item_start, first, request);
       if (lane == 0) {
-        bar.share = plan.share;
+        bar.deal = plan.deal;
         bar.workers = plan.workers;
       }
     }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
-    for (int b0 = 0; b0 < geo.batch; b0 += 32) {
+    for (int b0 = 0; !kSpan && b0 < geo.batch; b0 += 32) {
       const int p = b0 + lane;
       const int b = p < geo.batch ? (geo.batch <= kSortMax ? order[p] : p) : p;
       int cnt = 0;
-      if (kSpan && p < geo.batch) {
-        const SpanRequest r = request(b);
-        if (r.bad) record_error(status, GC_ERR_OUT_OF_RANGE);
-        const int steps = r.n > 0 ? span_steps(r.T) : 0;
-        if (steps > 0) cnt = geo.Hkv * span_tiles(r.n, geo.G) * (share ? steps + kSpanLead : 1);
-      } else if (p < geo.batch) {
+      if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
         const bool sane = n >= 0 && P >= 0 && cu >= 0 && cu + n <= geo.total_new;
@@ -1107,29 +1122,26 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
         if (lane >= o) incl += y;
       }
       if (p < geo.batch) item_start[p] = running + incl - cnt;
-      if (kSpan && geo.span.shared && p < geo.batch && geo.batch <= kSortMax)
-        first_of[b] = running + incl - cnt;
       running += __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (lane == 0) item_start[geo.batch] = running;
+    if (!kSpan && lane == 0) item_start[geo.batch] = running;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
   const int total_items = item_start[geo.batch];  // (shares: units)
-  const int share = kSpan ? bar.share : 0;
+  const SpanDeal deal = kSpan ? bar.deal : SpanDeal{0, 1};
 
   if (kSpan && warp >= 4) {
     const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
     const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
-    span_write_plan(geo.span, geo.batch, share, item_start, order, me, all);
+    span_write_plan(geo.span, deal, bar.workers, geo.Hkv, geo.G, item_start, order, request, me,
+                    all);
     if (geo.span.shared)
-      span_priors(geo.span, geo.batch, geo.G, geo.total_new,
-                  geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me, all);
+      span_priors(geo.span, deal, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
-      span_zeros(geo.span, geo.batch, geo.Hq, D, geo.total_new, prefix_lens, new_lens,
-                 cu_new_lens, out, me, all);
+      span_zeros(geo.Hq, D, request, out, me, all);
   }
   if (kOwn && static_cast<int>(blockIdx.x) >= bar.workers) {
     if constexpr (kOwn > 0) {
@@ -1144,12 +1156,12 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     regs_dec<kQ8 ? kRegsProducerQ8 : kRegsProducer>();
     if (warp == 0) {
       producer<D, kPages, kSpan>(smem_q, smem_kv, bar, q8, item_start, total_items, geo,
-                          share, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
+                          deal, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
                           work_counter);
     } else if (warp == 1 || warp == 2) {
       if (lane == 0)
         mma_issuer<D, kSpan>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
-                      share, prefix_lens, new_lens, cu_new_lens);
+                      deal, prefix_lens, new_lens, cu_new_lens);
       __syncwarp();
     }
   } else if (kQ8 && warp >= kThreads / 32) {
@@ -1158,10 +1170,10 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   } else {
     regs_inc<kQ8 ? kRegsSoftmaxQ8 : kRegsSoftmax>();
     if (warp < 8)
-      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, share, prefix_lens,
+      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, deal, prefix_lens,
                               new_lens, cu_new_lens, out);
     else
-      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, share, prefix_lens,
+      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, deal, prefix_lens,
                               new_lens, cu_new_lens, out);
   }
   tc_fence_before();
@@ -1306,7 +1318,7 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   const size_t smem = 1024 + 2 * C::kTileBytes + C::kStages * C::kTileBytes + sizeof(Barriers) +
                       (static_cast<size_t>(a.batch) + 1) * sizeof(int) +
                       kSortMax * sizeof(int16_t) + (q8 ? sizeof(Q8State) + 8 : 0) +
-                      (span && span->shared ? kSortMax * sizeof(int) : 0);
+                      (span ? kSortMax * sizeof(int) + kSpanHeldBytes : 0);
   static_assert(2 * kOwnBytes <= (2 + C::kStages) * C::kTileBytes, "own keys: shared memory");
   // (at d = 128 only the image variant is used: see below)
   constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
@@ -1340,7 +1352,8 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
     if (own) ctas = pool->num_sms;
     geo.span.workers = static_cast<int32_t>(ctas);
   }
-  if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
+  // (a join that follows leaves the counter at 0)
+  if (geo.more_items && !geo.span.cuts) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   e = launch_dependent(kernel,
                        static_cast<unsigned>(ctas),
@@ -1398,7 +1411,7 @@ bool converts_in_kernel(const gc_kv_pool* pool, const AttnArgs& a) {
 
 gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                               const SpanGeom& span, const OwnDecode* own) {
-  return launch<64>(pool, a, stream, pool->work_counter, nullptr, nullptr, &span, own);
+  return launch<64>(pool, a, stream, pool->span_counter, nullptr, nullptr, &span, own);
 }
 
 gc_status launch_attn_tc_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pages& q8,

@@ -110,7 +110,7 @@ struct Geom2 {
 // cluster.
 struct Place {
   uint32_t parity, lead, split, splits;
-  int share;  // kSpan: units of a share, 0: whole items (span.cuh)
+  SpanDeal deal;  // kSpan: how the work is dealt out
 };
 
 constexpr int kMessage = 12;  // ints of an item message, at most
@@ -132,7 +132,10 @@ struct Bars2 {
   uint64_t item_empty[2];     // even CTA: item slot read by every consumer of both CTAs
   uint64_t drain;             // even CTA: both issuers' last commits
   int item_msg[2][kMessage];  // a claimed item, decoded (item_message; it < 0: end)
-  int share, workers;         // kSpan: units of a share, workers that have one
+  SpanDeal deal;              // kSpan: how the work is dealt out
+  int workers;                // kSpan: workers that have a share
+  int next_unit;              // kSpan, shares: after the first piece
+  unsigned long long own_keys;  // kOwn: their sum
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -192,14 +195,12 @@ __device__ __forceinline__ void item_message(int it, const int* item_start, cons
 
 // kSpan: the message of the piece at unit (or of item) u; returns the unit after it, and
 // m[0] < 0 if there is none.
-__device__ __forceinline__ int span_message(int u, int end, const int* start, const Geom2& geo,
-                                            const Place& at, int worker, const int32_t* lens,
-                                            const int32_t* new_lens, const int32_t* cu, int* m) {
-  const SpanPiece w = span_piece(
-      u, at.share, worker, end, geo.batch, start,
-      reinterpret_cast<const int16_t*>(start + geo.batch + 1), geo.Hkv, geo.G, [&](int b) {
-        return span_request(geo.span, b, geo.total_new, lens, new_lens, cu);
-      });
+__device__ __forceinline__ int span_message(int u, const int* start, const Geom2& geo,
+                                            const Place& at, int worker,
+                                            const SpanRequests& request, int* m) {
+  const SpanPiece w =
+      span_piece(u, at.deal, worker, geo.batch, start,
+                 reinterpret_cast<const int16_t*>(start + geo.batch + 1), geo.Hkv, geo.G, request);
   m[0] = w.nt > 0 ? u : -1;
   m[1] = w.b;
   m[2] = w.tile;
@@ -357,7 +358,7 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
                           const int32_t* prefix_lens,
                           const int32_t* new_lens,
                           const int32_t* cu_new_lens, int32_t* status,
-                          int* work_counter) {
+                          int* work_counter, int* held) {
   const int lane = threadIdx.x & 31;
   Producer<kIsK> pr{smem_ring, bar.v_landed, kIsK ? bar.k_empty : bar.v_empty,
                     kIsK ? rm.k_full : rm.v_full, &bar.abort_flag, lane};
@@ -373,17 +374,17 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
   // kSpan, shares: this worker's units that are left
   const int worker = static_cast<int>(blockIdx.x / 2);
   int unit = 0, unit_end = 0;
-  if (kSpan && at.share) {
-    unit = static_cast<int>(min(static_cast<int64_t>(worker) * at.share,
-                                static_cast<int64_t>(total_items)));
-    unit_end = min(total_items, unit + at.share);
+  if (kSpan && at.deal.share) {
+    span_share(at.deal, worker, total_items, unit, unit_end);
+    unit = bar.next_unit;
   }
   for (uint32_t k = 0; ok; ++k) {
     const int s = k & 1;
     int it = -1;
     Item2 w;
-    if (claims) {
-      // claim the next item and send it, decoded, to every role of both CTAs
+    if (claims && (!kSpan || k > 0)) {
+      // claim the next item and send it, decoded, to every role of both CTAs (kSpan: the
+      // first one is there)
       ok = pr.wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1);
       if (!ok) break;
       int m[kMessageWords<kSpan>];
@@ -395,11 +396,12 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
         it = k > 0 && geo.more_items
                  ? clusters + atomicAdd(work_counter, 1)
                  : static_cast<int>(blockIdx.x / (2 * at.splits)) + static_cast<int>(k) * clusters;
-        if (kSpan && at.share) it = unit < unit_end ? unit : total_items;
+        if (kSpan && at.deal.share) it = unit < unit_end ? unit : total_items;
         if (it >= total_items) it = -1;
         if (kSpan && it >= 0) {
-          unit = span_message(it, unit_end, item_start, geo, at, worker, prefix_lens, new_lens,
-                              cu_new_lens, m);
+          unit = span_message(it, item_start, geo, at, worker,
+                              SpanRequests{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch,
+                                           geo.total_new, held}, m);
           it = m[0];
         } else if (it >= 0) {
           item_message(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, m);
@@ -1065,10 +1067,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   // kSpan, shared: first unit or item of each group, where that is not its place in work
   // order
   int* first_of = reinterpret_cast<int*>(xch + 2 * 2 * kRows);
+  int* held = first_of + kSortMax;  // kSpan: the requests, where there are few (SpanRequests)
+  const SpanRequests request{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch,
+                             geo.total_new, held};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   Place at{rank & 1u, rank & ~1u, kSplit ? rank >> 1 : 0u,
-           kSplit ? cluster_nctarank() >> 1 : 1u, 0};
+           kSplit ? cluster_nctarank() >> 1 : 1u, {0, 1}};
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -1093,8 +1098,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 4; ++i) mbar_init(&bar.l_full[i], 2);
     mbar_init(&bar.drain, 2);
     bar.abort_flag = 0;
+    bar.own_keys = 0;
     fence_barrier_init();
   }
+  if (kOwn) __syncthreads();  // (the sum of own keys begins at 0)
   if (warp == 0 && lane == 0) {
     prefetch_tensormap(&map_q);
     prefetch_tensormap(&map_k);
@@ -1108,11 +1115,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   for (int i = threadIdx.x; i < 2 * 2 * kRows; i += kThreads) xch[i] = 1;
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
+  if (kSpan) {
+    if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+    if (kOwn) span_own_keys(geo.own, kThreads, &bar.own_keys);
+    __syncthreads();
+  }
   if (geo.batch <= kSortMax) {
     // rank requests by total length, longest first (ties by index)
     // (kSpan: prefix_lens has the numbers of keys)
     auto length = [&](int b) {
-      return ld_plain(prefix_lens + b) + (kSpan ? 0 : ld_plain(new_lens + b));
+      return kSpan ? held[b] : ld_plain(prefix_lens + b) + ld_plain(new_lens + b);
     };
     for (int b = threadIdx.x; b < geo.batch; b += kThreads) {
       const int tb = length(b);
@@ -1126,31 +1138,38 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   if (warp == 2) {
-    auto request = [&](int b) {
-      return span_request(geo.span, b, geo.total_new, prefix_lens, new_lens, cu_new_lens);
-    };
     if (kSpan) {
-      const SpanPlan plan = span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                                      kOwn ? &geo.own : nullptr, 2, request);
-      at.share = plan.share;
+      int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
+      if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      const SpanPlan plan =
+          span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
+                    kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 2,
+                    item_start, order, request);
+      at.deal = plan.deal;
+      if (at.deal.share) span_scan(at.deal, geo.Hkv, geo.G, order, item_start, first, request);
       if (lane == 0) {
-        bar.share = plan.share;
+        bar.deal = plan.deal;
         bar.workers = plan.workers;
+        // Both CTAs of a pair work out their first piece here: sent by the producer of
+        // one, it came 2 us later.
+        const int worker = static_cast<int>(blockIdx.x / 2), units = item_start[geo.batch];
+        int u = worker, end = units;
+        if (at.deal.share) span_share(at.deal, worker, units, u, end);
+        int* m = bar.item_msg[0];
+        m[0] = -1;
+        bar.next_unit = 0;
+        if (u < end && worker < plan.workers)
+          bar.next_unit = span_message(u, item_start, geo, at, worker, request, m);
+        mbar_arrive(&bar.item_full[0]);
       }
     }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
     int running = 0;
-    for (int b0 = 0; b0 < geo.batch; b0 += 32) {
+    for (int b0 = 0; !kSpan && b0 < geo.batch; b0 += 32) {
       const int p = b0 + lane;
       const int b = p < geo.batch ? (geo.batch <= kSortMax ? order[p] : p) : p;
       int cnt = 0;
-      if (kSpan && p < geo.batch) {
-        const SpanRequest r = request(b);
-        if (r.bad && at.parity == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-        const int steps = r.n > 0 ? span_steps(r.T) : 0;
-        if (steps > 0)
-          cnt = geo.Hkv * span_tiles(r.n, geo.G) * (at.share ? steps + kSpanLead : 1);
-      } else if (p < geo.batch) {
+      if (p < geo.batch) {
         const int n = ld_plain(new_lens + b), P = ld_plain(prefix_lens + b);
         const int cu = ld_plain(cu_new_lens + b);
         const bool sane = n >= 0 && P >= 0 && cu >= 0 && cu + n <= geo.total_new;
@@ -1164,11 +1183,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane >= o) incl += y;
       }
       if (p < geo.batch) item_start[p] = running + incl - cnt;
-      if (kSpan && geo.span.shared && p < geo.batch && geo.batch <= kSortMax)
-        first_of[b] = running + incl - cnt;
       running += __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (lane == 0) item_start[geo.batch] = running;
+    if (!kSpan && lane == 0) item_start[geo.batch] = running;
   }
   Remote rm;
   {
@@ -1189,7 +1206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
   const int total_items = item_start[geo.batch];  // (shares: units)
-  if (kSpan) at.share = bar.share;
+  if (kSpan) at.deal = bar.deal;
   // each cluster has one item; should there be more (see producer2), every pair takes
   // whole ones
   if (kSplit && total_items > static_cast<int>(gridDim.x / (2 * at.splits)))
@@ -1199,13 +1216,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (kSpan && warp >= 4) {
     const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
     const int64_t all = static_cast<int64_t>(gridDim.x) * (kThreads - 128);
-    span_write_plan(geo.span, geo.batch, at.share, item_start, order, me, all);
+    span_write_plan(geo.span, at.deal, bar.workers, geo.Hkv, geo.G, item_start, order, request,
+                    me, all);
     if (geo.span.shared)
-      span_priors(geo.span, geo.batch, geo.G, geo.total_new,
-                  geo.batch <= kSortMax ? first_of : item_start, prefix_lens, cu_new_lens, me, all);
+      span_priors(geo.span, at.deal, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
-      span_zeros(geo.span, geo.batch, geo.Hq, kD, geo.total_new, prefix_lens, new_lens,
-                 cu_new_lens, out, me, all);
+      span_zeros(geo.Hq, kD, request, out, me, all);
   }
   float2* part = reinterpret_cast<float2*>(smem_k);  // splits: free once the roles are done
   if (own_cta) {
@@ -1220,7 +1236,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 0) {
     producer2<true, kImg, kSpan>(at, smem_q, smem_k, bar, rm, item_start, total_items, geo, &map_q,
                     &map_k, &map_img_k, block_table, prefix_lens, new_lens, cu_new_lens, status,
-                    work_counter);
+                    work_counter, held);
   } else if (warp == 1) {
     if (at.parity == 0 && lane == 0) s_issuer2<kSpan>(at, smem_q, smem_k, bar, rm, tmem, geo);
     __syncwarp();
@@ -1230,7 +1246,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 3) {
     producer2<false, kImg, kSpan>(at, smem_q, smem_v, bar, rm, item_start, total_items, geo, &map_q,
                      &map_v, &map_img_v, block_table, prefix_lens, new_lens, cu_new_lens, status,
-                     work_counter);
+                     work_counter, held);
   } else if (warp >= 4) {
     softmax2h<kSplit, kSpan>(at, smem_q, bar, rm, tmem, xch, geo, out, part);
   }
@@ -1277,8 +1293,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn2() {
   return fn;
 }
 
-size_t smem_bytes2(int batch, bool shared = false) {
-  return (shared && batch <= kSortMax ? kSortMax * sizeof(int) : 0) + 1024 + 2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
+size_t smem_bytes2(int batch, bool span = false) {
+  return (span && batch <= kSortMax ? kSortMax * sizeof(int) + kSpanHeldBytes : 0) + 1024 + 2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
          (static_cast<size_t>(batch) + 1) * sizeof(int) +
          (batch <= kSortMax ? kSortMax * sizeof(int16_t) : 0) + 2 * 2 * kRows * sizeof(uint16_t);
 }
@@ -1367,7 +1383,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   const auto& cfg = pool->cfg;
   if (cfg.head_dim != kD)
     return fail(GC_ERR_UNSUPPORTED, "%s: pair kernel needs head_dim 128", a.who);
-  const size_t smem = smem_bytes2(a.batch, span && span->shared);
+  const size_t smem = smem_bytes2(a.batch, span != nullptr);
   static_assert(2 * kOwnBytes <= 2 * kQBytes + 2 * kRing * kSlotBytes, "own keys: shared memory");
   // at most this many items, of at most this many 128-key steps
   const long long G = a.num_q_heads / cfg.num_kv_heads;
@@ -1480,7 +1496,8 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
                                 : kernel2(splits, unpacked != nullptr);
   cudaError_t e = prepare_kernel(kernel, splits, smem);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
-  if (geo.more_items) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
+  // (a join that follows leaves the counter at 0)
+  if (geo.more_items && !geo.span.cuts) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3(static_cast<unsigned>(2 * splits * clusters));

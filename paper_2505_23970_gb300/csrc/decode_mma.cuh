@@ -673,12 +673,17 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
       // holds (64 KB of loads in flight): 32 contexts of 8000 keys, 128 q / 8 kv heads,
       // 172.9 -> 165.4 us, 6.5 TB/s.  The variants of 12 warps lose by it (64
       // multi-turn contexts 155 -> 164 us).
-      if constexpr (D == 128 && NT == 2 && !kQ8) {
+      // So it does where other CTAs work on a shared prefix and the memory is not full.
+      if constexpr (!kQ8 && ((D == 128 && NT == 2) || S::kGroups > 1)) {
         const bool later = ((i + 2) >> 5) != (i >> 5);
         const uint64_t at = __shfl_sync(0xffffffffu, later ? nxt.k : cur.k, (i + 2) & 31) & ~1ull;
         if (key_of(i + 2) < k1 && at != 0) {
-          prefetch_l2(at + lane * 128);  // 16 rows of 256 bytes
-          prefetch_l2(at + v_after + lane * 128);
+          if constexpr (D == 128) {
+            prefetch_l2(at + lane * 128);  // 16 rows of 256 bytes
+            prefetch_l2(at + v_after + lane * 128);
+          } else {
+            prefetch_l2(at + (lane < 16 ? 0 : v_after) + (lane & 15) * 128);
+          }
         }
       }
       float s[NT][4];

@@ -129,6 +129,7 @@ gc_status gc_kv_pool_create(const gc_pool_config* cfg, void* dev_mem, size_t dev
   p->data_bytes = need - kTrailer;
   p->status = reinterpret_cast<int32_t*>(p->data + p->data_bytes);
   p->work_counter = p->status + 32;    // 128 bytes into the control block
+  p->span_counter = p->status + 48;    // 192 bytes in
   p->merge_counters = p->status + 64;  // 256 bytes in, kMergeCounters ints
   static_assert(256 + gc::kMergeCounters * 4 <= kTrailer, "control block too small");
   p->owned = owned;
@@ -179,6 +180,7 @@ gc_status gc_kv_pool_check(gc_kv_pool* pool, cudaStream_t stream, int32_t* devic
   if (e == cudaSuccess) e = cudaMemset(pool->status, 0, sizeof host);
   // a kernel that gave up on a wait may have left decode merge counters
   // raised: after any error, clear them (nothing runs on the pool now)
+  if (e == cudaSuccess && host != GC_OK) e = cudaMemset(pool->span_counter, 0, sizeof(int32_t));
   if (e == cudaSuccess && host != GC_OK)
     e = cudaMemset(pool->merge_counters, 0, gc::kMergeCounters * sizeof(int32_t));
   if (e == cudaSuccess) e = cudaDeviceSynchronize();

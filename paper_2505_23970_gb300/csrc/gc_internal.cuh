@@ -16,6 +16,7 @@ struct gc_kv_pool {
   size_t data_bytes;
   int32_t* status;        // device status word (first error recorded by a kernel)
   int32_t* work_counter;  // attention work items (control block, cleared by launches that need it)
+  int32_t* span_counter;  // the same of cross attention (kept at 0 where its join follows)
   int32_t* merge_counters;  // [kMergeCounters] decode merge counters (control block, kept at 0)
   void* owned;            // cudaMalloc'd block, or nullptr if caller-owned
   cudaMemPool_t scratch;  // stream-ordered scratch (kv_q8.cu), nullptr if there is none

@@ -13,6 +13,9 @@
 //    binary32) are joined afterwards:
 //        out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  M = max_s m_s.
 //    A share has at most two such pieces: its first (slot 0), and its last (slot 1).
+//    Where requests have several row tiles (as many nearly all of them), a share belongs
+//    to a team of as many workers, each of which takes one tile of every item in it: the
+//    tiles then read the same keys at the same time, from memory once.
 #pragma once
 
 #include "decode_mma.cuh"
@@ -37,10 +40,11 @@ struct OwnDecode {
 constexpr int kSpanRows = 256;      // q rows of an item
 constexpr int kSpanRequests = 512;  // most requests of a call that is cut into shares
 // An item costs about this many steps beyond its own (its first scores, the last
-// product and the results), a join about kSpanJoin.
+// product and the results); writing the pieces and joining them takes about kSpanJoin.
 constexpr int kSpanLead = 2;
-constexpr int kSpanJoin = 4;
+constexpr int kSpanJoin = 12;
 constexpr int kSpanMinShare = 4;
+constexpr int kSpanInL2 = 1024;  // steps and kv heads whose K and V stay in the L2: 64 MB at d = 128
 
 struct SpanGeom {
   int32_t cap;      // keys a block-table row can hold
@@ -49,22 +53,30 @@ struct SpanGeom {
   int32_t cuts;     // items may be cut
   int32_t shared;   // requests are groups (new_lens is not given); whole items' results
                     // go to `whole`, not to the output
-  int32_t* plan;    // SpanPlan, for the joins
+  int32_t* plan;    // SpanDeal, workers that have a share
+  int4* cuts_at;    // cross attention: per share, see SpanCutItem
   int4* prior;      // shared: per request, see SpanPrior
   DecodeParts whole;  // shared: [request][q head]
   float2* ml;       // [2 * workers][stride]: reference maximum, sum
   float* o;         // [2 * workers][stride][d]
 };
 
-// The plan in the workspace: [0] units of a share, 0: whole items; [1] all units;
-// where items may be cut: [2] requests, then from kPlanStart each one's first unit (and
-// the end), from kPlanOrder its number.
-constexpr int kPlanStart = 4, kPlanOrder = kPlanStart + kSpanRequests + 4;
-constexpr int kPlanWords = kPlanOrder + kSpanRequests;
+// The cut item that begins in a worker's share, as two int4: shares c0 (this one) to c1
+// (-1: there is none), slot of the first piece, kv head and tile; then first token and number of
+// tokens of its request.
+struct SpanCutItem {
+  int32_t c1, first, g, tile, cu, n, unused[2];
+};
+
+// How the work is dealt out: units of a share (0: whole items) and workers that have the
+// same share, a row tile each (1: the tiles of an item are items of their own).
+struct SpanDeal {
+  int share, team;
+};
 
 // A request of a shared prefix, as an int4: its G rows of kv head g are rows
-// [row, row + G) of the item whose first unit is unit + g * head_units.  steps: of the
-// item; 0: no shared keys, -1: the request is skipped.
+// [row, row + G) of the group's, in the item whose first unit is unit + g * head_units.
+// steps: of the item; 0: no shared keys, -1: the request is skipped.
 struct SpanPrior {
   int32_t unit, head_units, steps, row;
 };
@@ -91,67 +103,34 @@ __device__ __forceinline__ int span_tiles(int n, int G) {
   return (n * G + kSpanRows - 1) / kSpanRows;
 }
 
-// Units of a share, 0 for whole items, and the workers that take part, worked out by one
-// warp; every CTA comes to the same answer.  request(b) gives a SpanRequest.
-// own: the other workers decode own keys (shares always; own->geo.batch requests).
-constexpr int kSpanStart = 9;  // units in the time that a span CTA takes beyond an own one's
-struct SpanPlan {
-  int share, workers;
+// All requests of a call, held in shared memory (three words each) where there are at
+// most kSpanRequests: every role looks them up, and each look-up in global memory was a
+// latency in front of the first product (prologue 3.7 us, with them held 2).
+struct SpanRequests {
+  const SpanGeom& sp;
+  const int32_t *lens, *new_lens, *cu;
+  int batch, total_new;
+  int* held;
+
+  // every thread of a CTA of `threads`; true in those that saw a bad request
+  __device__ __forceinline__ bool hold(int threads) const {
+    bool bad = false;
+    for (int b = threadIdx.x; b < batch; b += threads) {
+      const SpanRequest r = span_request(sp, b, total_new, lens, new_lens, cu);
+      bad |= r.bad;
+      if (batch > kSpanRequests) continue;
+      held[b] = r.T;
+      held[kSpanRequests + b] = r.n;
+      held[2 * kSpanRequests + b] = r.cu;
+    }
+    return bad;
+  }
+  __device__ __forceinline__ SpanRequest operator()(int b) const {
+    if (batch > kSpanRequests) return span_request(sp, b, total_new, lens, new_lens, cu);
+    return {held[kSpanRequests + b], held[b], held[2 * kSpanRequests + b], false};
+  }
 };
-template <typename F>
-__device__ SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int G, const OwnDecode* own,
-                              int sms_per_worker, F request) {
-  if (!sp.cuts || batch > kSpanRequests) return {0, sp.workers};
-  const int lane = threadIdx.x & 31;
-  long long units = 0, items = 0;
-  int most = 0;
-  for (int b = lane; b < batch; b += 32) {
-    const SpanRequest r = request(b);
-    const int st = r.n > 0 ? span_steps(r.T) : 0;
-    if (st == 0) continue;
-    const long long n = static_cast<long long>(Hkv) * span_tiles(r.n, G);
-    items += n;
-    units += n * (st + kSpanLead);
-    most = max(most, st + kSpanLead);
-  }
-  long long keys = 0;  // own ones, a pair's fixed cost counted as 128
-  if (own)
-    for (int b = lane; b < own->geo.batch; b += 32) {
-      const int T = ld_plain(own->lens + b);
-      if (T > 0) keys += T + 128ll;
-    }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    units += __shfl_xor_sync(0xffffffffu, units, o);
-    items += __shfl_xor_sync(0xffffffffu, items, o);
-    if (own) keys += __shfl_xor_sync(0xffffffffu, keys, o);
-  }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if (own) {
-    // the number of span workers for which the slower side is fastest
-    if (units == 0) return {kSpanMinShare, 0};
-    const float u = static_cast<float>(units);
-    const float o = static_cast<float>(keys) * Hkv * own->weight * (1.f / (128 * 8));
-    float best = INFINITY;
-    int n = 1;
-    for (int w = 1 + lane; w < sp.workers; w += 32) {
-      const float t = fmaxf(fmaxf(u / w, kSpanMinShare) + kSpanStart,
-                            o / ((sp.workers - w) * sms_per_worker));
-      if (t < best) best = t, n = w;
-    }
-    const unsigned t = __reduce_min_sync(0xffffffffu, __float_as_uint(best));  // (positive)
-    n = __reduce_min_sync(0xffffffffu, __float_as_uint(best) == t ? n : sp.workers);
-    return {max(static_cast<int>((units + n - 1) / n), kSpanMinShare), n};
-  }
-  if (units + sp.workers >= (1ll << 30)) return {0, sp.workers};  // units are 32-bit ints
-  // Time in steps: of whole items, in rounds of the longest or as the last of them ends,
-  // against equal shares and their join.
-  const long long even = (units + sp.workers - 1) / sp.workers;
-  const long long rounds = (items + sp.workers - 1) / sp.workers;
-  const long long whole = min(rounds * most, even + most);
-  const long long share = max(even, static_cast<long long>(kSpanMinShare));
-  return {share + kSpanJoin < whole ? static_cast<int>(share) : 0, sp.workers};
-}
+constexpr size_t kSpanHeldBytes = 3 * kSpanRequests * sizeof(int);
 
 // The place of a request's items in work order; start: first unit (shares) or item.
 __device__ __forceinline__ int span_place(const int* start, int batch, int u) {
@@ -163,46 +142,193 @@ __device__ __forceinline__ int span_place(const int* start, int batch, int u) {
   return lo;
 }
 
-// The work at unit u of a share that ends before unit `end` (shares), or at item u
-// (share 0).  nt 0: there is none left in the share.  slot: of its pieces, -1 if it is a
-// whole item; next: the unit after it.
+// How a call is dealt out, and the workers that take part, worked out by one warp; every
+// CTA comes to the same answer.  start: each place's first item.
+// own_keys >= 0: the other workers decode so many own keys, 128 of them and a kv head
+// taking an SM own_weight eighths of a unit (then shares always).
+constexpr int kSpanStart = 5;  // units in the time that a span CTA takes beyond an own one's
+struct SpanPlan {
+  SpanDeal deal;
+  int workers;
+};
+__device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int G,
+                                     long long own_keys, int own_weight, int sms_per_worker,
+                                     const int* start, const int16_t* order,
+                                     const SpanRequests& request) {
+  if (!sp.cuts || batch > kSpanRequests) return {{0, 1}, sp.workers};
+  const int lane = threadIdx.x & 31;
+  long long units = 0, per_tile = 0;
+  int least = INT32_MAX, most = 0, tiles = 0;
+  for (int b = lane; b < batch; b += 32) {
+    const SpanRequest r = request(b);
+    const int st = r.n > 0 ? span_steps(r.T) : 0;
+    if (st == 0) continue;
+    const int t = span_tiles(r.n, G);
+    per_tile += static_cast<long long>(Hkv) * (st + kSpanLead);
+    units += static_cast<long long>(Hkv) * t * (st + kSpanLead);
+    least = min(least, st + kSpanLead);
+    most = max(most, st + kSpanLead);
+    tiles = max(tiles, t);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    units += __shfl_xor_sync(0xffffffffu, units, o);
+    per_tile += __shfl_xor_sync(0xffffffffu, per_tile, o);
+  }
+  tiles = __reduce_max_sync(0xffffffffu, tiles);
+  if (units == 0) return {{own_keys >= 0 ? kSpanMinShare : 0, 1}, own_keys >= 0 ? 0 : sp.workers};
+  // Where K and V are more than half of the L2, several tiles read them together (two
+  // questions of 43 tokens, 64/8 heads, on 131072 states each: 440 us without teams, 394);
+  // at most an eighth of a team's work may be tiles that a request does not have.
+  const bool apart = tiles > 1 && per_tile > kSpanInL2;
+  int team = apart && 4 * tiles <= sp.workers && 8 * per_tile * tiles <= 9 * units ? tiles : 1;
+  if (own_keys >= 0) {
+    // the number of teams for which the slower side is fastest
+    const float u = static_cast<float>(team > 1 ? per_tile : units);
+    const float o = static_cast<float>(own_keys) * Hkv * own_weight * (1.f / (128 * 8));
+    float best = INFINITY;
+    int n = 1;
+    for (int w = 1 + lane; w * team < sp.workers; w += 32) {
+      const float t = fmaxf(fmaxf(__fdividef(u, w), kSpanMinShare) + kSpanStart,
+                            __fdividef(o, (sp.workers - w * team) * sms_per_worker));
+      if (t < best) best = t, n = w;
+    }
+    const unsigned t = __reduce_min_sync(0xffffffffu, __float_as_uint(best));  // (positive)
+    n = __reduce_min_sync(0xffffffffu, __float_as_uint(best) == t ? n : sp.workers);
+    const int all = static_cast<int>(team > 1 ? per_tile : units);
+    return {{max((all + n - 1) / n, kSpanMinShare), team}, n * team};
+  }
+  if (units + sp.workers >= (1ll << 30)) return {{0, 1}, sp.workers};  // units are 32-bit ints
+  // Time in steps: of whole items, longest first, against equal shares and their join.  Of
+  // whole items at least r + 1 times the length of item r * workers, for every r; lane r.
+  // Shares without teams must gain an eighth besides where the tiles read K and V apart
+  // (8 x 1024 tokens of 64/8 heads over 8192 states: whole items 1440 us, shares 1640).
+  const int even = (static_cast<int>(units) + sp.workers - 1) / sp.workers;
+  const long long nth = static_cast<long long>(lane) * sp.workers;
+  int whole = 0;
+  if (nth < start[batch]) {
+    const int p = span_place(start, batch, static_cast<int>(nth));
+    whole = (lane + 1) * (span_steps(request(order[p]).T) + kSpanLead);
+  }
+  const long long rounds = (start[batch] + sp.workers - 1ll) / sp.workers;
+  const int end = even + __reduce_min_sync(0xffffffffu, least);  // as the shortest end last
+  whole = max(__reduce_max_sync(0xffffffffu, whole),
+              static_cast<int>(min(static_cast<long long>(end),
+                                   rounds * __reduce_max_sync(0xffffffffu, most))));
+  int share = max(even, kSpanMinShare), cost = share + (apart ? share / 8 : 0);
+  if (team > 1) {
+    const int teams = sp.workers / team;
+    const int s = max((static_cast<int>(per_tile) + teams - 1) / teams, kSpanMinShare);
+    if (s <= cost)
+      share = cost = s;
+    else
+      team = 1;
+  }
+  if (cost + kSpanJoin >= whole) return {{0, 1}, sp.workers};
+  return {{share, team}, sp.workers};
+}
+
+// Own keys of the requests behind shared prefixes, a request's fixed cost counted as the
+// decode kernel counts it, summed over the CTA by all of its threads (sum: cleared before).
+__device__ inline void span_own_keys(const OwnDecode& own, int threads, unsigned long long* sum) {
+  unsigned long long keys = 0;
+  for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
+    const int T = ld_plain(own.lens + b);
+    if (T > 0) keys += T + static_cast<unsigned>(kPairKeys);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xffffffffu, keys, o);
+  if ((threadIdx.x & 31) == 0 && keys > 0) atomicAdd(sum, keys);
+}
+
+// Worker's units [first, end) of its share.
+__device__ __forceinline__ void span_share(SpanDeal deal, int worker, int units, int& first,
+                                           int& end) {
+  const int64_t u = static_cast<int64_t>(worker / deal.team) * deal.share;
+  first = static_cast<int>(min(u, static_cast<int64_t>(units)));
+  end = static_cast<int>(min(u + deal.share, static_cast<int64_t>(units)));
+}
+
+// The work of a worker at unit u of its share, or (share 0) item u.  nt 0: there is none
+// left in the share.  slot: of its pieces, -1 if it is a whole item; next: the unit after.
 struct SpanPiece {
   int b, g, tile, n, T, cu, j0, nt, slot, next;
 };
-template <typename F>
-__device__ __forceinline__ SpanPiece span_piece(int u, int share, int worker, int end, int batch,
+__device__ __forceinline__ SpanPiece span_piece(int u, SpanDeal deal, int worker, int batch,
                                                 const int* start, const int16_t* order, int Hkv,
-                                                int G, F request) {
+                                                int G, const SpanRequests& request) {
   SpanPiece w;
-  const int p = span_place(start, batch, u);
-  w.b = batch <= kSpanRequests ? order[p] : p;
-  const SpanRequest r = request(w.b);
-  w.n = r.n;
-  w.T = r.T;
-  w.cu = r.cu;
-  const int steps = span_steps(r.T), tiles = span_tiles(r.n, G), local = u - start[p];
-  int item = local;
-  w.j0 = 0;
-  w.nt = steps;
-  w.slot = -1;
-  w.next = u + 1;
-  if (share) {
-    const int per = steps + kSpanLead;
-    item = local / per;
-    const int off = local - item * per, to = min(per, off + (end - u));
-    w.j0 = max(0, off - kSpanLead);
-    w.nt = max(0, to - kSpanLead - w.j0);
-    if (w.nt < steps) w.slot = 2 * worker + (u == worker * share ? 0 : 1);
-    w.next = u + to - off;
+  int first = 0, end = 0;
+  if (deal.share) span_share(deal, worker, start[batch], first, end);
+  while (true) {
+    const int p = span_place(start, batch, u);
+    w.b = batch <= kSpanRequests ? order[p] : p;
+    const SpanRequest r = request(w.b);
+    w.n = r.n;
+    w.T = r.T;
+    w.cu = r.cu;
+    const int steps = span_steps(r.T), tiles = span_tiles(r.n, G), local = u - start[p];
+    int item = local;
+    w.j0 = 0;
+    w.nt = steps;
+    w.slot = -1;
+    w.next = u + 1;
+    if (deal.share) {
+      const int per = steps + kSpanLead;
+      item = local / per;
+      const int off = local - item * per, to = min(per, off + (end - u));
+      w.j0 = max(0, off - kSpanLead);
+      w.nt = max(0, to - kSpanLead - w.j0);
+      if (w.nt < steps) w.slot = 2 * worker + (u == first ? 0 : 1);
+      w.next = u + to - off;
+    }
+    if (deal.team > 1) {
+      w.g = item;
+      w.tile = worker % deal.team;
+      if (w.tile >= tiles) w.nt = 0;  // the request has no such tile: the next one
+      if (w.nt > 0 || w.next >= end) return w;
+      u = w.next;
+      continue;
+    }
+    // the tiles that read the same keys one after the other
+    w.g = item / tiles;
+    w.tile = item - w.g * tiles;
+    return w;
   }
-  // the tiles that read the same keys one after the other
-  w.g = item / tiles;
-  w.tile = item - w.g * tiles;
-  return w;
+}
+
+// Exclusive scan, by one warp, of the places' items (share 0) or a team's units into start, and
+// each request's into first_of where it is given.
+__device__ inline void span_scan(SpanDeal deal, int Hkv, int G, const int16_t* order, int* start,
+                                 int* first_of, const SpanRequests& request) {
+  const int lane = threadIdx.x & 31, batch = request.batch;
+  int running = 0;
+  for (int p0 = 0; p0 < batch; p0 += 32) {
+    const int p = p0 + lane;
+    const int b = p < batch && batch <= kSpanRequests ? order[p] : p;
+    int cnt = 0;
+    if (p < batch) {
+      const SpanRequest r = request(b);
+      const int steps = r.n > 0 ? span_steps(r.T) : 0;
+      if (steps > 0)
+        cnt = Hkv * (deal.team > 1 ? 1 : span_tiles(r.n, G)) * (deal.share ? steps + kSpanLead : 1);
+    }
+    int incl = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (p < batch) start[p] = running + incl - cnt;
+    if (p < batch && first_of) first_of[b] = running + incl - cnt;
+    running += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) start[batch] = running;
+  __syncwarp();
 }
 
 // Pieces of the item whose first unit is u0: of shares c0 to c1, the first in slot
-// `first` of c0's, the others in slot 0.
+// `first` of c0's, the others in slot 0.  (A worker's slots: 2 worker + 0 and 1.)
 struct SpanCut {
   int c0, c1, first;
 };
@@ -215,55 +341,70 @@ __device__ __forceinline__ SpanCut span_cut(int u0, int steps, int share) {
 }
 
 // Thread `me` of `all`: the plan for the joins, where items may be cut.
-__device__ inline void span_write_plan(const SpanGeom& sp, int batch, int share, const int* start,
-                                       const int16_t* order, int64_t me, int64_t all) {
+__device__ inline void span_write_plan(const SpanGeom& sp, SpanDeal deal, int workers, int Hkv,
+                                       int G, const int* start, const int16_t* order,
+                                       const SpanRequests& request, int64_t me, int64_t all) {
   if (!sp.plan) return;
   if (me == 0) {
-    sp.plan[0] = share;
-    sp.plan[1] = start[batch];
-    sp.plan[2] = batch;
+    sp.plan[0] = deal.share;
+    sp.plan[1] = deal.team;
+    sp.plan[2] = workers;
   }
-  if (share == 0 || sp.shared) return;
-  for (int64_t p = me; p <= batch; p += all) {
-    sp.plan[kPlanStart + p] = start[p];
-    if (p < batch) sp.plan[kPlanOrder + p] = order[p];
+  if (deal.share == 0 || sp.shared) return;
+  const int batch = request.batch;
+  for (int64_t worker = me; worker < workers; worker += all) {
+    SpanCutItem x{-1, 0, 0, 0, 0, 0, {0, 0}};
+    const int c0 = static_cast<int>(worker) / deal.team;
+    const int64_t end = (c0 + 1ll) * deal.share;
+    if (end < start[batch]) {
+      // the item that the share's end lies in
+      const int p = span_place(start, batch, static_cast<int>(end));
+      const SpanRequest r = request(order[p]);
+      const int steps = span_steps(r.T), per = steps + kSpanLead, tiles = span_tiles(r.n, G);
+      const int local = static_cast<int>(end) - start[p], item = local / per;
+      const SpanCut cut = span_cut(static_cast<int>(end) - (local - item * per), steps, deal.share);
+      const int tile = deal.team > 1 ? static_cast<int>(worker) % deal.team : item % tiles;
+      if (cut.c0 == c0 && cut.c1 > c0 && tile < tiles)
+        x = SpanCutItem{cut.c1, cut.first, deal.team > 1 ? item : item / tiles, tile, r.cu, r.n,
+                        {0, 0}};
+    }
+    sp.cuts_at[2 * worker] = make_int4(x.c1, x.first, x.g, x.tile);
+    sp.cuts_at[2 * worker + 1] = make_int4(x.cu, x.n, 0, 0);
   }
 }
 
 // Thread `me` of `all`: the requests' rows of the groups' items.  first_of: each
 // group's first unit or item.
-__device__ inline void span_priors(const SpanGeom& sp, int groups, int G, int batch,
-                                   const int* first_of, const int32_t* lens, const int32_t* cu,
-                                   int64_t me, int64_t all) {
-  for (int64_t b = me; b < batch; b += all) {
-    int lo = 0, hi = groups;  // the last group whose first request is <= b
+__device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, int G, const int* first_of,
+                                   const SpanRequests& request, int64_t me, int64_t all) {
+  for (int64_t b = me; b < request.total_new; b += all) {
+    int lo = 0, hi = request.batch;  // the last group whose first request is <= b
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (ld_plain(cu + mid) <= b) lo = mid; else hi = mid;
+      if (ld_plain(request.cu + mid) <= b) lo = mid; else hi = mid;
     }
-    const SpanRequest r = span_request(sp, lo, batch, lens, nullptr, cu);
+    const SpanRequest r = request(lo);
     SpanPrior p{0, 0, -1, 0};
     if (!r.bad && b >= r.cu && b < r.cu + r.n) {
       const int row = (static_cast<int>(b) - r.cu) * G, per = span_steps(r.T) + kSpanLead;
       p.steps = span_steps(r.T);
-      p.unit = first_of[lo] + row / kSpanRows * per;
-      p.head_units = span_tiles(r.n, G) * per;
-      p.row = row % kSpanRows;
+      p.unit = first_of[lo] + (deal.team > 1 ? 0 : row / kSpanRows * per);
+      p.head_units = (deal.team > 1 ? 1 : span_tiles(r.n, G)) * per;
+      p.row = row;
     }
     sp.prior[b] = make_int4(p.unit, p.head_units, p.steps, p.row);
   }
 }
 
 // Thread `me` of `all` (whole warps): zeros for the rows of requests without keys.
-__device__ inline void span_zeros(const SpanGeom& sp, int batch, int Hq, int D, int total_new,
-                                  const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
-                                  __nv_bfloat16* out, int64_t me, int64_t all) {
+__device__ inline void span_zeros(int Hq, int D, const SpanRequests& request, __nv_bfloat16* out,
+                                  int64_t me, int64_t all) {
   const int lane = threadIdx.x & 31;
-  for (int b0 = 0; b0 < batch; b0 += 32) {
-    const bool none = b0 + lane < batch && ld_plain(lens + b0 + lane) == 0;
+  for (int b0 = 0; b0 < request.batch; b0 += 32) {
+    const bool none = b0 + lane < request.batch && request(b0 + lane).T == 0;
     uint32_t which = __ballot_sync(0xffffffffu, none);
     for (; which; which &= which - 1) {
-      const SpanRequest r = span_request(sp, b0 + __ffs(which) - 1, total_new, lens, new_lens, cu);
+      const SpanRequest r = request(b0 + __ffs(which) - 1);
       const int64_t words = static_cast<int64_t>(r.n) * Hq * D / 8;
       uint4* dst = reinterpret_cast<uint4*>(out) + static_cast<int64_t>(r.cu) * Hq * D / 8;
       for (int64_t i = me; i < words; i += all) dst[i] = make_uint4(0, 0, 0, 0);
@@ -275,7 +416,7 @@ __device__ inline void span_zeros(const SpanGeom& sp, int batch, int Hq, int D, 
 // A call's workspace: where its parts are, in bytes from its start.
 struct SpanSpace {
   int64_t slots, stride;
-  size_t plan, prior, whole_ml, whole_o, ml, o, end;
+  size_t plan, cuts_at, prior, whole_ml, whole_o, ml, o, end;
 };
 inline SpanSpace span_space(const gc_kv_pool* pool, int64_t rows, int64_t batch, int64_t max_blocks,
                             int num_q_heads, bool shared) {
@@ -294,7 +435,8 @@ inline SpanSpace span_space(const gc_kv_pool* pool, int64_t rows, int64_t batch,
     return x;
   };
   const size_t out_rows = static_cast<size_t>(rows) * num_q_heads, row = c.head_dim * sizeof(float);
-  s.plan = take(shared || s.slots ? kPlanWords * sizeof(int32_t) : 0);
+  s.plan = take(shared || s.slots ? 3 * sizeof(int32_t) : 0);
+  s.cuts_at = take(shared ? 0 : s.slots * sizeof(int4));
   s.prior = take(shared ? rows * sizeof(int4) : 0);
   s.whole_ml = take(shared ? out_rows * sizeof(float2) : 0);
   s.whole_o = take(shared ? out_rows * row : 0);
@@ -312,6 +454,7 @@ inline SpanGeom span_geom(const SpanSpace& s, int64_t cap, bool shared, void* wo
   g.cuts = s.slots > 0;
   g.shared = shared ? 1 : 0;
   g.plan = shared || s.slots ? reinterpret_cast<int32_t*>(w + s.plan) : nullptr;
+  g.cuts_at = shared ? nullptr : reinterpret_cast<int4*>(w + s.cuts_at);
   g.prior = shared ? reinterpret_cast<int4*>(w + s.prior) : nullptr;
   if (shared)
     g.whole = DecodeParts{reinterpret_cast<float*>(w + s.whole_o),

@@ -21,9 +21,11 @@ struct Join {
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  // row `row` of the slots of a cut item
+  // row `row` of a cut item's tile `tile`
   template <int D>
-  __device__ __forceinline__ void pieces(const SpanGeom& sp, const SpanCut& cut, int row, int c) {
+  __device__ __forceinline__ void pieces(const SpanGeom& sp, const SpanCut& cut, int team, int tile,
+                                         int row, int c) {
+    const int lane = team > 1 ? tile : 0;  // of the team
     constexpr int kBatch = 8;
     for (int s0 = cut.c0; s0 <= cut.c1; s0 += kBatch) {
       float2 ml[kBatch];
@@ -32,7 +34,8 @@ struct Join {
       for (int k = 0; k < kBatch; ++k) {
         const int s = s0 + k;
         const int64_t x =
-            static_cast<int64_t>(2 * s + (s == cut.c0 ? cut.first : 0)) * sp.stride + row;
+            static_cast<int64_t>(2 * (s * team + lane) + (s == cut.c0 ? cut.first : 0)) * sp.stride +
+            row;
         ml[k] = s <= cut.c1 ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
         o[k] = s <= cut.c1 ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
                            : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -79,38 +82,27 @@ struct Join {
 // which it begins and which it is the last of: block (share, row chunk).
 template <int D>
 __global__ void __launch_bounds__(256)
-    cross_join_kernel(SpanGeom sp, const int32_t* lens, const int32_t* new_lens, const int32_t* cu,
-                      __nv_bfloat16* out, int Hq, int G, int total_new) {
+    cross_join_kernel(SpanGeom sp, __nv_bfloat16* out, int Hq, int G, int* work_counter) {
   dependent_begin();
   constexpr int kLanes = D / 4;  // four columns each
   constexpr int kRowsPerBlock = 256 / kLanes;
   constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of an item
-  const int share = ld_plain(sp.plan), units = ld_plain(sp.plan + 1);
-  const int c0 = static_cast<int>(blockIdx.x) / kChunks, chunk = static_cast<int>(blockIdx.x) % kChunks;
-  const int64_t end = (static_cast<int64_t>(c0) + 1) * share;
-  if (share == 0 || end >= units) return;
-  const int* start = sp.plan + kPlanStart;
-  int lo = 0, hi = ld_plain(sp.plan + 2);  // the last request whose first unit is <= end
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (ld_plain(start + mid) <= end) lo = mid; else hi = mid;
-  }
-  const SpanRequest r =
-      span_request(sp, ld_plain(sp.plan + kPlanOrder + lo), total_new, lens, new_lens, cu);
-  const int steps = span_steps(r.T), per = steps + kSpanLead, tiles = span_tiles(r.n, G);
-  const int local = static_cast<int>(end) - ld_plain(start + lo), item = local / per;
-  const int u0 = static_cast<int>(end) - (local - item * per);
-  const SpanCut cut = span_cut(u0, steps, share);
-  if (cut.c0 != c0 || cut.c1 == c0) return;
-  const int g = item / tiles, tile = item - g * tiles;
-  const int row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
-  const int at = tile * kSpanRows + row;  // q row of the request and kv head
-  if (at >= r.n * G) return;
+  const int worker = static_cast<int>(blockIdx.x) / kChunks;
+  const int chunk = static_cast<int>(blockIdx.x) % kChunks;
+  const int share = ld_plain(sp.plan), team = ld_plain(sp.plan + 1), workers = ld_plain(sp.plan + 2);
+  // (a SpanCutItem)
+  const int4 x = ld_plain(sp.cuts_at + 2 * worker), y = ld_plain(sp.cuts_at + 2 * worker + 1);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *work_counter = 0;  // for the next call
+  if (share == 0 || worker >= workers || x.x < 0) return;
+  const SpanCut cut{worker / team, x.x, x.y};
+  const int g = x.z, cu = y.x, row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
+  const int at = x.w * kSpanRows + row;  // q row of the request and kv head
+  if (at >= y.y * G) return;
   const int c = static_cast<int>(threadIdx.x) % kLanes;
   Join j;
-  j.pieces<D>(sp, cut, row, c);
+  j.pieces<D>(sp, cut, team, x.w, row, c);
   *reinterpret_cast<uint2*>(
-      out + (static_cast<int64_t>(r.cu + at / G) * Hq + g * G + at % G) * D + 4 * c) = j.rounded();
+      out + (static_cast<int64_t>(cu + at / G) * Hq + g * G + at % G) * D + 4 * c) = j.rounded();
 }
 
 // Decode behind a shared prefix: every row of a request that is not skipped.
@@ -124,7 +116,7 @@ __global__ void __launch_bounds__(256)
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
   if (row >= rows) return;
   const int b = static_cast<int>(row / Hq), h = static_cast<int>(row - static_cast<int64_t>(b) * Hq);
-  const int T = ld_plain(own_lens + b), share = ld_plain(sp.plan);
+  const int T = ld_plain(own_lens + b), share = ld_plain(sp.plan), team = ld_plain(sp.plan + 1);
   const int4 p = ld_plain(sp.prior + b);  // SpanPrior
   if (p.z < 0) record_error(status, GC_ERR_OUT_OF_RANGE);
   if (T < 0 || T > own_cap || p.z < 0) return;
@@ -141,7 +133,7 @@ __global__ void __launch_bounds__(256)
   const int g = h / G;
   if (share && p.z > 0) cut = span_cut(p.x + g * p.y, p.z, share);
   if (cut.c1 > cut.c0) {
-    j.pieces<D>(sp, cut, p.w + (h - g * G), c);
+    j.pieces<D>(sp, cut, team, p.w / kSpanRows, p.w % kSpanRows + (h - g * G), c);
   } else {
     float2 sml;
     float4 so;
@@ -155,7 +147,7 @@ __global__ void __launch_bounds__(256)
 gc_status launch_items(const gc_kv_pool* pool, const AttnArgs& a, const SpanGeom& span,
                        cudaStream_t stream, const OwnDecode* own = nullptr) {
   return pool->cfg.head_dim == 128
-             ? launch_attn_tc2(pool, a, stream, pool->work_counter, nullptr, &span, own)
+             ? launch_attn_tc2(pool, a, stream, pool->span_counter, nullptr, &span, own)
              : launch_attn_tc_span(pool, a, stream, span, own);
 }
 
@@ -188,9 +180,9 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
   const int chunks = kSpanRows / (1024 / cfg.head_dim);
   const auto join = cfg.head_dim == 128 ? cross_join_kernel<128> : cross_join_kernel<64>;
   const cudaError_t e = launch_dependent(
-      join, static_cast<unsigned>(space.slots / 2 * chunks), 256, 0, stream, span, a.lens,
-      a.new_lens, a.start, static_cast<__nv_bfloat16*>(a.out), a.num_q_heads,
-      a.num_q_heads / cfg.num_kv_heads, a.rows);
+      join, static_cast<unsigned>(space.slots / 2 * chunks), 256, 0, stream, span,
+      static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, a.num_q_heads / cfg.num_kv_heads,
+      pool->span_counter);
   if (e != cudaSuccess) return cuda_fail(e, who);
   return GC_OK;
 }
@@ -257,7 +249,7 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
     if (st != GC_OK) return st;
     const OwnDecode with{static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.lens,
                          static_cast<float*>(own.workspace), pool->merge_counters,
-                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 15 : 5};
+                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 12 : 5};
     st = launch_items(pool, args, span, stream, &with);
   } else {
     st = launch_decode(pool, own, stream);
