@@ -70,6 +70,8 @@ _lib = None
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
     """Load libgc.so once; raise if it is missing (it is never emulated)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -138,10 +140,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
 def _addr(x) -> int | None:
     if x is None:
         return None
+    data_ptr = getattr(x, "data_ptr", None)  # most are tensors
+    if data_ptr is not None:
+        return data_ptr()
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "value"):  # ctypes.c_void_p
         return x.value
     raise TypeError(f"cannot take a device/host address of {type(x).__name__}")

@@ -27,13 +27,14 @@ namespace {
 using ptx::pack_bf16x2;
 
 constexpr int kBlock = 256;
-constexpr int kMinUnits = 8;  // units of a token, at least: one kv head of 64, K and V
+constexpr int kMinThreads = 4;  // of a token, at least: the units of a head of 64
 
 struct RopeGeom {
   int32_t Hq, Hkv, ps_shift, num_pages, batch, max_blocks, layer, total_new;
   int32_t head_shift;    // units of a head, log2 (d / 16)
   int32_t rot_units;     // units of a head that are rotated (rot / 16)
-  int32_t units;         // units of a token: (Hq + 2 Hkv) << head_shift
+  int32_t heads;         // Hq + 2 Hkv
+  int32_t threads;       // of a token: ceil(heads / W) << head_shift
   int32_t interleaved, n_positions;
   int64_t q_stride, k_stride, v_stride;  // 16-byte words between tokens
 };
@@ -92,71 +93,65 @@ __device__ __forceinline__ void turn(uint32_t& xy, float c, float s) {
   xy = pack_bf16x2(fmaf(x, c, -(y * s)), fmaf(y, c, x * s));
 }
 
+// A thread has the units of W neighbouring heads at one place of them.
 template <int W>
 __global__ void __launch_bounds__(kBlock)
     append_rope_kernel(const uint4* q, uint4* q_out, const uint4* k_new, const uint4* v_new,
                        uint8_t* pool, const int32_t* block_table, const int32_t* prefix_lens,
                        const int32_t* cu_new_lens, const float* cos_sin,
                        const int32_t* positions, RopeGeom g, int32_t* status) {
-  __shared__ Place places[kBlock * W / kMinUnits + 2];
+  __shared__ Place places[kBlock / kMinThreads + 2];
   dependent_begin();
-  const int64_t total = static_cast<int64_t>(g.total_new) * g.units;
+  const int64_t total = static_cast<int64_t>(g.total_new) * g.threads;
   const int hs = g.head_shift;
-  for (int64_t base = static_cast<int64_t>(blockIdx.x) * (kBlock * W); base < total;
-       base += static_cast<int64_t>(gridDim.x) * (kBlock * W)) {
-    const int64_t t0 = base / g.units;
-    const int first = static_cast<int>(base - t0 * g.units);  // unit of token t0
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * kBlock; base < total;
+       base += static_cast<int64_t>(gridDim.x) * kBlock) {
+    const int64_t t0 = base / g.threads;
+    const int first = static_cast<int>(base - t0 * g.threads);  // thread of token t0
+    const int local = first + static_cast<int>(threadIdx.x);
+    const int tl = local / g.threads, u = local - tl * g.threads;
+    const int64_t t = t0 + tl;
+    const int h0 = (u >> hs) * W, s = u & ((1 << hs) - 1);  // first head (q, then k, then v)
+    // the unit's words: of the rotated section (n apart), of the columns after it, or of V
+    const bool rotated = s < g.rot_units;
+    const int n = rotated ? g.rot_units : (1 << hs) - g.rot_units;
+    const int in_head = rotated ? s : g.rot_units + s;
     uint4 a[W], b[W];
-    int tl[W], head[W], s[W];  // token after t0, head (q, then k, then v), unit of the head
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const int local = first + w * kBlock + static_cast<int>(threadIdx.x);
-      tl[w] = local / g.units;
-      const int u = local - tl[w] * g.units;
-      head[w] = u >> hs;
-      s[w] = u & ((1 << hs) - 1);
-      const int64_t t = t0 + tl[w];
-      if (t >= g.total_new) {
-        head[w] = -1;
-        continue;
-      }
+      int h = h0 + w;
+      if (t >= g.total_new || h >= g.heads) continue;
       const uint4* src;
-      int h = head[w];
       if (h < g.Hq)
         src = q + t * g.q_stride;
       else if ((h -= g.Hq) < g.Hkv)
         src = k_new + t * g.k_stride;
       else
         src = v_new + t * g.v_stride, h -= g.Hkv;
-      // the unit's words: of the rotated section, of the columns after it, or of V
-      const int rot = head[w] < g.Hq + g.Hkv ? g.rot_units : 0;
-      const int n = s[w] < rot ? rot : (1 << hs) - rot;
-      const int at = (h << (hs + 1)) + (s[w] < rot ? s[w] : rot + s[w]);
-      a[w] = ld_plain(src + at);
-      b[w] = ld_plain(src + at + n);
+      src += (h << (hs + 1)) + in_head;
+      a[w] = ld_plain(src);
+      b[w] = ld_plain(src + n);
     }
-    const int tokens = (first + kBlock * W - 1) / g.units + 1;  // of this block's units
+    const int tokens = (first + kBlock - 1) / g.threads + 1;  // of this block's threads
     __syncthreads();  // the places of the round before have been read
     for (int i = threadIdx.x; i < tokens; i += kBlock)
       if (t0 + i < g.total_new)
         places[i] = look_up(t0 + i, g, block_table, prefix_lens, cu_new_lens, positions, status);
     __syncthreads();
+    if (t >= g.total_new) continue;
+    const Place p = places[tl];
+    if (p.pos < 0) continue;
+    if (rotated && h0 < g.Hq + g.Hkv) {
+      // angles of the unit's pairs: 8 in a row, or 4 of each word's
+      const float4* cs = reinterpret_cast<const float4*>(
+          cos_sin + static_cast<int64_t>(p.pos) * 16 * g.rot_units);
+      const int i0 = g.interleaved ? s : 2 * s;
+      const int i1 = g.interleaved ? s + g.rot_units : 2 * s + 1;
+      const float4 c0 = ld_plain(cs + i0), c1 = ld_plain(cs + i1);
+      const float4 s0 = ld_plain(cs + 2 * g.rot_units + i0), s1 = ld_plain(cs + 2 * g.rot_units + i1);
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      if (head[w] < 0) continue;
-      const Place p = places[tl[w]];
-      int h = head[w];
-      const int rot = h < g.Hq + g.Hkv ? g.rot_units : 0;
-      const int n = s[w] < rot ? rot : (1 << hs) - rot;
-      if (p.pos < 0 || (h >= g.Hq && p.page < 0)) continue;
-      if (s[w] < rot) {
-        // angles of the unit's pairs: 8 in a row, or 4 of each word's
-        const float4* cs = reinterpret_cast<const float4*>(
-            cos_sin + static_cast<int64_t>(p.pos) * 16 * g.rot_units);
-        const int i0 = g.interleaved ? s[w] : 2 * s[w];
-        const int i1 = g.interleaved ? s[w] + rot : 2 * s[w] + 1;
-        const float4 c0 = ld_plain(cs + i0), c1 = ld_plain(cs + i1);
-        const float4 s0 = ld_plain(cs + 2 * rot + i0), s1 = ld_plain(cs + 2 * rot + i1);
+      for (int w = 0; w < W; ++w) {
+        if (h0 + w >= g.Hq + g.Hkv) continue;
         if (g.interleaved) {
           turn(a[w].x, c0.x, s0.x);
           turn(a[w].y, c0.y, s0.y);
@@ -173,10 +168,14 @@ __global__ void __launch_bounds__(kBlock)
           turn(a[w].w, b[w].w, c1.z, s1.z, c1.w, s1.w);
         }
       }
-      const int in_head = s[w] < rot ? s[w] : rot + s[w];
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      int h = h0 + w;
+      if (h >= g.heads || (h >= g.Hq && p.page < 0)) continue;
       uint4* dst;
       if (h < g.Hq) {
-        dst = q_out + ((((t0 + tl[w]) * g.Hq + h) << (hs + 1)) + in_head);
+        dst = q_out + (((t * g.Hq + h) << (hs + 1)) + in_head);
       } else {
         const int kv = h < g.Hq + g.Hkv ? 0 : 1;
         h -= g.Hq + kv * g.Hkv;
@@ -212,21 +211,28 @@ gc_status launch_append_rope(const gc_kv_pool* pool, const RopeArgs& a, cudaStre
   g.total_new = a.total_new_tokens;
   g.head_shift = ilog2(cfg.head_dim / 16);
   g.rot_units = a.rot_dim / 16;
-  g.units = (g.Hq + 2 * g.Hkv) << g.head_shift;
+  g.heads = g.Hq + 2 * g.Hkv;
   g.interleaved = a.interleaved ? 1 : 0;
   g.n_positions = a.n_positions;
   g.q_stride = a.q_stride / 8;
   g.k_stride = a.k_stride / 8;
   g.v_stride = a.v_stride / 8;
-  const int64_t units = static_cast<int64_t>(g.total_new) * g.units;
-  const int64_t blocks = (units + kBlock - 1) / kBlock;
+  // Two units a thread, which then reads the angles once for both, where one each would
+  // not be resident at once (8 x 1024 tokens of 64/8 heads of 128: one 76.5 us, two 55.8,
+  // 6.1 TB/s, four 55.5, eight 64; 4400 tokens of 32/8 heads of 64: 15.4, 12.7, 14.1,
+  // 15.8); a call of few tokens is latency alone.
+  const bool few = (static_cast<int64_t>(g.total_new) * g.heads << g.head_shift) <=
+                   static_cast<int64_t>(pool->num_sms) * 2048;
+  const int W = few ? 1 : 2;
+  g.threads = (g.heads + W - 1) / W << g.head_shift;
+  const int64_t blocks = (static_cast<int64_t>(g.total_new) * g.threads + kBlock - 1) / kBlock;
   const int64_t cap = static_cast<int64_t>(pool->num_sms) * 32;
   const unsigned grid = static_cast<unsigned>(blocks < cap ? blocks : cap);
   const cudaError_t e = launch_dependent(
-      append_rope_kernel<1>, grid, kBlock, 0, stream, static_cast<const uint4*>(a.q),
-      static_cast<uint4*>(a.q_out), static_cast<const uint4*>(a.k_new),
-      static_cast<const uint4*>(a.v_new), pool->data, a.block_table, a.prefix_lens, a.cu_new_lens,
-      a.cos_sin, a.positions, g, pool->status);
+      few ? append_rope_kernel<1> : append_rope_kernel<2>, grid, kBlock, 0, stream,
+      static_cast<const uint4*>(a.q), static_cast<uint4*>(a.q_out),
+      static_cast<const uint4*>(a.k_new), static_cast<const uint4*>(a.v_new), pool->data,
+      a.block_table, a.prefix_lens, a.cu_new_lens, a.cos_sin, a.positions, g, pool->status);
   if (e != cudaSuccess) return cuda_fail(e, "gc_kv_append_rope: kernel launch");
   return GC_OK;
 }
