@@ -133,6 +133,8 @@ struct Barriers {
   uint64_t s_free[2];  // d = 64: S_i has been read by its softmax
   uint64_t item_full[2], item_empty[2];  // work-item ring, producer -> other roles
   int item_slot[2];
+  SpanPiece piece[2];  // kSpan: the items, decoded
+  int next_unit;       // kSpan, shares: after the first piece
   unsigned long long own_keys;  // kOwn: their sum
   uint32_t tmem_base;
   int abort_flag;
@@ -154,7 +156,6 @@ struct Item {
 struct SpanItem : Item {
   int j0;    // first K/V step of the piece
   int slot;  // the piece's, -1 for a whole item
-  int next;  // unit after it
 };
 template <bool kSpan>
 using ItemOf = std::conditional_t<kSpan, SpanItem, Item>;
@@ -172,38 +173,10 @@ __device__ __forceinline__ int* span_held(const int* item_start, int batch) {
 
 // item_start[p] = first item of the p-th request in work order; the request
 // itself is order[p] when the batch was sorted (order != nullptr), else p.
-// kSpan: prefix_lens has the numbers of keys, every row sees all of its request's, or of
-// a piece's range of steps; `it` is then a unit of this CTA's share, if there are shares.
-template <bool kSpan>
 __device__ __forceinline__ bool decode_item(int it, const int* item_start, const Geom& geo,
-                                            SpanDeal deal, const int32_t* prefix_lens,
+                                            const int32_t* prefix_lens,
                                             const int32_t* new_lens,
-                                            const int32_t* cu_new_lens,
-                                            ItemOf<kSpan>& w) {
-  if constexpr (kSpan) {
-    const int worker = static_cast<int>(blockIdx.x);
-    int* held = span_held(item_start, geo.batch);
-    const SpanPiece r = span_piece(
-        it, deal, worker, geo.batch, item_start, reinterpret_cast<const int16_t*>(item_start + geo.batch + 1), geo.Hkv, geo.G,
-        SpanRequests{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch, geo.total_new, held});
-    w.b = r.b;
-    w.g = r.g;
-    w.j0 = r.j0;
-    w.T = r.T;
-    w.n = r.n;
-    w.cu = r.cu;
-    w.nt = r.nt;
-    w.slot = r.slot;
-    w.next = r.next;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r0 = (r.tile * 2 + i) * kTileM;
-      w.valid[i] = r0 < r.n * geo.G;
-      w.tok0[i] = r0 / geo.G;
-      w.nt_i[i] = w.valid[i] ? w.nt : 0;
-    }
-    return true;
-  }
+                                            const int32_t* cu_new_lens, Item& w) {
   int lo = 0, hi = geo.batch;  // last b with item_start[b] <= it
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -236,6 +209,26 @@ __device__ __forceinline__ bool decode_item(int it, const int* item_start, const
   return true;
 }
 
+// kSpan: prefix_lens has the numbers of keys, every row sees all of its request's, or of
+// a piece's range of steps.  The producer decodes an item for all roles.
+__device__ __forceinline__ void item_from_piece(const SpanPiece& r, const Geom& geo, SpanItem& w) {
+  w.b = r.b;
+  w.g = r.g;
+  w.j0 = r.j0;
+  w.T = r.T;
+  w.n = r.n;
+  w.cu = r.cu;
+  w.nt = r.nt;
+  w.slot = r.slot;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r0 = (r.tile * 2 + i) * kTileM;
+    w.valid[i] = r0 < r.n * geo.G;
+    w.tok0[i] = r0 / geo.G;
+    w.nt_i[i] = w.valid[i] ? w.nt : 0;
+  }
+}
+
 // Work items are handed out dynamically: the producer warp claims the next
 // one from the launch's counter and publishes it to the other roles through a
 // 2-slot ring in shared memory; -1 ends the CTA's work.
@@ -259,32 +252,37 @@ __device__ __forceinline__ int claim_item(Barriers& bar, uint32_t k, int* work_c
   return __shfl_sync(0xffffffffu, it, 0);
 }
 
-// The same for the next piece of this CTA's share, from `unit` on; the item is decoded
-// here because a share may end in front of an item's first step.
-template <int D, bool kSpan>
+// kSpan: item k of the ring, decoded for all roles; the first one is there when the roles
+// begin.  unit: of this CTA's share, the next.
 __device__ __forceinline__ int claim_piece(Barriers& bar, uint32_t k, int& unit,
-                                           const int* item_start, const Geom& geo, SpanDeal deal,
-                                           const int32_t* prefix_lens, const int32_t* new_lens,
-                                           const int32_t* cu_new_lens, ItemOf<kSpan>& w,
+                                           const int* item_start, const int16_t* order,
+                                           int* work_counter, int total_items, const Geom& geo,
+                                           SpanDeal deal, const SpanRequests& request,
                                            volatile int* abortp, bool& ok) {
   const int s = k & 1;
-  ok = mbar_wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1, abortp);
+  ok = k == 0 ? mbar_wait(&bar.item_full[0], 0, abortp)
+              : mbar_wait(&bar.item_empty[s], ((k >> 1) & 1) ^ 1, abortp);
   ok = __all_sync(0xffffffffu, ok);
-  int it = -1;
-  int first, end;
-  span_share(deal, static_cast<int>(blockIdx.x), item_start[geo.batch], first, end);
-  if constexpr (kSpan) {
-    if (unit < end) {
-      decode_item<kSpan>(unit, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
-      if (w.nt > 0) it = unit;
-      unit = w.next;
+  if (ok && k > 0 && (threadIdx.x & 31) == 0) {
+    const int worker = static_cast<int>(blockIdx.x), grid = static_cast<int>(gridDim.x);
+    int first, end = total_items, it = unit;
+    if (deal.share)
+      span_share(deal, worker, total_items, first, end);
+    else  // (as claim_item)
+      it = geo.more_items ? grid + atomicAdd(work_counter, 1) : worker + static_cast<int>(k) * grid;
+    if (it < end) {
+      bar.piece[s] =
+          span_piece(it, deal, worker, geo.batch, item_start, order, geo.Hkv, geo.G, request);
+      unit = bar.piece[s].next;
+      if (bar.piece[s].nt == 0) it = -1;
+    } else {
+      it = -1;
     }
-  }
-  if ((threadIdx.x & 31) == 0 && ok) {
     bar.item_slot[s] = it;
     mbar_arrive(&bar.item_full[s]);
   }
-  return it;
+  __syncwarp();
+  return ok ? *reinterpret_cast<volatile int*>(&bar.item_slot[s]) : -1;
 }
 
 // Read item k of the ring (all consumer threads); the caller releases the
@@ -428,24 +426,25 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
   uint32_t armed8 = 0, armed8_par = 0;  // the same for the code copies of image pages
   int armed_q = -1, armed_vfix = -1;
   bool ok = true;
-  int unit = 0;  // kSpan, shares: this CTA's next
-  if (kSpan && deal.share) {
-    int end;
-    span_share(deal, static_cast<int>(blockIdx.x), total_items, unit, end);
-  }
+  int unit = bar.next_unit;  // kSpan, shares: this CTA's next
+  const int16_t* order = reinterpret_cast<const int16_t*>(item_start + geo.batch + 1);
+  const SpanRequests request{geo.span, prefix_lens, new_lens, cu_new_lens, geo.batch,
+                             geo.total_new, span_held(item_start, geo.batch)};
   const uint32_t box_bytes = static_cast<uint32_t>(geo.ps) * 128;  // one page, one column block
   const uint32_t page_codes = static_cast<uint32_t>(geo.ps) * D;   // one page of 8-bit codes
 
   for (uint32_t k = 0; ok; ++k) {
     ItemOf<kSpan> w;
-    int it;
-    if (kSpan && deal.share)
-      it = claim_piece<D, kSpan>(bar, k, unit, item_start, geo, deal, prefix_lens, new_lens,
-                                 cu_new_lens, w, abortp, ok);
-    else
-      it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
-    if (!ok || it < 0) break;
-    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
+    if constexpr (kSpan) {
+      const int it = claim_piece(bar, k, unit, item_start, order, work_counter, total_items, geo,
+                                 deal, request, abortp, ok);
+      if (!ok || it < 0) break;
+      item_from_piece(bar.piece[k & 1], geo, w);
+    } else {
+      const int it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
+      if (!ok || it < 0) break;
+      decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
+    }
     // ---- Q tiles
     ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
     if (!ok) break;
@@ -642,7 +641,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
 template <int D, bool kSpan>
 __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, uint32_t tmem,
                            const int* item_start, int total_items, const Geom& geo,
-                           SpanDeal deal, const int32_t* prefix_lens,
+                           const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens) {
   using C = Cfg<D>;
@@ -658,10 +657,13 @@ __device__ void mma_issuer(int i, uint8_t* smem_q, uint8_t* smem_kv, Barriers& b
   for (uint32_t k = 0; ok; ++k) {
     const int it = read_item(bar, k, abortp, ok);
     if (!ok) break;
+    ItemOf<kSpan> w;
+    if constexpr (kSpan) {
+      if (it >= 0) item_from_piece(bar.piece[k & 1], geo, w);
+    }
     mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
-    ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
+    if constexpr (!kSpan) decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -840,7 +842,7 @@ __device__ __forceinline__ bool tile_exp_after(const uint32_t (&sr)[4][32], uint
 
 template <int D, int i, bool kSpan>
 __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
-                           int total_items, const Geom& geo, SpanDeal deal,
+                           int total_items, const Geom& geo,
                            const int32_t* prefix_lens,
                            const int32_t* new_lens,
                            const int32_t* cu_new_lens,
@@ -860,11 +862,14 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
   for (uint32_t k = 0; ok; ++k) {
     const int it = read_item(bar, k, abortp, ok);
     if (!ok) break;
+    ItemOf<kSpan> w;
+    if constexpr (kSpan) {
+      if (it >= 0) item_from_piece(bar.piece[k & 1], geo, w);
+    }
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(&bar.item_empty[k & 1]);
     if (it < 0) break;
-    ItemOf<kSpan> w;
-    decode_item<kSpan>(it, item_start, geo, deal, prefix_lens, new_lens, cu_new_lens, w);
+    if constexpr (!kSpan) decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
     // K_j sits in ring use kv_base + 2j, V_j in use kv_base + 2j + 1
     const uint32_t kv_base = kv_count;
     kv_count += 2 * w.nt;
@@ -1068,11 +1073,13 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
   if (kSpan) {
+    const unsigned long long keys = kOwn ? span_own_keys(geo.own, kThreads) : 0;
     if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    if (kOwn) span_own_keys(geo.own, kThreads, &bar.own_keys);
+    if (kOwn) span_add_keys(keys, &bar.own_keys);
     __syncthreads();
   }
-  if (geo.batch <= kSortMax) {
+  const bool rank_in_warp = kSpan && geo.batch <= 32;  // (by the warp that plans)
+  if (geo.batch <= kSortMax && !rank_in_warp) {
     // rank requests by total length, longest first (ties by index)
     auto total_len = [&](int b) {
       return kSpan ? request.held[b] : ld_plain(prefix_lens + b) + ld_plain(new_lens + b);
@@ -1087,9 +1094,10 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       order[rank] = static_cast<int16_t>(b);
     }
   }
-  __syncthreads();
+  if (!rank_in_warp) __syncthreads();
   if (warp == 2) {
     if (kSpan) {
+      if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
       if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
@@ -1100,6 +1108,18 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       if (lane == 0) {
         bar.deal = plan.deal;
         bar.workers = plan.workers;
+        const int worker = static_cast<int>(blockIdx.x), units = item_start[geo.batch];
+        int u = worker, end = units;
+        if (plan.deal.share) span_share(plan.deal, worker, units, u, end);
+        bar.item_slot[0] = -1;
+        bar.next_unit = 0;
+        if (u < end && worker < plan.workers) {
+          bar.piece[0] = span_piece(u, plan.deal, worker, geo.batch, item_start, order, geo.Hkv,
+                                    geo.G, request);
+          bar.next_unit = bar.piece[0].next;
+          if (bar.piece[0].nt > 0) bar.item_slot[0] = u;
+        }
+        mbar_arrive(&bar.item_full[0]);
       }
     }
     // work items per request: Hkv * ceil(n_b * G / 256); exclusive scan in work order
@@ -1148,8 +1168,9 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       using S = dec::SharedShape<D, kOwn>;
       const int first = bar.workers, group = S::group();
       dec::decode_cta<S, D, kOwn, false, true>(
-          smem_q + group * kOwnBytes, 2 * (static_cast<int>(blockIdx.x) - first) + group,
-          2 * (static_cast<int>(gridDim.x) - first), geo.own.q, geo.own.block_table, geo.own.lens,
+          smem_q + group * kOwnBytes,
+          dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,
+                        2 * (static_cast<int>(gridDim.x) - first)}, geo.own.q, geo.own.block_table, geo.own.lens,
           out, geo.own.workspace, geo.own.geo, status, geo.own.merge_counters);
     }
   } else if (warp < 4) {
@@ -1161,7 +1182,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     } else if (warp == 1 || warp == 2) {
       if (lane == 0)
         mma_issuer<D, kSpan>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
-                      deal, prefix_lens, new_lens, cu_new_lens);
+                      prefix_lens, new_lens, cu_new_lens);
       __syncwarp();
     }
   } else if (kQ8 && warp >= kThreads / 32) {
@@ -1170,10 +1191,10 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   } else {
     regs_inc<kQ8 ? kRegsSoftmaxQ8 : kRegsSoftmax>();
     if (warp < 8)
-      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, deal, prefix_lens,
+      softmax_wg<D, 0, kSpan>(bar, tmem, item_start, total_items, geo, prefix_lens,
                               new_lens, cu_new_lens, out);
     else
-      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, deal, prefix_lens,
+      softmax_wg<D, 1, kSpan>(bar, tmem, item_start, total_items, geo, prefix_lens,
                               new_lens, cu_new_lens, out);
   }
   tc_fence_before();

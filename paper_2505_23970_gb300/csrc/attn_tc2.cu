@@ -1116,11 +1116,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
   if (kSpan) {
+    const unsigned long long keys = kOwn ? span_own_keys(geo.own, kThreads) : 0;
     if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    if (kOwn) span_own_keys(geo.own, kThreads, &bar.own_keys);
+    if (kOwn) span_add_keys(keys, &bar.own_keys);
     __syncthreads();
   }
-  if (geo.batch <= kSortMax) {
+  const bool rank_in_warp = kSpan && geo.batch <= 32;  // (by the warp that plans)
+  if (geo.batch <= kSortMax && !rank_in_warp) {
     // rank requests by total length, longest first (ties by index)
     // (kSpan: prefix_lens has the numbers of keys)
     auto length = [&](int b) {
@@ -1136,9 +1138,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       order[rk] = static_cast<int16_t>(b);
     }
   }
-  __syncthreads();
+  if (!rank_in_warp) __syncthreads();
   if (warp == 2) {
     if (kSpan) {
+      if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
       if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
@@ -1229,8 +1232,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       using S = dec::SharedShape<kD, 1>;
       const int first = 2 * bar.workers, group = S::group();
       dec::decode_cta<S, kD, 1, false, true>(
-          smem_q + group * kOwnBytes, 2 * (static_cast<int>(blockIdx.x) - first) + group,
-          2 * (static_cast<int>(gridDim.x) - first), geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo, status,
+          smem_q + group * kOwnBytes,
+          dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,
+                        2 * (static_cast<int>(gridDim.x) - first)}, geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo, status,
           geo.own.merge_counters);
     }
   } else if (warp == 0) {

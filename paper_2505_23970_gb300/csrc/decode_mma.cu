@@ -68,9 +68,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
                       int* merge_counters) {
   extern __shared__ __align__(16) uint8_t smem[];
   dependent_begin();
-  decode_cta<Shape<D, NT>, D, NT, kQ8, kParts>(smem, static_cast<int>(blockIdx.x),
-                                               static_cast<int>(gridDim.x), q, block_table,
-                                               seq_lens, out, ws, geo, status, merge_counters);
+  decode_cta<Shape<D, NT>, D, NT, kQ8, kParts>(smem, dec::ByBlock{}, q, block_table, seq_lens, out,
+                                               ws, geo, status, merge_counters);
 }
 
 template <int D, int NT, bool kQ8, bool kParts>

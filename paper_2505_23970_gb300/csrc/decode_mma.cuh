@@ -497,10 +497,20 @@ __device__ __forceinline__ void prefetch_l2(uint64_t at) {
 // ---------------------------------------------------------------- one CTA
 // kParts: the keys are a part of each request's (those after a shared prefix), and the
 // results go to geo.own; a request may have none of them.
-// (CTA, or group of S::kThreads threads of one, `cta` of `ctas`; the caller has waited for the kernel
-// before.)
-template <typename S, int D, int NT, bool kQ8, bool kParts>
-__device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
+// Which of the CTAs (or groups of S::kThreads threads of one) that decode a call this is.
+struct ByBlock {
+  __device__ int cta() const { return static_cast<int>(blockIdx.x); }
+  __device__ int ctas() const { return static_cast<int>(gridDim.x); }
+};
+struct ByNumber {
+  int cta_, ctas_;
+  __device__ int cta() const { return cta_; }
+  __device__ int ctas() const { return ctas_; }
+};
+
+// One of them; the caller has waited for the kernel before.
+template <typename S, int D, int NT, bool kQ8, bool kParts, typename Who>
+__device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
                                            const __nv_bfloat16* q, const int32_t* block_table,
                                            const int32_t* seq_lens, __nv_bfloat16* out, float* ws,
                                            const DecGeom& geo, int32_t* status,
@@ -526,7 +536,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
     for (int b = S::tid(); b < geo.batch; b += S::kThreads) {
       const int T = ld_plain(seq_lens + b);
       if (T < 1 || T > cap) {
-        if (cta == 0 && !(kParts && T == 0)) record_error(status, GC_ERR_OUT_OF_RANGE);
+        if (who.cta() == 0 && !(kParts && T == 0)) record_error(status, GC_ERR_OUT_OF_RANGE);
       } else {
         most = max(most, T);
         ++n;
@@ -541,7 +551,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
     }
   }
   S::sync();
-  const int grid = ctas;
+  const int grid = who.ctas();
   // A CTA's piece costs several us of latencies and merging however short it is,
   // so with enough short pairs to give half of the warps one each, a warp takes
   // a pair alone (128 contexts of 12-100 keys, 8 kv heads: 40.6 -> 9.1 us).
@@ -582,9 +592,9 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
   // by warp and ranges: every step-th unit; shares: this CTA's units [u0, end)
   const int per = max(max(1, kMinShare >> geo.unit_shift), (total + grid - 1) / grid);
   const int step = by_warp ? grid * S::kWarps : grid;
-  const int u0 = by_warp ? cta * S::kWarps + warp
-                 : geo.range_tiles ? cta
-                                   : min(total, cta * per);
+  const int u0 = by_warp ? who.cta() * S::kWarps + warp
+                 : geo.range_tiles ? who.cta()
+                                   : min(total, who.cta() * per);
   const int end = by_warp || geo.range_tiles ? total : min(total, u0 + per);
   // partials: O^T rows, then (reference max, sum) pairs; ranges by [head][split],
   // shares by [CTA][slot][head]
@@ -783,7 +793,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, int cta, int ctas,
     S::sync();
     const int64_t part0 = geo.range_tiles
                               ? head0 * geo.max_splits + w.part
-                              : (static_cast<int64_t>(cta) * 2 + w.part) * S::kHeads;
+                              : (static_cast<int64_t>(who.cta()) * 2 + w.part) * S::kHeads;
     const int64_t part_step = geo.range_tiles ? geo.max_splits : 1;
     for (int x = S::tid(); x < geo.G * (D / 2); x += S::kThreads) {
       const int h = x / (D / 2), d = 2 * (x % (D / 2));

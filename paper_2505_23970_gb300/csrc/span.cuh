@@ -34,7 +34,7 @@ struct OwnDecode {
   float* workspace;
   int* merge_counters;
   DecGeom geo;
-  int32_t weight;  // time of 128 own keys and a kv head on one SM, in eighths of a unit
+  int32_t weight;  // time of 128 own keys and a kv head on one SM, in 1/16 of a unit
 };
 
 constexpr int kSpanRows = 256;      // q rows of an item
@@ -145,7 +145,7 @@ __device__ __forceinline__ int span_place(const int* start, int batch, int u) {
 // How a call is dealt out, and the workers that take part, worked out by one warp; every
 // CTA comes to the same answer.  start: each place's first item.
 // own_keys >= 0: the other workers decode so many own keys, 128 of them and a kv head
-// taking an SM own_weight eighths of a unit (then shares always).
+// taking an SM own_weight / 16 of a unit (then shares always).
 constexpr int kSpanStart = 5;  // units in the time that a span CTA takes beyond an own one's
 struct SpanPlan {
   SpanDeal deal;
@@ -183,19 +183,20 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
   const bool apart = tiles > 1 && per_tile > kSpanInL2;
   int team = apart && 4 * tiles <= sp.workers && 8 * per_tile * tiles <= 9 * units ? tiles : 1;
   if (own_keys >= 0) {
-    // the number of teams for which the slower side is fastest
-    const float u = static_cast<float>(team > 1 ? per_tile : units);
-    const float o = static_cast<float>(own_keys) * Hkv * own_weight * (1.f / (128 * 8));
-    float best = INFINITY;
-    int n = 1;
-    for (int w = 1 + lane; w * team < sp.workers; w += 32) {
-      const float t = fmaxf(fmaxf(__fdividef(u, w), kSpanMinShare) + kSpanStart,
-                            __fdividef(o, (sp.workers - w * team) * sms_per_worker));
-      if (t < best) best = t, n = w;
-    }
-    const unsigned t = __reduce_min_sync(0xffffffffu, __float_as_uint(best));  // (positive)
-    n = __reduce_min_sync(0xffffffffu, __float_as_uint(best) == t ? n : sp.workers);
-    const int all = static_cast<int>(team > 1 ? per_tile : units);
+    // The number w of teams for which both sides take as long,
+    //     u / w + kSpanStart = o / (W - w),
+    // with u units, W teams in all and o the own keys' time if they had one team:
+    //     s w^2 - (s W - u - o) w - u W = 0.
+    const int all = static_cast<int>(team > 1 ? per_tile : units), most_teams = sp.workers / team;
+    const float W = static_cast<float>(most_teams), u = static_cast<float>(all);
+    const float o = static_cast<float>(own_keys) * Hkv * own_weight /
+                    (128.f * 16.f * sms_per_worker * team);
+    const float h = 0.5f * (kSpanStart * W - u - o);
+    const float root = sqrtf(h * h + kSpanStart * u * W);
+    const float w = h > 0.f ? (h + root) / kSpanStart : u * W / (root - h);
+    // (one at least for own keys, and no share below the least)
+    int n = min(static_cast<int>(w + 0.5f), all / kSpanMinShare);
+    n = max(1, min(n, most_teams - 1));
     return {{max((all + n - 1) / n, kSpanMinShare), team}, n * team};
   }
   if (units + sp.workers >= (1ll << 30)) return {{0, 1}, sp.workers};  // units are 32-bit ints
@@ -228,17 +229,35 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
   return {{share, team}, sp.workers};
 }
 
-// Own keys of the requests behind shared prefixes, a request's fixed cost counted as the
-// decode kernel counts it, summed over the CTA by all of its threads (sum: cleared before).
-__device__ inline void span_own_keys(const OwnDecode& own, int threads, unsigned long long* sum) {
+// Thread's own keys of the requests behind shared prefixes, a request's fixed cost counted
+// as kSpanOwnKeys; and their sum over the CTA (sum: cleared before).  The cost, and the
+// weight of a key, are from two calls of 64/8 and 32/8 heads of 128 on known numbers of
+// SMs: 64 requests of 1119 keys and 128 of 255.
+constexpr int kSpanOwnKeys = 768;
+__device__ __forceinline__ unsigned long long span_own_keys(const OwnDecode& own, int threads) {
   unsigned long long keys = 0;
   for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
     const int T = ld_plain(own.lens + b);
-    if (T > 0) keys += T + static_cast<unsigned>(kPairKeys);
+    if (T > 0) keys += T + static_cast<unsigned>(kSpanOwnKeys);
   }
+  return keys;
+}
+__device__ __forceinline__ void span_add_keys(unsigned long long keys, unsigned long long* sum) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xffffffffu, keys, o);
   if ((threadIdx.x & 31) == 0 && keys > 0) atomicAdd(sum, keys);
+}
+
+// Work order of up to 32 requests, longest first (ties by number), by one warp.
+__device__ __forceinline__ void span_rank32(const SpanRequests& request, int16_t* order) {
+  const int lane = threadIdx.x & 31, T = lane < request.batch ? request(lane).T : INT32_MIN;
+  int rank = 0;
+  for (int o = 0; o < request.batch; ++o) {
+    const int x = __shfl_sync(0xffffffffu, T, o);
+    rank += x > T || (x == T && o < lane);
+  }
+  if (lane < request.batch) order[rank] = static_cast<int16_t>(lane);
+  __syncwarp();
 }
 
 // Worker's units [first, end) of its share.

@@ -249,7 +249,7 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
     if (st != GC_OK) return st;
     const OwnDecode with{static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.lens,
                          static_cast<float*>(own.workspace), pool->merge_counters,
-                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 12 : 5};
+                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 14 : 5};
     st = launch_items(pool, args, span, stream, &with);
   } else {
     st = launch_decode(pool, own, stream);
