@@ -361,3 +361,99 @@ class LayerStack:
 
     def close(self):
         self.pool.close()
+
+
+class SharedContext:
+    """Generation for groups of requests whose contexts begin with the same
+    cached pages, each request optionally with cached states of another
+    sequence (an encoder's) that its tokens attend to.
+
+    A group's prefix is restored once (``restore``); a step of one layer
+    (``step``) takes the layer's q, k and v rows as one projection gives them,
+    rotates q and k to their positions behind the prefix and appends k and v to
+    the requests' own pages (gc_kv_append_rope), then attends to the shared and
+    the own keys (gc_shared_prefix_decode_attn); ``cross`` attends to the
+    states (gc_paged_cross_attn).  ``advance`` ends a token."""
+
+    def __init__(self, Hq, Hkv, d, ps, shared_lens, group_sizes, own_tokens, state_lens=None,
+                 rot_dim=None, base: float = 500000.0, L: int = 1, seed: int = 0,
+                 device: str = "cuda"):
+        import torch
+        self.Hq, self.Hkv, self.d, self.ps, self.L, self.device = Hq, Hkv, d, ps, L, device
+        self.shared_lens = np.asarray(shared_lens, np.int32)
+        sizes = np.asarray(group_sizes, np.int32)
+        self.group = np.repeat(np.arange(sizes.size), sizes)
+        self.B, self.own_tokens = int(sizes.sum()), int(own_tokens)
+        states = np.asarray([0] * self.B if state_lens is None else state_lens, np.int32)
+        counts = [-(-self.shared_lens // ps), np.full(self.B, -(-self.own_tokens // ps)),
+                  -(-states // ps)]
+        pages = max(1, int(sum(c.sum() for c in counts)))
+        perm = np.random.default_rng(seed).permutation(pages).astype(np.int32)
+        tables, at = [], 0
+        for c in counts:
+            t = np.full((c.size, max(1, int(c.max()))), -1, np.int32)
+            for b, n in enumerate(c):
+                t[b, :n] = perm[at:at + n]
+                at += int(n)
+            tables.append(t)
+        self.shared_table, self.own_table, self.state_table = tables
+        self.pool = gcb.KVPool.create(L, Hkv, d, ps, pages, device=device)
+        self._shared, self._own, self._states = (_i32(t, device) for t in tables)
+        self._S, self._state_lens = _i32(self.shared_lens, device), _i32(states, device)
+        self._cu_requests = _i32(np.concatenate([[0], np.cumsum(sizes)]), device)
+        self._cu = _i32(np.arange(self.B + 1), device)
+        self._ones = _i32(np.ones(self.B), device)
+        self.own_lens = _i32(np.zeros(self.B), device)        # before the token
+        self.seq_lens = _i32(np.ones(self.B), device)         # with it
+        self.positions = _i32(self.shared_lens[self.group], device)
+        self.rot_dim = d if rot_dim is None else rot_dim
+        angle = np.arange(int(self.shared_lens.max(initial=0)) + self.own_tokens)[:, None] * \
+            base ** (-np.arange(0, self.rot_dim, 2) / self.rot_dim)
+        self.cos_sin = torch.from_numpy(
+            np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).to(device)
+        self.q = torch.empty((self.B, Hq, d), dtype=torch.bfloat16, device=device)
+        need = gcb.gc_shared_prefix_decode_workspace_bytes(
+            self.pool.handle, self.B, sizes.size, tables[0].shape[1], tables[1].shape[1], Hq)
+        cross = gcb.gc_paged_cross_workspace_bytes(self.pool.handle, self.B, tables[2].shape[1],
+                                                   Hq, self.B)
+        self.workspace = torch.empty(max(need, cross, 16), dtype=torch.uint8, device=device)
+
+    def restore(self, image, table: str = "shared", stream=None):
+        """Cached pages [n][L][2][Hkv][ps][d] (device) of all prefixes ("shared") or
+        all states ("states"), list after list, into the pool."""
+        t = self.shared_table if table == "shared" else self.state_table
+        ids = _i32(t[t >= 0], self.device)
+        if ids.numel():
+            gcb.gc_kv_restore(self.pool.handle, image, ids, ids.numel(), stream, None,
+                              gcb.GC_RESTORE_SRC_DEVICE)
+
+    def step(self, qkv, out, layer: int = 0, stream=None):
+        """One layer of the current token: qkv [B][Hq + 2 Hkv][d] -> out [B][Hq][d]."""
+        Hq, Hkv, h = self.Hq, self.Hkv, self.pool.handle
+        row = qkv.stride(0)
+        gcb.gc_kv_append_rope(h, qkv[:, :Hq], row, self.q, qkv[:, Hq:Hq + Hkv], row,
+                              qkv[:, Hq + Hkv:], row, self._own, self.own_lens, stream, layer,
+                              self._cu, self.B, self.own_table.shape[1], self.B, Hq, self.cos_sin,
+                              self.cos_sin.shape[0], self.rot_dim, self.positions)
+        gcb.gc_shared_prefix_decode_attn(
+            self.q, h, self._shared, self._S, self._cu_requests, self.shared_lens.size,
+            self.shared_table.shape[1], self._own, self.seq_lens, out, stream, layer, self.B,
+            self.own_table.shape[1], Hq, self.d ** -0.5, self.workspace, self.workspace.numel())
+
+    def cross(self, q, out, layer: int = 0, stream=None):
+        """q [B][Hq][d] over each request's cached states."""
+        gcb.gc_paged_cross_attn(q, self.pool.handle, self._states, self._state_lens, self._ones,
+                                out, stream, layer, self._cu, self.B, self.state_table.shape[1],
+                                self.Hq, self.d ** -0.5, self.B, self.workspace,
+                                self.workspace.numel())
+
+    def advance(self):
+        """The token is done in every layer."""
+        for x in (self.own_lens, self.seq_lens, self.positions):
+            x.add_(1)
+
+    def check(self, stream=None) -> int:
+        return self.pool.check(stream)
+
+    def close(self):
+        self.pool.close()
