@@ -140,6 +140,7 @@ struct Barriers {
   int abort_flag;
   SpanDeal deal;  // kSpan: how the work is dealt out
   int workers;    // kSpan: workers that have a share
+  bool fits;      // kSpan: the units fit their numbers
   int p0_steps;  // P tiles tile 0's softmax has published so far (pacing hint)
 };
 
@@ -1099,15 +1100,19 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     if (kSpan) {
       if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
-      if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      bool fits = true;
+      if (!kOwn) fits = span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
                     kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 1,
                     item_start, order, request);
-      if (plan.deal.share) span_scan(plan.deal, geo.Hkv, geo.G, order, item_start, first, request);
+      if (plan.deal.share)
+        fits = span_scan(plan.deal, geo.Hkv, geo.G, order, item_start, first, request);
       if (lane == 0) {
         bar.deal = plan.deal;
         bar.workers = plan.workers;
+        bar.fits = fits && plan.workers >= 0;
+        if (!bar.fits && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
         const int worker = static_cast<int>(blockIdx.x), units = item_start[geo.batch];
         int u = worker, end = units;
         if (plan.deal.share) span_share(plan.deal, worker, units, u, end);
@@ -1159,14 +1164,14 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     span_write_plan(geo.span, deal, bar.workers, geo.Hkv, geo.G, item_start, order, request, me,
                     all);
     if (geo.span.shared)
-      span_priors(geo.span, deal, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
+      span_priors(geo.span, deal, bar.fits, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
       span_zeros(geo.Hq, D, request, out, me, all);
   }
   if (kOwn && static_cast<int>(blockIdx.x) >= bar.workers) {
     if constexpr (kOwn > 0) {
       using S = dec::SharedShape<D, kOwn>;
-      const int first = bar.workers, group = S::group();
+      const int first = max(bar.workers, 0), group = S::group();
       dec::decode_cta<S, D, kOwn, false, true>(
           smem_q + group * kOwnBytes,
           dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,

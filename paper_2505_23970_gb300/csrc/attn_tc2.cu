@@ -134,6 +134,7 @@ struct Bars2 {
   int item_msg[2][kMessage];  // a claimed item, decoded (item_message; it < 0: end)
   SpanDeal deal;              // kSpan: how the work is dealt out
   int workers;                // kSpan: workers that have a share
+  bool fits;                  // kSpan: the units fit their numbers
   int next_unit;              // kSpan, shares: after the first piece
   unsigned long long own_keys;  // kOwn: their sum
   uint32_t tmem_base;
@@ -1143,16 +1144,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (kSpan) {
       if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
-      if (!kOwn) span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      bool fits = true;
+      if (!kOwn) fits = span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
                     kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 2,
                     item_start, order, request);
       at.deal = plan.deal;
-      if (at.deal.share) span_scan(at.deal, geo.Hkv, geo.G, order, item_start, first, request);
+      if (at.deal.share)
+        fits = span_scan(at.deal, geo.Hkv, geo.G, order, item_start, first, request);
       if (lane == 0) {
         bar.deal = plan.deal;
         bar.workers = plan.workers;
+        bar.fits = fits && plan.workers >= 0;
+        if (!bar.fits && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
         // Both CTAs of a pair work out their first piece here: sent by the producer of
         // one, it came 2 us later.
         const int worker = static_cast<int>(blockIdx.x / 2), units = item_start[geo.batch];
@@ -1222,7 +1227,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     span_write_plan(geo.span, at.deal, bar.workers, geo.Hkv, geo.G, item_start, order, request,
                     me, all);
     if (geo.span.shared)
-      span_priors(geo.span, at.deal, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
+      span_priors(geo.span, at.deal, bar.fits, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
       span_zeros(geo.Hq, kD, request, out, me, all);
   }
@@ -1230,7 +1235,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (own_cta) {
     if constexpr (kOwn) {
       using S = dec::SharedShape<kD, 1>;
-      const int first = 2 * bar.workers, group = S::group();
+      const int first = 2 * max(bar.workers, 0), group = S::group();
       dec::decode_cta<S, kD, 1, false, true>(
           smem_q + group * kOwnBytes,
           dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,

@@ -60,7 +60,7 @@ namespace {
 using dec::decode_cta;
 using dec::Shape;
 
-template <int D, int NT, bool kQ8, bool kParts>
+template <int D, int NT, bool kQ8, bool kParts, bool kTwo>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
     decode_mma_kernel(const __nv_bfloat16* q, const int32_t* block_table,
                       const int32_t* seq_lens, __nv_bfloat16* out,
@@ -68,16 +68,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
                       int* merge_counters) {
   extern __shared__ __align__(16) uint8_t smem[];
   dependent_begin();
-  decode_cta<Shape<D, NT>, D, NT, kQ8, kParts>(smem, dec::ByBlock{}, q, block_table, seq_lens, out,
+  decode_cta<Shape<D, NT>, D, NT, kQ8, kParts, kTwo>(smem, dec::ByBlock{}, q, block_table, seq_lens, out,
                                                ws, geo, status, merge_counters);
 }
 
-template <int D, int NT, bool kQ8, bool kParts>
+template <int D, int NT, bool kQ8, bool kParts, bool kTwo>
 gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo, int grid,
                  cudaStream_t stream) {
   using S = Shape<D, NT>;
-  const size_t smem = decode_smem_bytes<S>(a.batch);
-  auto kernel = decode_mma_kernel<D, NT, kQ8, kParts>;
+  const size_t smem = decode_smem_bytes<S>(a.batch, kTwo);
+  auto kernel = decode_mma_kernel<D, NT, kQ8, kParts, kTwo>;
   cudaError_t e = cudaSuccess;
   // a block gets 48 KB without asking, its static words (well below 1 KB) included
   if (smem > 47 * 1024)
@@ -92,15 +92,15 @@ gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo
   return GC_OK;
 }
 
-template <int D, bool kQ8, bool kParts>
+template <int D, bool kQ8, bool kParts = false, bool kTwo = false>
 gc_status launch_heads(const gc_kv_pool* pool, const DecodeArgs& a, DecGeom geo, int max_ranges,
                        cudaStream_t stream) {
   const bool narrow = geo.G <= 8;
   const int ctas = narrow ? Shape<D, 1>::kCtas : Shape<D, 2>::kCtas;
   int grid = min(ctas * pool->num_sms, kMergeCounters);
   if (geo.range_tiles) grid = min(grid, max_ranges);
-  return narrow ? launch<D, 1, kQ8, kParts>(pool, a, geo, grid, stream)
-                : launch<D, 2, kQ8, kParts>(pool, a, geo, grid, stream);
+  return narrow ? launch<D, 1, kQ8, kParts, kTwo>(pool, a, geo, grid, stream)
+                : launch<D, 2, kQ8, kParts, kTwo>(pool, a, geo, grid, stream);
 }
 
 }  // namespace
@@ -119,13 +119,16 @@ gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const D
   const long long ranges =
       split ? static_cast<long long>(a.batch) * cfg.num_kv_heads * split->splits : 0;
   const int max_ranges = static_cast<int>(ranges < kMergeCounters ? ranges : kMergeCounters);
+  const bool two = a.prefix.groups > 0;
   if (cfg.head_dim == 128)
-    return a.own.o ? launch_heads<128, false, true>(pool, a, geo, max_ranges, stream)
-           : q8    ? launch_heads<128, true, false>(pool, a, geo, max_ranges, stream)
-                   : launch_heads<128, false, false>(pool, a, geo, max_ranges, stream);
-  return a.own.o ? launch_heads<64, false, true>(pool, a, geo, max_ranges, stream)
-         : q8    ? launch_heads<64, true, false>(pool, a, geo, max_ranges, stream)
-                 : launch_heads<64, false, false>(pool, a, geo, max_ranges, stream);
+    return two       ? launch_heads<128, false, false, true>(pool, a, geo, max_ranges, stream)
+           : a.own.o ? launch_heads<128, false, true>(pool, a, geo, max_ranges, stream)
+           : q8      ? launch_heads<128, true>(pool, a, geo, max_ranges, stream)
+                     : launch_heads<128, false>(pool, a, geo, max_ranges, stream);
+  return two       ? launch_heads<64, false, false, true>(pool, a, geo, max_ranges, stream)
+         : a.own.o ? launch_heads<64, false, true>(pool, a, geo, max_ranges, stream)
+         : q8      ? launch_heads<64, true>(pool, a, geo, max_ranges, stream)
+                   : launch_heads<64, false>(pool, a, geo, max_ranges, stream);
 }
 
 }  // namespace gc

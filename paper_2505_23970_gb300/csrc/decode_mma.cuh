@@ -22,6 +22,11 @@ struct DecGeom {
   int32_t q8_n_blocks, q8_layer_major;
   uint32_t q8_hdr, q8_chunk;
   DecodeParts own;  // kParts
+  // kTwo: the groups' shared pages (gc_shared_prefix_decode_attn)
+  const int32_t* shared_table;
+  const int32_t* shared_lens;
+  const int32_t* cu_requests;
+  int32_t groups, shared_blocks;
 };
 
 // The geometry of a call; keys are cut into the ranges of `split`, or into shares.
@@ -50,6 +55,11 @@ inline DecGeom decode_geom(const gc_kv_pool* pool, const DecodeArgs& a, const De
   geo.q8_hdr = static_cast<uint32_t>(q8_header_bytes(cfg));
   geo.q8_chunk = static_cast<uint32_t>(q8_chunk_bytes(cfg));
   geo.own = a.own;
+  geo.shared_table = a.prefix.table;
+  geo.shared_lens = a.prefix.lens;
+  geo.cu_requests = a.prefix.cu_requests;
+  geo.groups = a.prefix.groups;
+  geo.shared_blocks = a.prefix.max_blocks;
   geo.range_tiles = split ? split->split_tiles : 0;
   geo.max_splits = split ? split->splits : 1;
   const DecodeUnits units = decode_units(static_cast<int64_t>(a.batch) * cfg.num_kv_heads,
@@ -115,6 +125,13 @@ struct SharedShape {
 // the request (ranges); -1: the whole context.
 struct DecPiece {
   int b, g, k0, k1, part;
+};
+
+// kTwo: the shared keys [0, S) in front of a request's own ones, which are numbered from
+// the next multiple of 16 on (a group lies in one list).
+struct SharedKeys {
+  int S, own0;
+  const int32_t* table;
 };
 
 __device__ __forceinline__ int find_request(const int* start, int batch, int u) {
@@ -396,13 +413,27 @@ struct Where {
   float sk, sv;  // the image page's scales
 };
 
-template <int D, bool kQ8>
+template <int D, bool kQ8, bool kTwo>
 __device__ __forceinline__ Where look_up(const DecGeom& geo, const DecPiece& w, uint32_t key,
                                          const uint8_t* pool_k,
                                          const int32_t* block_table,
-                                         int32_t* status) {
+                                         int32_t* status, const SharedKeys& shared) {
   Where x{0, 0.f, 0.f};
   if (key >= static_cast<uint32_t>(w.k1)) return x;
+  if (kTwo) {
+    const bool own = key >= static_cast<uint32_t>(shared.own0);
+    if (own) key -= static_cast<uint32_t>(shared.own0);
+    const int blk = static_cast<int>(key >> geo.ps_shift);
+    const int page = own ? ld_plain(block_table + static_cast<int64_t>(w.b) * geo.max_blocks + blk)
+                         : ld_plain(shared.table + blk);
+    const int64_t row = static_cast<int64_t>(w.g) * geo.ps + (key & static_cast<uint32_t>(geo.ps - 1));
+    if (page < 0 || page >= geo.num_pages)
+      record_error(status, GC_ERR_OUT_OF_RANGE);
+    else
+      x.k = reinterpret_cast<uint64_t>(
+          pool_k + (static_cast<int64_t>(page) * geo.Hkv * geo.ps + row) * D * 2);
+    return x;
+  }
   const int blk = static_cast<int>(key >> geo.ps_shift);  // < max_blocks: T is at most the table's capacity
   const int64_t e = static_cast<int64_t>(w.b) * geo.max_blocks + blk;
   const int64_t row = static_cast<int64_t>(w.g) * geo.ps + (key & static_cast<uint32_t>(geo.ps - 1));
@@ -509,7 +540,9 @@ struct ByNumber {
 };
 
 // One of them; the caller has waited for the kernel before.
-template <typename S, int D, int NT, bool kQ8, bool kParts, typename Who>
+// kTwo: a request has a group's shared keys in front of its own, and may have none at all
+// (then its row is 0).
+template <typename S, int D, int NT, bool kQ8, bool kParts, bool kTwo = false, typename Who>
 __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
                                            const __nv_bfloat16* q, const int32_t* block_table,
                                            const int32_t* seq_lens, __nv_bfloat16* out, float* ws,
@@ -533,7 +566,29 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
   {
     const int cap = geo.max_blocks << geo.ps_shift;
     int most = 0, n = 0;
-    for (int b = S::tid(); b < geo.batch; b += S::kThreads) {
+    if constexpr (kTwo) {
+      int* context = start + geo.batch + 1;  // [batch] keys, -1: skipped; then the groups
+      for (int b = S::tid(); b < geo.batch; b += S::kThreads) {
+        int lo = 0, hi = geo.groups;  // the last group whose first request is <= b
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (ld_plain(geo.cu_requests + mid) <= b) lo = mid; else hi = mid;
+        }
+        const int first = ld_plain(geo.cu_requests + lo), last = ld_plain(geo.cu_requests + lo + 1);
+        const int shared = ld_plain(geo.shared_lens + lo);
+        const int own = seq_lens ? ld_plain(seq_lens + b) : 0;
+        const bool bad = first < 0 || first > b || last <= b || last > geo.batch || shared < 0 ||
+                         shared > (geo.shared_blocks << geo.ps_shift) || own < 0 || own > cap;
+        if (bad && who.cta() == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
+        const int T = bad ? -1 : ((shared + kGroup - 1) & -kGroup) + own;
+        context[b] = T;
+        context[geo.batch + b] = lo;
+        start[b] = bad ? 0 : max(T, 1);
+        most = max(most, T);
+        n += !bad;
+      }
+    }
+    for (int b = S::tid(); !kTwo && b < geo.batch; b += S::kThreads) {
       const int T = ld_plain(seq_lens + b);
       if (T < 1 || T > cap) {
         if (who.cta() == 0 && !(kParts && T == 0)) record_error(status, GC_ERR_OUT_OF_RANGE);
@@ -607,7 +662,15 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
   for (int u = u0; u < end;) {
     DecPiece w;
     w.b = find_request(start, geo.batch, u);
-    const int T = ld_plain(seq_lens + w.b);
+    const int* context = start + geo.batch + 1;
+    const int T = kTwo ? context[w.b] : ld_plain(seq_lens + w.b);
+    SharedKeys shared{0, 0, nullptr};
+    if constexpr (kTwo) {
+      const int group = context[geo.batch + w.b];
+      shared.S = ld_plain(geo.shared_lens + group);
+      shared.own0 = (shared.S + kGroup - 1) & -kGroup;
+      shared.table = geo.shared_table + static_cast<int64_t>(group) * geo.shared_blocks;
+    }
     const int local = u - start[w.b];
     const int nu = (start[w.b + 1] - start[w.b]) / geo.Hkv;  // units (ranges) of the pair
     if (by_warp) {
@@ -636,13 +699,13 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
     auto key_of = [&](int i) {
       return static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first + i * every) * kGroup;
     };
-    Where cur = look_up<D, kQ8>(geo, w, key_of(lane), pool_k, block_table, status);
+    Where cur = look_up<D, kQ8, kTwo>(geo, w, key_of(lane), pool_k, block_table, status, shared);
     acc.reset();
     const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq + w.g * geo.G;
     acc.load_q(q + head0 * D, geo.G);
     Where nxt{0, 0.f, 0.f};
     if (key_of(32) < k1)
-      nxt = look_up<D, kQ8>(geo, w, key_of(32 + lane), pool_k, block_table, status);
+      nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(32 + lane), pool_k, block_table, status, shared);
 
     struct Cursor {
       const uint8_t* k;  // the group's K rows, null: no data
@@ -671,11 +734,13 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
       vf.load(c.k + v_after);
     }
     for (int i = 0; key_of(i) < k1; ++i) {
-      const int n = static_cast<int>(k1 - key_of(i));  // keys of the group (16 or more: all)
+      int n = static_cast<int>(k1 - key_of(i));  // keys of the group (16 or more: all)
+      if (kTwo && key_of(i) < static_cast<uint32_t>(shared.own0))
+        n = min(n, shared.S - static_cast<int>(key_of(i)));
       if (i > 0 && (i & 31) == 0) {
         cur = nxt;
         if (key_of(i + 32) < k1)
-          nxt = look_up<D, kQ8>(geo, w, key_of(i + 32 + lane), pool_k, block_table, status);
+          nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(i + 32 + lane), pool_k, block_table, status, shared);
       }
       Cursor cn{nullptr, false, 0.f, 0.f};
       if (key_of(i + 1) < k1) cn = locate(i + 1);
@@ -749,7 +814,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
             if (lane < 4) geo.own.ml[head0 + h] = make_float2(acc.m[t][x], acc.l[t][x]);
             continue;
           }
-          const float inv = 1.f / acc.l[t][x];
+          const float inv = kTwo && acc.l[t][x] == 0.f ? 0.f : 1.f / acc.l[t][x];
           uint4* dst = reinterpret_cast<uint4*>(out + (head0 + h) * D + (lane >> 2) * (D / 8));
 #pragma unroll
           for (int v = 0; v < D / 64; ++v) {
@@ -819,7 +884,8 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
         }
       }
       if (w.part < 0) {
-        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) = pack_bf16x2(o.x / L, o.y / L);
+        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) =
+            kTwo && L == 0.f ? 0u : pack_bf16x2(o.x / L, o.y / L);
       } else {
         *reinterpret_cast<float2*>(ws + (part0 + h * part_step) * D + d) = o;
         if (d == 0) part_ml[part0 + h * part_step] = make_float2(M, L);
@@ -854,8 +920,8 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
 }  // namespace
 
 template <typename S>
-size_t decode_smem_bytes(int batch) {
-  return S::kRedFloats * sizeof(float) + S::kWarps * S::kHeads * sizeof(float2) +
+size_t decode_smem_bytes(int batch, bool two = false) {
+  return (two ? 2 * static_cast<size_t>(batch) * sizeof(int) : 0) + S::kRedFloats * sizeof(float) + S::kWarps * S::kHeads * sizeof(float2) +
          (static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 

@@ -268,6 +268,13 @@ struct DecodeParts {
   float* o;
   float2* ml;
 };
+// Shared pages in front of the requests' own ones (groups 0: none).
+struct DecodePrefix {
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu_requests;
+  int32_t groups, max_blocks;
+};
 struct DecodeArgs {
   const void* q;
   void* out;
@@ -279,6 +286,7 @@ struct DecodeArgs {
   size_t workspace_bytes;
   const char* who = "gc_paged_decode_attn";  // for messages
   DecodeParts own = {nullptr, nullptr};      // given: the results go there instead of to out
+  DecodePrefix prefix = {nullptr, nullptr, nullptr, 0, 0};
 };
 struct DecodeSplit {
   int32_t splits, split_tiles;  // key ranges per request (at most), their 128-key tiles

@@ -142,8 +142,8 @@ __device__ __forceinline__ int span_place(const int* start, int batch, int u) {
   return lo;
 }
 
-// How a call is dealt out, and the workers that take part, worked out by one warp; every
-// CTA comes to the same answer.  start: each place's first item.
+// How a call is dealt out, and the workers that take part (-1: the units are too many),
+// worked out by one warp; every CTA comes to the same answer.  start: each place's first item.
 // own_keys >= 0: the other workers decode so many own keys, 128 of them and a kv head
 // taking an SM own_weight / 16 of a unit (then shares always).
 constexpr int kSpanStart = 5;  // units in the time that a span CTA takes beyond an own one's
@@ -183,6 +183,7 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
   const bool apart = tiles > 1 && per_tile > kSpanInL2;
   int team = apart && 4 * tiles <= sp.workers && 8 * per_tile * tiles <= 9 * units ? tiles : 1;
   if (own_keys >= 0) {
+    if (units >= (1ll << 30)) return {{kSpanMinShare, 1}, -1};  // (see span_scan)
     // The number w of teams for which both sides take as long,
     //     u / w + kSpanStart = o / (W - w),
     // with u units, W teams in all and o the own keys' time if they had one team:
@@ -230,15 +231,15 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
 }
 
 // Thread's own keys of the requests behind shared prefixes, a request's fixed cost counted
-// as kSpanOwnKeys; and their sum over the CTA (sum: cleared before).  The cost, and the
-// weight of a key, are from two calls of 64/8 and 32/8 heads of 128 on known numbers of
-// SMs: 64 requests of 1119 keys and 128 of 255.
+// as up to kSpanOwnKeys (short ones are done several at a time); and their sum over the CTA
+// (sum: cleared before).  The cost, and the weight of a key, are from two calls of 64/8 and
+// 32/8 heads of 128 on known numbers of SMs: 64 requests of 1119 keys and 128 of 255.
 constexpr int kSpanOwnKeys = 768;
 __device__ __forceinline__ unsigned long long span_own_keys(const OwnDecode& own, int threads) {
   unsigned long long keys = 0;
   for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
     const int T = ld_plain(own.lens + b);
-    if (T > 0) keys += T + static_cast<unsigned>(kSpanOwnKeys);
+    if (T > 0) keys += T + min(kSpanOwnKeys, 2 * min(T, kSpanOwnKeys) + 128);
   }
   return keys;
 }
@@ -316,34 +317,41 @@ __device__ __forceinline__ SpanPiece span_piece(int u, SpanDeal deal, int worker
   }
 }
 
-// Exclusive scan, by one warp, of the places' items (share 0) or a team's units into start, and
-// each request's into first_of where it is given.
-__device__ inline void span_scan(SpanDeal deal, int Hkv, int G, const int16_t* order, int* start,
+// Exclusive scan, by one warp, of the places' items (share 0) or a team's units into start,
+// and each request's into first_of where it is given.  False, and nothing to do, if there
+// are too many for 32-bit ints: the host has checked that for requests that divide the
+// rows, so some have rows in common.
+__device__ inline bool span_scan(SpanDeal deal, int Hkv, int G, const int16_t* order, int* start,
                                  int* first_of, const SpanRequests& request) {
   const int lane = threadIdx.x & 31, batch = request.batch;
-  int running = 0;
+  long long running = 0;
   for (int p0 = 0; p0 < batch; p0 += 32) {
     const int p = p0 + lane;
     const int b = p < batch && batch <= kSpanRequests ? order[p] : p;
-    int cnt = 0;
+    long long cnt = 0;
     if (p < batch) {
       const SpanRequest r = request(b);
       const int steps = r.n > 0 ? span_steps(r.T) : 0;
       if (steps > 0)
-        cnt = Hkv * (deal.team > 1 ? 1 : span_tiles(r.n, G)) * (deal.share ? steps + kSpanLead : 1);
+        cnt = static_cast<long long>(Hkv) * (deal.team > 1 ? 1 : span_tiles(r.n, G)) *
+              (deal.share ? steps + kSpanLead : 1);
     }
-    int incl = cnt;
+    long long incl = cnt;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += y;
     }
-    if (p < batch) start[p] = running + incl - cnt;
-    if (p < batch && first_of) first_of[b] = running + incl - cnt;
+    if (p < batch) start[p] = static_cast<int>(running + incl - cnt);
+    if (p < batch && first_of) first_of[b] = static_cast<int>(running + incl - cnt);
     running += __shfl_sync(0xffffffffu, incl, 31);
   }
-  if (lane == 0) start[batch] = running;
+  const bool fits = running < INT32_MAX - 4096;  // (workers look one past it)
+  if (!fits)
+    for (int p = lane; p < batch; p += 32) start[p] = 0;
+  if (lane == 0) start[batch] = fits ? static_cast<int>(running) : 0;
   __syncwarp();
+  return fits;
 }
 
 // Pieces of the item whose first unit is u0: of shares c0 to c1, the first in slot
@@ -394,7 +402,8 @@ __device__ inline void span_write_plan(const SpanGeom& sp, SpanDeal deal, int wo
 
 // Thread `me` of `all`: the requests' rows of the groups' items.  first_of: each
 // group's first unit or item.
-__device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, int G, const int* first_of,
+__device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, bool fits, int G,
+                                   const int* first_of,
                                    const SpanRequests& request, int64_t me, int64_t all) {
   for (int64_t b = me; b < request.total_new; b += all) {
     int lo = 0, hi = request.batch;  // the last group whose first request is <= b
@@ -404,7 +413,7 @@ __device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, int G, con
     }
     const SpanRequest r = request(lo);
     SpanPrior p{0, 0, -1, 0};
-    if (!r.bad && b >= r.cu && b < r.cu + r.n) {
+    if (fits && !r.bad && b >= r.cu && b < r.cu + r.n) {
       const int row = (static_cast<int>(b) - r.cu) * G, per = span_steps(r.T) + kSpanLead;
       p.steps = span_steps(r.T);
       p.unit = first_of[lo] + (deal.team > 1 ? 0 : row / kSpanRows * per);

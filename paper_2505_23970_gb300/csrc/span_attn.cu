@@ -159,17 +159,55 @@ gc_status check_space(const char* who, size_t need, const void* workspace, size_
 
 }  // namespace
 
+// Small calls are decoded row by row, the shared keys (or states) in front of the row's own
+// ones: the keys are then read once for every row, mostly from the L2, but in one launch
+// of the decode kernel, without a join and without the start of the tensor-core kernels.
+// By the room in the block tables, as the lengths are on the device: rows x `keys` x kv
+// heads.  Measured at lengths that fill it, row by row | tiles (us, heads of 128 then 64):
+//   shared: 4 requests behind 256 tokens, 1 kv head, 7.0 | 13.7, 7.3 | 11.6; 16 behind
+//   1000, 8 kv heads, 16.1 | 17.2, 13.2 | 16.7; 32 behind 2000, 4 kv heads, 17.7 | 17.2,
+//   15.1 | 16.2; 128 behind 1000, 8 kv heads, 53 | 47, 38 | 33;
+//   cross: 16 tokens over 1000 states each, 1 kv head, 9.2 | 18.3, 8.2 | 20.6; 12 over
+//   1000, 8 kv heads, 13.1 | 18.1, 11.3 | 20.2; 320 over 300, 2 kv heads, 38.6 | 15.3,
+//   22.3 | 18.6.  With two steps of keys nothing is cut and tiles take 9 us: 64 over 256,
+//   1 kv head, 9.2 | 8.7, 8.1 | 9.2; 2 kv heads, 16.0 | 8.9, 10.1 | 9.2.
+static bool row_by_row(const gc_kv_pool* pool, int64_t rows, int64_t keys, bool shared) {
+  const bool wide = pool->cfg.head_dim == 128;
+  const int64_t most = shared ? (wide ? 262144 : 458752)
+                       : keys > 256 ? (wide ? 131072 : 163840) : (wide ? 8192 : 16384);
+  return rows <= 8192 && rows * keys * pool->cfg.num_kv_heads <= most;
+}
+
 size_t cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
                              int32_t num_q_heads, int32_t total_new_tokens) {
+  if (row_by_row(pool, total_new_tokens, static_cast<int64_t>(max_blocks) * pool->cfg.page_size,
+                 false))
+    return decode_share_workspace_bytes(pool);
   return span_space(pool, total_new_tokens, batch, max_blocks, num_q_heads, false).end;
+}
+
+// The rows of a call one by one; own_lens: nullptr if they have no keys of their own.
+static gc_status launch_rows(const gc_kv_pool* pool, const SpanArgs& a, const char* who,
+                             const int32_t* own_table, const int32_t* own_lens, int32_t own_blocks,
+                             const DecodePrefix& prefix, cudaStream_t stream) {
+  DecodeArgs all{a.q, a.out, own_table, own_lens, a.rows, own_blocks, a.layer, a.num_q_heads,
+                 a.softmax_scale, a.workspace, a.workspace_bytes, who};
+  all.prefix = prefix;
+  const gc_status st = check_decode(pool, all);
+  return st == GC_OK ? launch_decode_mma(pool, all, nullptr, stream, nullptr) : st;
 }
 
 gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t stream) {
   const char* who = "gc_paged_cross_attn";
   const auto& cfg = pool->cfg;
-  const SpanSpace space = span_space(pool, a.rows, a.batch, a.max_blocks, a.num_q_heads, false);
-  gc_status st = check_space(who, space.end, a.workspace, a.workspace_bytes);
+  gc_status st = check_space(
+      who, cross_workspace_bytes(pool, a.batch, a.max_blocks, a.num_q_heads, a.rows), a.workspace,
+      a.workspace_bytes);
   if (st != GC_OK) return st;
+  if (row_by_row(pool, a.rows, static_cast<int64_t>(a.max_blocks) * cfg.page_size, false))
+    return launch_rows(pool, a, who, nullptr, nullptr, 1,
+                       DecodePrefix{a.block_table, a.lens, a.start, a.batch, a.max_blocks}, stream);
+  const SpanSpace space = span_space(pool, a.rows, a.batch, a.max_blocks, a.num_q_heads, false);
   const SpanGeom span = span_geom(space, static_cast<int64_t>(a.max_blocks) * cfg.page_size, false,
                                   a.workspace);
   const AttnArgs args{a.q, a.out, a.block_table, a.lens, a.new_lens, a.start, a.batch,
@@ -201,6 +239,12 @@ static bool decodes_in_kernel(const gc_kv_pool* pool, const SpanArgs& a) {
          items * (steps + kSpanLead) < (1ll << 30) - pool->num_sms;
 }
 
+static bool shared_rows(const gc_kv_pool* pool, int32_t batch, int32_t max_shared_blocks,
+                        int32_t max_blocks) {
+  const int64_t blocks = static_cast<int64_t>(max_shared_blocks) + max_blocks;
+  return row_by_row(pool, batch, blocks * pool->cfg.page_size, true);
+}
+
 // A shared call's workspace: the prefixes' pieces, the own parts, then the decode
 // kernel's.
 struct SharedSpace {
@@ -210,7 +254,11 @@ struct SharedSpace {
 static SharedSpace shared_space(const gc_kv_pool* pool, int32_t batch, int32_t groups,
                                 int32_t max_shared_blocks, int32_t max_blocks,
                                 int32_t num_q_heads) {
-  SharedSpace s;
+  SharedSpace s{};
+  if (shared_rows(pool, batch, max_shared_blocks, max_blocks)) {
+    s.end = decode_share_workspace_bytes(pool);
+    return s;
+  }
   s.span = span_space(pool, batch, groups, max_shared_blocks, num_q_heads, true);
   const size_t rows = static_cast<size_t>(batch) * num_q_heads;
   s.ml = s.span.end;
@@ -236,6 +284,10 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
   gc_status st = check_space(who, space.end, a.workspace, a.workspace_bytes);
   if (st != GC_OK) return st;
   uint8_t* w = static_cast<uint8_t*>(a.workspace);
+  if (shared_rows(pool, a.batch, a.max_shared_blocks, a.max_blocks))
+    return launch_rows(pool, a, who, a.block_table, a.lens, a.max_blocks,
+                       DecodePrefix{a.shared_table, a.shared_lens, a.start, a.groups,
+                                    a.max_shared_blocks}, stream);
   const SpanGeom span = span_geom(
       space.span, static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size, true, w);
   DecodeArgs own{a.q, a.out, a.block_table, a.lens, a.batch, a.max_blocks, a.layer, a.num_q_heads,
