@@ -1101,7 +1101,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
       bool fits = true;
-      if (!kOwn) fits = span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
                     kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 1,
@@ -1156,7 +1156,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   tc_fence_after();
   const uint32_t tmem = bar.tmem_base;
   const int total_items = item_start[geo.batch];  // (shares: units)
-  const SpanDeal deal = kSpan ? bar.deal : SpanDeal{0, 1};
+  const SpanDeal deal = kSpan ? bar.deal : SpanDeal{0, 0};
 
   if (kSpan && warp >= 4) {
     const int64_t me = static_cast<int64_t>(blockIdx.x) * (kThreads - 128) + threadIdx.x - 128;
@@ -1164,7 +1164,8 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     span_write_plan(geo.span, deal, bar.workers, geo.Hkv, geo.G, item_start, order, request, me,
                     all);
     if (geo.span.shared)
-      span_priors(geo.span, deal, bar.fits, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
+      span_priors(geo.span, deal, bar.fits, geo.Hkv, geo.G,
+                  geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
       span_zeros(geo.Hq, D, request, out, me, all);
   }

@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   Place at{rank & 1u, rank & ~1u, kSplit ? rank >> 1 : 0u,
-           kSplit ? cluster_nctarank() >> 1 : 1u, {0, 1}};
+           kSplit ? cluster_nctarank() >> 1 : 1u, {0, 0}};
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -1145,7 +1145,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (rank_in_warp) span_rank32(request, order);
       int* first = geo.span.shared && geo.batch <= kSortMax ? first_of : nullptr;
       bool fits = true;
-      if (!kOwn) fits = span_scan({0, 1}, geo.Hkv, geo.G, order, item_start, first, request);
+      if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
                     kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 2,
@@ -1227,7 +1227,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     span_write_plan(geo.span, at.deal, bar.workers, geo.Hkv, geo.G, item_start, order, request,
                     me, all);
     if (geo.span.shared)
-      span_priors(geo.span, at.deal, bar.fits, geo.G, geo.batch <= kSortMax ? first_of : item_start, request, me, all);
+      span_priors(geo.span, at.deal, bar.fits, geo.Hkv, geo.G,
+                  geo.batch <= kSortMax ? first_of : item_start, request, me, all);
     else
       span_zeros(geo.Hq, kD, request, out, me, all);
   }

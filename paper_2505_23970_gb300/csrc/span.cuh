@@ -13,9 +13,11 @@
 //    binary32) are joined afterwards:
 //        out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  M = max_s m_s.
 //    A share has at most two such pieces: its first (slot 0), and its last (slot 1).
-//    Where requests have several row tiles (as many nearly all of them), a share belongs
-//    to a team of as many workers, each of which takes one tile of every item in it: the
-//    tiles then read the same keys at the same time, from memory once.
+//    Where requests have several row tiles over more keys than the L2 holds, the units go
+//    tile by tile, all heads of a tile and then the next tile, and each such run begins
+//    with a share (aligned): the workers of a request's tiles then read the same keys at
+//    the same time, from memory once (questions of 43 tokens, 64/8 heads, on 131072 states:
+//    440 us where the tiles of a head follow each other, 385 so).
 #pragma once
 
 #include "decode_mma.cuh"
@@ -53,7 +55,7 @@ struct SpanGeom {
   int32_t cuts;     // items may be cut
   int32_t shared;   // requests are groups (new_lens is not given); whole items' results
                     // go to `whole`, not to the output
-  int32_t* plan;    // SpanDeal, workers that have a share
+  int32_t* plan;    // [0] units of a share, 0: whole items, [1] workers that have one
   int4* cuts_at;    // cross attention: per share, see SpanCutItem
   int4* prior;      // shared: per request, see SpanPrior
   DecodeParts whole;  // shared: [request][q head]
@@ -68,17 +70,28 @@ struct SpanCutItem {
   int32_t c1, first, g, tile, cu, n, unused[2];
 };
 
-// How the work is dealt out: units of a share (0: whole items) and workers that have the
-// same share, a row tile each (1: the tiles of an item are items of their own).
+__device__ __forceinline__ int span_steps(int T) { return T > 0 ? ((T - 1) >> 7) + 1 : 0; }
+__device__ __forceinline__ int span_tiles(int n, int G) {
+  return (n * G + kSpanRows - 1) / kSpanRows;
+}
+
+// How the work is dealt out: units of a share (0: whole items), and whether the runs of a
+// request's tiles begin with shares.
 struct SpanDeal {
-  int share, team;
+  int share, aligned;
 };
+// Units of an item, and of one tile's items of a request.
+__device__ __forceinline__ int span_per(int steps) { return steps + kSpanLead; }
+__device__ __forceinline__ int span_run(SpanDeal deal, int Hkv, int steps) {
+  const int run = Hkv * span_per(steps);
+  return deal.aligned ? (run + deal.share - 1) / deal.share * deal.share : run;
+}
 
 // A request of a shared prefix, as an int4: its G rows of kv head g are rows
-// [row, row + G) of the group's, in the item whose first unit is unit + g * head_units.
+// [row, row + G) of the group's, in the item whose first unit is unit + g * span_per(steps).
 // steps: of the item; 0: no shared keys, -1: the request is skipped.
 struct SpanPrior {
-  int32_t unit, head_units, steps, row;
+  int32_t unit, unused, steps, row;  // (16 bytes: one load)
 };
 
 // One request's rows, keys and first token; rows 0 if there is nothing to do.
@@ -98,11 +111,6 @@ __device__ __forceinline__ SpanRequest span_request(const SpanGeom& sp, int b, i
   r.n = r.bad ? 0 : static_cast<int>(n);
   return r;
 }
-__device__ __forceinline__ int span_steps(int T) { return T > 0 ? ((T - 1) >> 7) + 1 : 0; }
-__device__ __forceinline__ int span_tiles(int n, int G) {
-  return (n * G + kSpanRows - 1) / kSpanRows;
-}
-
 // All requests of a call, held in shared memory (three words each) where there are at
 // most kSpanRequests: every role looks them up, and each look-up in global memory was a
 // latency in front of the first product (prologue 3.7 us, with them held 2).
@@ -142,6 +150,28 @@ __device__ __forceinline__ int span_place(const int* start, int batch, int u) {
   return lo;
 }
 
+// The least share, from `share` on, with which aligned runs need at most `workers` of them;
+// 0 if it is not found soon.  By one warp.
+__device__ inline int span_aligned_share(int share, int workers, int batch, int Hkv, int G,
+                                         const SpanRequests& request) {
+  for (int tries = 0; tries < 8; ++tries) {
+    long long need = 0;
+    for (int b = threadIdx.x & 31; b < batch; b += 32) {
+      const SpanRequest r = request(b);
+      const int st = r.n > 0 ? span_steps(r.T) : 0;
+      if (st > 0)
+        need += static_cast<long long>(span_tiles(r.n, G)) *
+                ((Hkv * span_per(st) + share - 1) / share);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) need += __shfl_xor_sync(0xffffffffu, need, o);
+    if (need <= workers) return share;
+    if (need >= 2ll * workers) return 0;
+    share += static_cast<int>(share * (need - workers) / (2 * workers)) + 1;
+  }
+  return 0;
+}
+
 // How a call is dealt out, and the workers that take part (-1: the units are too many),
 // worked out by one warp; every CTA comes to the same answer.  start: each place's first item.
 // own_keys >= 0: the other workers decode so many own keys, 128 of them and a kv head
@@ -155,7 +185,7 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
                                      long long own_keys, int own_weight, int sms_per_worker,
                                      const int* start, const int16_t* order,
                                      const SpanRequests& request) {
-  if (!sp.cuts || batch > kSpanRequests) return {{0, 1}, sp.workers};
+  if (!sp.cuts || batch > kSpanRequests) return {{0, 0}, sp.workers};
   const int lane = threadIdx.x & 31;
   long long units = 0, per_tile = 0;
   int least = INT32_MAX, most = 0, tiles = 0;
@@ -164,10 +194,10 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
     const int st = r.n > 0 ? span_steps(r.T) : 0;
     if (st == 0) continue;
     const int t = span_tiles(r.n, G);
-    per_tile += static_cast<long long>(Hkv) * (st + kSpanLead);
-    units += static_cast<long long>(Hkv) * t * (st + kSpanLead);
-    least = min(least, st + kSpanLead);
-    most = max(most, st + kSpanLead);
+    per_tile += static_cast<long long>(Hkv) * span_per(st);
+    units += static_cast<long long>(Hkv) * t * span_per(st);
+    least = min(least, span_per(st));
+    most = max(most, span_per(st));
     tiles = max(tiles, t);
   }
 #pragma unroll
@@ -176,64 +206,63 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
     per_tile += __shfl_xor_sync(0xffffffffu, per_tile, o);
   }
   tiles = __reduce_max_sync(0xffffffffu, tiles);
-  if (units == 0) return {{own_keys >= 0 ? kSpanMinShare : 0, 1}, own_keys >= 0 ? 0 : sp.workers};
-  // Where K and V are more than half of the L2, several tiles read them together (two
-  // questions of 43 tokens, 64/8 heads, on 131072 states each: 440 us without teams, 394);
-  // at most an eighth of a team's work may be tiles that a request does not have.
+  // K and V more than half of the L2, and several tiles to read them
   const bool apart = tiles > 1 && per_tile > kSpanInL2;
-  int team = apart && 4 * tiles <= sp.workers && 8 * per_tile * tiles <= 9 * units ? tiles : 1;
   if (own_keys >= 0) {
-    if (units >= (1ll << 30)) return {{kSpanMinShare, 1}, -1};  // (see span_scan)
-    // The number w of teams for which both sides take as long,
+    if (units == 0) return {{kSpanMinShare, 0}, 0};
+    if (units >= (1ll << 30)) return {{kSpanMinShare, 0}, -1};  // (see span_scan)
+    // The number w of workers for which both sides take as long,
     //     u / w + kSpanStart = o / (W - w),
-    // with u units, W teams in all and o the own keys' time if they had one team:
+    // with u units, W workers in all and o the own keys' time if they had one worker's SMs:
     //     s w^2 - (s W - u - o) w - u W = 0.
-    const int all = static_cast<int>(team > 1 ? per_tile : units), most_teams = sp.workers / team;
-    const float W = static_cast<float>(most_teams), u = static_cast<float>(all);
+    const int all = static_cast<int>(units);
+    const float W = static_cast<float>(sp.workers), u = static_cast<float>(all);
     const float o = static_cast<float>(own_keys) * Hkv * own_weight /
-                    (128.f * 16.f * sms_per_worker * team);
+                    (128.f * 16.f * sms_per_worker);
     const float h = 0.5f * (kSpanStart * W - u - o);
     const float root = sqrtf(h * h + kSpanStart * u * W);
     const float w = h > 0.f ? (h + root) / kSpanStart : u * W / (root - h);
     // (one at least for own keys, and no share below the least)
     int n = min(static_cast<int>(w + 0.5f), all / kSpanMinShare);
-    n = max(1, min(n, most_teams - 1));
-    return {{max((all + n - 1) / n, kSpanMinShare), team}, n * team};
+    n = max(1, min(n, sp.workers - 1));
+    const int share = max((all + n - 1) / n, kSpanMinShare);
+    const int aligned = apart ? span_aligned_share(share, n, batch, Hkv, G, request) : 0;
+    if (aligned > 0 && aligned <= share + share / 8) return {{aligned, 1}, n};
+    return {{share, 0}, n};
   }
-  if (units + sp.workers >= (1ll << 30)) return {{0, 1}, sp.workers};  // units are 32-bit ints
+  if (units == 0 || units + sp.workers >= (1ll << 30)) return {{0, 0}, sp.workers};  // (32-bit units)
   // Time in steps: of whole items, longest first, against equal shares and their join.  Of
   // whole items at least r + 1 times the length of item r * workers, for every r; lane r.
-  // Shares without teams must gain an eighth besides where the tiles read K and V apart
-  // (8 x 1024 tokens of 64/8 heads over 8192 states: whole items 1440 us, shares 1640).
+  // Shares whose tiles read K and V apart must gain an eighth besides (8 x 1024 tokens of
+  // 64/8 heads over 8192 states: whole items 1440 us, shares 1640).
   const int even = (static_cast<int>(units) + sp.workers - 1) / sp.workers;
   const long long nth = static_cast<long long>(lane) * sp.workers;
   int whole = 0;
   if (nth < start[batch]) {
     const int p = span_place(start, batch, static_cast<int>(nth));
-    whole = (lane + 1) * (span_steps(request(order[p]).T) + kSpanLead);
+    whole = (lane + 1) * span_per(span_steps(request(order[p]).T));
   }
   const long long rounds = (start[batch] + sp.workers - 1ll) / sp.workers;
   const int end = even + __reduce_min_sync(0xffffffffu, least);  // as the shortest end last
   whole = max(__reduce_max_sync(0xffffffffu, whole),
               static_cast<int>(min(static_cast<long long>(end),
                                    rounds * __reduce_max_sync(0xffffffffu, most))));
-  int share = max(even, kSpanMinShare), cost = share + (apart ? share / 8 : 0);
-  if (team > 1) {
-    const int teams = sp.workers / team;
-    const int s = max((static_cast<int>(per_tile) + teams - 1) / teams, kSpanMinShare);
-    if (s <= cost)
-      share = cost = s;
-    else
-      team = 1;
-  }
-  if (cost + kSpanJoin >= whole) return {{0, 1}, sp.workers};
-  return {{share, team}, sp.workers};
+  const int share = max(even, kSpanMinShare);
+  if (share + kSpanJoin >= whole) return {{0, 0}, sp.workers};
+  int cost = share + (apart ? share / 8 : 0);
+  const int aligned = apart ? span_aligned_share(share, sp.workers, batch, Hkv, G, request) : 0;
+  const bool align = aligned > 0 && aligned < cost;
+  if (align) cost = aligned;
+  if (cost + kSpanJoin >= whole) return {{0, 0}, sp.workers};
+  return {{align ? aligned : share, align ? 1 : 0}, sp.workers};
 }
 
 // Thread's own keys of the requests behind shared prefixes, a request's fixed cost counted
 // as up to kSpanOwnKeys (short ones are done several at a time); and their sum over the CTA
-// (sum: cleared before).  The cost, and the weight of a key, are from two calls of 64/8 and
-// 32/8 heads of 128 on known numbers of SMs: 64 requests of 1119 keys and 128 of 255.
+// (sum: cleared before).  The cost, and the weight of a key (14
+// sixteenths of a unit at d = 128, 5 at 64), are from calls of 8 to 128 requests with 200 to
+// 2048 own keys: at d = 128, with cost 512 they take from 2 % less to 6 % more, with weight
+// 12 up to 13 % more, with 16 from 3 % less to 8 % more.
 constexpr int kSpanOwnKeys = 768;
 __device__ __forceinline__ unsigned long long span_own_keys(const OwnDecode& own, int threads) {
   unsigned long long keys = 0;
@@ -264,7 +293,7 @@ __device__ __forceinline__ void span_rank32(const SpanRequests& request, int16_t
 // Worker's units [first, end) of its share.
 __device__ __forceinline__ void span_share(SpanDeal deal, int worker, int units, int& first,
                                            int& end) {
-  const int64_t u = static_cast<int64_t>(worker / deal.team) * deal.share;
+  const int64_t u = static_cast<int64_t>(worker) * deal.share;
   first = static_cast<int>(min(u, static_cast<int64_t>(units)));
   end = static_cast<int>(min(u + deal.share, static_cast<int64_t>(units)));
 }
@@ -278,46 +307,42 @@ __device__ __forceinline__ SpanPiece span_piece(int u, SpanDeal deal, int worker
                                                 const int* start, const int16_t* order, int Hkv,
                                                 int G, const SpanRequests& request) {
   SpanPiece w;
-  int first = 0, end = 0;
-  if (deal.share) span_share(deal, worker, start[batch], first, end);
-  while (true) {
-    const int p = span_place(start, batch, u);
-    w.b = batch <= kSpanRequests ? order[p] : p;
-    const SpanRequest r = request(w.b);
-    w.n = r.n;
-    w.T = r.T;
-    w.cu = r.cu;
-    const int steps = span_steps(r.T), tiles = span_tiles(r.n, G), local = u - start[p];
-    int item = local;
+  const int p = span_place(start, batch, u);
+  w.b = batch <= kSpanRequests ? order[p] : p;
+  const SpanRequest r = request(w.b);
+  w.n = r.n;
+  w.T = r.T;
+  w.cu = r.cu;
+  const int steps = span_steps(r.T), tiles = span_tiles(r.n, G), local = u - start[p];
+  if (deal.share == 0) {
+    // the tiles that read the same keys one after the other
+    w.g = local / tiles;
+    w.tile = local - w.g * tiles;
     w.j0 = 0;
     w.nt = steps;
     w.slot = -1;
     w.next = u + 1;
-    if (deal.share) {
-      const int per = steps + kSpanLead;
-      item = local / per;
-      const int off = local - item * per, to = min(per, off + (end - u));
-      w.j0 = max(0, off - kSpanLead);
-      w.nt = max(0, to - kSpanLead - w.j0);
-      if (w.nt < steps) w.slot = 2 * worker + (u == first ? 0 : 1);
-      w.next = u + to - off;
-    }
-    if (deal.team > 1) {
-      w.g = item;
-      w.tile = worker % deal.team;
-      if (w.tile >= tiles) w.nt = 0;  // the request has no such tile: the next one
-      if (w.nt > 0 || w.next >= end) return w;
-      u = w.next;
-      continue;
-    }
-    // the tiles that read the same keys one after the other
-    w.g = item / tiles;
-    w.tile = item - w.g * tiles;
     return w;
   }
+  int first, end;
+  span_share(deal, worker, start[batch], first, end);
+  const int per = span_per(steps), run = span_run(deal, Hkv, steps);
+  w.tile = local / run;
+  const int in_run = local - w.tile * run;
+  w.g = in_run / per;
+  const int off = in_run - w.g * per, to = min(per, off + (end - u));
+  w.j0 = max(0, off - kSpanLead);
+  w.nt = max(0, to - kSpanLead - w.j0);
+  w.slot = w.nt < steps ? 2 * worker + (u == first ? 0 : 1) : -1;
+  w.next = u + to - off;
+  if (w.g >= Hkv) {  // what fills a run's last share
+    w.nt = 0;
+    w.next = end;
+  }
+  return w;
 }
 
-// Exclusive scan, by one warp, of the places' items (share 0) or a team's units into start,
+// Exclusive scan, by one warp, of the places' items (share 0) or units into start,
 // and each request's into first_of where it is given.  False, and nothing to do, if there
 // are too many for 32-bit ints: the host has checked that for requests that divide the
 // rows, so some have rows in common.
@@ -333,8 +358,8 @@ __device__ inline bool span_scan(SpanDeal deal, int Hkv, int G, const int16_t* o
       const SpanRequest r = request(b);
       const int steps = r.n > 0 ? span_steps(r.T) : 0;
       if (steps > 0)
-        cnt = static_cast<long long>(Hkv) * (deal.team > 1 ? 1 : span_tiles(r.n, G)) *
-              (deal.share ? steps + kSpanLead : 1);
+        cnt = static_cast<long long>(span_tiles(r.n, G)) *
+              (deal.share ? span_run(deal, Hkv, steps) : Hkv);
     }
     long long incl = cnt;
 #pragma unroll
@@ -355,7 +380,7 @@ __device__ inline bool span_scan(SpanDeal deal, int Hkv, int G, const int16_t* o
 }
 
 // Pieces of the item whose first unit is u0: of shares c0 to c1, the first in slot
-// `first` of c0's, the others in slot 0.  (A worker's slots: 2 worker + 0 and 1.)
+// `first` of c0's, the others in slot 0.
 struct SpanCut {
   int c0, c1, first;
 };
@@ -374,26 +399,23 @@ __device__ inline void span_write_plan(const SpanGeom& sp, SpanDeal deal, int wo
   if (!sp.plan) return;
   if (me == 0) {
     sp.plan[0] = deal.share;
-    sp.plan[1] = deal.team;
-    sp.plan[2] = workers;
+    sp.plan[1] = workers;
   }
   if (deal.share == 0 || sp.shared) return;
   const int batch = request.batch;
   for (int64_t worker = me; worker < workers; worker += all) {
     SpanCutItem x{-1, 0, 0, 0, 0, 0, {0, 0}};
-    const int c0 = static_cast<int>(worker) / deal.team;
-    const int64_t end = (c0 + 1ll) * deal.share;
+    const int64_t end = (worker + 1) * deal.share;
     if (end < start[batch]) {
       // the item that the share's end lies in
       const int p = span_place(start, batch, static_cast<int>(end));
       const SpanRequest r = request(order[p]);
-      const int steps = span_steps(r.T), per = steps + kSpanLead, tiles = span_tiles(r.n, G);
-      const int local = static_cast<int>(end) - start[p], item = local / per;
-      const SpanCut cut = span_cut(static_cast<int>(end) - (local - item * per), steps, deal.share);
-      const int tile = deal.team > 1 ? static_cast<int>(worker) % deal.team : item % tiles;
-      if (cut.c0 == c0 && cut.c1 > c0 && tile < tiles)
-        x = SpanCutItem{cut.c1, cut.first, deal.team > 1 ? item : item / tiles, tile, r.cu, r.n,
-                        {0, 0}};
+      const int steps = span_steps(r.T), per = span_per(steps), run = span_run(deal, Hkv, steps);
+      const int local = static_cast<int>(end) - start[p], tile = local / run;
+      const int in_run = local - tile * run, g = in_run / per;
+      const SpanCut cut = span_cut(static_cast<int>(end) - (in_run - g * per), steps, deal.share);
+      if (g < Hkv && cut.c0 == worker && cut.c1 > cut.c0)
+        x = SpanCutItem{cut.c1, cut.first, g, tile, r.cu, r.n, {0, 0}};
     }
     sp.cuts_at[2 * worker] = make_int4(x.c1, x.first, x.g, x.tile);
     sp.cuts_at[2 * worker + 1] = make_int4(x.cu, x.n, 0, 0);
@@ -402,9 +424,9 @@ __device__ inline void span_write_plan(const SpanGeom& sp, SpanDeal deal, int wo
 
 // Thread `me` of `all`: the requests' rows of the groups' items.  first_of: each
 // group's first unit or item.
-__device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, bool fits, int G,
-                                   const int* first_of,
-                                   const SpanRequests& request, int64_t me, int64_t all) {
+__device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, bool fits, int Hkv, int G,
+                                   const int* first_of, const SpanRequests& request, int64_t me,
+                                   int64_t all) {
   for (int64_t b = me; b < request.total_new; b += all) {
     int lo = 0, hi = request.batch;  // the last group whose first request is <= b
     while (hi - lo > 1) {
@@ -414,13 +436,11 @@ __device__ inline void span_priors(const SpanGeom& sp, SpanDeal deal, bool fits,
     const SpanRequest r = request(lo);
     SpanPrior p{0, 0, -1, 0};
     if (fits && !r.bad && b >= r.cu && b < r.cu + r.n) {
-      const int row = (static_cast<int>(b) - r.cu) * G, per = span_steps(r.T) + kSpanLead;
       p.steps = span_steps(r.T);
-      p.unit = first_of[lo] + (deal.team > 1 ? 0 : row / kSpanRows * per);
-      p.head_units = (deal.team > 1 ? 1 : span_tiles(r.n, G)) * per;
-      p.row = row;
+      p.row = (static_cast<int>(b) - r.cu) * G;
+      if (deal.share) p.unit = first_of[lo] + p.row / kSpanRows * span_run(deal, Hkv, p.steps);
     }
-    sp.prior[b] = make_int4(p.unit, p.head_units, p.steps, p.row);
+    sp.prior[b] = make_int4(p.unit, 0, p.steps, p.row);
   }
 }
 
@@ -463,7 +483,7 @@ inline SpanSpace span_space(const gc_kv_pool* pool, int64_t rows, int64_t batch,
     return x;
   };
   const size_t out_rows = static_cast<size_t>(rows) * num_q_heads, row = c.head_dim * sizeof(float);
-  s.plan = take(shared || s.slots ? 3 * sizeof(int32_t) : 0);
+  s.plan = take(shared || s.slots ? 2 * sizeof(int32_t) : 0);
   s.cuts_at = take(shared ? 0 : s.slots * sizeof(int4));
   s.prior = take(shared ? rows * sizeof(int4) : 0);
   s.whole_ml = take(shared ? out_rows * sizeof(float2) : 0);

@@ -21,11 +21,9 @@ struct Join {
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  // row `row` of a cut item's tile `tile`
+  // row `row` of a cut item
   template <int D>
-  __device__ __forceinline__ void pieces(const SpanGeom& sp, const SpanCut& cut, int team, int tile,
-                                         int row, int c) {
-    const int lane = team > 1 ? tile : 0;  // of the team
+  __device__ __forceinline__ void pieces(const SpanGeom& sp, const SpanCut& cut, int row, int c) {
     constexpr int kBatch = 8;
     for (int s0 = cut.c0; s0 <= cut.c1; s0 += kBatch) {
       float2 ml[kBatch];
@@ -34,8 +32,7 @@ struct Join {
       for (int k = 0; k < kBatch; ++k) {
         const int s = s0 + k;
         const int64_t x =
-            static_cast<int64_t>(2 * (s * team + lane) + (s == cut.c0 ? cut.first : 0)) * sp.stride +
-            row;
+            static_cast<int64_t>(2 * s + (s == cut.c0 ? cut.first : 0)) * sp.stride + row;
         ml[k] = s <= cut.c1 ? ld_plain(sp.ml + x) : make_float2(-INFINITY, 0.f);
         o[k] = s <= cut.c1 ? ld_plain(reinterpret_cast<const float4*>(sp.o + x * D) + c)
                            : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -89,18 +86,18 @@ __global__ void __launch_bounds__(256)
   constexpr int kChunks = kSpanRows / kRowsPerBlock;  // of an item
   const int worker = static_cast<int>(blockIdx.x) / kChunks;
   const int chunk = static_cast<int>(blockIdx.x) % kChunks;
-  const int share = ld_plain(sp.plan), team = ld_plain(sp.plan + 1), workers = ld_plain(sp.plan + 2);
+  const int share = ld_plain(sp.plan), workers = ld_plain(sp.plan + 1);
   // (a SpanCutItem)
   const int4 x = ld_plain(sp.cuts_at + 2 * worker), y = ld_plain(sp.cuts_at + 2 * worker + 1);
   if (blockIdx.x == 0 && threadIdx.x == 0) *work_counter = 0;  // for the next call
   if (share == 0 || worker >= workers || x.x < 0) return;
-  const SpanCut cut{worker / team, x.x, x.y};
+  const SpanCut cut{worker, x.x, x.y};
   const int g = x.z, cu = y.x, row = chunk * kRowsPerBlock + static_cast<int>(threadIdx.x) / kLanes;
   const int at = x.w * kSpanRows + row;  // q row of the request and kv head
   if (at >= y.y * G) return;
   const int c = static_cast<int>(threadIdx.x) % kLanes;
   Join j;
-  j.pieces<D>(sp, cut, team, x.w, row, c);
+  j.pieces<D>(sp, cut, row, c);
   *reinterpret_cast<uint2*>(
       out + (static_cast<int64_t>(cu + at / G) * Hq + g * G + at % G) * D + 4 * c) = j.rounded();
 }
@@ -116,7 +113,7 @@ __global__ void __launch_bounds__(256)
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
   if (row >= rows) return;
   const int b = static_cast<int>(row / Hq), h = static_cast<int>(row - static_cast<int64_t>(b) * Hq);
-  const int T = ld_plain(own_lens + b), share = ld_plain(sp.plan), team = ld_plain(sp.plan + 1);
+  const int T = ld_plain(own_lens + b), share = ld_plain(sp.plan);
   const int4 p = ld_plain(sp.prior + b);  // SpanPrior
   if (p.z < 0) record_error(status, GC_ERR_OUT_OF_RANGE);
   if (T < 0 || T > own_cap || p.z < 0) return;
@@ -131,9 +128,9 @@ __global__ void __launch_bounds__(256)
   Join j;
   SpanCut cut{0, 0, 0};
   const int g = h / G;
-  if (share && p.z > 0) cut = span_cut(p.x + g * p.y, p.z, share);
+  if (share && p.z > 0) cut = span_cut(p.x + g * span_per(p.z), p.z, share);
   if (cut.c1 > cut.c0) {
-    j.pieces<D>(sp, cut, team, p.w / kSpanRows, p.w % kSpanRows + (h - g * G), c);
+    j.pieces<D>(sp, cut, p.w % kSpanRows + (h - g * G), c);
   } else {
     float2 sml;
     float4 so;

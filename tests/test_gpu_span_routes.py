@@ -1,6 +1,6 @@
 """Cross attention and shared-prefix decode on tiles: the same cases as their own tests,
 with block tables wide enough (unused columns) that a call is not small by their room, so
-that the tensor-core kernels, the division of the SMs, shares, teams and joins take them;
+that the tensor-core kernels, the division of the SMs, shares, aligned runs and joins take them;
 and calls that reach each of those."""
 import numpy as np
 import pytest
@@ -54,14 +54,14 @@ def test_shared_on_tiles(name):
 
 @pytest.mark.parametrize("Hq,Hkv,d,ps,kv,n", [
     (8, 1, 128, 16, [150000], [5]),                  # one item over many pairs
-    (16, 2, 128, 64, [70000, 69000], [40, 35]),      # two tiles of long keys: teams
+    (16, 2, 128, 64, [70000, 69000], [40, 35]),      # two tiles of long keys: aligned runs
     (16, 2, 64, 64, [70000, 69000], [40, 35]),
     (64, 8, 128, 16, [18000, 200, 3000], [90, 500, 10]),  # tiles that not all have
     (32, 8, 128, 16, [2000] * 12, [130] * 12),       # whole items, several rounds
     (32, 8, 64, 16, [2000] * 24, [130] * 24),
     (2, 1, 64, 32, [1, 128, 129, 60000], [1, 1, 1, 1]),
 ])
-def test_cross_shares_and_teams(Hq, Hkv, d, ps, kv, n):
+def test_cross_shares_and_runs(Hq, Hkv, d, ps, kv, n):
     c = wide_cross(Hq, Hkv, d, ps, kv, n, seed=Hq + d, reuse=64)
     for _ in range(2):  # the second call finds the counters as the first left them
         c.out.fill_(float("nan"))
@@ -72,9 +72,10 @@ def test_cross_shares_and_teams(Hq, Hkv, d, ps, kv, n):
 
 @pytest.mark.parametrize("Hq,Hkv,d,ps,sizes,S,own", [
     (8, 1, 128, 16, [3], [150000], [300, 1, 0]),
-    (16, 2, 128, 64, [40], [70000], [1 + 3 * i for i in range(40)]),      # two tiles: teams
+    (16, 2, 128, 64, [40], [70000], [1 + 3 * i for i in range(40)]),      # two tiles: aligned runs
     (16, 2, 64, 64, [40], [70000], [1 + 3 * i for i in range(40)]),
-    (16, 2, 128, 64, [40, 3], [70000, 66000], [1 + 3 * i for i in range(43)]),
+    (16, 2, 128, 64, [40, 3], [70000, 66000], [1 + 3 * i for i in range(43)]),  # and one
+    (16, 2, 64, 64, [40, 3], [70000, 66000], [1 + 3 * i for i in range(43)]),
     (4, 1, 128, 16, [2, 1], [0, 0], [9000, 5, 12000]),                    # own keys alone
     (4, 1, 64, 16, [2, 1], [0, 0], [9000, 5, 12000]),
     (4, 1, 128, 16, [2, 1], [30000, 1], [0, 0, 0]),                       # shared alone
