@@ -49,7 +49,7 @@
  *    valid no-ops.
  *  - A pool handle is not thread-safe; distinct pools are independent.
  *    Attention calls on one pool must not run concurrently on the GPU: they
- *    share the work counter in the pool's control block.
+ *    share the counters in the pool's control block.
  *  - bf16 is the only element type.  All tensors are dense and row-major.
  *
  * Layouts (element = bf16 unless stated)
@@ -106,7 +106,7 @@ typedef struct gc_pool_config {
 
 /* Device bytes a pool of this shape needs: the KV planes
  * (L*2*num_pages*Hkv*ps*d*2 bytes, rounded up to 256) plus a 2048-byte
- * control block (device status word, attention work counter, decode merge
+ * control block (device status word, attention work counters, decode merge
  * counters).
  * Returns 0 for an invalid configuration. */
 GC_API size_t gc_kv_pool_bytes(const gc_pool_config* cfg);
@@ -597,7 +597,12 @@ GC_API gc_status gc_paged_decode_attn_q8(const void* q, const gc_kv_pool* pool,
  * A request whose length is outside [0, max_blocks_per_seq*ps], or whose rows
  * would pass T_new, is skipped (its rows are not written); a bad page leaves
  * its request's output unspecified; both are recorded as
- * GC_ERR_OUT_OF_RANGE.
+ * GC_ERR_OUT_OF_RANGE.  Calls on one pool must not overlap on the GPU with
+ * each other or with the other attention calls.  The same call gives the same
+ * bits again; the order of its sums depends on the call's sizes and on what
+ * its tables can hold (few rows over short tables are taken one by one, long
+ * items cut into pieces), so that the last bits of a row may differ between
+ * calls that hold it.
  * Errors: GC_ERR_INVALID_ARG (null, unaligned, workspace too small),
  * GC_ERR_OUT_OF_RANGE (layer), GC_ERR_UNSUPPORTED (head grouping, batch >
  * 8192, sizes past 32-bit numbering), GC_ERR_CUDA. */
@@ -642,7 +647,8 @@ GC_API gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool,
  * table's capacity, is skipped (its rows are not written); a bad page leaves
  * the outputs of those who read it unspecified; both are recorded as
  * GC_ERR_OUT_OF_RANGE.  Calls on one pool must not overlap on the GPU with
- * each other or with the other attention calls.
+ * each other or with the other attention calls; the order of sums is as with
+ * gc_paged_cross_attn.
  * Errors: GC_ERR_INVALID_ARG (null, unaligned, workspace too small),
  * GC_ERR_OUT_OF_RANGE (layer), GC_ERR_UNSUPPORTED (head grouping, batch or
  * num_groups > 8192, sizes past 32-bit numbering), GC_ERR_CUDA. */

@@ -49,6 +49,8 @@
 //    image page's codes (TMA) into the page's rows of the ring slot and whose
 //    fourth warpgroup dequantises them there (see "pages of the 8-bit image"
 //    below).
+//  * Cross attention and shared prefixes at d = 64 (kSpan, kOwn): as in attn_tc2.cu, an
+//    item's two Q tiles on one SM.
 //  * Every mbarrier wait and spin is bounded; a timeout raises the CTA's
 //    abort flag, all roles leave their loops, in-flight copies and MMAs are
 //    drained, TMEM is freed and GC_ERR_TIMEOUT is recorded in the pool
@@ -135,7 +137,7 @@ struct Barriers {
   int item_slot[2];
   SpanPiece piece[2];  // kSpan: the items, decoded
   int next_unit;       // kSpan, shares: after the first piece
-  unsigned long long own_keys;  // kOwn: their sum
+  SpanOwn own_keys;  // kOwn
   uint32_t tmem_base;
   int abort_flag;
   SpanDeal deal;  // kSpan: how the work is dealt out
@@ -1057,7 +1059,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       mbar_init(&bar.item_empty[s], kItemConsumers);
     }
     bar.abort_flag = 0;
-    bar.own_keys = 0;
+    bar.own_keys.clear();
     bar.p0_steps = 0;
     fence_barrier_init();
   }
@@ -1074,9 +1076,10 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
   if (kSpan) {
-    const unsigned long long keys = kOwn ? span_own_keys(geo.own, kThreads) : 0;
+    SpanOwn keys{0, 0, 0, 0};
+    if (kOwn) keys.count(geo.own, kThreads);
     if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    if (kOwn) span_add_keys(keys, &bar.own_keys);
+    if (kOwn) keys.add_to(&bar.own_keys);
     __syncthreads();
   }
   const bool rank_in_warp = kSpan && geo.batch <= 32;  // (by the warp that plans)
@@ -1104,7 +1107,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                    kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 1,
+                    kOwn ? bar.own_keys.cost(geo.Hkv) : -1, geo.own, 1,
                     item_start, order, request);
       if (plan.deal.share)
         fits = span_scan(plan.deal, geo.Hkv, geo.G, order, item_start, first, request);

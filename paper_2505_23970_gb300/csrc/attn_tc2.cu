@@ -46,6 +46,14 @@
 //  * Few items: a cluster holds 2, 4 or 8 pairs that share an item's keys (see
 //    merge2_send).  Pages of an 8-bit image may have been dequantised for the call
 //    (kImg): the producers then take each page from the pool or from those.
+//  * Cross attention and shared prefixes (kSpan; span.cuh): the same roles, every row sees
+//    all keys, and a pair may have a piece of an item, whose rows it leaves unscaled with
+//    their maximum and sum.  Behind shared prefixes some of the CTAs decode the requests'
+//    own keys instead (kOwn; decode_mma.cuh).  A step is as long as in a prefill (0.79 us
+//    with all pairs busy); start to first product 8 us, last product to end 3.5.
+//    8 x 1024 tokens of 64/8 heads over 8192 states 1.45 ms (1520 TFLOP/s), 16 requests of
+//    uneven lengths, 120 GFLOP, 110 us (tensor pipe 51 % active), 64 requests behind 9
+//    shared prefixes (256 MB of keys) 63 us with the join 68.
 //  * Bound by the chain S -> softmax -> PV over the three S buffers (about 1570
 //    cycles a step, of which the tensor pipe needs 1024) and, in launches of a
 //    millisecond and more, by the GPU's power limit.
@@ -136,7 +144,7 @@ struct Bars2 {
   int workers;                // kSpan: workers that have a share
   bool fits;                  // kSpan: the units fit their numbers
   int next_unit;              // kSpan, shares: after the first piece
-  unsigned long long own_keys;  // kOwn: their sum
+  SpanOwn own_keys;  // kOwn
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -1099,7 +1107,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 4; ++i) mbar_init(&bar.l_full[i], 2);
     mbar_init(&bar.drain, 2);
     bar.abort_flag = 0;
-    bar.own_keys = 0;
+    bar.own_keys.clear();
     fence_barrier_init();
   }
   if (kOwn) __syncthreads();  // (the sum of own keys begins at 0)
@@ -1117,9 +1125,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   // everything above is this CTA's own; from here on inputs are read
   dependent_begin();
   if (kSpan) {
-    const unsigned long long keys = kOwn ? span_own_keys(geo.own, kThreads) : 0;
+    SpanOwn keys{0, 0, 0, 0};
+    if (kOwn) keys.count(geo.own, kThreads);
     if (request.hold(kThreads) && blockIdx.x == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-    if (kOwn) span_add_keys(keys, &bar.own_keys);
+    if (kOwn) keys.add_to(&bar.own_keys);
     __syncthreads();
   }
   const bool rank_in_warp = kSpan && geo.batch <= 32;  // (by the warp that plans)
@@ -1148,7 +1157,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
           span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                    kOwn ? static_cast<long long>(bar.own_keys) : -1, geo.own.weight, 2,
+                    kOwn ? bar.own_keys.cost(geo.Hkv) : -1, geo.own, 2,
                     item_start, order, request);
       at.deal = plan.deal;
       if (at.deal.share)
@@ -1240,8 +1249,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       dec::decode_cta<S, kD, 1, false, true>(
           smem_q + group * kOwnBytes,
           dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,
-                        2 * (static_cast<int>(gridDim.x) - first)}, geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo, status,
-          geo.own.merge_counters);
+                        2 * (static_cast<int>(gridDim.x) - first)},
+          geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo,
+          status, geo.own.merge_counters);
     }
   } else if (warp == 0) {
     producer2<true, kImg, kSpan>(at, smem_q, smem_k, bar, rm, item_start, total_items, geo, &map_q,
@@ -1304,7 +1314,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn2() {
 }
 
 size_t smem_bytes2(int batch, bool span = false) {
-  return (span && batch <= kSortMax ? kSortMax * sizeof(int) + kSpanHeldBytes : 0) + 1024 + 2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
+  return (span && batch <= kSortMax ? kSortMax * sizeof(int) + kSpanHeldBytes : 0) + 1024 +
+         2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
          (static_cast<size_t>(batch) + 1) * sizeof(int) +
          (batch <= kSortMax ? kSortMax * sizeof(int16_t) : 0) + 2 * 2 * kRows * sizeof(uint16_t);
 }

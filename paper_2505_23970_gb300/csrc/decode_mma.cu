@@ -43,6 +43,10 @@
 // bf16 and 8-bit pages run the same products in the same order, so decode over
 // 8-bit pages equals the 8-bit restore followed by decode bit for bit.
 //
+// Small calls of shared prefixes and cross attention (kTwo): a row's keys are those of its
+// group's (or request's) page list, then its own.  Four requests of 4 q heads and 1 kv head
+// of 64 behind 256 tokens take 7 us, of which the kernel's start and end are most.
+//
 // Measured (one call, back to back; tcgen05 kernel -> this one): 8 contexts of 9216
 // keys, 64 q / 8 kv heads of 128, bf16 55.7 -> 52.8 us (5.7 TB/s), 8-bit 85.8 -> 42.7
 // us; 64 multi-turn contexts (243k keys) bf16 182 -> 151 us (6.6 TB/s), 8-bit 295 ->

@@ -12,8 +12,8 @@
 
 namespace {
 thread_local char g_msg[512] = "";
-// control block after the KV planes: status word, work counter (at 128 bytes),
-// the decode merge counters (from 256 bytes)
+// control block after the KV planes: status word, work counter (at 128 bytes), that of the
+// calls whose join leaves it at 0 (at 192), the decode merge counters (from 256)
 constexpr size_t kTrailer = 2048;
 }  // namespace
 

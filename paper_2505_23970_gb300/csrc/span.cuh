@@ -37,6 +37,7 @@ struct OwnDecode {
   int* merge_counters;
   DecGeom geo;
   int32_t weight;  // time of 128 own keys and a kv head on one SM, in 1/16 of a unit
+  int32_t start;   // units that the own side takes beyond (its last merges)
 };
 
 constexpr int kSpanRows = 256;      // q rows of an item
@@ -174,15 +175,14 @@ __device__ inline int span_aligned_share(int share, int workers, int batch, int 
 
 // How a call is dealt out, and the workers that take part (-1: the units are too many),
 // worked out by one warp; every CTA comes to the same answer.  start: each place's first item.
-// own_keys >= 0: the other workers decode so many own keys, 128 of them and a kv head
-// taking an SM own_weight / 16 of a unit (then shares always).
-constexpr int kSpanStart = 5;  // units in the time that a span CTA takes beyond an own one's
+// own_keys >= 0: the other workers decode so many own keys, as OwnDecode says (then shares
+// always).
 struct SpanPlan {
   SpanDeal deal;
   int workers;
 };
 __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int G,
-                                     long long own_keys, int own_weight, int sms_per_worker,
+                                     long long own_keys, const OwnDecode& own, int sms_per_worker,
                                      const int* start, const int16_t* order,
                                      const SpanRequests& request) {
   if (!sp.cuts || batch > kSpanRequests) return {{0, 0}, sp.workers};
@@ -212,18 +212,21 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
     if (units == 0) return {{kSpanMinShare, 0}, 0};
     if (units >= (1ll << 30)) return {{kSpanMinShare, 0}, -1};  // (see span_scan)
     // The number w of workers for which both sides take as long,
-    //     u / w + kSpanStart = o / (W - w),
-    // with u units, W workers in all and o the own keys' time if they had one worker's SMs:
-    //     s w^2 - (s W - u - o) w - u W = 0.
+    //     u / w = o / (W - w) + s,
+    // with u units, W workers in all, o the own keys' time if they had one worker's SMs and
+    // s (own.start > 0) what their side takes beyond:
+    //     s w^2 - (s W + u + o) w + u W = 0;
+    // the smaller root, as below W.
     const int all = static_cast<int>(units);
     const float W = static_cast<float>(sp.workers), u = static_cast<float>(all);
-    const float o = static_cast<float>(own_keys) * Hkv * own_weight /
+    const float o = static_cast<float>(own_keys) * Hkv * own.weight /
                     (128.f * 16.f * sms_per_worker);
-    const float h = 0.5f * (kSpanStart * W - u - o);
-    const float root = sqrtf(h * h + kSpanStart * u * W);
-    const float w = h > 0.f ? (h + root) / kSpanStart : u * W / (root - h);
-    // (one at least for own keys, and no share below the least)
-    int n = min(static_cast<int>(w + 0.5f), all / kSpanMinShare);
+    const float h = 0.5f * (own.start * W + u + o);
+    const float w = u * W / (h + sqrtf(fmaxf(0.f, h * h - own.start * u * W)));
+    // One more than that: shares are whole units, and the span side too long costs more
+    // than a worker less on the other.  (One at least for own keys, and no share below the
+    // least.)
+    int n = min(static_cast<int>(w + 1.5f), all / kSpanMinShare);
     n = max(1, min(n, sp.workers - 1));
     const int share = max((all + n - 1) / n, kSpanMinShare);
     const int aligned = apart ? span_aligned_share(share, n, batch, Hkv, G, request) : 0;
@@ -257,26 +260,48 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
   return {{align ? aligned : share, align ? 1 : 0}, sp.workers};
 }
 
-// Thread's own keys of the requests behind shared prefixes, a request's fixed cost counted
-// as up to kSpanOwnKeys (short ones are done several at a time); and their sum over the CTA
-// (sum: cleared before).  The cost, and the weight of a key (14
-// sixteenths of a unit at d = 128, 5 at 64), are from calls of 8 to 128 requests with 200 to
-// 2048 own keys: at d = 128, with cost 512 they take from 2 % less to 6 % more, with weight
-// 12 up to 13 % more, with 16 from 3 % less to 8 % more.
-constexpr int kSpanOwnKeys = 768;
-__device__ __forceinline__ unsigned long long span_own_keys(const OwnDecode& own, int threads) {
-  unsigned long long keys = 0;
-  for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
-    const int T = ld_plain(own.lens + b);
-    if (T > 0) keys += T + min(kSpanOwnKeys, 2 * min(T, kSpanOwnKeys) + 128);
+// The own keys of the requests behind shared prefixes, as the division of the SMs counts
+// them (summed over a CTA's threads; cleared before).  A request of T costs T + 256 keys,
+// longer ones up to 1024 more (2 T between), or T + 48 where decode_cta takes a pair per
+// warp (all short, and enough of them).  This and OwnDecode's two figures were fitted to 18
+// (d = 128) and 15 (d = 64) calls of 12 to 512 requests with 30 to 6000 own keys, timed with
+// the workers divided in every way: 2.1 and 2.6 % on average above the best division, 8 and
+// 11 % at most (with up to 768 keys for all alike, and s = -5: 10 and 8.5 %, 38 and 30 %).
+struct SpanOwn {
+  unsigned long long keys;
+  int by_warp, longest, valid;
+
+  __device__ __forceinline__ void clear() { *this = SpanOwn{0, 0, 0, 0}; }
+  __device__ __forceinline__ void count(const OwnDecode& own, int threads) {
+    for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
+      const int T = ld_plain(own.lens + b);
+      if (T <= 0) continue;
+      keys += T + min(max(T, 256), 1024);
+      by_warp += min(T, dec::kShort) + 48;
+      longest = max(longest, T);
+      ++valid;
+    }
   }
-  return keys;
-}
-__device__ __forceinline__ void span_add_keys(unsigned long long keys, unsigned long long* sum) {
+  __device__ __forceinline__ void add_to(SpanOwn* sum) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xffffffffu, keys, o);
-  if ((threadIdx.x & 31) == 0 && keys > 0) atomicAdd(sum, keys);
-}
+    for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xffffffffu, keys, o);
+    by_warp = __reduce_add_sync(0xffffffffu, by_warp);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    valid = __reduce_add_sync(0xffffffffu, valid);
+    if ((threadIdx.x & 31) == 0 && valid > 0) {
+      atomicAdd(&sum->keys, keys);
+      atomicAdd(&sum->by_warp, by_warp);
+      atomicMax(&sum->longest, longest);
+      atomicAdd(&sum->valid, valid);
+    }
+  }
+  // (decode_cta's rule, as if every CTA were on the own side)
+  __device__ __forceinline__ long long cost(int Hkv) const {
+    const bool warps = longest <= dec::kShort &&
+                       static_cast<long long>(valid) * Hkv >= 6ll * gridDim.x;
+    return warps ? by_warp : static_cast<long long>(keys);
+  }
+};
 
 // Work order of up to 32 requests, longest first (ties by number), by one warp.
 __device__ __forceinline__ void span_rank32(const SpanRequests& request, int16_t* order) {

@@ -5,9 +5,13 @@
 // shared pages.  The kernels of the prefill attention take them (attn_tc2.cu at
 // head_dim 128, attn_tc.cu at 64) without the causal limit, cut where the items alone
 // would leave SMs idle (span.cuh); the rows of a group's requests lie next to each
-// other, so the shared keys are read once for 256 of them.  The pieces of cut requests are
-// joined here, those of a shared prefix with what the decode kernel (decode_mma.cu)
-// has for the request's own keys.
+// other, so the shared keys are read once for 256 of them.  The requests' own keys are
+// decoded by some of the same kernel's CTAs (or by the decode kernel before it), and small
+// calls by the decode kernel alone, row by row (row_by_row).
+//
+// Here: which way a call goes, its workspace, and the joins of pieces.  A join is bound by
+// latency: its blocks read the plan, the row's place and then eight pieces at a time
+// (pieces one after the other 10 to 37 us, eight together 4 to 8, at 512 to 4096 rows).
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
 #include "span.cuh"
@@ -232,7 +236,8 @@ static bool decodes_in_kernel(const gc_kv_pool* pool, const SpanArgs& a) {
   const int64_t steps = static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size / 128 + 1;
   const int64_t own = static_cast<int64_t>(a.batch) * cfg.num_kv_heads *
                       (static_cast<int64_t>(a.max_blocks) * cfg.page_size / 128 + 1);
-  return own + 2 * kMergeCounters < 2147483647LL && (cfg.head_dim == 64 || G <= 8) && a.groups <= kSpanRequests &&
+  return own + 2 * kMergeCounters < 2147483647LL && (cfg.head_dim == 64 || G <= 8) &&
+         a.groups <= kSpanRequests &&
          items * (steps + kSpanLead) < (1ll << 30) - pool->num_sms;
 }
 
@@ -298,7 +303,8 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
     if (st != GC_OK) return st;
     const OwnDecode with{static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.lens,
                          static_cast<float*>(own.workspace), pool->merge_counters,
-                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 14 : 5};
+                         decode_geom(pool, own, nullptr, nullptr), cfg.head_dim == 128 ? 15 : 5,
+                         cfg.head_dim == 128 ? 4 : 1};
     st = launch_items(pool, args, span, stream, &with);
   } else {
     st = launch_decode(pool, own, stream);
