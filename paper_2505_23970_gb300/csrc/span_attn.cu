@@ -165,9 +165,10 @@ gc_status check_space(const char* who, size_t need, const void* workspace, size_
 // of the decode kernel, without a join and without the start of the tensor-core kernels.
 // By the room in the block tables, as the lengths are on the device: rows x `keys` x kv
 // heads.  Measured at lengths that fill it, row by row | tiles (us, heads of 128 then 64):
-//   shared: 4 requests behind 256 tokens, 1 kv head, 7.0 | 13.7, 7.3 | 11.6; 16 behind
-//   1000, 8 kv heads, 16.1 | 17.2, 13.2 | 16.7; 32 behind 2000, 4 kv heads, 17.7 | 17.2,
-//   15.1 | 16.2; 128 behind 1000, 8 kv heads, 53 | 47, 38 | 33;
+//   shared: 4 requests behind 256 tokens, 1 kv head, 7.0 | 13.7, 7.3 | 11.6; behind 1000
+//   tokens with 100 own ones, 8 kv heads, 16 requests 16.0 | 19.4, 13.0 | 16.7, 32 20.7 |
+//   19.8, 16.4 | 20.9, 128 56 | 32, 39 | 28; 32 behind 3500 and 100, 4 kv heads, 24.3 |
+//   19.5, 18.8 | 20.5;
 //   cross: 16 tokens over 1000 states each, 1 kv head, 9.2 | 18.3, 8.2 | 20.6; 12 over
 //   1000, 8 kv heads, 13.1 | 18.1, 11.3 | 20.2; 320 over 300, 2 kv heads, 38.6 | 15.3,
 //   22.3 | 18.6.  With two steps of keys nothing is cut and tiles take 9 us: 64 over 256,
