@@ -149,8 +149,9 @@ gc_status gc_kv_pool_create(const gc_pool_config* cfg, void* dev_mem, size_t dev
   return GC_OK;
 }
 
+// (Keeps the message of the last failing call: a finaliser may come between that call and
+// whoever reads it.)
 gc_status gc_kv_pool_destroy(gc_kv_pool* pool) {
-  g_msg[0] = 0;
   if (!pool) return GC_OK;
   gc::release_scratch(pool->device, pool->scratch, pool->scratch_context);
   if (pool->owned) {

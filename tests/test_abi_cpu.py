@@ -85,3 +85,13 @@ def test_status_strings(lib):
 
 def test_destroy_null_is_noop(lib):
     gcb.gc_kv_pool_destroy(None)
+
+
+def test_destroying_a_pool_keeps_the_message():
+    """A finaliser may run between a failing call and whoever reads its message."""
+    lib = gcb.load()
+    assert lib.gc_kv_pool_create(None, None, 0, None) == gcb.GC_ERR_INVALID_ARG
+    message = gcb.gc_last_error()
+    assert message
+    assert lib.gc_kv_pool_destroy(None) == gcb.GC_OK
+    assert gcb.gc_last_error() == message
