@@ -131,6 +131,20 @@ def test_rotates_and_appends(Hq, Hkv, d, ps, rot, interleaved, fused, P, n):
     c.check()
 
 
+@pytest.mark.parametrize("heads", [(0, 1), (4, 2)])
+@pytest.mark.parametrize("batch", [7, 8, 9, 63, 64, 65, 200, 513])
+def test_finds_each_request(batch, heads):
+    """Few tokens of many requests, some with none, at the steps of the search."""
+    rng = np.random.default_rng(batch)
+    n = rng.choice([0, 1, 1, 1, 5], batch).astype(int)
+    n[[0, -1]] = [0, 2]
+    P = rng.integers(0, 70, batch)
+    c = Call(P, n, *heads, 64, 16, 32, seed=batch, positions=rng.integers(0, 99, n.sum()))
+    c.run()
+    assert c.pool.check() == gcb.GC_OK
+    c.check()
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_positions_are_not_the_slots(interleaved):
     P, n = [0, 3, 40], [1, 17, 2]
