@@ -148,7 +148,8 @@ struct Barriers {
 
 // Consumers of the work-item ring: the two MMA issuer threads and one
 // elected thread per softmax warp.
-constexpr int kItemConsumers = 2 + 2 * kTileM / 32;
+template <bool kVWarp>  // (and the V producer)
+constexpr int kItemConsumers = 2 + 2 * kTileM / 32 + (kVWarp ? 1 : 0);
 
 // A work item and the quantities every role derives from it.
 struct Item {
@@ -410,8 +411,9 @@ __device__ void converter(uint8_t* smem_kv, Barriers& bar, Q8State& q8, const Ge
 }
 
 // ------------------------------------------------------------------ roles
-template <int D, Pages kPages, bool kSpan>
-__device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8State* q8,
+// kVWarp: two warps, `which` 0 for Q and K, 1 for V (see launch).
+template <int D, Pages kPages, bool kSpan, bool kVWarp>
+__device__ void producer(int which, uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8State* q8,
                          const int* item_start, int total_items, const Geom& geo,
                          SpanDeal deal, const CUtensorMap* map_q, const CUtensorMap* map_kv,
                          const CUtensorMap* map_img,
@@ -439,34 +441,46 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
   for (uint32_t k = 0; ok; ++k) {
     ItemOf<kSpan> w;
     if constexpr (kSpan) {
-      const int it = claim_piece(bar, k, unit, item_start, order, work_counter, total_items, geo,
-                                 deal, request, abortp, ok);
-      if (!ok || it < 0) break;
-      item_from_piece(bar.piece[k & 1], geo, w);
+      if (!kVWarp || which == 0) {
+        const int it = claim_piece(bar, k, unit, item_start, order, work_counter, total_items,
+                                   geo, deal, request, abortp, ok);
+        if (!ok || it < 0) break;
+        item_from_piece(bar.piece[k & 1], geo, w);
+      } else {
+        const int it = read_item(bar, k, abortp, ok);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (it >= 0) item_from_piece(bar.piece[k & 1], geo, w);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.item_empty[k & 1]);
+        if (it < 0) break;
+      }
     } else {
       const int it = claim_item(bar, k, work_counter, total_items, geo.more_items, abortp, ok);
       if (!ok || it < 0) break;
       decode_item(it, item_start, geo, prefix_lens, new_lens, cu_new_lens, w);
     }
     // ---- Q tiles
-    ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
-    if (!ok) break;
-    if (lane == 0) {
-      uint32_t bytes = 0;
+    if (!kVWarp || which == 0) {
+      ok = mbar_wait(&bar.q_empty, (q_count & 1) ^ 1, abortp);
+      if (!ok) break;
+      if (lane == 0) {
+        uint32_t bytes = 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (w.valid[i]) bytes += C::kTileBytes;
-      mbar_arrive_expect_tx(&bar.q_full, bytes);
+        for (int i = 0; i < 2; ++i)
+          if (w.valid[i]) bytes += C::kTileBytes;
+        mbar_arrive_expect_tx(&bar.q_full, bytes);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (w.valid[i])
+        for (int i = 0; i < 2; ++i)
+          if (w.valid[i])
 #pragma unroll
-          for (int h = 0; h < C::kHalves; ++h)
-            tma_load_3d(smem_q + i * C::kTileBytes + h * C::kHalfBytes, map_q, &bar.q_full, h * 64,
-                        w.g * geo.G, w.cu + w.tok0[i]);
+            for (int h = 0; h < C::kHalves; ++h)
+              tma_load_3d(smem_q + i * C::kTileBytes + h * C::kHalfBytes, map_q, &bar.q_full,
+                          h * 64, w.g * geo.G, w.cu + w.tok0[i]);
+      }
+      armed_q = q_count & 1;
+      ++q_count;
     }
-    armed_q = q_count & 1;
-    ++q_count;
     // ---- K/V tiles, page by page.  The copies of a tile are issued by
     // several lanes at once (lane = page * halves + half): one thread issuing
     // every box of a 16-row-page tile could not keep up with the MMAs.
@@ -541,9 +555,10 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
       const int my_page = __shfl_sync(0xffffffffu, page, pg < 32 ? pg : 0);
       const bool issues = pg < kTileN / 16 && my_page >= 0;
 #pragma unroll 1
-      for (int kv = 0; kv < 2; ++kv) {
-        const int slot = kv_count % C::kStages;
-        ok = mbar_wait(&bar.kv_empty[slot], ((kv_count / C::kStages) & 1) ^ 1, abortp);
+      for (int kv = kVWarp ? which : 0; kv < (kVWarp ? which + 1 : 2); ++kv) {
+        const uint32_t use = kVWarp ? kv_count + kv : kv_count;
+        const int slot = use % C::kStages;
+        ok = mbar_wait(&bar.kv_empty[slot], ((use / C::kStages) & 1) ^ 1, abortp);
         if (!ok) break;
         uint8_t* dst = smem_kv + slot * C::kTileBytes;
         const bool fix = kv == 1 && nkeys < kTileN;
@@ -565,7 +580,7 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
                         static_cast<int32_t>(q8_chunk_index(geo, cur.blk, kv)));
           }
           armed8 |= 1u << slot;
-          armed8_par = (armed8_par & ~(1u << slot)) | (((kv_count / C::kStages) & 1u) << slot);
+          armed8_par = (armed8_par & ~(1u << slot)) | (((use / C::kStages) & 1u) << slot);
         }
         if (lane == 0)
           mbar_arrive_expect_tx(full, static_cast<uint32_t>(good) * box_bytes * C::kHalves);
@@ -603,10 +618,11 @@ __device__ void producer(uint8_t* smem_q, uint8_t* smem_kv, Barriers& bar, Q8Sta
           if (lane == 0) mbar_arrive(&bar.kv_full[slot]);
         } else {
           armed |= 1u << slot;
-          armed_par = (armed_par & ~(1u << slot)) | (((kv_count / C::kStages) & 1u) << slot);
+          armed_par = (armed_par & ~(1u << slot)) | (((use / C::kStages) & 1u) << slot);
         }
-        ++kv_count;
+        if (!kVWarp) ++kv_count;
       }
+      if (kVWarp) kv_count += 2;
     }
   }
   if (kQ8 && ok) {
@@ -1008,8 +1024,8 @@ __device__ void softmax_wg(Barriers& bar, uint32_t tmem, const int* item_start,
 }
 
 // kOwn: some of the CTAs decode the requests' own keys (span.cuh), with NT tiles of 8
-// heads.
-template <int D, Pages kPages, bool kSpan = false, int kOwn = 0>
+// heads.  kVWarp: a second producer warp.
+template <int D, Pages kPages, bool kSpan = false, int kOwn = 0, bool kVWarp = false>
 __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThreads, 1)
     attn_tc_kernel(const __grid_constant__ CUtensorMap map_q,
                    const __grid_constant__ CUtensorMap map_kv,
@@ -1056,7 +1072,7 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&bar.item_full[s], 1);
-      mbar_init(&bar.item_empty[s], kItemConsumers);
+      mbar_init(&bar.item_empty[s], kItemConsumers<kVWarp>);
     }
     bar.abort_flag = 0;
     bar.own_keys.clear();
@@ -1179,15 +1195,17 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       dec::decode_cta<S, D, kOwn, false, true>(
           smem_q + group * kOwnBytes,
           dec::ByNumber{2 * (static_cast<int>(blockIdx.x) - first) + group,
-                        2 * (static_cast<int>(gridDim.x) - first)}, geo.own.q, geo.own.block_table, geo.own.lens,
-          out, geo.own.workspace, geo.own.geo, status, geo.own.merge_counters);
+                        2 * (static_cast<int>(gridDim.x) - first)},
+          geo.own.q, geo.own.block_table, geo.own.lens, out, geo.own.workspace, geo.own.geo,
+          status, geo.own.merge_counters);
     }
   } else if (warp < 4) {
     regs_dec<kQ8 ? kRegsProducerQ8 : kRegsProducer>();
-    if (warp == 0) {
-      producer<D, kPages, kSpan>(smem_q, smem_kv, bar, q8, item_start, total_items, geo,
-                          deal, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens, status,
-                          work_counter);
+    if (warp == 0 || (kVWarp && warp == 3)) {
+      producer<D, kPages, kSpan, kVWarp>(
+          kVWarp && warp == 3 ? 1 : 0, smem_q, smem_kv, bar, q8, item_start, total_items, geo,
+          deal, &map_q, &map_kv, &map_img, block_table, prefix_lens, new_lens, cu_new_lens,
+          status, work_counter);
     } else if (warp == 1 || warp == 2) {
       if (lane == 0)
         mma_issuer<D, kSpan>(warp - 1, smem_q, smem_kv, bar, tmem, item_start, total_items, geo,
@@ -1355,8 +1373,15 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   constexpr Pages kUnpacked = D == 128 ? Pages::kImage : Pages::kUnpacked;
   // (and nothing is cut there)
   constexpr bool kSpan = D == 64;
+  // Cross attention whose requests have one tile of rows: K and V by a warp each.  With
+  // pages of 16 one warp's copies are such a step's longest part (us, one warp | two; 8 kv
+  // heads: 40 requests of 120 rows over 4000 keys 98 | 86, 19 over 8192 83 | 71, 1 of 64
+  // over 60000 44 | 41, with pages of 64 85 | 85; of 240 rows over 4000 135 | 141).
+  const bool v_warp = span && !own && static_cast<long long>(a.total_new_tokens) * geo.G <=
+                                          static_cast<long long>(kTileM) * a.batch;
   auto kernel = own && geo.G > 8 ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 2 : 0>
                 : own      ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 1 : 0>
+                : v_warp   ? attn_tc_kernel<D, kPool, kSpan, 0, kSpan>
                 : span     ? attn_tc_kernel<D, kPool, kSpan>
                 : q8       ? attn_tc_kernel<D, Pages::kImage>
                 : unpacked ? attn_tc_kernel<D, kUnpacked>
