@@ -1465,8 +1465,8 @@ bool converts_in_kernel(const gc_kv_pool* pool, const AttnArgs& a) {
 }
 
 gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                              const SpanGeom& span, const OwnDecode* own) {
-  return launch<64>(pool, a, stream, pool->span_counter, nullptr, nullptr, &span, own);
+                              int* work_counter, const SpanGeom& span, const OwnDecode* own) {
+  return launch<64>(pool, a, stream, work_counter, nullptr, nullptr, &span, own);
 }
 
 gc_status launch_attn_tc_q8(const gc_kv_pool* pool, const AttnArgs& a, const Q8Pages& q8,

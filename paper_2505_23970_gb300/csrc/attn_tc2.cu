@@ -402,10 +402,12 @@ __device__ void producer2(const Place& at, uint8_t* smem_q, uint8_t* smem_ring, 
         // out the rest.  Without one there are no more unless new_lens sums up to
         // more than T_new (requests that share rows); they are dealt out in turn
         const int clusters = static_cast<int>(gridDim.x / (2 * at.splits));
-        it = k > 0 && geo.more_items
-                 ? clusters + atomicAdd(work_counter, 1)
-                 : static_cast<int>(blockIdx.x / (2 * at.splits)) + static_cast<int>(k) * clusters;
-        if (kSpan && at.deal.share) it = unit < unit_end ? unit : total_items;
+        if (kSpan && at.deal.share)
+          it = unit < unit_end ? unit : total_items;
+        else if (k > 0 && geo.more_items)
+          it = clusters + atomicAdd(work_counter, 1);
+        else
+          it = static_cast<int>(blockIdx.x / (2 * at.splits)) + static_cast<int>(k) * clusters;
         if (it >= total_items) it = -1;
         if (kSpan && it >= 0) {
           unit = span_message(it, item_start, geo, at, worker,

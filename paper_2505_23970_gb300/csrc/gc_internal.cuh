@@ -16,7 +16,9 @@ struct gc_kv_pool {
   size_t data_bytes;
   int32_t* status;        // device status word (first error recorded by a kernel)
   int32_t* work_counter;  // attention work items (control block, cleared by launches that need it)
-  int32_t* span_counter;  // the same of cross attention (kept at 0 where its join follows)
+  // The same of calls whose items may be cut (span.cuh): at 0 between calls.  A join follows
+  // each of them and leaves it so; a call without a join uses work_counter.
+  int32_t* span_counter;
   int32_t* merge_counters;  // [kMergeCounters] decode merge counters (control block, kept at 0)
   void* owned;            // cudaMalloc'd block, or nullptr if caller-owned
   cudaMemPool_t scratch;  // stream-ordered scratch (kv_q8.cu), nullptr if there is none
@@ -255,7 +257,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
                           const SpanGeom* span = nullptr, const OwnDecode* own = nullptr);
 // The same at head_dim 64, on single SMs.
 gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
-                              const SpanGeom& span, const OwnDecode* own);
+                              int* work_counter, const SpanGeom& span, const OwnDecode* own);
 // Host-side bound of the attention kernels' 32-bit work numbering (items and
 // q rows of one call, with a margin of two claims per CTA of `grid`):
 // GC_ERR_UNSUPPORTED before anything is launched when a call could pass it.

@@ -110,8 +110,10 @@ __global__ void __launch_bounds__(256)
 template <int D>
 __global__ void __launch_bounds__(256)
     shared_join_kernel(SpanGeom sp, const int32_t* own_lens, int own_cap, DecodeParts own,
-                       __nv_bfloat16* out, int Hq, int G, int64_t rows, int32_t* status) {
+                       __nv_bfloat16* out, int Hq, int G, int64_t rows, int32_t* status,
+                       int* work_counter) {
   dependent_begin();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *work_counter = 0;  // for the next call
   constexpr int kLanes = D / 4;
   const int c = static_cast<int>(threadIdx.x) % kLanes;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
@@ -145,11 +147,26 @@ __global__ void __launch_bounds__(256)
   *reinterpret_cast<uint2*>(out + row * D + 4 * c) = j.rounded();
 }
 
+// Items that may be cut: claimed from the counter that the join behind them leaves at 0.
+// Others may have no join: claimed from the one that the launch clears, as a prefill's.
 gc_status launch_items(const gc_kv_pool* pool, const AttnArgs& a, const SpanGeom& span,
                        cudaStream_t stream, const OwnDecode* own = nullptr) {
+  int* counter = span.cuts ? pool->span_counter : pool->work_counter;
   return pool->cfg.head_dim == 128
-             ? launch_attn_tc2(pool, a, stream, pool->span_counter, nullptr, &span, own)
-             : launch_attn_tc_span(pool, a, stream, span, own);
+             ? launch_attn_tc2(pool, a, stream, counter, nullptr, &span, own)
+             : launch_attn_tc_span(pool, a, stream, counter, span, own);
+}
+
+// The join behind a call's items.
+template <typename... P, typename... A>
+gc_status launch_join(const gc_kv_pool* pool, const char* who, void (*join)(P...), int64_t blocks,
+                      cudaStream_t stream, A... args) {
+  const cudaError_t e =
+      launch_dependent(join, static_cast<unsigned>(blocks), 256, 0, stream, args...);
+  if (e == cudaSuccess) return GC_OK;
+  // (no join to do it)
+  cudaMemsetAsync(pool->span_counter, 0, sizeof(int), stream);
+  return cuda_fail(e, who);
 }
 
 gc_status check_space(const char* who, size_t need, const void* workspace, size_t bytes) {
@@ -219,12 +236,9 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
   // (one block per share and 1024 / d rows)
   const int chunks = kSpanRows / (1024 / cfg.head_dim);
   const auto join = cfg.head_dim == 128 ? cross_join_kernel<128> : cross_join_kernel<64>;
-  const cudaError_t e = launch_dependent(
-      join, static_cast<unsigned>(space.slots / 2 * chunks), 256, 0, stream, span,
-      static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, a.num_q_heads / cfg.num_kv_heads,
-      pool->span_counter);
-  if (e != cudaSuccess) return cuda_fail(e, who);
-  return GC_OK;
+  return launch_join(pool, who, join, space.slots / 2 * chunks, stream, span,
+                     static_cast<__nv_bfloat16*>(a.out), a.num_q_heads,
+                     a.num_q_heads / cfg.num_kv_heads, pool->span_counter);
 }
 
 // One kernel for both sides of a call, unless the own keys' side needs more registers
@@ -315,13 +329,10 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
   const int64_t rows = static_cast<int64_t>(a.batch) * a.num_q_heads;
   const int per_block = 256 / (cfg.head_dim / 4);
   const auto join = cfg.head_dim == 128 ? shared_join_kernel<128> : shared_join_kernel<64>;
-  const cudaError_t e = launch_dependent(
-      join, static_cast<unsigned>((rows + per_block - 1) / per_block), 256, 0, stream, span, a.lens,
-      static_cast<int>(static_cast<int64_t>(a.max_blocks) * cfg.page_size), own.own,
-      static_cast<__nv_bfloat16*>(a.out), a.num_q_heads, a.num_q_heads / cfg.num_kv_heads, rows,
-      pool->status);
-  if (e != cudaSuccess) return cuda_fail(e, who);
-  return GC_OK;
+  return launch_join(pool, who, join, (rows + per_block - 1) / per_block, stream, span, a.lens,
+                     static_cast<int>(static_cast<int64_t>(a.max_blocks) * cfg.page_size), own.own,
+                     static_cast<__nv_bfloat16*>(a.out), a.num_q_heads,
+                     a.num_q_heads / cfg.num_kv_heads, rows, pool->status, pool->span_counter);
 }
 
 }  // namespace gc
