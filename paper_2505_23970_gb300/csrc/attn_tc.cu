@@ -1122,9 +1122,9 @@ __global__ void __launch_bounds__(kPages == Pages::kImage ? kThreadsQ8 : kThread
       bool fits = true;
       if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
-          span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                    kOwn ? bar.own_keys.cost(geo.Hkv) : -1, geo.own, 1,
-                    item_start, order, request);
+          span_plan<(kOwn > 0)>(geo.span, geo.batch, geo.Hkv, geo.G,
+                                kOwn ? bar.own_keys.cost(geo.Hkv) : 0, geo.own, 1, item_start,
+                                order, request);
       if (plan.deal.share)
         fits = span_scan(plan.deal, geo.Hkv, geo.G, order, item_start, first, request);
       if (lane == 0) {

@@ -1158,9 +1158,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool fits = true;
       if (!kOwn) fits = span_scan({0, 0}, geo.Hkv, geo.G, order, item_start, first, request);
       const SpanPlan plan =
-          span_plan(geo.span, geo.batch, geo.Hkv, geo.G,
-                    kOwn ? bar.own_keys.cost(geo.Hkv) : -1, geo.own, 2,
-                    item_start, order, request);
+          span_plan<kOwn>(geo.span, geo.batch, geo.Hkv, geo.G,
+                          kOwn ? bar.own_keys.cost(geo.Hkv) : 0, geo.own, 2, item_start, order,
+                          request);
       at.deal = plan.deal;
       if (at.deal.share)
         fits = span_scan(at.deal, geo.Hkv, geo.G, order, item_start, first, request);

@@ -22,6 +22,7 @@
 
 #include "decode_mma.cuh"
 #include "gc_internal.cuh"
+#include "own_keys.h"
 #include "sm103_ptx.cuh"
 
 namespace gc {
@@ -175,12 +176,12 @@ __device__ inline int span_aligned_share(int share, int workers, int batch, int 
 
 // How a call is dealt out, and the workers that take part (-1: the units are too many),
 // worked out by one warp; every CTA comes to the same answer.  start: each place's first item.
-// own_keys >= 0: the other workers decode so many own keys, as OwnDecode says (then shares
-// always).
+// kOwn: the other workers decode so many own keys, as OwnDecode says (then shares always).
 struct SpanPlan {
   SpanDeal deal;
   int workers;
 };
+template <bool kOwn>
 __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int G,
                                      long long own_keys, const OwnDecode& own, int sms_per_worker,
                                      const int* start, const int16_t* order,
@@ -208,7 +209,7 @@ __device__ inline SpanPlan span_plan(const SpanGeom& sp, int batch, int Hkv, int
   tiles = __reduce_max_sync(0xffffffffu, tiles);
   // K and V more than half of the L2, and several tiles to read them
   const bool apart = tiles > 1 && per_tile > kSpanInL2;
-  if (own_keys >= 0) {
+  if constexpr (kOwn) {
     if (units == 0) return {{kSpanMinShare, 0}, 0};
     if (units >= (1ll << 30)) return {{kSpanMinShare, 0}, -1};  // (see span_scan)
     // The number w of workers for which both sides take as long,
@@ -273,11 +274,12 @@ struct SpanOwn {
 
   __device__ __forceinline__ void clear() { *this = SpanOwn{0, 0, 0, 0}; }
   __device__ __forceinline__ void count(const OwnDecode& own, int threads) {
+    const int cap = own.geo.max_blocks << own.geo.ps_shift;
     for (int b = threadIdx.x; b < own.geo.batch; b += threads) {
       const int T = ld_plain(own.lens + b);
-      if (T <= 0) continue;
-      keys += T + min(max(T, 256), 1024);
-      by_warp += min(T, dec::kShort) + 48;
+      if (!own_keys_count(T, cap)) continue;
+      keys += static_cast<unsigned long long>(own_keys_cost(T));
+      by_warp += own_keys_cost_by_warp(T, dec::kShort);
       longest = max(longest, T);
       ++valid;
     }
