@@ -595,8 +595,9 @@ GC_API gc_status gc_paged_decode_attn_q8(const void* q, const gc_kv_pool* pool,
  *               after the stream passes the call; no initial contents needed.
  *               Calls sharing a workspace must not overlap on the GPU.
  * A request whose length is outside [0, max_blocks_per_seq*ps], or whose rows
- * would pass T_new, is skipped (its rows are not written); a bad page leaves
- * its request's output unspecified; both are recorded as
+ * would pass T_new, is skipped: its rows are not written, nor are rows that
+ * cu_new_lens leaves between the requests' new_lens[b].  A bad page leaves its
+ * request's output unspecified.  Skipped requests and bad pages are recorded as
  * GC_ERR_OUT_OF_RANGE.  Calls on one pool must not overlap on the GPU with
  * each other or with the other attention calls.  The same call gives the same
  * bits again; the order of its sums depends on the call's sizes and on what

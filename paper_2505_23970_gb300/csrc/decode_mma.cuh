@@ -26,6 +26,7 @@ struct DecGeom {
   const int32_t* shared_table;
   const int32_t* shared_lens;
   const int32_t* cu_requests;
+  const int32_t* group_rows;
   int32_t groups, shared_blocks;
 };
 
@@ -58,6 +59,7 @@ inline DecGeom decode_geom(const gc_kv_pool* pool, const DecodeArgs& a, const De
   geo.shared_table = a.prefix.table;
   geo.shared_lens = a.prefix.lens;
   geo.cu_requests = a.prefix.cu_requests;
+  geo.group_rows = a.prefix.rows;
   geo.groups = a.prefix.groups;
   geo.shared_blocks = a.prefix.max_blocks;
   geo.range_tiles = split ? split->split_tiles : 0;
@@ -567,26 +569,42 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
     const int cap = geo.max_blocks << geo.ps_shift;
     int most = 0, n = 0;
     if constexpr (kTwo) {
+      // A group's rows [first, first + rows) and shared keys; false: it is skipped.  (The
+      // rule of span_request.  In cross attention the rows are given, and a row may be
+      // no request's.)
+      auto group = [&](int g, int& first, int64_t& rows, int& keys) -> bool {
+        first = ld_plain(geo.cu_requests + g);
+        rows = geo.group_rows ? ld_plain(geo.group_rows + g)
+                              : static_cast<int64_t>(ld_plain(geo.cu_requests + g + 1)) - first;
+        keys = ld_plain(geo.shared_lens + g);
+        return rows >= 0 && first >= 0 && first + rows <= geo.batch &&
+               (rows == 0 || (keys >= 0 && keys <= geo.shared_blocks << geo.ps_shift));
+      };
+      int first, shared;
+      int64_t rows;
+      bool bad = false;
+      if (who.cta() == who.ctas() - 1)  // (in a small call it has no keys to work on)
+        for (int g = S::tid(); g < geo.groups; g += S::kThreads)
+          bad |= !group(g, first, rows, shared);
       int* context = start + geo.batch + 1;  // [batch] keys, -1: skipped; then the groups
       for (int b = S::tid(); b < geo.batch; b += S::kThreads) {
+        const int own = seq_lens ? ld_plain(seq_lens + b) : 0;
         int lo = 0, hi = geo.groups;  // the last group whose first request is <= b
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
           if (ld_plain(geo.cu_requests + mid) <= b) lo = mid; else hi = mid;
         }
-        const int first = ld_plain(geo.cu_requests + lo), last = ld_plain(geo.cu_requests + lo + 1);
-        const int shared = ld_plain(geo.shared_lens + lo);
-        const int own = seq_lens ? ld_plain(seq_lens + b) : 0;
-        const bool bad = first < 0 || first > b || last <= b || last > geo.batch || shared < 0 ||
-                         shared > (geo.shared_blocks << geo.ps_shift) || own < 0 || own > cap;
-        if (bad && who.cta() == 0) record_error(status, GC_ERR_OUT_OF_RANGE);
-        const int T = bad ? -1 : ((shared + kGroup - 1) & -kGroup) + own;
+        const bool found = group(lo, first, rows, shared) && first <= b && b < first + rows;
+        const bool fits = own >= 0 && own <= cap;
+        bad |= who.cta() == 0 && (!fits || (!found && !geo.group_rows));
+        const int T = found && fits ? ((shared + kGroup - 1) & -kGroup) + own : -1;
         context[b] = T;
         context[geo.batch + b] = lo;
-        start[b] = bad ? 0 : max(T, 1);
+        start[b] = T < 0 ? 0 : max(T, 1);
         most = max(most, T);
-        n += !bad;
+        n += T >= 0;
       }
+      if (bad) record_error(status, GC_ERR_OUT_OF_RANGE);
     }
     for (int b = S::tid(); !kTwo && b < geo.batch; b += S::kThreads) {
       const int T = ld_plain(seq_lens + b);

@@ -275,6 +275,7 @@ struct DecodePrefix {
   const int32_t* table;
   const int32_t* lens;
   const int32_t* cu_requests;
+  const int32_t* rows;  // of each group; nullptr: up to the next group's first
   int32_t groups, max_blocks;
 };
 struct DecodeArgs {
@@ -288,7 +289,7 @@ struct DecodeArgs {
   size_t workspace_bytes;
   const char* who = "gc_paged_decode_attn";  // for messages
   DecodeParts own = {nullptr, nullptr};      // given: the results go there instead of to out
-  DecodePrefix prefix = {nullptr, nullptr, nullptr, 0, 0};
+  DecodePrefix prefix = {nullptr, nullptr, nullptr, nullptr, 0, 0};
 };
 struct DecodeSplit {
   int32_t splits, split_tiles;  // key ranges per request (at most), their 128-key tiles

@@ -225,7 +225,8 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
   if (st != GC_OK) return st;
   if (row_by_row(pool, a.rows, static_cast<int64_t>(a.max_blocks) * cfg.page_size, false))
     return launch_rows(pool, a, who, nullptr, nullptr, 1,
-                       DecodePrefix{a.block_table, a.lens, a.start, a.batch, a.max_blocks}, stream);
+                       DecodePrefix{a.block_table, a.lens, a.start, a.new_lens, a.batch,
+                                    a.max_blocks}, stream);
   const SpanSpace space = span_space(pool, a.rows, a.batch, a.max_blocks, a.num_q_heads, false);
   const SpanGeom span = span_geom(space, static_cast<int64_t>(a.max_blocks) * cfg.page_size, false,
                                   a.workspace);
@@ -303,7 +304,7 @@ gc_status launch_shared_decode(const gc_kv_pool* pool, const SpanArgs& a, cudaSt
   uint8_t* w = static_cast<uint8_t*>(a.workspace);
   if (shared_rows(pool, a.batch, a.max_shared_blocks, a.max_blocks))
     return launch_rows(pool, a, who, a.block_table, a.lens, a.max_blocks,
-                       DecodePrefix{a.shared_table, a.shared_lens, a.start, a.groups,
+                       DecodePrefix{a.shared_table, a.shared_lens, a.start, nullptr, a.groups,
                                     a.max_shared_blocks}, stream);
   const SpanGeom span = span_geom(
       space.span, static_cast<int64_t>(a.max_shared_blocks) * cfg.page_size, true, w);
