@@ -373,7 +373,8 @@ class SharedContext:
     rotates q and k to their positions behind the prefix and appends k and v to
     the requests' own pages (gc_kv_append_rope), then attends to the shared and
     the own keys (gc_shared_prefix_decode_attn); ``cross`` attends to the
-    states (gc_paged_cross_attn).  ``advance`` ends a token."""
+    states (gc_paged_cross_attn).  ``advance`` ends a token, on the stream of
+    the last step."""
 
     def __init__(self, Hq, Hkv, d, ps, shared_lens, group_sizes, own_tokens, state_lens=None,
                  rot_dim=None, base: float = 500000.0, L: int = 1, seed: int = 0,
@@ -399,6 +400,10 @@ class SharedContext:
         self.shared_table, self.own_table, self.state_table = tables
         self.pool = gcb.KVPool.create(L, Hkv, d, ps, pages, device=device)
         self._shared, self._own, self._states = (_i32(t, device) for t in tables)
+        # (kept: a restore reads them when its stream comes to it)
+        self._ids = {name: _i32(t[t >= 0], device)
+                     for name, t in (("shared", tables[0]), ("states", tables[2]))}
+        self._stream = None  # of the last step
         self._S, self._state_lens = _i32(self.shared_lens, device), _i32(states, device)
         self._cu_requests = _i32(np.concatenate([[0], np.cumsum(sizes)]), device)
         self._cu = _i32(np.arange(self.B + 1), device)
@@ -421,8 +426,7 @@ class SharedContext:
     def restore(self, image, table: str = "shared", stream=None):
         """Cached pages [n][L][2][Hkv][ps][d] (device) of all prefixes ("shared") or
         all states ("states"), list after list, into the pool."""
-        t = self.shared_table if table == "shared" else self.state_table
-        ids = _i32(t[t >= 0], self.device)
+        ids = self._ids[table]
         if ids.numel():
             gcb.gc_kv_restore(self.pool.handle, image, ids, ids.numel(), stream, None,
                               gcb.GC_RESTORE_SRC_DEVICE)
@@ -430,6 +434,7 @@ class SharedContext:
     def step(self, qkv, out, layer: int = 0, stream=None):
         """One layer of the current token: qkv [B][Hq + 2 Hkv][d] -> out [B][Hq][d]."""
         Hq, Hkv, h = self.Hq, self.Hkv, self.pool.handle
+        self._stream = stream
         row = qkv.stride(0)
         gcb.gc_kv_append_rope(h, qkv[:, :Hq], row, self.q, qkv[:, Hq:Hq + Hkv], row,
                               qkv[:, Hq + Hkv:], row, self._own, self.own_lens, stream, layer,
@@ -448,9 +453,16 @@ class SharedContext:
                                 self.workspace.numel())
 
     def advance(self):
-        """The token is done in every layer."""
-        for x in (self.own_lens, self.seq_lens, self.positions):
-            x.add_(1)
+        """The token is done in every layer: behind the last step, on its stream."""
+        import torch
+        s = self._stream
+        if not s:
+            s = torch.cuda.default_stream(self.device)
+        elif isinstance(s, int):
+            s = torch.cuda.ExternalStream(s, self.device)
+        with torch.cuda.stream(s):
+            for x in (self.own_lens, self.seq_lens, self.positions):
+                x.add_(1)
 
     def check(self, stream=None) -> int:
         return self.pool.check(stream)
