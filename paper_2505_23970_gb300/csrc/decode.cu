@@ -116,7 +116,7 @@ DecodeSplit decode_split(const gc_kv_pool* pool, int32_t batch, int32_t max_bloc
 
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
                               int32_t num_q_heads) {
-  if (decode_shares(pool, num_q_heads)) return decode_share_workspace_bytes(pool);
+  if (decode_shares(pool, num_q_heads)) return decode_share_workspace_bytes(pool, num_q_heads);
   return decode_split(pool, batch, max_blocks, num_q_heads).workspace_bytes;
 }
 
@@ -143,7 +143,7 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
   DecodeSplit sp = {};
   size_t need;
   if (shares) {
-    need = decode_share_workspace_bytes(pool);
+    need = decode_share_workspace_bytes(pool, a.num_q_heads);
   } else {
     sp = decode_split(pool, a.batch, a.max_blocks, a.num_q_heads);
     need = sp.workspace_bytes;

@@ -109,11 +109,10 @@ gc_status launch_heads(const gc_kv_pool* pool, const DecodeArgs& a, DecGeom geo,
 
 }  // namespace
 
-// head_dim 128: two partials of 16 heads per SM (two CTAs of 8 heads, or one of
-// 16), at most one CTA per merge counter of the pool's control block.
-size_t decode_share_workspace_bytes(const gc_kv_pool* pool) {
-  const size_t sms = static_cast<size_t>(min(pool->num_sms, kMergeCounters));
-  return sms * 2 * 16 * 128 * sizeof(float) + sms * 2 * 16 * sizeof(float2);
+// (At most one CTA per merge counter of the pool's control block.)
+size_t decode_share_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads) {
+  return decode_share_bytes(pool->cfg.head_dim, num_q_heads / pool->cfg.num_kv_heads,
+                            pool->num_sms, kMergeCounters);
 }
 
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,

@@ -90,7 +90,7 @@ constexpr float kRescaleLog2 = 56.0f;
 template <int D, int NT>
 struct Shape {
   static constexpr int kWarps = D * NT == 128 ? 6 : 8;
-  static constexpr int kCtas = D * NT <= 128 ? 2 : 1;
+  static constexpr int kCtas = decode_ctas(D, 8 * NT);
   static constexpr int kGroups = 1;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kHeads = 8 * NT;
@@ -108,6 +108,7 @@ struct Shape {
 template <int D, int NT>
 struct SharedShape {
   static constexpr int kGroups = 2;
+  static_assert(kGroups <= decode_ctas(D, 8 * NT), "the workspace has no room for their partials");
   static constexpr int kWarps = 6;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kHeads = 8 * NT;

@@ -1,5 +1,7 @@
-// How decode at head_dim 128 numbers its work with 32-bit ints (host arithmetic).
+// How decode in shares numbers its work with 32-bit ints, and the room that it needs
+// (host arithmetic).
 #pragma once
+#include <cstddef>
 #include <cstdint>
 #include <initializer_list>
 
@@ -27,6 +29,17 @@ inline DecodeUnits decode_units(int64_t pairs, int64_t cap, int64_t margin) {
     if (((cap - 1) >> shift) + 1 + lead <= per_pair) return {shift, lead};
   }
   return {7, 0};
+}
+
+// CTAs on an SM, or groups of a CTA, that decode with `heads` (8 or 16) q heads in registers:
+// two where their accumulators leave room for both.
+constexpr int decode_ctas(int head_dim, int heads) { return head_dim * heads <= 1024 ? 2 : 1; }
+
+// Bytes of the partials of a call's shares: each CTA (or group) has two, of the heads' O and
+// their maxima and sums, in binary32.  `per_kv_head` q heads, at most `most` CTAs.
+inline size_t decode_share_bytes(int head_dim, int per_kv_head, int num_sms, int most) {
+  const int heads = per_kv_head <= 8 ? 8 : 16, all = decode_ctas(head_dim, heads) * num_sms;
+  return static_cast<size_t>(all < most ? all : most) * 2 * heads * (head_dim + 2) * sizeof(float);
 }
 
 }  // namespace gc

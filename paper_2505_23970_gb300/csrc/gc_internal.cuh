@@ -307,7 +307,7 @@ gc_status launch_decode(const gc_kv_pool* pool, const DecodeArgs& a, cudaStream_
 // the 8-bit image instead of the pool.
 gc_status launch_decode_mma(const gc_kv_pool* pool, const DecodeArgs& a, const DecodeSplit* split,
                             cudaStream_t stream, const Q8Pages* q8);
-size_t decode_share_workspace_bytes(const gc_kv_pool* pool);
+size_t decode_share_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads);
 // Limits of a decode call's sizes, GC_OK if they are kept.
 gc_status check_decode(const gc_kv_pool* pool, const DecodeArgs& a);
 // Workspace bytes of a decode call on either path.

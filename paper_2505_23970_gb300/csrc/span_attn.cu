@@ -201,7 +201,7 @@ size_t cross_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_
                              int32_t num_q_heads, int32_t total_new_tokens) {
   if (row_by_row(pool, total_new_tokens, static_cast<int64_t>(max_blocks) * pool->cfg.page_size,
                  false))
-    return decode_share_workspace_bytes(pool);
+    return decode_share_workspace_bytes(pool, num_q_heads);
   return span_space(pool, total_new_tokens, batch, max_blocks, num_q_heads, false).end;
 }
 
@@ -244,7 +244,7 @@ gc_status launch_cross(const gc_kv_pool* pool, const SpanArgs& a, cudaStream_t s
 
 // One kernel for both sides of a call, unless the own keys' side needs more registers
 // than the span kernel's threads have (16 heads of 128), or the units could not be
-// numbered.  Otherwise a kernel each.
+// numbered, or two groups an SM not counted.  Otherwise a kernel each.
 static bool decodes_in_kernel(const gc_kv_pool* pool, const SpanArgs& a) {
   const auto& cfg = pool->cfg;
   const int64_t G = a.num_q_heads / cfg.num_kv_heads;
@@ -253,7 +253,7 @@ static bool decodes_in_kernel(const gc_kv_pool* pool, const SpanArgs& a) {
   const int64_t own = static_cast<int64_t>(a.batch) * cfg.num_kv_heads *
                       (static_cast<int64_t>(a.max_blocks) * cfg.page_size / 128 + 1);
   return own + 2 * kMergeCounters < 2147483647LL && (cfg.head_dim == 64 || G <= 8) &&
-         a.groups <= kSpanRequests &&
+         a.groups <= kSpanRequests && 2 * pool->num_sms <= kMergeCounters &&
          items * (steps + kSpanLead) < (1ll << 30) - pool->num_sms;
 }
 
@@ -274,7 +274,7 @@ static SharedSpace shared_space(const gc_kv_pool* pool, int32_t batch, int32_t g
                                 int32_t num_q_heads) {
   SharedSpace s{};
   if (shared_rows(pool, batch, max_shared_blocks, max_blocks)) {
-    s.end = decode_share_workspace_bytes(pool);
+    s.end = decode_share_workspace_bytes(pool, num_q_heads);
     return s;
   }
   s.span = span_space(pool, batch, groups, max_shared_blocks, num_q_heads, true);
@@ -282,7 +282,7 @@ static SharedSpace shared_space(const gc_kv_pool* pool, int32_t batch, int32_t g
   s.ml = s.span.end;
   s.o = s.ml + (rows * sizeof(float2) + 255) / 256 * 256;
   s.decode = s.o + rows * pool->cfg.head_dim * sizeof(float);  // (rows of 256 bytes or more)
-  const size_t shares = decode_share_workspace_bytes(pool);  // (in the span kernel)
+  const size_t shares = decode_share_workspace_bytes(pool, num_q_heads);  // (in the span kernel)
   const size_t alone = decode_workspace_bytes(pool, batch, max_blocks, num_q_heads);
   s.end = s.decode + (shares > alone ? shares : alone);
   return s;
