@@ -632,7 +632,8 @@ GC_API gc_status gc_paged_cross_attn(const void* q, const gc_kv_pool* pool,
  * the page size), to the attention tolerance.  The new token's K/V must
  * already be in the request's own pages (gc_kv_append, or gc_kv_append_rope
  * with its position given, with seq_lens[b] - 1 as the offset).
- *   q, out        [batch][Hq][d] bf16, device.
+ *   q, out        [batch][Hq][d] bf16, device; fp32 accumulation, P rounded
+ *                 to bf16 before the PV product, out rounded to nearest even.
  *   shared_table  int32 [num_groups][max_shared_blocks], device.
  *   shared_lens   int32 [num_groups], device: 0 (no prefix) or more; the last
  *                 shared page may be partly filled.

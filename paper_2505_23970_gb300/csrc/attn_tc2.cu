@@ -51,9 +51,9 @@
 //    their maximum and sum.  Behind shared prefixes some of the CTAs decode the requests'
 //    own keys instead (kOwn; decode_mma.cuh).  A step is as long as in a prefill (0.79 us
 //    with all pairs busy); start to first product 8 us, last product to end 3.5.
-//    8 x 1024 tokens of 64/8 heads over 8192 states 1.45 ms (1520 TFLOP/s), 16 requests of
-//    uneven lengths, 120 GFLOP, 110 us (tensor pipe 51 % active), 64 requests behind 9
-//    shared prefixes (256 MB of keys) 63 us with the join 68.
+//    8 x 1024 tokens of 64/8 heads over 8192 states 1.45 to 1.54 ms (1430 to 1520 TFLOP/s);
+//    with the join, 16 requests of uneven lengths, 120 GFLOP, 118 us (tensor pipe 51 %
+//    active), 64 requests behind 9 shared prefixes (256 MB of keys) 66 us.
 //  * Bound by the chain S -> softmax -> PV over the three S buffers (about 1570
 //    cycles a step, of which the tensor pipe needs 1024) and, in launches of a
 //    millisecond and more, by the GPU's power limit.

@@ -9,6 +9,10 @@
 // decoded by some of the same kernel's CTAs (or by the decode kernel before it), and small
 // calls by the decode kernel alone, row by row (row_by_row).
 //
+// P is rounded to bf16 for its product, on the tiles and row by row (the tensor cores take it
+// with V as it is kept); scores, maxima, sums, O and the pieces are binary32.  Against 64 bits
+// the relative error is 0.0020 to 0.0024; the output's rounding alone is 0.0017.
+//
 // Here: which way a call goes, its workspace, and the joins of pieces.  A join is bound by
 // latency: its blocks read the plan, the row's place and then eight pieces at a time
 // (pieces one after the other 10 to 37 us, eight together 4 to 8, at 512 to 4096 rows).
