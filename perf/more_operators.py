@@ -29,7 +29,7 @@ prefill: ``prefix`` cached and ``new`` new tokens.
 
 A 4-bit value is c s: per token, head and 32 columns one bf16 scale
 s = amax / 7 and codes c = -7..7 (x times the binary32 reciprocal of s, rounded
-to the nearest whole number, ties to even).
+once to the nearest whole number, ties to even).
 """
 import math
 
@@ -285,7 +285,8 @@ def _quantise(x):
     s = (x.abs().amax(-1, keepdim=True) / 7.0).clamp_(max=2.0 ** 15).to(_BF16).float()
     s = torch.where(s < 2.0 ** -24, 0.0, s)
     inv = torch.where(s > 0, 1.0 / s, 0.0)
-    return (x * inv).round_().clamp_(-7, 7), s
+    # (in 64 bits: many values lie on a border between two codes, or next to one)
+    return (x.double() * inv).round_().clamp_(-7, 7).float(), s
 
 
 def _pack(x, is_k):
@@ -450,7 +451,7 @@ def _nearest4(x):
     s[s < 2.0 ** -24] = 0
     inv = torch.zeros_like(s)
     inv[s > 0] = (1 / s[s > 0]).float().double()
-    c = torch.clamp(torch.round((g * inv[:, None]).float().double()), -7, 7)
+    c = torch.clamp(torch.round(g * inv[:, None]), -7, 7)
     return (c * s[:, None]).reshape(shape)
 
 
