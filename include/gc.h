@@ -30,6 +30,11 @@
  *                           (an encoder's), all of them seen by every row
  *   gc_shared_prefix_decode_attn  decode of requests that share a cached
  *                           prefix, which is read once for all of them
+ *   gc_kv_append_rope_q4,   a cache kept in 4 bits: tokens quantised as they
+ *   gc_kv_pack_q4,          are written, whole pages quantised, and read
+ *   gc_kv_unpack_q4         back
+ *   gc_paged_decode_attn_q4,  attention that reads the 4-bit pages as they
+ *   gc_prefix_prefill_attn_q4 are
  *
  * Conventions for every call
  *  - All device work is ordered on the caller's stream; no call synchronises
@@ -665,6 +670,149 @@ GC_API gc_status gc_shared_prefix_decode_attn(
     int32_t max_shared_blocks, const int32_t* block_table, const int32_t* seq_lens, void* out,
     cudaStream_t stream, int32_t layer, int32_t batch, int32_t max_blocks_per_seq,
     int32_t num_q_heads, float softmax_scale, void* workspace, size_t workspace_bytes);
+
+/* ---- A cache kept in 4 bits.  The 70B runs of Sec. 6.1 keep what they can in
+ * few bits, and what a cache holds and a decode step reads is what the paper's
+ * tradeoff is about (Sec. 3.2, Sec. 2.1).  Unlike the 8-bit tier's image, which
+ * holds whole saved pages, this cache is written token by token and attended to
+ * as it is.  It has the pool's layers, heads and page size, pages of its own,
+ * and is device memory of the caller's:
+ *     q4_cache  [L][2][n_q4_pages][Hkv][ps*(d/2 + d/16) bytes], 16-byte aligned,
+ *               gc_kv_q4_bytes(cfg, n_q4_pages) bytes, plane 0 = K, 1 = V.
+ * Groups of 32 columns of a token's head x share a bf16 scale s:
+ *     s = bf16_round_half_even(min(amax / 7, 2^15)), 0 if that is below 2^-24
+ *         (amax = max |x| over the group's finite values)
+ *     c = clamp(round_half_even(x * (1 / s)), -7, 7)
+ *         (c = 0 for NaN x; every c = 0 when s = 0)
+ * quotients rounded once in binary32, the product only to the whole number.  The
+ * value that is held is c * s.  A head's rows of a page are its codes [ps][d/2] bytes, then
+ * its scales [ps][d/32] bf16; c + 8 is a nibble (the lower one of a byte first):
+ *     K row: 32-bit word q*(d/32) + g has columns 32g + 8q + j (q < 4, j < 8),
+ *            column j in nibble {0, 4, 2, 6, 1, 5, 3, 7}[j]
+ *     V row: 16-bit word r*(d/32) + g has columns 32g + 4r + j (r < 8, j < 4),
+ *            column j in nibble j
+ * 4.5 bits a value: 0.28 of the bytes of the pool's pages.
+ * In every call q4_table is int32 [batch][max_blocks_per_seq], device: the
+ * 4-bit page of each block of a request's sequence, in [0, n_q4_pages). */
+GC_API size_t gc_kv_q4_bytes(const gc_pool_config* cfg, int32_t n_q4_pages); /* 0 if invalid */
+
+/* gc_kv_append_rope with the new tokens' K and V quantised as they are written
+ * to 4-bit pages: k' (rounded to bf16, as the 16-bit page would have it) and v
+ * go to slot seq_lens[b] + t of request b's pages in q4_table, q' to q_out.
+ * Arguments as gc_kv_append_rope, with q4_cache, n_q4_pages and q4_table in the
+ * place of block_table, and rot_dim 0 valid: then nothing is rotated, q is
+ * copied, and cos_sin, n_positions and positions are not looked at.  The
+ * rotation is x' = fma(x, cos, -(y sin)), y' = fma(y, cos, x sin) in binary32
+ * (the product in brackets rounded, then the rest once).
+ * A token's place in a page is written whole (codes and scales of its heads);
+ * no other byte of the cache changes.  What is skipped and recorded is as for
+ * gc_kv_append_rope, q4_table and n_q4_pages in the place of the pool's pages:
+ * a token whose entry is not a 4-bit page (-1 included) has its q written and
+ * its K and V skipped.  Two tokens may not have the same slot.
+ * Errors: as gc_kv_append_rope; GC_ERR_INVALID_ARG also for n_q4_pages < 0 and
+ * a misaligned or (with tokens to write) NULL q4_cache. */
+GC_API gc_status gc_kv_append_rope_q4(gc_kv_pool* pool, const void* q, int64_t q_stride,
+                                      void* q_out, const void* k_new, int64_t k_stride,
+                                      const void* v_new, int64_t v_stride, void* q4_cache,
+                                      int32_t n_q4_pages, const int32_t* q4_table,
+                                      const int32_t* seq_lens, cudaStream_t stream, int32_t layer,
+                                      const int32_t* cu_new_lens, int32_t batch,
+                                      int32_t max_blocks_per_seq, int32_t total_new_tokens,
+                                      int32_t num_q_heads, const float* cos_sin,
+                                      int32_t n_positions, int32_t rot_dim,
+                                      const int32_t* positions, uint32_t flags);
+
+/* Quantise whole pages: pool pages pool_ids[i] into 4-bit pages q4_ids[i], layers
+ * [layer_begin, layer_begin + layer_count) of them, i < n_blocks (a page that is
+ * finished leaves the 16-bit pool).  Every row of the page is quantised by
+ * itself, rows that hold no token included, so that a partly filled page may be
+ * packed and appended to later.
+ *   pool_ids, q4_ids  int32 [n_blocks], device.  A pair with an id outside the
+ *                pool or the cache is skipped and recorded as
+ *                GC_ERR_OUT_OF_RANGE.  The same q4 id twice gives an
+ *                unspecified choice, row by row, between the two.
+ * Errors: GC_ERR_INVALID_ARG (null, negative, misaligned), GC_ERR_OUT_OF_RANGE
+ * (layer range), GC_ERR_CUDA. */
+GC_API gc_status gc_kv_pack_q4(gc_kv_pool* pool, const int32_t* pool_ids, void* q4_cache,
+                               int32_t n_q4_pages, const int32_t* q4_ids, int32_t n_blocks,
+                               int32_t layer_begin, int32_t layer_count, cudaStream_t stream);
+
+/* Read whole pages back: pool pages pool_ids[i] <- bf16_round_half_even(c * s) of
+ * 4-bit pages q4_ids[i], the same layers, ids and errors as gc_kv_pack_q4 (the
+ * same pool id twice gives an unspecified choice, row by row). */
+GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t n_q4_pages,
+                                 const int32_t* q4_ids, const int32_t* pool_ids, int32_t n_blocks,
+                                 int32_t layer_begin, int32_t layer_count, cudaStream_t stream);
+
+/* gc_paged_decode_attn over 4-bit pages, for one new token of every request or
+ * for a few that are drafted and looked at together (at least one more is then
+ * known per step): row i < tokens of request b is at position
+ * seq_lens[b] - tokens + i and sees the keys up to itself,
+ *     out[b][i][h] = sum_{j <= seq_lens[b]-tokens+i} softmax_j(softmax_scale *
+ *                        q[b][i][h] . k_j) v_j,   g = h / (Hq/Hkv)
+ * with k_j, v_j the values c * s of the request's 4-bit pages (not rounded to
+ * bf16 in between) or of its 16-bit pages:
+ *   block_table  int32 [batch][max_blocks_per_seq], device.
+ *   q4_table     an entry >= 0 is a 4-bit page; where it is -1 the block is pool
+ *                page block_table[b][j] (a request's newest page, say, before
+ *                it is packed).  An entry >= n_q4_pages, or a pool page outside
+ *                the pool, is skipped (its keys left out) and recorded.
+ *   tokens       1 to 16 / (Hq/Hkv).
+ *   q, out       [batch][tokens][Hq][d] bf16, device; fp32 accumulation, P and
+ *                P * s rounded to bf16 before the PV product (a term is off by
+ *                2^-8 of itself at most), out rounded to nearest even.
+ *   seq_lens     int32 [batch], device: context lengths, the tokens included; a
+ *                request whose length is outside [tokens, max_blocks_per_seq*ps]
+ *                is skipped (its rows are not written) and recorded as
+ *                GC_ERR_OUT_OF_RANGE.  Keys at or past it are never used.
+ *   workspace    device scratch of gc_paged_decode_q4_workspace_bytes bytes for
+ *                the same arguments, with the rules of gc_paged_decode_attn's.
+ * K, V and q may have any finite values of bf16 up to 2^60 in magnitude; the
+ * cache's own values are far below that.  Calls on one pool must not overlap on
+ * the GPU with each other or with the other attention calls.  The same call gives
+ * the same bits again; the order of its sums depends on the lengths in the call.
+ * Errors: as gc_paged_decode_attn; GC_ERR_INVALID_ARG also for n_q4_pages < 0,
+ * tokens < 1, a NULL q4_table (or q4_cache with n_q4_pages > 0), a misaligned
+ * q4_cache; GC_ERR_UNSUPPORTED for tokens * Hq/Hkv > 16. */
+GC_API size_t gc_paged_decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                                 int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                                 int32_t tokens);
+GC_API gc_status gc_paged_decode_attn_q4(const void* q, const gc_kv_pool* pool,
+                                         const int32_t* block_table, const int32_t* seq_lens,
+                                         void* out, cudaStream_t stream, int32_t layer,
+                                         int32_t batch, int32_t max_blocks_per_seq,
+                                         int32_t num_q_heads, float softmax_scale, void* workspace,
+                                         size_t workspace_bytes, const void* q4_cache,
+                                         const int32_t* q4_table, int32_t n_q4_pages,
+                                         int32_t tokens);
+
+/* gc_prefix_prefill_attn over 4-bit pages: exactly that of gc_kv_unpack_q4 of the
+ * 4-bit pages followed by gc_prefix_prefill_attn, but the pool is not written.
+ * The pages that the call reads, one layer of them, are read back once into the
+ * workspace, which the attention kernels then read.
+ * Arguments as gc_prefix_prefill_attn; q4_cache, q4_table and n_q4_pages as
+ * gc_paged_decode_attn_q4 (-1: pool page block_table[b][j]; an entry >= n_q4_pages
+ * is recorded as GC_ERR_OUT_OF_RANGE and leaves that request's output
+ * unspecified), plus
+ *   workspace    device scratch of gc_prefix_prefill_q4_workspace_bytes bytes for
+ *                the same arguments (two bf16 planes of min(n_q4_pages,
+ *                batch * max_blocks_per_seq) pages), 16-byte aligned, owned by
+ *                the caller, not used after the stream passes the call; no
+ *                initial contents needed.  Calls sharing a workspace must not
+ *                overlap on the GPU.
+ * Errors: as gc_prefix_prefill_attn; GC_ERR_INVALID_ARG also for n_q4_pages < 0, a
+ * NULL q4_table (or q4_cache with n_q4_pages > 0), a misaligned q4_cache or
+ * workspace, a workspace too small; GC_ERR_UNSUPPORTED for a workspace of 2^31 or
+ * more rows of d values, or batch * max_blocks_per_seq >= 2^31. */
+GC_API size_t gc_prefix_prefill_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                                   int32_t max_blocks_per_seq,
+                                                   int32_t n_q4_pages);
+GC_API gc_status gc_prefix_prefill_attn_q4(
+    const void* q, const gc_kv_pool* pool, const int32_t* block_table, const int32_t* prefix_lens,
+    const int32_t* new_lens, void* out, cudaStream_t stream, int32_t layer,
+    const int32_t* cu_new_lens, int32_t batch, int32_t max_blocks_per_seq, int32_t num_q_heads,
+    float softmax_scale, int32_t total_new_tokens, const void* q4_cache, const int32_t* q4_table,
+    int32_t n_q4_pages, void* workspace, size_t workspace_bytes);
 
 /* Test hook, not part of the method (the paper has no counterpart): launches
  * one thread that waits on a device barrier nobody arrives at, with the same

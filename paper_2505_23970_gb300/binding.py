@@ -46,6 +46,9 @@ EXPORTED = (
     "gc_paged_decode_workspace_bytes", "gc_paged_decode_attn", "gc_selftest_wait_timeout",
     "gc_paged_cross_workspace_bytes", "gc_paged_cross_attn",
     "gc_shared_prefix_decode_workspace_bytes", "gc_shared_prefix_decode_attn",
+    "gc_kv_q4_bytes", "gc_kv_append_rope_q4", "gc_kv_pack_q4", "gc_kv_unpack_q4",
+    "gc_paged_decode_q4_workspace_bytes", "gc_paged_decode_attn_q4",
+    "gc_prefix_prefill_q4_workspace_bytes", "gc_prefix_prefill_attn_q4",
     "gc_last_error",
     "gc_status_string",
 )
@@ -120,7 +123,22 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.gc_shared_prefix_decode_workspace_bytes.restype = sz
         lib.gc_shared_prefix_decode_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp,
                                                      i32, i32, i32, i32, ctypes.c_float, vp, sz]
-        for f in ("gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
+        lib.gc_kv_q4_bytes.argtypes = [cfgp, i32]
+        lib.gc_kv_q4_bytes.restype = sz
+        lib.gc_kv_append_rope_q4.argtypes = [vp, vp, i64, vp, vp, i64, vp, i64, vp, i32, vp, vp,
+                                             vp, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp,
+                                             u32]
+        lib.gc_kv_pack_q4.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp]
+        lib.gc_kv_unpack_q4.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp]
+        lib.gc_paged_decode_q4_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+        lib.gc_paged_decode_q4_workspace_bytes.restype = sz
+        lib.gc_paged_decode_attn_q4.argtypes = lib.gc_paged_decode_attn.argtypes + [vp, vp, i32,
+                                                                                  i32]
+        lib.gc_prefix_prefill_q4_workspace_bytes.argtypes = [vp, i32, i32, i32]
+        lib.gc_prefix_prefill_q4_workspace_bytes.restype = sz
+        lib.gc_prefix_prefill_attn_q4.argtypes = attn + [vp, vp, i32, vp, sz]
+        for f in ("gc_kv_append_rope_q4", "gc_kv_pack_q4", "gc_kv_unpack_q4",
+                  "gc_paged_decode_attn_q4", "gc_prefix_prefill_attn_q4", "gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
                   "gc_kv_pool_check", "gc_kv_restore", "gc_kv_save", "gc_kv_restore_layers",
                   "gc_kv_save_layers", "gc_kv_stage_layers", "gc_kv_save_q8", "gc_kv_restore_q8",
                   "gc_kv_append", "gc_kv_append_rope",
@@ -445,6 +463,84 @@ def gc_shared_prefix_decode_attn(q, pool, shared_table, shared_lens, cu_requests
         max_shared_blocks, _addr(block_table), _addr(seq_lens), _addr(out), _stream(stream), layer,
         batch, max_blocks_per_seq, num_q_heads, softmax_scale, _addr(workspace), workspace_bytes),
         "gc_shared_prefix_decode_attn")
+
+
+def gc_kv_q4_bytes(cfg: gc_pool_config, n_q4_pages: int) -> int:
+    """Bytes of a 4-bit cache of n_q4_pages pages with the pool's geometry."""
+    return int(load().gc_kv_q4_bytes(ctypes.byref(cfg), n_q4_pages))
+
+
+def gc_kv_append_rope_q4(pool, q, q_stride: int, q_out, k_new, k_stride: int, v_new, v_stride: int,
+                         q4_cache, n_q4_pages: int, q4_table, seq_lens, stream, layer: int,
+                         cu_new_lens, batch: int, max_blocks_per_seq: int, total_new_tokens: int,
+                         num_q_heads: int, cos_sin=None, n_positions: int = 0, rot_dim: int = 0,
+                         positions=None, flags: int = 0) -> None:
+    """gc_kv_append_rope with k and v quantised as they are written to 4-bit
+    pages; rot_dim 0: nothing is rotated."""
+    _check(load().gc_kv_append_rope_q4(pool, _addr(q), q_stride, _addr(q_out), _addr(k_new),
+                                       k_stride, _addr(v_new), v_stride, _addr(q4_cache),
+                                       n_q4_pages, _addr(q4_table), _addr(seq_lens),
+                                       _stream(stream), layer, _addr(cu_new_lens), batch,
+                                       max_blocks_per_seq, total_new_tokens, num_q_heads,
+                                       _addr(cos_sin), n_positions, rot_dim, _addr(positions),
+                                       flags), "gc_kv_append_rope_q4")
+
+
+def gc_kv_pack_q4(pool, pool_ids, q4_cache, n_q4_pages: int, q4_ids, n_blocks: int,
+                  layer_begin: int, layer_count: int, stream=None) -> None:
+    """Pool pages pool_ids[i] quantised into 4-bit pages q4_ids[i]."""
+    _check(load().gc_kv_pack_q4(pool, _addr(pool_ids), _addr(q4_cache), n_q4_pages, _addr(q4_ids),
+                                n_blocks, layer_begin, layer_count, _stream(stream)),
+           "gc_kv_pack_q4")
+
+
+def gc_kv_unpack_q4(pool, q4_cache, n_q4_pages: int, q4_ids, pool_ids, n_blocks: int,
+                    layer_begin: int, layer_count: int, stream=None) -> None:
+    """4-bit pages q4_ids[i] read back into pool pages pool_ids[i]."""
+    _check(load().gc_kv_unpack_q4(pool, _addr(q4_cache), n_q4_pages, _addr(q4_ids),
+                                  _addr(pool_ids), n_blocks, layer_begin, layer_count,
+                                  _stream(stream)), "gc_kv_unpack_q4")
+
+
+def gc_paged_decode_q4_workspace_bytes(pool, batch: int, max_blocks_per_seq: int,
+                                       num_q_heads: int, tokens: int = 1) -> int:
+    return int(load().gc_paged_decode_q4_workspace_bytes(pool, batch, max_blocks_per_seq,
+                                                         num_q_heads, tokens))
+
+
+def gc_paged_decode_attn_q4(q, pool, block_table, seq_lens, out, stream, layer: int, batch: int,
+                            max_blocks_per_seq: int, num_q_heads: int, softmax_scale: float,
+                            workspace, workspace_bytes: int, q4_cache, q4_table, n_q4_pages: int,
+                            tokens: int = 1) -> None:
+    """gc_paged_decode_attn of `tokens` rows per request, with the pages that
+    q4_table maps (>= 0) read from the 4-bit cache instead of the pool."""
+    _check(load().gc_paged_decode_attn_q4(_addr(q), pool, _addr(block_table), _addr(seq_lens),
+                                          _addr(out), _stream(stream), layer, batch,
+                                          max_blocks_per_seq, num_q_heads, softmax_scale,
+                                          _addr(workspace), workspace_bytes, _addr(q4_cache),
+                                          _addr(q4_table), n_q4_pages, tokens),
+           "gc_paged_decode_attn_q4")
+
+
+def gc_prefix_prefill_q4_workspace_bytes(pool, batch: int, max_blocks_per_seq: int,
+                                         n_q4_pages: int) -> int:
+    return int(load().gc_prefix_prefill_q4_workspace_bytes(pool, batch, max_blocks_per_seq,
+                                                           n_q4_pages))
+
+
+def gc_prefix_prefill_attn_q4(q, pool, block_table, prefix_lens, new_lens, out, stream, layer: int,
+                              cu_new_lens, batch: int, max_blocks_per_seq: int, num_q_heads: int,
+                              softmax_scale: float, total_new_tokens: int, q4_cache, q4_table,
+                              n_q4_pages: int, workspace, workspace_bytes: int) -> None:
+    """gc_prefix_prefill_attn with the pages that q4_table maps (>= 0) read from
+    the 4-bit cache instead of the pool."""
+    _check(load().gc_prefix_prefill_attn_q4(_addr(q), pool, _addr(block_table), _addr(prefix_lens),
+                                            _addr(new_lens), _addr(out), _stream(stream), layer,
+                                            _addr(cu_new_lens), batch, max_blocks_per_seq,
+                                            num_q_heads, softmax_scale, total_new_tokens,
+                                            _addr(q4_cache), _addr(q4_table), n_q4_pages,
+                                            _addr(workspace), workspace_bytes),
+           "gc_prefix_prefill_attn_q4")
 
 
 def gc_selftest_wait_timeout(pool, stream=None) -> None:

@@ -519,6 +519,52 @@ gc_status gc_kv_append(gc_kv_pool* pool, const void* k_new, const void* v_new,
                            max_blocks_per_seq, layer, total_new_tokens, stream);
 }
 
+// The checks that the appends with a rotation share; *noop: there is nothing to do.
+static gc_status append_rope_common(const char* who, const gc_kv_pool* pool, const gc::RopeArgs& a,
+                                    int least_rot, uint32_t flags, bool* noop) {
+  *noop = false;
+  if (!pool) return fail(GC_ERR_INVALID_ARG, "%s: pool is NULL", who);
+  if (a.batch < 0 || a.total_new_tokens < 0 || a.max_blocks < 0 || a.n_positions < 0)
+    return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (flags & ~GC_ROPE_INTERLEAVED)
+    return fail(GC_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
+  if (a.layer < 0 || a.layer >= pool->cfg.num_layers)
+    return fail(GC_ERR_OUT_OF_RANGE, "%s: layer %d outside [0, %d)", who, a.layer,
+                pool->cfg.num_layers);
+  const int hkv = pool->cfg.num_kv_heads, d = pool->cfg.head_dim, heads = a.num_q_heads;
+  if (heads < 0 || heads % hkv)
+    return fail(GC_ERR_INVALID_ARG, "%s: num_q_heads %d not a multiple of num_kv_heads %d", who,
+                heads, hkv);
+  if (a.rot_dim < least_rot || a.rot_dim > d || a.rot_dim % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: rot_dim %d not a multiple of 16 in [%d, %d]", who,
+                a.rot_dim, least_rot, d);
+  // units of 16 elements of a token are numbered with 32-bit ints
+  if ((static_cast<int64_t>(heads) + 2 * static_cast<int64_t>(hkv)) * d >= (1ll << 30))
+    return fail(GC_ERR_UNSUPPORTED, "%s: %d q heads and %d kv heads", who, heads, hkv);
+  const int64_t kv_row = static_cast<int64_t>(hkv) * d, q_row = static_cast<int64_t>(heads) * d;
+  if (a.k_stride < kv_row || a.v_stride < kv_row || a.q_stride < q_row)
+    return fail(GC_ERR_INVALID_ARG, "%s: a token stride is shorter than the token's heads", who);
+  if ((a.k_stride | a.v_stride | (heads ? a.q_stride : 0)) % 8)
+    return fail(GC_ERR_INVALID_ARG, "%s: token strides must be multiples of 8 elements", who);
+  if (a.batch == 0 || a.total_new_tokens == 0) {
+    *noop = true;
+    return GC_OK;
+  }
+  if (!a.k_new || !a.v_new || !a.block_table || !a.prefix_lens || !a.cu_new_lens ||
+      (a.rot_dim && !a.cos_sin) || (heads && (!a.q || !a.q_out)))
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
+  if (a.max_blocks == 0) return fail(GC_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
+  if ((reinterpret_cast<uintptr_t>(a.k_new) | reinterpret_cast<uintptr_t>(a.v_new) |
+       (a.rot_dim ? reinterpret_cast<uintptr_t>(a.cos_sin) : 0) |
+       (heads ? reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.q_out) : 0)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q / q_out / k_new / v_new / cos_sin not 16-byte aligned",
+                who);
+  // in place only row by row: each thread has read what it writes, and nobody else reads it
+  if (heads && a.q == a.q_out && a.q_stride != q_row)
+    return fail(GC_ERR_INVALID_ARG, "%s: q_out may be q only if q's tokens are dense", who);
+  return GC_OK;
+}
+
 gc_status gc_kv_append_rope(gc_kv_pool* pool, const void* q, int64_t q_stride, void* q_out,
                             const void* k_new, int64_t k_stride, const void* v_new,
                             int64_t v_stride, const int32_t* block_table, const int32_t* seq_lens,
@@ -529,49 +575,83 @@ gc_status gc_kv_append_rope(gc_kv_pool* pool, const void* q, int64_t q_stride, v
   Range range_("gc_kv_append_rope");
   g_msg[0] = 0;
   const char* who = "gc_kv_append_rope";
+  const gc::RopeArgs a{q, q_out, k_new, v_new, q_stride, k_stride, v_stride, block_table, seq_lens,
+                       cu_new_lens, cos_sin, positions, batch, max_blocks_per_seq, layer,
+                       total_new_tokens, num_q_heads, n_positions, rot_dim,
+                       (flags & GC_ROPE_INTERLEAVED) != 0};
+  bool noop;
+  const gc_status s = append_rope_common(who, pool, a, 16, flags, &noop);
+  if (s != GC_OK || noop) return s;
+  return gc::launch_append_rope(pool, a, stream);
+}
+
+gc_status gc_kv_append_rope_q4(gc_kv_pool* pool, const void* q, int64_t q_stride, void* q_out,
+                               const void* k_new, int64_t k_stride, const void* v_new,
+                               int64_t v_stride, void* q4_cache, int32_t n_q4_pages,
+                               const int32_t* q4_table, const int32_t* seq_lens,
+                               cudaStream_t stream, int32_t layer, const int32_t* cu_new_lens,
+                               int32_t batch, int32_t max_blocks_per_seq, int32_t total_new_tokens,
+                               int32_t num_q_heads, const float* cos_sin, int32_t n_positions,
+                               int32_t rot_dim, const int32_t* positions, uint32_t flags) {
+  Range range_("gc_kv_append_rope_q4");
+  g_msg[0] = 0;
+  const char* who = "gc_kv_append_rope_q4";
+  // (without a rotation a position is only a number that every slot has)
+  const bool turn = rot_dim != 0;
+  const gc::RopeArgs a{q, q_out, k_new, v_new, q_stride, k_stride, v_stride, q4_table, seq_lens,
+                       cu_new_lens, cos_sin, turn ? positions : nullptr, batch, max_blocks_per_seq,
+                       layer, total_new_tokens, num_q_heads, turn ? n_positions : INT32_MAX,
+                       rot_dim, (flags & GC_ROPE_INTERLEAVED) != 0};
+  bool noop;
+  const gc_status s = append_rope_common(who, pool, a, 0, flags, &noop);
+  if (s != GC_OK) return s;
+  if (n_q4_pages < 0) return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (noop) return GC_OK;
+  if (!q4_cache) return fail(GC_ERR_INVALID_ARG, "%s: q4_cache is NULL", who);
+  if (reinterpret_cast<uintptr_t>(q4_cache) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q4_cache not 16-byte aligned", who);
+  return gc::launch_append_q4(
+      pool, a, gc::Q4Cache{static_cast<const uint8_t*>(q4_cache), n_q4_pages, q4_table}, stream);
+}
+
+size_t gc_kv_q4_bytes(const gc_pool_config* cfg, int32_t n_q4_pages) {
+  if (!pool_config_ok(cfg) || !pool_config_supported(cfg) || n_q4_pages < 0) return 0;
+  return gc::q4_bytes(*cfg, n_q4_pages);
+}
+
+static gc_status pages_q4(const char* who, const gc_kv_pool* pool, const int32_t* pool_ids,
+                          const void* q4_cache, int32_t n_q4_pages, const int32_t* q4_ids,
+                          int32_t n_blocks, int32_t layer_begin, int32_t layer_count, bool pack,
+                          cudaStream_t stream) {
+  g_msg[0] = 0;
   if (!pool) return fail(GC_ERR_INVALID_ARG, "%s: pool is NULL", who);
-  if (batch < 0 || total_new_tokens < 0 || max_blocks_per_seq < 0 || n_positions < 0)
-    return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
-  if (flags & ~GC_ROPE_INTERLEAVED)
-    return fail(GC_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
-  if (layer < 0 || layer >= pool->cfg.num_layers)
-    return fail(GC_ERR_OUT_OF_RANGE, "%s: layer %d outside [0, %d)", who, layer,
-                pool->cfg.num_layers);
-  const int hkv = pool->cfg.num_kv_heads, d = pool->cfg.head_dim;
-  if (num_q_heads < 0 || num_q_heads % hkv)
-    return fail(GC_ERR_INVALID_ARG, "%s: num_q_heads %d not a multiple of num_kv_heads %d", who,
-                num_q_heads, hkv);
-  if (rot_dim < 16 || rot_dim > d || rot_dim % 16)
-    return fail(GC_ERR_INVALID_ARG, "%s: rot_dim %d not a multiple of 16 in [16, %d]", who,
-                rot_dim, d);
-  // units of 16 elements of a token are numbered with 32-bit ints
-  if ((static_cast<int64_t>(num_q_heads) + 2 * static_cast<int64_t>(hkv)) * d >= (1ll << 30))
-    return fail(GC_ERR_UNSUPPORTED, "%s: %d q heads and %d kv heads", who, num_q_heads, hkv);
-  const int64_t kv_row = static_cast<int64_t>(hkv) * d, q_row = static_cast<int64_t>(num_q_heads) * d;
-  if (k_stride < kv_row || v_stride < kv_row || q_stride < q_row)
-    return fail(GC_ERR_INVALID_ARG, "%s: a token stride is shorter than the token's heads", who);
-  if ((k_stride | v_stride | (num_q_heads ? q_stride : 0)) % 8)
-    return fail(GC_ERR_INVALID_ARG, "%s: token strides must be multiples of 8 elements", who);
-  if (batch == 0 || total_new_tokens == 0) return GC_OK;
-  if (!k_new || !v_new || !block_table || !seq_lens || !cu_new_lens || !cos_sin ||
-      (num_q_heads && (!q || !q_out)))
+  if (n_blocks < 0 || n_q4_pages < 0) return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  const gc_status st = check_layers(who, pool, layer_begin, layer_count);
+  if (st != GC_OK) return st;
+  if (n_blocks == 0 || layer_count == 0) return GC_OK;
+  if (!pool_ids || !q4_ids || !q4_cache)
     return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
-  if (max_blocks_per_seq == 0) return fail(GC_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
-  if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new) |
-       reinterpret_cast<uintptr_t>(cos_sin) |
-       (num_q_heads ? reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) : 0)) % 16)
-    return fail(GC_ERR_INVALID_ARG, "%s: q / q_out / k_new / v_new / cos_sin not 16-byte aligned",
-                who);
-  // in place only row by row: each thread has read what it writes, and nobody else reads it
-  if (num_q_heads && q == q_out && q_stride != q_row)
-    return fail(GC_ERR_INVALID_ARG, "%s: q_out may be q only if q's tokens are dense", who);
-  return gc::launch_append_rope(
-      pool,
-      gc::RopeArgs{q, q_out, k_new, v_new, q_stride, k_stride, v_stride, block_table, seq_lens,
-                   cu_new_lens, cos_sin, positions, batch, max_blocks_per_seq, layer,
-                   total_new_tokens, num_q_heads, n_positions, rot_dim,
-                   (flags & GC_ROPE_INTERLEAVED) != 0},
-      stream);
+  if (reinterpret_cast<uintptr_t>(q4_cache) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q4_cache not 16-byte aligned", who);
+  return gc::launch_pages_q4(
+      pool, gc::Q4Cache{static_cast<const uint8_t*>(q4_cache), n_q4_pages, nullptr}, pool_ids,
+      q4_ids, n_blocks, layer_begin, layer_count, pack, stream);
+}
+
+gc_status gc_kv_pack_q4(gc_kv_pool* pool, const int32_t* pool_ids, void* q4_cache,
+                        int32_t n_q4_pages, const int32_t* q4_ids, int32_t n_blocks,
+                        int32_t layer_begin, int32_t layer_count, cudaStream_t stream) {
+  Range range_("gc_kv_pack_q4");
+  return pages_q4("gc_kv_pack_q4", pool, pool_ids, q4_cache, n_q4_pages, q4_ids, n_blocks,
+                  layer_begin, layer_count, true, stream);
+}
+
+gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t n_q4_pages,
+                          const int32_t* q4_ids, const int32_t* pool_ids, int32_t n_blocks,
+                          int32_t layer_begin, int32_t layer_count, cudaStream_t stream) {
+  Range range_("gc_kv_unpack_q4");
+  return pages_q4("gc_kv_unpack_q4", pool, pool_ids, q4_cache, n_q4_pages, q4_ids, n_blocks,
+                  layer_begin, layer_count, false, stream);
 }
 
 static gc_status attn_common(const char* who, const void* q, const gc_kv_pool* pool,
@@ -676,6 +756,51 @@ gc_status gc_prefix_prefill_attn_q8(const void* q, const gc_kv_pool* pool,
   return gc::launch_attn_tc_q8(pool, a, q8, stream);
 }
 
+size_t gc_prefix_prefill_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                            int32_t max_blocks_per_seq, int32_t n_q4_pages) {
+  if (!pool || batch <= 0 || max_blocks_per_seq <= 0 || n_q4_pages <= 0) return 0;
+  return static_cast<size_t>(gc::q4_scratch_pages(batch, max_blocks_per_seq, n_q4_pages)) * 2 *
+         gc::page_bytes(pool->cfg);
+}
+
+gc_status gc_prefix_prefill_attn_q4(const void* q, const gc_kv_pool* pool,
+                                    const int32_t* block_table, const int32_t* prefix_lens,
+                                    const int32_t* new_lens, void* out, cudaStream_t stream,
+                                    int32_t layer, const int32_t* cu_new_lens, int32_t batch,
+                                    int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                    float softmax_scale, int32_t total_new_tokens,
+                                    const void* q4_cache, const int32_t* q4_table,
+                                    int32_t n_q4_pages, void* workspace, size_t workspace_bytes) {
+  Range range_("gc_prefix_prefill_attn_q4");
+  g_msg[0] = 0;
+  const char* who = "gc_prefix_prefill_attn_q4";
+  gc::AttnArgs a;
+  bool noop;
+  const gc_status s = attn_common(who, q, pool, block_table, prefix_lens, new_lens, out, layer,
+                                  cu_new_lens, batch, max_blocks_per_seq, num_q_heads,
+                                  softmax_scale, total_new_tokens, &a, &noop);
+  if (s != GC_OK) return s;
+  if (n_q4_pages < 0) return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (noop) return GC_OK;
+  if (!q4_table || (n_q4_pages > 0 && !q4_cache))
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL q4_cache / q4_table", who);
+  if ((reinterpret_cast<uintptr_t>(q4_cache) | reinterpret_cast<uintptr_t>(workspace)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q4_cache / workspace not 16-byte aligned", who);
+  if (static_cast<int64_t>(batch) * max_blocks_per_seq > 2147483647LL)
+    return fail(GC_ERR_UNSUPPORTED, "%s: block tables of %d x %d pages", who, batch,
+                max_blocks_per_seq);
+  const size_t need =
+      gc_prefix_prefill_q4_workspace_bytes(pool, batch, max_blocks_per_seq, n_q4_pages);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(GC_ERR_INVALID_ARG,
+                "%s: workspace of %zu bytes needed (gc_prefix_prefill_q4_workspace_bytes), got %zu",
+                who, need, workspace_bytes);
+  a.who = who;
+  return gc::launch_prefill_q4(
+      pool, a, gc::Q4Cache{static_cast<const uint8_t*>(q4_cache), n_q4_pages, q4_table}, workspace,
+      stream);
+}
+
 gc_status gc_prefix_prefill_attn_simt(const void* q, const gc_kv_pool* pool,
                                       const int32_t* block_table, const int32_t* prefix_lens,
                                       const int32_t* new_lens, void* out, cudaStream_t stream,
@@ -772,6 +897,60 @@ gc_status gc_paged_decode_attn_q8(const void* q, const gc_kv_pool* pool,
   const gc::Q8Pages q8{static_cast<const uint8_t*>(q8_image), q8_table, n_image_blocks,
                        (flags & GC_RESTORE_LAYER_MAJOR) != 0};
   return gc::launch_decode(pool, a, stream, &q8);
+}
+
+size_t gc_paged_decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
+                                          int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                          int32_t tokens) {
+  if (!pool || batch <= 0 || max_blocks_per_seq <= 0 || num_q_heads <= 0 || tokens <= 0 ||
+      num_q_heads % pool->cfg.num_kv_heads ||
+      static_cast<int64_t>(num_q_heads / pool->cfg.num_kv_heads) * tokens > 16)
+    return 0;
+  return gc::decode_q4_workspace_bytes(pool, num_q_heads, tokens);
+}
+
+gc_status gc_paged_decode_attn_q4(const void* q, const gc_kv_pool* pool,
+                                  const int32_t* block_table, const int32_t* seq_lens, void* out,
+                                  cudaStream_t stream, int32_t layer, int32_t batch,
+                                  int32_t max_blocks_per_seq, int32_t num_q_heads,
+                                  float softmax_scale, void* workspace, size_t workspace_bytes,
+                                  const void* q4_cache, const int32_t* q4_table,
+                                  int32_t n_q4_pages, int32_t tokens) {
+  Range range_("gc_paged_decode_attn_q4");
+  g_msg[0] = 0;
+  const char* who = "gc_paged_decode_attn_q4";
+  if (!pool) return fail(GC_ERR_INVALID_ARG, "%s: pool is NULL", who);
+  if (batch < 0 || max_blocks_per_seq < 0 || n_q4_pages < 0)
+    return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (layer < 0 || layer >= pool->cfg.num_layers)
+    return fail(GC_ERR_OUT_OF_RANGE, "%s: layer %d outside [0, %d)", who, layer,
+                pool->cfg.num_layers);
+  const int hkv = pool->cfg.num_kv_heads;
+  if (num_q_heads <= 0 || num_q_heads % hkv)
+    return fail(GC_ERR_INVALID_ARG, "%s: num_q_heads %d not a multiple of num_kv_heads %d", who,
+                num_q_heads, hkv);
+  const int G = num_q_heads / hkv;
+  if (G != 1 && G != 2 && G != 4 && G != 8 && G != 16)
+    return fail(GC_ERR_UNSUPPORTED, "%s: q heads per kv head %d not in {1,2,4,8,16}", who, G);
+  if (tokens < 1) return fail(GC_ERR_INVALID_ARG, "%s: tokens %d < 1", who, tokens);
+  if (tokens > 16 / G)
+    return fail(GC_ERR_UNSUPPORTED, "%s: %d tokens of %d q heads per kv head (at most 16 rows)", who,
+                tokens, G);
+  if (!(softmax_scale > 0.0f) || softmax_scale == __builtin_inff())
+    return fail(GC_ERR_INVALID_ARG, "%s: softmax_scale must be positive and finite", who);
+  if (batch == 0) return GC_OK;
+  if (!q || !out || !block_table || !seq_lens || !q4_table || (n_q4_pages > 0 && !q4_cache))
+    return fail(GC_ERR_INVALID_ARG, "%s: NULL array argument", who);
+  if (max_blocks_per_seq == 0) return fail(GC_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) |
+       reinterpret_cast<uintptr_t>(workspace) | reinterpret_cast<uintptr_t>(q4_cache)) % 16)
+    return fail(GC_ERR_INVALID_ARG, "%s: q / out / workspace / q4_cache not 16-byte aligned", who);
+  gc::DecodeArgs a{q, out, block_table, seq_lens, batch, max_blocks_per_seq, layer,
+                   num_q_heads, softmax_scale, workspace, workspace_bytes};
+  a.who = who;
+  return gc::launch_decode_q4(
+      pool, a, gc::Q4Cache{static_cast<const uint8_t*>(q4_cache), n_q4_pages, q4_table}, tokens,
+      stream);
 }
 
 static gc_status span_common(const char* who, const gc_kv_pool* pool, int32_t layer, int32_t batch,

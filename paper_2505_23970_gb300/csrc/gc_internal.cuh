@@ -263,6 +263,10 @@ gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStr
 // GC_ERR_UNSUPPORTED before anything is launched when a call could pass it.
 gc_status check_item_bound(const gc_kv_pool* pool, const AttnArgs& a, int grid);
 
+// The same calls with image or 4-bit pages dequantised already (page numbers: see above).
+gc_status launch_attn_tc_unpacked(const gc_kv_pool* pool, const AttnArgs& a,
+                                  const UnpackedPages& unpacked, cudaStream_t stream);
+
 // Paged decode attention (one new token per request), split-KV.
 // Results over a part of each request's keys, per [request][q head]: O unscaled [d],
 // reference maximum in log2 units and sum.  (Not written for a request without keys.)
@@ -313,6 +317,33 @@ gc_status check_decode(const gc_kv_pool* pool, const DecodeArgs& a);
 // Workspace bytes of a decode call on either path.
 size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max_blocks,
                               int32_t num_q_heads);
+
+// A cache in 4 bits with the pool's geometry and pages of its own (q4_format.cuh); table:
+// [batch][max_blocks], its pages of the requests (-1: the pool's).
+struct Q4Cache {
+  const uint8_t* data;
+  int32_t pages;
+  const int32_t* table;
+};
+size_t q4_bytes(const gc_pool_config& c, int32_t pages);
+struct Q4Geom;
+Q4Geom q4_geom(const gc_kv_pool* pool, const Q4Cache& cache);
+// (a.block_table: the 4-bit pages)
+gc_status launch_append_q4(const gc_kv_pool* pool, const RopeArgs& a, const Q4Cache& cache,
+                           cudaStream_t stream);
+// Pages pool_ids[i] of the pool into q4_ids[i] of the cache (pack) or back, i < n.
+gc_status launch_pages_q4(const gc_kv_pool* pool, const Q4Cache& cache, const int32_t* pool_ids,
+                          const int32_t* q4_ids, int32_t n, int32_t layer0, int32_t layers,
+                          bool pack, cudaStream_t stream);
+// Prefill: the pages that the call reads are dequantised into the workspace (of
+// q4_scratch_pages pages of K and of V), which the 16-bit kernels then read.
+int64_t q4_scratch_pages(int32_t batch, int32_t max_blocks, int32_t q4_pages);
+gc_status launch_prefill_q4(const gc_kv_pool* pool, const AttnArgs& a, const Q4Cache& cache,
+                            void* workspace, cudaStream_t stream);
+// Decode of `tokens` rows per request (decode_q4.cu).
+size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads, int32_t tokens);
+gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4Cache& cache,
+                           int32_t tokens, cudaStream_t stream);
 
 // Attention in which every row sees all keys: cross attention (rows are new
 // tokens, `start` the requests' first ones) and decode behind a shared prefix

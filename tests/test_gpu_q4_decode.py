@@ -1,0 +1,221 @@
+"""gc_paged_decode_attn_q4 against attention over the values that the 4-bit pages hold,
+in 64 bits; the bound of a value is derived in _q4.decode_reference."""
+import numpy as np
+import pytest
+
+from paper_2505_23970_gb300 import binding as gcb
+from paper_2505_23970_gb300 import workloads as wl
+from paper_2505_23970_gb300.harness import _i32, bf16_tensor
+
+from . import _q4
+
+pytestmark = pytest.mark.gpu
+
+
+class Decode:
+    def __init__(self, ctx, Hq, tokens=1, q_bits=None, scale=None, seed=0):
+        import torch
+        self.ctx, self.Hq, self.tokens = ctx, Hq, tokens
+        self.B = len(ctx.lens)
+        self.q_bits = wl.normal_bf16(seed, 71, (self.B, tokens, Hq, ctx.d)) if q_bits is None else q_bits
+        self.q = bf16_tensor(self.q_bits)
+        self.scale = ctx.d ** -0.5 if scale is None else scale
+        self.out = torch.full((self.B, tokens, Hq, ctx.d), float("nan"), dtype=torch.bfloat16,
+                              device="cuda")
+        self.need = gcb.gc_paged_decode_q4_workspace_bytes(ctx.pool.handle, self.B, ctx.width, Hq,
+                                                           tokens)
+        self.ws = torch.full((self.need,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def args(self, **change):
+        c = self.ctx
+        a = dict(q=self.q, pool=c.pool.handle, block_table=c.dev16, seq_lens=c.seq_lens,
+                 out=self.out, stream=None, layer=c.layer, batch=self.B,
+                 max_blocks_per_seq=c.width, num_q_heads=self.Hq, softmax_scale=self.scale,
+                 workspace=self.ws, workspace_bytes=self.need, q4_cache=c.cache, q4_table=c.dev4,
+                 n_q4_pages=c.pages4, tokens=self.tokens)
+        return {**a, **change}
+
+    def run(self, **change):
+        gcb.gc_paged_decode_attn_q4(**self.args(**change))
+        return self
+
+    def check(self, skip=()):
+        c = self.ctx
+        got = self.out.double().cpu().numpy()
+        for b in range(self.B):
+            if b in skip:
+                assert np.isnan(got[b]).all(), b
+                continue
+            kv, s = c.keys(b)
+            want, bound = _q4.decode_reference(_q4.f32(self.q_bits[b]).astype(np.float64), kv, s,
+                                               self.scale, self.tokens)
+            assert np.isfinite(got[b]).all(), (b, c.lens[b])
+            over = np.abs(got[b] - want) - bound
+            assert (over <= 0).all(), (b, c.lens[b], int((over > 0).sum()), over.max(),
+                                       np.abs(got[b] - want).max())
+        return self
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,ps,lens", [
+    (4, 1, 64, 16, [321]),
+    (4, 1, 128, 16, [1]),
+    (1, 1, 64, 16, [1, 2, 15, 16, 17, 31, 32, 33, 64, 255, 256, 257]),
+    (8, 8, 128, 16, [1, 2, 15, 16, 17, 31, 32, 33, 64, 255, 256, 257]),
+    (16, 2, 128, 16, [9216, 1, 700]),
+    (64, 8, 128, 16, [3000, 17, 1234, 5]),
+    (16, 1, 128, 64, [2100, 63, 64, 65]),
+    (32, 2, 64, 128, [130, 1000, 4097]),
+    (2, 1, 64, 32, [40, 5000]),
+    (6, 3, 128, 32, [777, 31]),
+    (16, 1, 64, 16, [100] * 40),
+    (64, 8, 128, 16, [12 + 5 * i for i in range(60)]),
+])
+def test_decode(Hq, Hkv, d, ps, lens):
+    ctx = _q4.Context(lens, Hkv, d, ps, seed=len(lens) + d)
+    Decode(ctx, Hq).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+@pytest.mark.parametrize("recent", [1, 3, 1000])
+@pytest.mark.parametrize("Hq,Hkv,d,ps,lens", [
+    (8, 2, 64, 16, [1, 16, 17, 300, 2000]),
+    (16, 2, 128, 16, [1, 16, 33, 300, 2000]),
+    (16, 1, 128, 64, [500, 129, 64]),
+])
+def test_newest_pages_in_16_bits(Hq, Hkv, d, ps, lens, recent):
+    ctx = _q4.Context(lens, Hkv, d, ps, recent=recent, seed=recent)
+    Decode(ctx, Hq).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+@pytest.mark.parametrize("recent", [0, 1])
+@pytest.mark.parametrize("Hq,Hkv,d,ps,tokens,lens", [
+    (4, 1, 64, 16, 4, [4, 5, 16, 17, 18, 19, 20, 600]),
+    (32, 8, 128, 16, 4, [8192, 33, 4, 50]),
+    (32, 8, 128, 32, 2, [64, 2, 3, 700]),
+    (8, 8, 64, 16, 16, [16, 17, 31, 32, 47, 48, 1000]),
+    (8, 8, 128, 16, 7, [7, 8, 16, 20, 22, 23, 500]),
+    (4, 2, 128, 16, 3, [3, 17, 18, 33, 34] * 12),
+])
+def test_drafted_tokens(Hq, Hkv, d, ps, tokens, lens, recent):
+    ctx = _q4.Context(lens, Hkv, d, ps, recent=recent, seed=tokens)
+    Decode(ctx, Hq, tokens).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+def test_a_layer_of_several_and_a_wide_table():
+    ctx = _q4.Context([100, 1500], 2, 64, 16, recent=1, L=3, layer=1, width=4000)
+    Decode(ctx, 8).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+@pytest.mark.parametrize("size,q_size", [(1e-5, 1.0), (3e4, 1e-4), (1.0, 1e-20), (1e-3, 1e3),
+                                         (1.0, 30.0)])
+def test_sizes_of_values(size, q_size):
+    """Small and large keys, values and queries; scores that leave one key."""
+    ctx = _q4.Context([500, 33], 2, 128, 16, size=size, recent=1, seed=8)
+    bits = wl.normal_bf16(8, 71, (2, 1, 8, 128))
+    bits = wl.f32_to_bf16_bits((_q4.f32(bits) * np.float32(q_size)).astype(np.float32))
+    Decode(ctx, 8, q_bits=bits).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+def test_scores_that_keep_rising():
+    """Each group of keys far above the ones before: the reference maximum is raised."""
+    ctx = _q4.Context([640], 1, 128, 16, seed=3)
+    bits = ctx.bits4.copy()
+    for j in range(40):
+        p = ctx.table4[0, j]
+        bits[0, 0, p] = wl.f32_to_bf16_bits(
+            (_q4.f32(bits[0, 0, p]) * np.float32(0.05 + j * 0.3)).astype(np.float32))
+    ctx.bits4 = bits
+    import torch
+    ctx.cache.copy_(torch.from_numpy(_q4.cache_bytes(bits)))
+    Decode(ctx, 8).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+def test_queries_of_zero_and_not_finite():
+    ctx = _q4.Context([300], 1, 64, 16, seed=4)
+    bits = wl.normal_bf16(4, 71, (1, 1, 4, 64))
+    bits[0, 0, 1] = 0
+    bits[0, 0, 2, 5] = 0x7FC0
+    d = Decode(ctx, 4, q_bits=bits).run()
+    got = d.out.double().cpu().numpy()[0, 0]
+    assert np.isnan(got[2]).all()
+    kv, s = ctx.keys(0)
+    keep = [0, 1, 3]
+    want, bound = _q4.decode_reference(_q4.f32(bits[0][:, keep]).astype(np.float64)[:, :], kv, s,
+                                       d.scale, 1)
+    assert (np.abs(got[keep] - want[0]) <= bound[0]).all()
+
+
+def test_lengths_outside_the_table_are_skipped():
+    ctx = _q4.Context([300, 40, 64, 20], 2, 64, 16, seed=5)
+    cap = ctx.width * 16
+    d = Decode(ctx, 4, tokens=2)
+    d.run(seq_lens=_i32([300, 1, cap + 1, -5], "cuda"))
+    assert ctx.pool.check() == gcb.GC_ERR_OUT_OF_RANGE
+    d.check(skip=(1, 2, 3))
+    d.out.fill_(float("nan"))
+    d.run(seq_lens=_i32([0, 40, 64, 20], "cuda"))
+    assert ctx.pool.check() == gcb.GC_ERR_OUT_OF_RANGE
+    d.check(skip=(0,))
+
+
+def test_bad_pages_are_left_out():
+    ctx = _q4.Context([300, 40], 2, 64, 16, seed=6)
+    t4, t16 = ctx.table4.copy(), ctx.table16.copy()
+    t4[0, 3], t4[0, 7], t16[0, 7] = ctx.pages4, -1, ctx.pages16
+    d = Decode(ctx, 4).run(q4_table=_i32(t4, "cuda"), block_table=_i32(t16, "cuda"))
+    assert ctx.pool.check() == gcb.GC_ERR_OUT_OF_RANGE
+    assert ctx.pool.check() == gcb.GC_OK
+    kv, s = ctx.keys(0)
+    left = np.array([t not in range(48, 64) and t not in range(112, 128) for t in range(300)])
+    want, bound = _q4.decode_reference(_q4.f32(d.q_bits[0]).astype(np.float64), kv[:, left],
+                                       s[:, left], d.scale, 1)
+    assert (np.abs(d.out.double().cpu().numpy()[0] - want) <= bound).all()
+
+
+def test_the_same_call_gives_the_same_bits():
+    import torch
+    ctx = _q4.Context([5000, 3, 800, 77], 8, 128, 16, recent=1, seed=7)
+    d = Decode(ctx, 64)
+    first = d.run().out.clone()
+    for _ in range(5):
+        d.out.zero_()
+        d.ws.random_(0, 255)
+        assert torch.equal(d.run().out, first)
+
+
+def refused(status, d, **change):
+    with pytest.raises(gcb.GcError) as e:
+        d.run(**change)
+    assert e.value.status == status, change
+
+
+def test_refusals():
+    ctx = _q4.Context([100], 2, 64, 16)
+    d = Decode(ctx, 8)
+    for change in (dict(batch=-1), dict(max_blocks_per_seq=-1), dict(n_q4_pages=-1), dict(tokens=0),
+                   dict(tokens=-3), dict(num_q_heads=7), dict(num_q_heads=0),
+                   dict(softmax_scale=0.0), dict(softmax_scale=float("inf")),
+                   dict(softmax_scale=float("nan")), dict(q=None), dict(out=None),
+                   dict(block_table=None), dict(seq_lens=None), dict(q4_table=None),
+                   dict(q4_cache=None), dict(max_blocks_per_seq=0),
+                   dict(q4_cache=ctx.cache.data_ptr() + 8), dict(q=d.q.data_ptr() + 2),
+                   dict(workspace=None), dict(workspace_bytes=d.need - 1)):
+        refused(gcb.GC_ERR_INVALID_ARG, d, **change)
+    refused(gcb.GC_ERR_OUT_OF_RANGE, d, layer=1)
+    for change in (dict(tokens=5), dict(num_q_heads=24), dict(batch=8193),
+                   dict(max_blocks_per_seq=2 ** 28)):
+        refused(gcb.GC_ERR_UNSUPPORTED, d, **change)
+    d.run(batch=0, workspace=None, workspace_bytes=0)
+    assert ctx.pool.check() == gcb.GC_OK
+    assert np.isnan(d.out.double().cpu().numpy()).all()
+
+
+def test_a_cache_without_pages():
+    ctx = _q4.Context([100, 7], 2, 64, 16, recent=100)
+    Decode(ctx, 4).run(q4_cache=None, n_q4_pages=0).check()
+    assert ctx.pool.check() == gcb.GC_OK
