@@ -34,6 +34,8 @@ struct DecGeom {
   const uint8_t* q4_cache;
   const int32_t* q4_table;  // >= 0: the 4-bit page
   int32_t q4_pages, tokens, g_shift;  // q heads per kv head, log2
+  uint32_t q4_page;  // bytes of a page's plane
+  int64_t q4_plane;  // of all of them
 };
 
 // The geometry of a call; keys are cut into the ranges of `split`, or into shares.
@@ -71,6 +73,8 @@ inline DecGeom decode_geom(const gc_kv_pool* pool, const DecodeArgs& a, const De
   geo.q4_cache = nullptr;
   geo.q4_table = nullptr;
   geo.q4_pages = 0;
+  geo.q4_page = 0;
+  geo.q4_plane = 0;
   geo.tokens = 1;
   geo.g_shift = 0;
   geo.range_tiles = split ? split->split_tiles : 0;
@@ -734,7 +738,10 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
     const int first = by_warp ? 0 : warp, every = by_warp ? 1 : S::kWarps;
     const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq * (kQ4 ? geo.tokens : 1) + w.g * geo.G;
     if constexpr (kQ4) {
-      acc.run(geo, w, T, first, every, q + head0 * D, pool_k, plane_bytes, block_table, status);
+      acc.template run<S::kStages>(
+          static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::kRingBytes, geo, w, T,
+          first, every, q + head0 * D, pool_k, plane_bytes, block_table, status);
+      if (!by_warp) S::sync();  // the merge buffers lie over the stages
     } else {
       // (unsigned: look-ups run past a piece that may end near 2^31)
       const uint32_t k1 = static_cast<uint32_t>(w.k1);

@@ -15,23 +15,41 @@ namespace {
 
 using dec::decode_cta;
 using dec::Keys4;
-using dec::Shape;
+
+// Threads, resident CTAs and stages of shared memory of a variant.
+template <int D, int NT>
+struct Shape4 {
+  static constexpr int kWarps = 8;
+  static constexpr int kCtas = decode_ctas(D, 8 * NT);
+  static constexpr int kStages = 3;
+  static constexpr int kGroups = 1;
+  static constexpr int kThreads = 32 * kWarps;
+  static constexpr int kHeads = 8 * NT;
+  static constexpr int kStride = D + 4;
+  static constexpr int kRingBytes = 2 * kStages * dec::Stage4<D>::kBytes;  // of a warp
+  static constexpr int kRedFloats =
+      kWarps * kHeads * kStride > kWarps * kRingBytes / 4 ? kWarps * kHeads * kStride
+                                                          : kWarps * kRingBytes / 4;
+  __device__ static int group() { return 0; }
+  __device__ static int tid() { return static_cast<int>(threadIdx.x); }
+  __device__ static void sync() { __syncthreads(); }
+};
 
 template <int D, int NT>
-__global__ void __launch_bounds__(Shape<D, NT>::kThreads, Shape<D, NT>::kCtas)
+__global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
     decode_q4_kernel(const __nv_bfloat16* q, const int32_t* block_table, const int32_t* seq_lens,
                      __nv_bfloat16* out, float* ws, DecGeom geo, int32_t* status,
                      int* merge_counters) {
   extern __shared__ __align__(16) uint8_t smem[];
   dependent_begin();
-  decode_cta<Shape<D, NT>, D, NT, false, false, false, Keys4<D, NT>>(
+  decode_cta<Shape4<D, NT>, D, NT, false, false, false, Keys4<D, NT>>(
       smem, dec::ByBlock{}, q, block_table, seq_lens, out, ws, geo, status, merge_counters);
 }
 
 template <int D, int NT>
 gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo,
                  cudaStream_t stream) {
-  using S = Shape<D, NT>;
+  using S = Shape4<D, NT>;
   const size_t smem = decode_smem_bytes<S>(a.batch);
   auto kernel = decode_q4_kernel<D, NT>;
   cudaError_t e = cudaSuccess;
@@ -75,6 +93,9 @@ gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4
   geo.q4_cache = cache.data;
   geo.q4_table = cache.table;
   geo.q4_pages = cache.pages;
+  geo.q4_page = static_cast<uint32_t>(
+      geo.Hkv * q4_head_bytes(pool->cfg.head_dim, pool->cfg.page_size));
+  geo.q4_plane = static_cast<int64_t>(cache.pages) * geo.q4_page;
   geo.tokens = tokens;
   while ((1 << geo.g_shift) < geo.G) ++geo.g_shift;
   const bool narrow = geo.G * tokens <= 8;

@@ -8,8 +8,8 @@
 // word of 8 codes so costs one shift and four masks, no conversion and no offset:
 //  * the weight 16 of the second kind is taken out of the other operand (K: Q's columns
 //    are divided by 16) or of the result's row (V: row r + 8 of a tile), exactly;
-//  * the offset 8 starts the accumulators of S (-8 sum q over the group, worked out once
-//    per piece) and is one more product with a constant operand for O;
+//  * the offset 8 is one more product: for S of a key's scales with the groups' sums of
+//    -8 q, in three bf16 parts that make up their 24 bits, for O of a constant with P;
 //  * S is scaled group by group in binary32, S += s_g D_g; P is scaled by V's s_g before
 //    its product, P s_g rounded to bf16 (2^-9 of a term, as P itself is).
 // Powers of two keep everything in range: Q's columns are brought to 2^60 at the most, P
@@ -23,9 +23,10 @@ namespace gc {
 namespace {
 namespace dec {
 
-constexpr int kQTop = 60;          // exponent of a column's largest |q|
+constexpr int kQTop = 100;         // exponent of a column's largest |q|
 constexpr float kPBias = 90.0f;    // P is 2^kPBias at the reference maximum
 constexpr float kRaise4 = 8.0f;    // scores this far above it raise it
+constexpr float kNone = -3e38f;    // the reference maximum of a column without a key yet
 constexpr uint32_t kLowNibbles = 0x000f000fu, kHighNibbles = 0x00f000f0u;
 
 __device__ __forceinline__ float pow2(int e) {  // -126 <= e <= 127
@@ -36,61 +37,96 @@ __device__ __forceinline__ float times_pow2(float x, int e) {
   return x * pow2(e / 2) * pow2(e - e / 2);
 }
 
-__device__ __forceinline__ void mma_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1, float c0,
-                                         float c1) {
+// x to 8 bits, towards 0
+__device__ __forceinline__ float bf16_part(float x) {
+  return __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+}
+
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                          uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-      "{%8,%9}, {%10,%11,%10,%11};"
+      "{%8,%9}, {%10,%10,%10,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-template <int N>
-__device__ __forceinline__ void ldg_words(const uint8_t* p, uint32_t (&r)[N]) {
-  if constexpr (N == 1)
-    asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(r[0]) : "l"(p));
-  else
-    ldg(p, r);
-}
-
-// Sixteen keys' rows of a 4-bit page, as thread (r = lane / 4, q = lane % 4) needs them.
+// A group of keys in shared memory: K's codes and scales, V's codes and scales.
 template <int D>
-struct Rows4 {
+struct Stage4 {
   static constexpr int GR = D / 32;
-  uint32_t k[2][GR];       // keys r and r + 8: 8 codes of each group
-  uint32_t sk[2][GR / 2];  // their scales
-  uint32_t v[4][GR / 2];   // keys 2q, 2q + 1, 2q + 8, 2q + 9: 4 codes of each group
-  uint32_t sv[2][GR];      // their scales, two keys' each
+  static constexpr int kCodes = kGroup * D / 2, kScales = kGroup * D / 16;
+  static constexpr int kBytes = 2 * (kCodes + kScales);
 
-  // codes: the first key's row of K; scales: its scales; v_after: from K to V
-  __device__ __forceinline__ void load_k(const uint8_t* codes, const uint8_t* scales) {
-    const int lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
+};
+
+// (a predicate in place of a branch: branches are most of what a small loop adds)
+__device__ __forceinline__ void copy16_if(bool on, uint32_t to, const uint8_t* from) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t"
+               "@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(to),
+               "l"(from), "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
+// Keeps a value in its register: worked out again at each use it would take more
+// instructions than all else that the use is about.
+__device__ __forceinline__ uint32_t kept(uint32_t x) {
+  asm volatile("" : "+r"(x));
+  return x;
+}
+
+// What a lane copies of a group of keys, and where it reads its operands in a stage.  Row i
+// of S^T and of P^T is the key i & 8 + 4 (i & 1) + (i & 7) / 2: with this order the rows of V
+// that the lanes of a warp read together lie side by side.
+template <int D>
+struct Parts4 {
+  static constexpr int kCodes = Stage4<D>::kCodes, kScales = Stage4<D>::kScales;
+  uint32_t k, s, v;  // codes of its K rows, their (and V's) scales, codes of its V rows
+  uint32_t bytes;
+
+  __device__ __forceinline__ static int row() {  // the key of its first row of P
+    const int r = (threadIdx.x & 31) >> 2;
+    return (r & 1) * 4 + (r >> 1);
+  }
+  __device__ __forceinline__ Parts4() {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    k = kept(row() * (D / 2) + c * (D / 8));
+    s = kept(kCodes + row() * (D / 16));
+    v = kept(kCodes + kScales + c * (D / 2) + r * (D / 16));
+    bytes = kept(16 * lane);
+  }
+  // codes: the row of K of the group's first key; after: from there to its scales; plane:
+  // from K to V
+  __device__ __forceinline__ void copy_if(bool on, uint32_t to, const uint8_t* codes, int after,
+                                          int64_t plane) const {
+    constexpr int kV = kCodes + kScales;
+    codes += bytes;
+    to += bytes;
+    const uint8_t* const v = codes + plane;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      ldg_words(codes + (r + 8 * x) * (D / 2) + q * (D / 8), k[x]);
-      ldg_words(scales + (r + 8 * x) * (D / 16), sk[x]);
+    for (int i = 0; i < kCodes / 512; ++i) {
+      copy16_if(on, to + 512 * i, codes + 512 * i);
+      copy16_if(on, to + kV + 512 * i, v + 512 * i);
     }
-  }
-  __device__ __forceinline__ void load_v(const uint8_t* codes, const uint8_t* scales) {
-    const int lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      ldg_words(codes + (2 * q + (x & 1) + 8 * (x >> 1)) * (D / 2) + r * (D / 16), v[x]);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) ldg_words(scales + (2 * q + 8 * x) * (D / 16), sv[x]);
-  }
-  // keys at or past n: what lies there may be anything, and 0 times NaN is NaN
-  __device__ __forceinline__ void clear_from(int n) {
-    const int q = threadIdx.x & 3;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-        if (2 * q + y + 8 * x >= n)
-#pragma unroll
-          for (int i = 0; i < GR / 2; ++i) sv[x][y * (GR / 2) + i] = 0;
+    const bool scales = on && bytes < kScales;
+    copy16_if(scales, to + kCodes, codes + after);
+    copy16_if(scales, to + kV + kCodes, v + after);
   }
 };
+
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&r)[N]) {
+  static_assert(N == 1 || N == 2 || N == 4, "a load");
+  if constexpr (N == 1)
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(at));
+  else if constexpr (N == 2)
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at));
+  else
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(at));
+}
+__device__ __forceinline__ float half_f32(uint32_t pair, int i) {  // of two bf16
+  return __uint_as_float(i ? pair & 0xffff0000u : pair << 16);
+}
 
 template <int D, int NT>
 struct Keys4 {
@@ -98,15 +134,13 @@ struct Keys4 {
   float o[NT][D / 16][4];     // tile (g, t): columns 32 g + 4 r + 2 t (+ 1: rows r + 8)
   float m[NT][2], l[NT][2];
   uint32_t q[NT][D / 16][2];  // Q^T: columns 32 g + 8 q ... + 7, the last four over 16
-  float off[NT][GR][2];       // -8 2^-133 sum q of a group
-  float back[NT][2];          // what undoes the column's power of two
-  bool first;
+  uint32_t off[NT][GR / 2];   // -8 2^-133 times the groups' sums of q (B operand, see load_q)
+  float scale[NT][2];         // softmax_scale log2(e), and what undoes the powers of two
 
   __device__ __forceinline__ void reset() {
-    first = true;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      m[t][0] = m[t][1] = -INFINITY;
+      m[t][0] = m[t][1] = kNone;
       l[t][0] = l[t][1] = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
@@ -135,8 +169,11 @@ struct Keys4 {
       }
       top = max(top, __shfl_xor_sync(all, top, 1));
       top = max(top, __shfl_xor_sync(all, top, 2));
-      // (a column of zeros, or with a NaN or infinity, stays as it is)
-      const int e = top == 0 || top >= 0x7f80u ? 0 : kQTop + 127 - static_cast<int>(top >> 7);
+      // (a column of zeros, or with a NaN or infinity, stays as it is; 20 keeps the scale
+      // in range where |q| passes 2^80)
+      const int e = top == 0 || top >= 0x7f80u
+                        ? kQTop
+                        : max(20, kQTop + 127 - static_cast<int>(top >> 7));
       float sum[GR];
 #pragma unroll
       for (int g = 0; g < GR; ++g) {
@@ -144,56 +181,80 @@ struct Keys4 {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float a = times_pow2(__uint_as_float(x[i] << 16), e);
-          const float b = times_pow2(__uint_as_float(x[i] & 0xffff0000u), e);
+          const float a = times_pow2(half_f32(x[i], 0), e);
+          const float b = times_pow2(half_f32(x[i], 1), e);
           s += a + b;
           q[t][2 * g + i / 2][i & 1] = i < 2 ? pack_bf16x2(a, b)
                                              : pack_bf16x2(a * 0.0625f, b * 0.0625f);
         }
         s += __shfl_xor_sync(all, s, 1);
         s += __shfl_xor_sync(all, s, 2);
-        sum[g] = s * pow2(-65) * pow2(-65);
+        sum[g] = s * -pow2(-65) * pow2(-65);
       }
-      const float undo = times_pow2(1.f, 53 - e);
+      // Row k of the operand is part k / GR of group k % GR's sum: two rows (groups) to a
+      // register, parts 0 to 2 in turn; a key's scales are the other operand as they lie.
+#pragma unroll
+      for (int i = 0; i < GR / 2; ++i) {
+        const int k = 2 * c + 8 * i, part = k / GR;
+        float v[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float s = sum[j];
+          if (GR == 4 && k % GR) s = sum[GR - 2 + j];
+          const float hi = bf16_part(s), mid = bf16_part(s - hi);
+          v[j] = part == 0 ? hi : part == 1 ? mid : part == 2 ? s - hi - mid : 0.f;
+        }
+        off[t][i] = pack_bf16x2(v[0], v[1]);
+      }
+      const float undo = times_pow2(geo.scale_log2, 133 - e);
       // from the lanes of a column (r) to those of its scores (2 c, 2 c + 1)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int from = 4 * (2 * c + x);
-        back[t][x] = __shfl_sync(all, undo, from);
-#pragma unroll
-        for (int g = 0; g < GR; ++g) off[t][g][x] = -__shfl_sync(all, sum[g], from);
+        scale[t][x] = __shfl_sync(all, undo, from);
       }
     }
   }
 
   // S^T of a group of keys, times 2^(e - 133)
-  __device__ __forceinline__ void scores(const Rows4<D>& f, float (&s)[NT][4]) const {
+  __device__ __forceinline__ void scores(uint32_t at, const Parts4<D>& mine,
+                                         float (&s)[NT][4]) const {
+    uint32_t k[2][GR], sk[2][GR / 2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      lds_words(at + mine.k + 8 * x * (D / 2), k[x]);
+      lds_words(at + mine.s + 8 * x * (D / 16), sk[x]);
+    }
+    // -8 2^-133 sum_g s_g sum q
+    const bool odd = GR == 4 && (mine.bytes & 16);
+    const uint32_t x01 = odd ? sk[0][GR / 2 - 1] : sk[0][0];
+    const uint32_t y01 = odd ? sk[1][GR / 2 - 1] : sk[1][0];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      mma_first(s[t], x01, y01, GR == 4 ? x01 : 0u, GR == 4 ? y01 : 0u, off[t][0],
+                GR == 4 ? off[t][GR / 2 - 1] : 0u);
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
-      const uint32_t x = f.k[0][g], y = f.k[1][g], x8 = x >> 8, y8 = y >> 8;
-      const float s0 = __uint_as_float(g & 1 ? f.sk[0][g / 2] & 0xffff0000u : f.sk[0][g / 2] << 16);
-      const float s1 = __uint_as_float(g & 1 ? f.sk[1][g / 2] & 0xffff0000u : f.sk[1][g / 2] << 16);
+      const uint32_t x = k[0][g], y = k[1][g], x8 = x >> 8, y8 = y >> 8;
+      const float s0 = half_f32(sk[0][g / 2], g & 1), s1 = half_f32(sk[1][g / 2], g & 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float c[4];
-        mma_from(c, x & kLowNibbles, y & kLowNibbles, x8 & kLowNibbles, y8 & kLowNibbles,
-                 q[t][2 * g][0], q[t][2 * g][1], off[t][g][0], off[t][g][1]);
-        mma(c, x & kHighNibbles, y & kHighNibbles, x8 & kHighNibbles, y8 & kHighNibbles,
+        float d[4];
+        mma_first(d, x & kLowNibbles, y & kLowNibbles, x8 & kLowNibbles, y8 & kLowNibbles,
+                  q[t][2 * g][0], q[t][2 * g][1]);
+        mma(d, x & kHighNibbles, y & kHighNibbles, x8 & kHighNibbles, y8 & kHighNibbles,
             q[t][2 * g + 1][0], q[t][2 * g + 1][1]);
-        if (g == 0) {
-          s[t][0] = c[0] * s0, s[t][1] = c[1] * s0;
-          s[t][2] = c[2] * s1, s[t][3] = c[3] * s1;
-        } else {
-          s[t][0] = fmaf(c[0], s0, s[t][0]), s[t][1] = fmaf(c[1], s0, s[t][1]);
-          s[t][2] = fmaf(c[2], s1, s[t][2]), s[t][3] = fmaf(c[3], s1, s[t][3]);
-        }
+        s[t][0] = fmaf(d[0], s0, s[t][0]), s[t][1] = fmaf(d[1], s0, s[t][1]);
+        s[t][2] = fmaf(d[2], s1, s[t][2]), s[t][3] = fmaf(d[3], s1, s[t][3]);
       }
     }
   }
 
-  // The same of rows of a 16-bit page.
-  __device__ __forceinline__ void scores16(const uint8_t* kp, float (&s)[NT][4]) const {
-    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+  // The same of rows of a 16-bit page, which are taken times 2^-60 so that no product with
+  // Q's columns overflows.
+  __device__ __forceinline__ void scores16(const uint8_t* kp, const Parts4<D>& mine,
+                                           float (&s)[NT][4]) const {
+    const int c = threadIdx.x & 3;
     float a[NT][4], b[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -202,8 +263,13 @@ struct Keys4 {
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
       uint32_t x[4], y[4];
-      ldg(kp + (r * D + 32 * g + 8 * c) * 2, x);
-      ldg(kp + ((r + 8) * D + 32 * g + 8 * c) * 2, y);
+      ldg(kp + (mine.row() * D + 32 * g + 8 * c) * 2, x);
+      ldg(kp + ((mine.row() + 8) * D + 32 * g + 8 * c) * 2, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = q4::mul_bf16x2(x[i], 0x21802180u);
+        y[i] = q4::mul_bf16x2(y[i], 0x21802180u);
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         mma(a[t], x[0], y[0], x[1], y[1], q[t][2 * g][0], q[t][2 * g][1]);
@@ -213,87 +279,101 @@ struct Keys4 {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s[t][e] = fmaf(b[t][e], 16.f, a[t][e]) * pow2(-66) * pow2(-67);
+      for (int e = 0; e < 4; ++e) s[t][e] = fmaf(b[t][e], 16.f, a[t][e]) * pow2(-73);
   }
 
-  // scores -> P^T (B operand of the V product), times 2^kPBias; the column of token i of
-  // the request's last `tokens` sees the keys below n - (tokens - 1 - i)
-  __device__ __forceinline__ void softmax(float (&s)[NT][4], int n, const DecGeom& geo,
-                                          uint32_t (&p)[NT][2]) {
-    const int lane = threadIdx.x & 31, r = lane >> 2;
-    const float scale = geo.scale_log2 * pow2(80);
-    bool grow = false;
+  // The column of token i of the request's last `tokens` sees the keys below
+  // n - (tokens - 1 - i).
+  __device__ __forceinline__ void mask(float (&s)[NT][4], const Parts4<D>& mine, int n,
+                                       const DecGeom& geo) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float f = back[t][x];
-        s[t][x] *= scale, s[t][x] *= f;
-        s[t][x + 2] *= scale, s[t][x + 2] *= f;
+      for (int e = 0; e < 4; ++e) {
+        const int token = (8 * t + 2 * static_cast<int>(threadIdx.x & 3) + (e & 1)) >> geo.g_shift;
+        if (mine.row() + 8 * (e >> 1) + geo.tokens - 1 - token >= n) s[t][e] = -INFINITY;
       }
-    if (n < kGroup + geo.tokens - 1) {
+  }
+
+  // scores of H groups -> P, times 2^kPBias
+  template <int H>
+  __device__ __forceinline__ void softmax(float (&s)[H][NT][4]) {
+    float top = -INFINITY;
+    float x[H][NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float b[2] = {kPBias - m[t][0], kPBias - m[t][1]};
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[h][t][e] = fmaf(s[h][t][e], scale[t][e & 1], b[e & 1]);
+          top = fmaxf(top, x[h][t][e]);
+        }
+    }
+    if (__any_sync(0xffffffffu, top > kPBias + kRaise4)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < H; ++h) mx = fmaxf(mx, fmaxf(s[h][t][i], s[h][t][i + 2]));
+          mx *= scale[t][i];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          if (mx > m[t][i]) {
+            const float alpha = ex2_approx(m[t][i] - mx);
+            l[t][i] *= alpha;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+              o[t][j][i] *= alpha;
+              o[t][j][i + 2] *= alpha;
+            }
+            m[t][i] = mx;
+          }
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            x[h][t][i] = fmaf(s[h][t][i], scale[t][i], kPBias - m[t][i]);
+            x[h][t][i + 2] = fmaf(s[h][t][i + 2], scale[t][i], kPBias - m[t][i]);
+          }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int token = (8 * t + 2 * (lane & 3) + (e & 1)) >> geo.g_shift;
-          if (r + 8 * (e >> 1) + geo.tokens - 1 - token >= n) s[t][e] = -INFINITY;
+          s[h][t][e] = ex2_approx(x[h][t][e]);
+          l[t][e & 1] += s[h][t][e];
         }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) grow |= s[t][e] - m[t][e & 1] > kRaise4;
-    if (first || __any_sync(0xffffffffu, grow)) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float mx = fmaxf(s[t][x], s[t][x + 2]);
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-          if (first) {
-            m[t][x] = mx;
-          } else if (mx > m[t][x]) {
-            const float alpha = ex2_approx(m[t][x] - mx);
-            l[t][x] *= alpha;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-              o[t][i][x] *= alpha;
-              o[t][i][x + 2] *= alpha;
-            }
-            m[t][x] = mx;
-          }
-        }
-      first = false;
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float e[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        // (a column may have no key yet: its maximum is -inf then)
-        e[x] = s[t][x] == -INFINITY ? 0.f : ex2_approx(s[t][x] - m[t][x & 1] + kPBias);
-        l[t][x & 1] += e[x];
-      }
-      p[t][0] = transpose8(pack_bf16x2(e[0], e[1]));
-      p[t][1] = transpose8(pack_bf16x2(e[2], e[3]));
-    }
   }
 
-  // O^T += V^T P^T
-  __device__ __forceinline__ void values(const Rows4<D>& f, const uint32_t (&p)[NT][2]) {
+  // O^T += V^T P^T; kTail: keys at or past n left out (their scale may be anything)
+  template <bool kTail>
+  __device__ __forceinline__ void values(uint32_t at, const Parts4<D>& mine, int n,
+                                         const float (&p)[NT][4]) {
+    uint32_t v[4][GR / 2], sv[2][GR / 2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) lds_words(at + mine.v + 4 * x * (D / 2), v[x]);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      lds_words(at + mine.s + Stage4<D>::kCodes + Stage4<D>::kScales + 8 * x * (D / 16), sv[x]);
+      if (kTail && mine.row() + 8 * x >= n)
+#pragma unroll
+        for (int i = 0; i < GR / 2; ++i) sv[x][i] = 0;
+    }
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
       const uint32_t half = g & 1 ? 0x7632 : 0x5410;
-      const uint32_t x = __byte_perm(f.v[0][g / 2], f.v[1][g / 2], half), x8 = x >> 8;
-      const uint32_t y = __byte_perm(f.v[2][g / 2], f.v[3][g / 2], half), y8 = y >> 8;
-      const uint32_t s0 = __byte_perm(f.sv[0][g / 2], f.sv[0][g / 2 + GR / 2], half);
-      const uint32_t s1 = __byte_perm(f.sv[1][g / 2], f.sv[1][g / 2 + GR / 2], half);
+      const uint32_t x = __byte_perm(v[0][g / 2], v[1][g / 2], half), x8 = x >> 8;
+      const uint32_t y = __byte_perm(v[2][g / 2], v[3][g / 2], half), y8 = y >> 8;
+      const float s0 = half_f32(sv[0][g / 2], g & 1), s1 = half_f32(sv[1][g / 2], g & 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t b0 = q4::mul_bf16x2(p[t][0], s0), b1 = q4::mul_bf16x2(p[t][1], s1);
+        const uint32_t b0 = transpose8(pack_bf16x2(p[t][0] * s0, p[t][1] * s0));
+        const uint32_t b1 = transpose8(pack_bf16x2(p[t][2] * s1, p[t][3] * s1));
         mma(o[t][2 * g], x & kLowNibbles, x & kHighNibbles, y & kLowNibbles, y & kHighNibbles, b0,
             b1);
         mma(o[t][2 * g + 1], x8 & kLowNibbles, x8 & kHighNibbles, y8 & kLowNibbles,
@@ -305,8 +385,8 @@ struct Keys4 {
     }
   }
 
-  // The same of rows of a 16-bit page, keys at or past n left out.
-  __device__ __forceinline__ void values16(const uint8_t* vp, int n, const uint32_t (&p)[NT][2]) {
+  // The same of rows of a 16-bit page.
+  __device__ __forceinline__ void values16(const uint8_t* vp, int n, const float (&p)[NT][4]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     uint32_t b[NT][2], b16[NT][2];
 #pragma unroll
@@ -314,7 +394,8 @@ struct Keys4 {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         // P 2^-133, and 16 times that for the rows r + 8
-        b[t][i] = q4::mul_bf16x2(q4::mul_bf16x2(p[t][i], 0x1e801e80u), 0x1e001e00u);
+        b[t][i] = transpose8(pack_bf16x2(p[t][2 * i], p[t][2 * i + 1]));
+        b[t][i] = q4::mul_bf16x2(q4::mul_bf16x2(b[t][i], 0x1e801e80u), 0x1e001e00u);
         b16[t][i] = q4::mul_bf16x2(b[t][i], 0x41804180u);
       }
 #pragma unroll
@@ -322,7 +403,7 @@ struct Keys4 {
       uint32_t v[4][2];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const int key = 2 * c + (x & 1) + 8 * (x >> 1);
+        const int key = c + 4 * x;
         v[x][0] = v[x][1] = 0;
         if (key < n) ldg(vp + (key * D + 32 * g + 4 * r) * 2, v[x]);
       }
@@ -341,89 +422,122 @@ struct Keys4 {
     }
   }
 
-  // The groups first, first + every, ... of piece w of a request of T keys, to O, reference
-  // maxima and sums as decode_cta merges them.
-  __device__ __forceinline__ void run(const DecGeom& geo, const DecPiece& w, int T, int first_group,
-                                      int every, const __nv_bfloat16* q_g, const uint8_t* pool_k,
-                                      int64_t plane16, const int32_t* block_table,
-                                      int32_t* status) {
+  // Any group: in 16 bits, with keys that some column does not see, or none.
+  template <typename Look>
+  __device__ __forceinline__ void one(uint32_t from, uint32_t key, int h, uint32_t ready, int T,
+                                      uint32_t k1, const Parts4<D>& mine, const Look& look,
+                                      int64_t plane16, const DecGeom& geo) {
+    key += h * kGroup;
+    from += h * Stage4<D>::kBytes;
+    if (key >= k1) return;
+    const bool four = ready >> h & 1;
+    const uint8_t* kp = nullptr;
+    if (!four) look(key, &kp);
+    if (!four && kp == nullptr) return;
+    const int n = T - static_cast<int>(key);
+    float s[1][NT][4];
+    if (four)
+      scores(from, mine, s[0]);
+    else
+      scores16(kp, mine, s[0]);
+    mask(s[0], mine, n, geo);
+    softmax(s);
+    if (four)
+      values<true>(from, mine, n, s[0]);
+    else
+      values16(kp + plane16, n, s[0]);
+  }
+
+  // The pairs of groups first, first + every, ... of piece w of a request of T keys, to O,
+  // reference maxima and sums as decode_cta merges them.  `ring`: the warp's kStages stages
+  // in shared memory, each for a pair.
+  template <int kStages>
+  __device__ __forceinline__ void run(uint32_t ring, const DecGeom& geo, const DecPiece& w, int T,
+                                      int first, int every, const __nv_bfloat16* q_g,
+                                      const uint8_t* pool_k, int64_t plane16,
+                                      const int32_t* block_table, int32_t* status) {
+    constexpr uint32_t kStage = 2 * Stage4<D>::kBytes;
     const int lane = threadIdx.x & 31;
-    const uint32_t k1 = static_cast<uint32_t>(w.k1), mask = static_cast<uint32_t>(geo.ps - 1);
-    const uint64_t head = q4_head_bytes(D, geo.ps);
-    const int64_t plane4 = static_cast<int64_t>(geo.q4_pages) * geo.Hkv * head;
-    const uint8_t* q4_k = geo.q4_cache + geo.layer * 2 * plane4;
-    auto key_of = [&](int i) {
-      return static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first_group + i * every) * kGroup;
-    };
-    // lane i looks up the warp's groups i, i + 32, ...: the address of the first key's row,
-    // lowest bit set in a 16-bit page, 0: none (bad, or past the piece)
-    auto look = [&](uint32_t key) -> uint64_t {
-      if (key >= k1) return 0;
+    const uint32_t k1 = static_cast<uint32_t>(w.k1), slots = static_cast<uint32_t>(geo.ps - 1);
+    // K of the layer and head
+    const uint8_t* q4_k = geo.q4_cache + geo.layer * 2 * geo.q4_plane +
+                          static_cast<uint64_t>(w.g) * q4_head_bytes(D, geo.ps);
+    // The 4-bit page of a key, -1: in 16 bits (wide: its row of K there), bad, or past the
+    // piece.
+    auto look = [&](uint32_t key, const uint8_t** wide = nullptr) -> int {
+      if (key >= k1) return -1;
       const int64_t e = static_cast<int64_t>(w.b) * geo.max_blocks + (key >> geo.ps_shift);
       const int p4 = ld_plain(geo.q4_table + e);
-      const uint32_t slot = key & mask;
-      if (p4 >= 0) {
-        if (p4 < geo.q4_pages)
-          return reinterpret_cast<uint64_t>(
-              q4_k + (static_cast<uint64_t>(p4) * geo.Hkv + w.g) * head + slot * (D / 2));
-      } else {
-        const int page = ld_plain(block_table + e);
-        if (page >= 0 && page < geo.num_pages)
-          return reinterpret_cast<uint64_t>(
-                     pool_k + ((static_cast<int64_t>(page) * geo.Hkv + w.g) * geo.ps + slot) * D * 2) |
-                 1;
-      }
-      record_error(status, GC_ERR_OUT_OF_RANGE);
-      return 0;
+      if (p4 >= 0 && p4 < geo.q4_pages) return p4;
+      const int page = p4 < 0 ? ld_plain(block_table + e) : -1;
+      if (page < 0 || page >= geo.num_pages)
+        record_error(status, GC_ERR_OUT_OF_RANGE);
+      else if (wide)
+        *wide = pool_k +
+                ((static_cast<int64_t>(page) * geo.Hkv + w.g) * geo.ps + (key & slots)) * D * 2;
+      return -1;
     };
-    uint64_t cur = look(key_of(lane));
+    // A window of 16 pairs is looked up at once, lane i a group of pair i / 2, and the next
+    // one ahead of its use.
+    const uint32_t step = static_cast<uint32_t>(every) * 2 * kGroup;
+    const uint32_t key0 = static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first) * 2 * kGroup;
+    const uint32_t mine_in = static_cast<uint32_t>(lane >> 1) * step + (lane & 1) * kGroup;
+    int cur = look(key0 + mine_in);
+    int nxt = key0 + 16 * step < k1 ? look(key0 + 16 * step + mine_in) : -1;
+    const Parts4<D> mine;
+    // Pairs are copied kStages - 1 before their turn, into the stage whose reader of the round
+    // before is done in every lane.  Bits 2 j, 2 j + 1 of `ready`: the groups of pair j from
+    // now on are in 4 bits.
+    const uint32_t end = ring + kStages * kStage;
+    uint32_t to = ring, ahead = key0, ready = 0;
+    int ahead_i = 0;
+    auto fetch = [&]() {
+      ready >>= 2;
+      if (ahead_i == 32) {
+        ahead_i = 0;
+        cur = nxt;
+        nxt = ahead + 16 * step < k1 ? look(ahead + 16 * step + mine_in) : -1;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int page = __shfl_sync(0xffffffffu, cur, ahead_i + h);  // -1 past the piece
+        const uint32_t slot = (ahead + h * kGroup) & slots;
+        mine.copy_if(page >= 0, to + h * Stage4<D>::kBytes,
+                     q4_k + (static_cast<uint64_t>(static_cast<uint32_t>(page)) * geo.q4_page +
+                             slot * (D / 2)),
+                     static_cast<int>(geo.ps * 8 - slot * 7) * (D / 16), geo.q4_plane);
+        ready |= (static_cast<uint32_t>(~page) >> 31) << (2 * (kStages - 1) + h);
+      }
+      ahead += step;
+      ahead_i += 2;
+      to = to + kStage == end ? ring : to + kStage;
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int i = 0; i < kStages - 1; ++i) fetch();
     reset();
     load_q(q_g, geo);
-    uint64_t nxt = key_of(32) < k1 ? look(key_of(32 + lane)) : 0;
-    Rows4<D> f[2];
-    uint64_t at[2];
-    // Two groups are under way: one is loaded as soon as the one before the last is done.
-    auto fetch = [&](int i, Rows4<D>& to) -> uint64_t {
-      if (key_of(i) >= k1) return 0;
-      if ((i & 31) == 0 && i > 0) {
-        cur = nxt;
-        nxt = key_of(i + 32) < k1 ? look(key_of(i + 32 + lane)) : 0;
+    uint32_t from = ring;
+    // keys below this are seen by every column
+    const uint32_t seen = min(k1, static_cast<uint32_t>(T - geo.tokens + 1));
+    for (uint32_t key = key0; key < k1; key += step) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      __syncwarp();
+      fetch();
+      // (the same in every lane; the vote says so)
+      if (__all_sync(0xffffffffu, (ready & 3) == 3 && key + 2 * kGroup <= seen)) {
+        float s[2][NT][4];
+        scores(from, mine, s[0]);
+        scores(from + Stage4<D>::kBytes, mine, s[1]);
+        softmax(s);
+        values<false>(from, mine, kGroup, s[0]);
+        values<false>(from + Stage4<D>::kBytes, mine, kGroup, s[1]);
+      } else {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, look, plane16, geo);
       }
-      const uint64_t a = __shfl_sync(0xffffffffu, cur, i & 31);
-      if (a != 0 && !(a & 1)) {
-        const uint8_t* codes = reinterpret_cast<const uint8_t*>(a);
-        const uint32_t slot = key_of(i) & mask;
-        const uint8_t* scales = codes + (geo.ps * 8 - static_cast<int>(slot) * 7) * (D / 16);
-        to.load_k(codes, scales);
-        to.load_v(codes + plane4, scales + plane4);
-      }
-      return a;
-    };
-    at[0] = fetch(0, f[0]);
-    at[1] = fetch(1, f[1]);
-    for (int i = 0; key_of(i) < k1; i += 2) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (key_of(i + u) >= k1) break;
-        const uint64_t a = at[u];
-        // keys of the group before the request's end (16 or more: all of them)
-        const int n = T - static_cast<int>(key_of(i + u));
-        float s[NT][4];
-        uint32_t p[NT][2];
-        if (a != 0 && !(a & 1)) {
-          scores(f[u], s);
-          softmax(s, n, geo, p);
-          if (n < kGroup) f[u].clear_from(n);
-          values(f[u], p);
-        } else if (a != 0) {
-          const uint8_t* kp = reinterpret_cast<const uint8_t*>(a & ~1ull);
-          scores16(kp, s);
-          softmax(s, n, geo, p);
-          values16(kp + plane16, n, p);
-        }
-        at[u] = fetch(i + u + 2, f[u]);
-      }
+      from = from + kStage == end ? ring : from + kStage;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     // the powers of two leave: 2^(kPBias - 133) of O, 16 of its rows r + 8, 2^kPBias of l
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
