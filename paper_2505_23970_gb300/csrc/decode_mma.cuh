@@ -3,8 +3,6 @@
 // its CTAs to it.
 #pragma once
 
-#include <type_traits>
-
 #include "decode_units.h"
 #include "gc_internal.cuh"
 #include "sm103_ptx.cuh"
@@ -30,12 +28,6 @@ struct DecGeom {
   const int32_t* cu_requests;
   const int32_t* group_rows;
   int32_t groups, shared_blocks;
-  // 4-bit pages (decode_q4.cu): columns of a product are (token, q head) pairs
-  const uint8_t* q4_cache;
-  const int32_t* q4_table;  // >= 0: the 4-bit page
-  int32_t q4_pages, tokens, g_shift;  // q heads per kv head, log2
-  uint32_t q4_page;  // bytes of a page's plane
-  int64_t q4_plane;  // of all of them
 };
 
 // The geometry of a call; keys are cut into the ranges of `split`, or into shares.
@@ -70,13 +62,6 @@ inline DecGeom decode_geom(const gc_kv_pool* pool, const DecodeArgs& a, const De
   geo.group_rows = a.prefix.rows;
   geo.groups = a.prefix.groups;
   geo.shared_blocks = a.prefix.max_blocks;
-  geo.q4_cache = nullptr;
-  geo.q4_table = nullptr;
-  geo.q4_pages = 0;
-  geo.q4_page = 0;
-  geo.q4_plane = 0;
-  geo.tokens = 1;
-  geo.g_shift = 0;
   geo.range_tiles = split ? split->split_tiles : 0;
   geo.max_splits = split ? split->splits : 1;
   const DecodeUnits units = decode_units(static_cast<int64_t>(a.batch) * cfg.num_kv_heads,
@@ -486,11 +471,10 @@ __device__ __forceinline__ Where look_up(const DecGeom& geo, const DecPiece& w, 
 //     out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  M = max_s m_s,
 // four columns of one head per thread at a time.  The partials come from other
 // SMs, so they are read through L2.  kParts: the sums and M go to own_o and own_ml.
-// `row` gives the output row of a column.
-template <typename S, int D, bool kParts, typename Row>
+template <typename S, int D, bool kParts>
 __device__ void merge_shares(const float* part_o, const float2* part_ml, int c0, int c1,
                              int first_slot, int G, __nv_bfloat16* out_g, float* own_o,
-                             float2* own_ml, Row row) {
+                             float2* own_ml) {
   for (int x = S::tid(); x < G * (D / 4); x += S::kThreads) {
     const int h = x / (D / 4), d4 = x % (D / 4);
     float M = -INFINITY, L = 0.f;
@@ -536,7 +520,7 @@ __device__ void merge_shares(const float* part_o, const float2* part_ml, int c0,
     uint2 pk;
     pk.x = pack_bf16x2(acc.x / L, acc.y / L);
     pk.y = pack_bf16x2(acc.z / L, acc.w / L);
-    *reinterpret_cast<uint2*>(out_g + static_cast<int64_t>(row(h)) * D + 4 * d4) = pk;
+    *reinterpret_cast<uint2*>(out_g + static_cast<int64_t>(h) * D + 4 * d4) = pk;
   }
 }
 
@@ -561,20 +545,13 @@ struct ByNumber {
 // One of them; the caller has waited for the kernel before.
 // kTwo: a request has a group's shared keys in front of its own, and may have none at all
 // (then its row is 0).
-// Four: the keys are in 4-bit pages, and a warp's work on them is this type's (decode_q4.cuh);
-// a request has geo.tokens rows.
-template <typename S, int D, int NT, bool kQ8, bool kParts, bool kTwo = false,
-          typename Four = void, typename Who>
+template <typename S, int D, int NT, bool kQ8, bool kParts, bool kTwo = false, typename Who>
 __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
                                            const __nv_bfloat16* q, const int32_t* block_table,
                                            const int32_t* seq_lens, __nv_bfloat16* out, float* ws,
                                            const DecGeom& geo, int32_t* status,
                                            int* merge_counters) {
   constexpr int kE = kQ8 ? 1 : 2;
-  constexpr bool kQ4 = !std::is_void_v<Four>;
-  const int cols = kQ4 ? geo.G * geo.tokens : geo.G;
-  // the row of a column, from the first one's
-  auto row = [&](int h) { return kQ4 ? (h >> geo.g_shift) * geo.Hq + (h & (geo.G - 1)) : h; };
   float* red = reinterpret_cast<float*>(smem);                      // [warps][heads][kStride]
   float2* red_ml = reinterpret_cast<float2*>(red + S::kRedFloats);  // [warps][heads]
   int* start = reinterpret_cast<int*>(red_ml + S::kWarps * S::kHeads);  // [batch + 1]
@@ -631,14 +608,14 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
       if (bad) record_error(status, GC_ERR_OUT_OF_RANGE);
     }
     for (int b = S::tid(); !kTwo && b < geo.batch; b += S::kThreads) {
-      const int T = ld_plain(seq_lens + b), least = kQ4 ? geo.tokens : 1;
-      if (T < least || T > cap) {
+      const int T = ld_plain(seq_lens + b);
+      if (T < 1 || T > cap) {
         if (who.cta() == 0 && !(kParts && T == 0)) record_error(status, GC_ERR_OUT_OF_RANGE);
       } else {
         most = max(most, T);
         ++n;
       }
-      start[b] = T < least || T > cap ? 0 : T;
+      start[b] = T < 1 || T > cap ? 0 : T;
     }
     most = __reduce_max_sync(0xffffffffu, most);
     n = __reduce_add_sync(0xffffffffu, n);
@@ -734,108 +711,101 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
     }
 
     // ---- this warp's groups: warp, warp + kWarps, ... of the piece, or all of them
-    std::conditional_t<kQ4, Four, Acc<D, NT>> acc;
+    Acc<D, NT> acc;
     const int first = by_warp ? 0 : warp, every = by_warp ? 1 : S::kWarps;
-    const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq * (kQ4 ? geo.tokens : 1) + w.g * geo.G;
-    if constexpr (kQ4) {
-      acc.template run<S::kStages>(
-          static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::kRingBytes, geo, w, T,
-          first, every, q + head0 * D, pool_k, plane_bytes, block_table, status);
-      if (!by_warp) S::sync();  // the merge buffers lie over the stages
-    } else {
-      // (unsigned: look-ups run past a piece that may end near 2^31)
-      const uint32_t k1 = static_cast<uint32_t>(w.k1);
-      auto key_of = [&](int i) {
-        return static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first + i * every) * kGroup;
-      };
-      Where cur = look_up<D, kQ8, kTwo>(geo, w, key_of(lane), pool_k, block_table, status, shared);
-      acc.reset();
-      acc.load_q(q + head0 * D, geo.G);
-      Where nxt{0, 0.f, 0.f};
-      if (key_of(32) < k1)
-        nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(32 + lane), pool_k, block_table, status, shared);
+    // (unsigned: look-ups run past a piece that may end near 2^31)
+    const uint32_t k1 = static_cast<uint32_t>(w.k1);
+    auto key_of = [&](int i) {
+      return static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first + i * every) * kGroup;
+    };
+    Where cur = look_up<D, kQ8, kTwo>(geo, w, key_of(lane), pool_k, block_table, status, shared);
+    acc.reset();
+    const int64_t head0 = static_cast<int64_t>(w.b) * geo.Hq + w.g * geo.G;
+    acc.load_q(q + head0 * D, geo.G);
+    Where nxt{0, 0.f, 0.f};
+    if (key_of(32) < k1)
+      nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(32 + lane), pool_k, block_table, status, shared);
 
-      struct Cursor {
-        const uint8_t* k;  // the group's K rows, null: no data
-        bool image;
-        float sk, sv;
-      };
-      auto locate = [&](int i) -> Cursor {
-        const bool later = (i & 31) == 0 && i > 0;  // the next 32 groups begin
-        const uint64_t a = __shfl_sync(0xffffffffu, later ? nxt.k : cur.k, i & 31);
-        Cursor c{reinterpret_cast<const uint8_t*>(a & ~1ull), kQ8 && (a & 1), 0.f, 0.f};
-        if (kQ8) {
-          c.sk = __shfl_sync(0xffffffffu, later ? nxt.sk : cur.sk, i & 31);
-          c.sv = __shfl_sync(0xffffffffu, later ? nxt.sv : cur.sv, i & 31);
+    struct Cursor {
+      const uint8_t* k;  // the group's K rows, null: no data
+      bool image;
+      float sk, sv;
+    };
+    auto locate = [&](int i) -> Cursor {
+      const bool later = (i & 31) == 0 && i > 0;  // the next 32 groups begin
+      const uint64_t a = __shfl_sync(0xffffffffu, later ? nxt.k : cur.k, i & 31);
+      Cursor c{reinterpret_cast<const uint8_t*>(a & ~1ull), kQ8 && (a & 1), 0.f, 0.f};
+      if (kQ8) {
+        c.sk = __shfl_sync(0xffffffffu, later ? nxt.sk : cur.sk, i & 31);
+        c.sv = __shfl_sync(0xffffffffu, later ? nxt.sv : cur.sv, i & 31);
+      }
+      return c;
+    };
+    // group data in the kernel's own element size is loaded ahead; a pool page
+    // met by the 8-bit variant is loaded when its turn comes
+    auto ahead = [&](const Cursor& c) { return c.k != nullptr && c.image == kQ8; };
+    const int64_t v_after = kQ8 ? geo.q8_chunk : plane_bytes;  // from K rows to V rows
+    Keys<D, kE> kf;
+    Values<D, kE> vf;
+    Cursor c = locate(0);
+    if (ahead(c)) {
+      kf.load(c.k);
+      vf.load(c.k + v_after);
+    }
+    for (int i = 0; key_of(i) < k1; ++i) {
+      int n = static_cast<int>(k1 - key_of(i));  // keys of the group (16 or more: all)
+      if (kTwo && key_of(i) < static_cast<uint32_t>(shared.own0))
+        n = min(n, shared.S - static_cast<int>(key_of(i)));
+      if (i > 0 && (i & 31) == 0) {
+        cur = nxt;
+        if (key_of(i + 32) < k1)
+          nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(i + 32 + lane), pool_k, block_table, status, shared);
+      }
+      Cursor cn{nullptr, false, 0.f, 0.f};
+      if (key_of(i + 1) < k1) cn = locate(i + 1);
+      // The group after that one goes to the L2 where 8 warps are all that an SM
+      // holds (64 KB of loads in flight): 32 contexts of 8000 keys, 128 q / 8 kv heads,
+      // 172.9 -> 165.4 us, 6.5 TB/s.  The variants of 12 warps lose by it (64
+      // multi-turn contexts 155 -> 164 us).
+      // So it does where other CTAs work on a shared prefix and the memory is not full.
+      if constexpr (!kQ8 && ((D == 128 && NT == 2) || S::kGroups > 1)) {
+        const bool later = ((i + 2) >> 5) != (i >> 5);
+        const uint64_t at = __shfl_sync(0xffffffffu, later ? nxt.k : cur.k, (i + 2) & 31) & ~1ull;
+        if (key_of(i + 2) < k1 && at != 0) {
+          if constexpr (D == 128) {
+            prefetch_l2(at + lane * 128);  // 16 rows of 256 bytes
+            prefetch_l2(at + v_after + lane * 128);
+          } else {
+            prefetch_l2(at + (lane < 16 ? 0 : v_after) + (lane & 15) * 128);
+          }
         }
-        return c;
-      };
-      // group data in the kernel's own element size is loaded ahead; a pool page
-      // met by the 8-bit variant is loaded when its turn comes
-      auto ahead = [&](const Cursor& c) { return c.k != nullptr && c.image == kQ8; };
-      const int64_t v_after = kQ8 ? geo.q8_chunk : plane_bytes;  // from K rows to V rows
-      Keys<D, kE> kf;
-      Values<D, kE> vf;
-      Cursor c = locate(0);
+      }
+      float s[NT][4];
+      uint32_t p[NT][2];
       if (ahead(c)) {
-        kf.load(c.k);
-        vf.load(c.k + v_after);
-      }
-      for (int i = 0; key_of(i) < k1; ++i) {
-        int n = static_cast<int>(k1 - key_of(i));  // keys of the group (16 or more: all)
-        if (kTwo && key_of(i) < static_cast<uint32_t>(shared.own0))
-          n = min(n, shared.S - static_cast<int>(key_of(i)));
-        if (i > 0 && (i & 31) == 0) {
-          cur = nxt;
-          if (key_of(i + 32) < k1)
-            nxt = look_up<D, kQ8, kTwo>(geo, w, key_of(i + 32 + lane), pool_k, block_table, status, shared);
-        }
-        Cursor cn{nullptr, false, 0.f, 0.f};
-        if (key_of(i + 1) < k1) cn = locate(i + 1);
-        // The group after that one goes to the L2 where 8 warps are all that an SM
-        // holds (64 KB of loads in flight): 32 contexts of 8000 keys, 128 q / 8 kv heads,
-        // 172.9 -> 165.4 us, 6.5 TB/s.  The variants of 12 warps lose by it (64
-        // multi-turn contexts 155 -> 164 us).
-        // So it does where other CTAs work on a shared prefix and the memory is not full.
-        if constexpr (!kQ8 && ((D == 128 && NT == 2) || S::kGroups > 1)) {
-          const bool later = ((i + 2) >> 5) != (i >> 5);
-          const uint64_t at = __shfl_sync(0xffffffffu, later ? nxt.k : cur.k, (i + 2) & 31) & ~1ull;
-          if (key_of(i + 2) < k1 && at != 0) {
-            if constexpr (D == 128) {
-              prefetch_l2(at + lane * 128);  // 16 rows of 256 bytes
-              prefetch_l2(at + v_after + lane * 128);
-            } else {
-              prefetch_l2(at + (lane < 16 ? 0 : v_after) + (lane & 15) * 128);
-            }
-          }
-        }
-        float s[NT][4];
-        uint32_t p[NT][2];
-        if (ahead(c)) {
-          acc.template scores<kE>(kf, twice(c.sk), s);
-          if (ahead(cn)) kf.load(cn.k);
+        acc.template scores<kE>(kf, twice(c.sk), s);
+        if (ahead(cn)) kf.load(cn.k);
+        acc.softmax(s, n, geo.scale_log2, p);
+        if (n < kGroup) vf.clear_from(n);
+        acc.template values<kE>(vf, twice(c.sv), p);
+        if (ahead(cn)) vf.load(cn.k + v_after);
+      } else {
+        if (kQ8 && c.k != nullptr) {
+          Keys<D, 2> kg;
+          Values<D, 2> vg;
+          kg.load(c.k);
+          vg.load(c.k + plane_bytes);
+          acc.template scores<2>(kg, 0, s);
           acc.softmax(s, n, geo.scale_log2, p);
-          if (n < kGroup) vf.clear_from(n);
-          acc.template values<kE>(vf, twice(c.sv), p);
-          if (ahead(cn)) vf.load(cn.k + v_after);
-        } else {
-          if (kQ8 && c.k != nullptr) {
-            Keys<D, 2> kg;
-            Values<D, 2> vg;
-            kg.load(c.k);
-            vg.load(c.k + plane_bytes);
-            acc.template scores<2>(kg, 0, s);
-            acc.softmax(s, n, geo.scale_log2, p);
-            if (n < kGroup) vg.clear_from(n);
-            acc.template values<2>(vg, 0, p);
-          }
-          if (ahead(cn)) {
-            kf.load(cn.k);
-            vf.load(cn.k + v_after);
-          }
+          if (n < kGroup) vg.clear_from(n);
+          acc.template values<2>(vg, 0, p);
         }
-        c = cn;
+        if (ahead(cn)) {
+          kf.load(cn.k);
+          vf.load(cn.k + v_after);
+        }
       }
+      c = cn;
     }
 
 #pragma unroll
@@ -852,7 +822,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int h = 8 * t + 2 * (lane & 3) + x;
-          if (h >= cols) continue;
+          if (h >= geo.G) continue;
           if constexpr (kParts) {
             float4* dst = reinterpret_cast<float4*>(geo.own.o + (head0 + h) * D +
                                                     (lane >> 2) * (D / 8));
@@ -864,16 +834,6 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
             continue;
           }
           const float inv = kTwo && acc.l[t][x] == 0.f ? 0.f : 1.f / acc.l[t][x];
-          if constexpr (kQ4) {
-            // ... and 4 in each group of 32
-#pragma unroll
-            for (int v = 0; v < D / 32; ++v)
-              *reinterpret_cast<uint2*>(out + (head0 + row(h)) * D + 32 * v + (lane >> 2) * 4) =
-                  make_uint2(pack_bf16x2(acc.o[t][2 * v][x] * inv, acc.o[t][2 * v][x + 2] * inv),
-                             pack_bf16x2(acc.o[t][2 * v + 1][x] * inv,
-                                         acc.o[t][2 * v + 1][x + 2] * inv));
-            continue;
-          }
           uint4* dst = reinterpret_cast<uint4*>(out + (head0 + h) * D + (lane >> 2) * (D / 8));
 #pragma unroll
           for (int v = 0; v < D / 64; ++v) {
@@ -919,10 +879,9 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
                               ? head0 * geo.max_splits + w.part
                               : (static_cast<int64_t>(who.cta()) * 2 + w.part) * S::kHeads;
     const int64_t part_step = geo.range_tiles ? geo.max_splits : 1;
-    for (int x = S::tid(); x < cols * (D / 2); x += S::kThreads) {
+    for (int x = S::tid(); x < geo.G * (D / 2); x += S::kThreads) {
       const int h = x / (D / 2), d = 2 * (x % (D / 2));
-      const int pos = kQ4 ? 16 * (2 * (d / 32) + (d % 4) / 2) + 2 * (d % 32 / 4)
-                          : 16 * ((d % (D / 8)) / 2) + 2 * (d / (D / 8));
+      const int pos = 16 * ((d % (D / 8)) / 2) + 2 * (d / (D / 8));
       float M = -INFINITY, L = 0.f;
       float2 o = make_float2(0.f, 0.f);
 #pragma unroll
@@ -944,7 +903,7 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
         }
       }
       if (w.part < 0) {
-        *reinterpret_cast<uint32_t*>(out + (head0 + row(h)) * D + d) =
+        *reinterpret_cast<uint32_t*>(out + (head0 + h) * D + d) =
             kTwo && L == 0.f ? 0u : pack_bf16x2(o.x / L, o.y / L);
       } else {
         *reinterpret_cast<float2*>(ws + (part0 + h * part_step) * D + d) = o;
@@ -968,9 +927,9 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
       }
       S::sync();
       if (merge_flag)
-        merge_shares<S, D, kParts>(ws, part_ml, c0, c1, c0 * per >= pair0 ? 0 : 1, cols,
+        merge_shares<S, D, kParts>(ws, part_ml, c0, c1, c0 * per >= pair0 ? 0 : 1, geo.G,
                                     out + head0 * D, kParts ? geo.own.o + head0 * D : nullptr,
-                                    kParts ? geo.own.ml + head0 : nullptr, row);
+                                    kParts ? geo.own.ml + head0 : nullptr);
     }
     S::sync();  // the merge buffers are free again
   }

@@ -4,67 +4,247 @@
 //     out[b][i][h] = sum_{j < T - n + 1 + i} softmax_j(scale q[b][i][h] . k_j) v_j,
 // k_j and v_j being c s of the codes and scales of the page (or a 16-bit page's values).
 //
-// Bound: HBM (9/32 of the bytes of 16-bit pages), so the kernel has 3.5 times fewer
-// cycles a key than the 16-bit one.  Its work split, merging and prologue are
-// decode_mma.cuh's, in shares at either head size; a warp's work on its keys is
-// decode_q4.cuh's.
+// Bound: HBM (9/32 of the bytes of 16-bit pages), with the instructions that a key takes
+// close behind: the kernel has 3.5 times fewer cycles a key than the 16-bit one.  A warp's
+// work on its keys is decode_q4.cuh's.
+//
+// Work split.  The keys of all (request, kv head) pairs are numbered in units of 32, a pair
+// having kLead more of them for its fixed cost, and every warp has an equal share of the
+// units, so that no warp waits for another before its share is done: a warp that comes to
+// the end of a pair writes its rows and goes on with the next one.  (With the CTA's warps on
+// one pair together, as in the 16-bit kernel, each change of pair cost it 5 us, a third of
+// the time of a batch of contexts of some thousand keys.)  Of a share, the first pair and
+// the last may be parts of one; these are joined in fixed order, the parts of a CTA's warps
+// through shared memory, those of several CTAs by the last of them to arrive (a counter per
+// cut pair in the pool's control block).
 #include "decode_q4.cuh"
 
 namespace gc {
 namespace {
 
-using dec::decode_cta;
+using dec::DecPiece;
+using dec::Joined;
 using dec::Keys4;
+
+constexpr int kLead = 1;      // units without keys in front of each pair's
+constexpr int kMinUnits = 2;  // of a warp's share, at least
 
 // Threads, resident CTAs and stages of shared memory of a variant.
 template <int D, int NT>
 struct Shape4 {
   static constexpr int kWarps = 8;
   static constexpr int kCtas = decode_ctas(D, 8 * NT);
-  static constexpr int kStages = 3;
-  static constexpr int kGroups = 1;
+  static constexpr int kStages = 2;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kHeads = 8 * NT;
-  static constexpr int kStride = D + 4;
+  static constexpr int kStride = D + 4;                              // floats of a head
   static constexpr int kRingBytes = 2 * kStages * dec::Stage4<D>::kBytes;  // of a warp
-  static constexpr int kRedFloats =
-      kWarps * kHeads * kStride > kWarps * kRingBytes / 4 ? kWarps * kHeads * kStride
-                                                          : kWarps * kRingBytes / 4;
-  __device__ static int group() { return 0; }
-  __device__ static int tid() { return static_cast<int>(threadIdx.x); }
-  __device__ static void sync() { __syncthreads(); }
+  static constexpr int kPartBytes = kHeads * kStride * 4;
+  static_assert(kPartBytes <= kRingBytes, "a warp's last part lies over its stages");
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
-    decode_q4_kernel(const __nv_bfloat16* q, const int32_t* block_table, const int32_t* seq_lens,
-                     __nv_bfloat16* out, float* ws, DecGeom geo, int32_t* status,
-                     int* merge_counters) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  dependent_begin();
-  decode_cta<Shape4<D, NT>, D, NT, false, false, false, Keys4<D, NT>>(
-      smem, dec::ByBlock{}, q, block_table, seq_lens, out, ws, geo, status, merge_counters);
+// Shared memory: the warps' stages, over which the warps' last parts are kept, their first
+// parts, maxima and sums of both, the pairs they belong to, and the requests' first units.
+template <typename S>
+size_t smem_bytes(int batch) {
+  return S::kWarps * (S::kRingBytes + S::kPartBytes + 2 * S::kHeads * sizeof(float2) +
+                      2 * sizeof(int)) +
+         (static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 
 template <int D, int NT>
-gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo,
+__global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
+    decode_q4_kernel(const __nv_bfloat16* q, const int32_t* seq_lens, __nv_bfloat16* out,
+                     float* ws, Dec4Geom geo, int32_t* status, int* merge_counters) {
+  using S = Shape4<D, NT>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* first_parts = reinterpret_cast<float*>(smem + S::kWarps * S::kRingBytes);
+  float2* mls = reinterpret_cast<float2*>(first_parts + S::kWarps * S::kHeads * S::kStride);
+  int* part_pairs = reinterpret_cast<int*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
+  int* start = part_pairs + 2 * S::kWarps;                                    // [batch + 1]
+  __shared__ int scan[S::kWarps], merge_flag;
+  dependent_begin();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int cta = blockIdx.x, warps = static_cast<int>(gridDim.x) * S::kWarps;
+
+  // the units of each request, exclusive scan; a length outside [tokens, block table
+  // capacity] is recorded
+  {
+    const int64_t cap = static_cast<int64_t>(geo.max_blocks) << geo.ps_shift;
+    int running = 0;
+    for (int b0 = 0; b0 < geo.batch; b0 += S::kThreads) {
+      const int b = b0 + tid;
+      int units = 0;
+      if (b < geo.batch) {
+        const int T = ld_plain(seq_lens + b);
+        if (T >= geo.tokens && T <= cap)
+          units = geo.Hkv * (kLead + ((T - 1) >> geo.unit_shift) + 1);
+        else if (cta == 0)
+          record_error(status, GC_ERR_OUT_OF_RANGE);
+      }
+      int incl = units;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 31) scan[warp] = incl;
+      __syncthreads();
+      int before = running;
+#pragma unroll
+      for (int i = 0; i < S::kWarps; ++i) {
+        if (i < warp) before += scan[i];
+        running += scan[i];
+      }
+      if (b < geo.batch) start[b] = before + incl - units;
+      __syncthreads();
+    }
+    if (tid == 0) start[geo.batch] = running;
+    if (tid < 2 * S::kWarps) part_pairs[tid] = -1;
+    __syncthreads();
+  }
+  const int total = start[geo.batch];
+  const int per = max(kMinUnits, (total + warps - 1) / warps);
+  const int cols = geo.G * geo.tokens;
+  // a pair's first output (and q) row, and a column's row from there
+  auto first_row = [&](int b, int g) {
+    return static_cast<int64_t>(b) * geo.tokens * geo.Hq + g * geo.G;
+  };
+  auto row = [&](int h) { return (h >> geo.g_shift) * geo.Hq + (h & (geo.G - 1)); };
+
+  // ---- this warp's units
+  const int mine = cta * S::kWarps + warp;
+  auto unit_of = [&](long long w) { return static_cast<int>(min(w * per, (long long)total)); };
+  const int end = unit_of(mine + 1);
+  for (int u = unit_of(mine); u < end;) {
+    DecPiece w;
+    w.b = dec::find_request(start, geo.batch, u);
+    const int T = ld_plain(seq_lens + w.b);
+    const int local = u - start[w.b], nu = (start[w.b + 1] - start[w.b]) / geo.Hkv;
+    w.g = local / nu;
+    // units of the pair, counted from its first one with keys
+    const int j = local - w.g * nu, last = min(nu, j + (end - u));
+    const int j0 = max(0, j - kLead), j1 = last - kLead, all = nu - kLead;
+    u += last - j;
+    if (j1 <= 0) break;  // the share ends in front of the pair's first key
+    w.k0 = j0 << geo.unit_shift;
+    w.k1 = j1 == all ? T : j1 << geo.unit_shift;
+    w.part = j0 == 0 && j1 == all ? -1 : j0 > 0 ? 0 : 1;
+    Keys4<D, NT> keys;
+    keys.template run<S::kStages>(
+        static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::kRingBytes, geo, w, T,
+        q + first_row(w.b, w.g) * D, status);
+    if (w.part < 0) {
+      keys.store(out + first_row(w.b, w.g) * D, cols, row);
+      continue;
+    }
+    // (the last part of a share lies over the warp's stages, which every lane has read)
+    __syncwarp();
+    keys.template keep<S::kStride>(
+        w.part ? reinterpret_cast<float*>(smem + warp * S::kRingBytes)
+               : first_parts + warp * S::kHeads * S::kStride,
+        mls + (2 * warp + w.part) * S::kHeads);
+    if (lane == 0) part_pairs[2 * warp + w.part] = w.b * geo.Hkv + w.g;
+  }
+  __syncthreads();
+
+  // ---- the parts of this CTA's warps joined, pair after pair
+  // partials of CTAs: O, then (reference maximum, sum), two to a CTA: of a pair that began
+  // before it, and of one that goes on after it
+  float2* ws_ml = reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
+  int cut[2] = {-1, -1};
+  for (int s0 = 0, s1; s0 < 2 * S::kWarps; s0 = s1) {
+    const int pair = part_pairs[s0];
+    s1 = s0 + 1;
+    if (pair < 0) continue;
+    while (s1 < 2 * S::kWarps && (part_pairs[s1] == pair || part_pairs[s1] < 0)) ++s1;
+    const int b = pair / geo.Hkv, g = pair - b * geo.Hkv;
+    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
+    const int w0 = (pair0 + kLead) / per, w1 = (pair0 + nu - 1) / per;  // warps with its keys
+    const bool before = w0 < cta * S::kWarps, after = w1 >= (cta + 1) * S::kWarps;
+    const int part = before ? 0 : 1;
+    if (before)
+      cut[0] = pair;
+    else if (after)
+      cut[1] = pair;
+    for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
+      const int h = x / (D / 4), d = 4 * (x % (D / 4));
+      Joined sum;
+      for (int s = s0; s < s1; ++s) {
+        if (part_pairs[s] < 0) continue;
+        const float* o = s & 1 ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
+                               : first_parts + (s >> 1) * S::kHeads * S::kStride;
+        sum.add(mls[s * S::kHeads + h], *reinterpret_cast<const float4*>(o + h * S::kStride + d));
+      }
+      if (!before && !after) {
+        sum.store(out + (first_row(b, g) + row(h)) * D + d);
+      } else {
+        const int64_t at = (static_cast<int64_t>(cta) * 2 + part) * S::kHeads + h;
+        *reinterpret_cast<float4*>(ws + at * D + d) = sum.o;
+        if (d == 0) ws_ml[at] = make_float2(sum.M, sum.L);
+      }
+    }
+  }
+  // ---- the last CTA with keys of a cut pair joins the CTAs' parts
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (cut[i] < 0) continue;  // (the same in every thread)
+    const int b = cut[i] / geo.Hkv, g = cut[i] - b * geo.Hkv;
+    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
+    const int c0 = (pair0 + kLead) / per / S::kWarps, c1 = (pair0 + nu - 1) / per / S::kWarps;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+      const int last = atomicAdd(merge_counters + c0, 1) == c1 - c0;
+      if (last) merge_counters[c0] = 0;
+      __threadfence();
+      merge_flag = last;
+    }
+    __syncthreads();
+    if (!merge_flag) continue;
+    for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
+      const int h = x / (D / 4), d = 4 * (x % (D / 4));
+      Joined sum;
+      for (int c = c0; c <= c1; c += 8) {
+        float2 ml[8];
+        float4 o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int64_t at = (static_cast<int64_t>(c + k) * 2 + (c + k == c0)) * S::kHeads + h;
+          ml[k] = c + k <= c1 ? __ldcg(ws_ml + at) : make_float2(dec::kNone, 0.f);
+          o[k] = c + k <= c1 ? __ldcg(reinterpret_cast<const float4*>(ws + at * D + d))
+                             : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum.add(ml[k], o[k]);
+      }
+      sum.store(out + (first_row(b, g) + row(h)) * D + d);
+    }
+  }
+}
+
+template <int D, int NT>
+gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const Dec4Geom& geo,
                  cudaStream_t stream) {
   using S = Shape4<D, NT>;
-  const size_t smem = decode_smem_bytes<S>(a.batch);
+  const size_t smem = smem_bytes<S>(a.batch);
   auto kernel = decode_q4_kernel<D, NT>;
-  cudaError_t e = cudaSuccess;
-  // a block gets 48 KB without asking, its static words (well below 1 KB) included
-  if (smem > 47 * 1024)
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem));
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   const int grid = min(S::kCtas * pool->num_sms, kMergeCounters);
   e = launch_dependent(kernel, grid, S::kThreads, smem, stream,
-                       static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.seq_lens,
+                       static_cast<const __nv_bfloat16*>(a.q), a.seq_lens,
                        static_cast<__nv_bfloat16*>(a.out), static_cast<float*>(a.workspace), geo,
                        pool->status, pool->merge_counters);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   return GC_OK;
+}
+
+int ilog2(int x) {
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
 }
 
 }  // namespace
@@ -76,6 +256,7 @@ size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads, in
 
 gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4Cache& cache,
                            int32_t tokens, cudaStream_t stream) {
+  const auto& cfg = pool->cfg;
   gc_status st = check_decode(pool, a);
   if (st != GC_OK) return st;
   const size_t need = decode_q4_workspace_bytes(pool, a.num_q_heads, tokens);
@@ -83,23 +264,40 @@ gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4
     return fail(GC_ERR_INVALID_ARG,
                 "%s: workspace of %zu bytes needed (gc_paged_decode_q4_workspace_bytes), got %zu",
                 a.who, need, a.workspace_bytes);
-  // the work is numbered in units of keys with 32-bit ints (decode_units)
-  const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
-  const long long units =
-      static_cast<long long>(a.batch) * pool->cfg.num_kv_heads * ((cap + 127) / 128);
-  if (units + 2LL * pool->num_sms > 2147483647LL)
-    return fail(GC_ERR_UNSUPPORTED, "%s: %lld work items", a.who, units);
-  DecGeom geo = decode_geom(pool, a, nullptr, nullptr);
-  geo.q4_cache = cache.data;
-  geo.q4_table = cache.table;
-  geo.q4_pages = cache.pages;
-  geo.q4_page = static_cast<uint32_t>(
-      geo.Hkv * q4_head_bytes(pool->cfg.head_dim, pool->cfg.page_size));
-  geo.q4_plane = static_cast<int64_t>(cache.pages) * geo.q4_page;
+  Dec4Geom geo;
+  geo.batch = a.batch;
+  geo.Hq = a.num_q_heads;
+  geo.Hkv = cfg.num_kv_heads;
+  geo.G = geo.Hq / geo.Hkv;
+  geo.g_shift = ilog2(geo.G);
   geo.tokens = tokens;
-  while ((1 << geo.g_shift) < geo.G) ++geo.g_shift;
+  geo.ps = cfg.page_size;
+  geo.ps_shift = ilog2(cfg.page_size);
+  geo.num_pages = cfg.num_pages;
+  geo.q4_pages = cache.pages;
+  geo.max_blocks = a.max_blocks;
+  geo.scale_log2 = a.softmax_scale * 1.4426950408889634f;
+  const uint64_t head = q4_head_bytes(cfg.head_dim, cfg.page_size);
+  geo.q4_page = static_cast<uint32_t>(geo.Hkv * head);
+  geo.q4_plane = static_cast<int64_t>(cache.pages) * geo.q4_page;
+  geo.plane16 = static_cast<int64_t>(cfg.num_pages * page_bytes(cfg));
+  geo.q4_k = cache.data + 2 * a.layer * geo.q4_plane;
+  geo.pool_k = pool->data + 2 * a.layer * geo.plane16;
+  geo.q4_table = cache.table;
+  geo.block_table = a.block_table;
+  // units are numbered with 32-bit ints, with a margin for the shares' rounding
+  const int64_t cap = static_cast<int64_t>(a.max_blocks) * cfg.page_size;
+  const int64_t pairs = static_cast<int64_t>(a.batch) * geo.Hkv;
+  const int64_t margin = 1 << 16;
+  geo.unit_shift = 5;
+  while (geo.unit_shift < 12 &&
+         pairs * (((cap - 1) >> geo.unit_shift) + 1 + kLead) > INT32_MAX - margin)
+    ++geo.unit_shift;
+  if (pairs * (((cap - 1) >> geo.unit_shift) + 1 + kLead) > INT32_MAX - margin)
+    return fail(GC_ERR_UNSUPPORTED, "%s: %lld pairs of up to %lld keys", a.who,
+                static_cast<long long>(pairs), static_cast<long long>(cap));
   const bool narrow = geo.G * tokens <= 8;
-  if (pool->cfg.head_dim == 128)
+  if (cfg.head_dim == 128)
     return narrow ? launch<128, 1>(pool, a, geo, stream) : launch<128, 2>(pool, a, geo, stream);
   return narrow ? launch<64, 1>(pool, a, geo, stream) : launch<64, 2>(pool, a, geo, stream);
 }

@@ -20,6 +20,21 @@
 #include "q4_format.cuh"
 
 namespace gc {
+
+// A call's sizes and where its keys are.
+struct Dec4Geom {
+  int32_t batch, Hq, Hkv, G, g_shift, tokens, ps, ps_shift, num_pages, q4_pages, max_blocks;
+  int32_t unit_shift;  // keys per unit of work, log2 (at least 5)
+  float scale_log2;
+  uint32_t q4_page;     // bytes of a 4-bit page's plane
+  int64_t q4_plane;     // of all of them
+  int64_t plane16;      // bytes of the pool's plane
+  const uint8_t* q4_k;  // the layer's K
+  const uint8_t* pool_k;
+  const int32_t* q4_table;
+  const int32_t* block_table;
+};
+
 namespace {
 namespace dec {
 
@@ -149,7 +164,7 @@ struct Keys4 {
     }
   }
 
-  __device__ __forceinline__ void load_q(const __nv_bfloat16* q_g, const DecGeom& geo) {
+  __device__ __forceinline__ void load_q(const __nv_bfloat16* q_g, const Dec4Geom& geo) {
     constexpr uint32_t all = 0xffffffffu;
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     const int cols = geo.G * geo.tokens;
@@ -285,7 +300,7 @@ struct Keys4 {
   // The column of token i of the request's last `tokens` sees the keys below
   // n - (tokens - 1 - i).
   __device__ __forceinline__ void mask(float (&s)[NT][4], const Parts4<D>& mine, int n,
-                                       const DecGeom& geo) const {
+                                       const Dec4Geom& geo) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -426,7 +441,7 @@ struct Keys4 {
   template <typename Look>
   __device__ __forceinline__ void one(uint32_t from, uint32_t key, int h, uint32_t ready, int T,
                                       uint32_t k1, const Parts4<D>& mine, const Look& look,
-                                      int64_t plane16, const DecGeom& geo) {
+                                      const Dec4Geom& geo) {
     key += h * kGroup;
     from += h * Stage4<D>::kBytes;
     if (key >= k1) return;
@@ -445,23 +460,19 @@ struct Keys4 {
     if (four)
       values<true>(from, mine, n, s[0]);
     else
-      values16(kp + plane16, n, s[0]);
+      values16(kp + geo.plane16, n, s[0]);
   }
 
-  // The pairs of groups first, first + every, ... of piece w of a request of T keys, to O,
-  // reference maxima and sums as decode_cta merges them.  `ring`: the warp's kStages stages
-  // in shared memory, each for a pair.
+  // The keys of piece w of a request of T keys, two groups at a time, to O, reference
+  // maxima and sums.  `ring`: the warp's kStages stages in shared memory, each for a pair.
   template <int kStages>
-  __device__ __forceinline__ void run(uint32_t ring, const DecGeom& geo, const DecPiece& w, int T,
-                                      int first, int every, const __nv_bfloat16* q_g,
-                                      const uint8_t* pool_k, int64_t plane16,
-                                      const int32_t* block_table, int32_t* status) {
-    constexpr uint32_t kStage = 2 * Stage4<D>::kBytes;
+  __device__ __forceinline__ void run(uint32_t ring, const Dec4Geom& geo, const DecPiece& w, int T,
+                                      const __nv_bfloat16* q_g, int32_t* status) {
+    constexpr uint32_t kStage = 2 * Stage4<D>::kBytes, step = 2 * kGroup;
     const int lane = threadIdx.x & 31;
+    // (unsigned: look-ups run past a piece that may end near 2^31)
     const uint32_t k1 = static_cast<uint32_t>(w.k1), slots = static_cast<uint32_t>(geo.ps - 1);
-    // K of the layer and head
-    const uint8_t* q4_k = geo.q4_cache + geo.layer * 2 * geo.q4_plane +
-                          static_cast<uint64_t>(w.g) * q4_head_bytes(D, geo.ps);
+    const uint8_t* q4_k = geo.q4_k + static_cast<uint64_t>(w.g) * q4_head_bytes(D, geo.ps);
     // The 4-bit page of a key, -1: in 16 bits (wide: its row of K there), bad, or past the
     // piece.
     auto look = [&](uint32_t key, const uint8_t** wide = nullptr) -> int {
@@ -469,19 +480,17 @@ struct Keys4 {
       const int64_t e = static_cast<int64_t>(w.b) * geo.max_blocks + (key >> geo.ps_shift);
       const int p4 = ld_plain(geo.q4_table + e);
       if (p4 >= 0 && p4 < geo.q4_pages) return p4;
-      const int page = p4 < 0 ? ld_plain(block_table + e) : -1;
+      const int page = p4 < 0 ? ld_plain(geo.block_table + e) : -1;
       if (page < 0 || page >= geo.num_pages)
         record_error(status, GC_ERR_OUT_OF_RANGE);
       else if (wide)
-        *wide = pool_k +
+        *wide = geo.pool_k +
                 ((static_cast<int64_t>(page) * geo.Hkv + w.g) * geo.ps + (key & slots)) * D * 2;
       return -1;
     };
     // A window of 16 pairs is looked up at once, lane i a group of pair i / 2, and the next
     // one ahead of its use.
-    const uint32_t step = static_cast<uint32_t>(every) * 2 * kGroup;
-    const uint32_t key0 = static_cast<uint32_t>(w.k0) + static_cast<uint32_t>(first) * 2 * kGroup;
-    const uint32_t mine_in = static_cast<uint32_t>(lane >> 1) * step + (lane & 1) * kGroup;
+    const uint32_t key0 = static_cast<uint32_t>(w.k0), mine_in = static_cast<uint32_t>(lane) * kGroup;
     int cur = look(key0 + mine_in);
     int nxt = key0 + 16 * step < k1 ? look(key0 + 16 * step + mine_in) : -1;
     const Parts4<D> mine;
@@ -533,7 +542,7 @@ struct Keys4 {
         values<false>(from + Stage4<D>::kBytes, mine, kGroup, s[1]);
       } else {
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, look, plane16, geo);
+        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, look, geo);
       }
       from = from + kStage == end ? ring : from + kStage;
     }
@@ -541,13 +550,78 @@ struct Keys4 {
     // the powers of two leave: 2^(kPBias - 133) of O, 16 of its rows r + 8, 2^kPBias of l
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      l[t][0] *= pow2(-90), l[t][1] *= pow2(-90);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        l[t][x] *= pow2(-90);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[t][x] += __shfl_xor_sync(0xffffffffu, l[t][x], d);
+      }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         o[t][i][0] *= pow2(43), o[t][i][1] *= pow2(43);
         o[t][i][2] *= pow2(39), o[t][i][3] *= pow2(39);
       }
     }
+  }
+
+  // Four columns 32 g + 4 r ... of the head of tile t, column 2 c + x.
+  __device__ __forceinline__ float4 four(int t, int g, int x) const {
+    return make_float4(o[t][2 * g][x], o[t][2 * g][x + 2], o[t][2 * g + 1][x],
+                       o[t][2 * g + 1][x + 2]);
+  }
+  // The whole context's rows; row(h): the output row of column h, from out's first.
+  template <typename Row>
+  __device__ __forceinline__ void store(__nv_bfloat16* out, int cols, const Row& row) const {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int h = 8 * t + 2 * c + x;
+        if (h >= cols) continue;
+        const float inv = 1.f / l[t][x];
+        __nv_bfloat16* to = out + static_cast<int64_t>(row(h)) * D + 4 * r;
+#pragma unroll
+        for (int g = 0; g < GR; ++g) {
+          const float4 v = four(t, g, x);
+          *reinterpret_cast<uint2*>(to + 32 * g) =
+              make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+        }
+      }
+  }
+  // A part of one: O [heads][kStride], reference maxima and sums.
+  template <int kStride>
+  __device__ __forceinline__ void keep(float* part, float2* ml) const {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int h = 8 * t + 2 * c + x;
+#pragma unroll
+        for (int g = 0; g < GR; ++g)
+          *reinterpret_cast<float4*>(part + h * kStride + 32 * g + 4 * r) = four(t, g, x);
+        if (r == 0) ml[h] = make_float2(m[t][x], l[t][x]);
+      }
+  }
+};
+
+// Parts joined one by one: O 2^(m - M) and sums, relative to the largest maximum yet.
+struct Joined {
+  float M = kNone, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(float2 ml, float4 v) {
+    const float top = fmaxf(M, ml.x);
+    const float a = ex2_approx(M - top), b = ex2_approx(ml.x - top);
+    M = top;
+    L = fmaf(L, a, ml.y * b);
+    o.x = fmaf(o.x, a, v.x * b), o.y = fmaf(o.y, a, v.y * b);
+    o.z = fmaf(o.z, a, v.z * b), o.w = fmaf(o.w, a, v.w * b);
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* to) const {
+    const float inv = 1.f / L;
+    *reinterpret_cast<uint2*>(to) =
+        make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
   }
 };
 
