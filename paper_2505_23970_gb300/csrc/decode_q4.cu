@@ -26,7 +26,7 @@ using dec::DecPiece;
 using dec::Joined;
 using dec::Keys4;
 
-constexpr int kLead = 1;      // units without keys in front of each pair's
+constexpr int kLead = 4;      // units without keys in front of each pair's
 constexpr int kMinUnits = 2;  // of a warp's share, at least
 
 // Threads, resident CTAs and stages of shared memory of a variant.
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
   float2* mls = reinterpret_cast<float2*>(first_parts + S::kWarps * S::kHeads * S::kStride);
   int* part_pairs = reinterpret_cast<int*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
   int* start = part_pairs + 2 * S::kWarps;                                    // [batch + 1]
-  __shared__ int scan[S::kWarps], merge_flag;
+  __shared__ int scan[S::kWarps], merge_flag[2];
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = blockIdx.x, warps = static_cast<int>(gridDim.x) * S::kWarps;
@@ -186,22 +186,32 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
     }
   }
   // ---- the last CTA with keys of a cut pair joins the CTAs' parts
+  if (cut[0] < 0 && cut[1] < 0) return;  // (the same in every thread)
+  auto ctas_of = [&](int pair, int& c0, int& c1) {
+    const int b = pair / geo.Hkv, g = pair - b * geo.Hkv;
+    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
+    c0 = (pair0 + kLead) / per / S::kWarps;
+    c1 = (pair0 + nu - 1) / per / S::kWarps;
+  };
+  __syncthreads();
+  // (the barrier has the CTA's parts before the fence of the one thread that counts)
+  if ((tid == 0 && cut[0] >= 0) || (tid == 32 && cut[1] >= 0)) {
+    const int i = tid >> 5;
+    int c0, c1;
+    ctas_of(i ? cut[1] : cut[0], c0, c1);
+    __threadfence();
+    const int last = atomicAdd(merge_counters + c0, 1) == c1 - c0;
+    if (last) merge_counters[c0] = 0;
+    __threadfence();
+    merge_flag[i] = last;
+  }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (cut[i] < 0) continue;  // (the same in every thread)
+    if (cut[i] < 0 || !merge_flag[i]) continue;
     const int b = cut[i] / geo.Hkv, g = cut[i] - b * geo.Hkv;
-    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
-    const int c0 = (pair0 + kLead) / per / S::kWarps, c1 = (pair0 + nu - 1) / per / S::kWarps;
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
-      const int last = atomicAdd(merge_counters + c0, 1) == c1 - c0;
-      if (last) merge_counters[c0] = 0;
-      __threadfence();
-      merge_flag = last;
-    }
-    __syncthreads();
-    if (!merge_flag) continue;
+    int c0, c1;
+    ctas_of(cut[i], c0, c1);
     for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
       const int h = x / (D / 4), d = 4 * (x % (D / 4));
       Joined sum;
