@@ -767,13 +767,14 @@ GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t
  *                GC_ERR_OUT_OF_RANGE.  Keys at or past it are never used.
  *   workspace    device scratch of gc_paged_decode_q4_workspace_bytes bytes for
  *                the same arguments, with the rules of gc_paged_decode_attn's.
- * K, V and q may have any finite values of bf16 up to 2^60 in magnitude; the
- * cache's own values are far below that.  Calls on one pool must not overlap on
+ * Powers of two inside the kernel leave room for |q| up to 2^100 and, in 16-bit
+ * pages, |K| up to 2^60; beyond that a row may become NaN.  Calls on one pool must not overlap on
  * the GPU with each other or with the other attention calls.  The same call gives
  * the same bits again; the order of its sums depends on the lengths in the call.
  * Errors: as gc_paged_decode_attn; GC_ERR_INVALID_ARG also for n_q4_pages < 0,
  * tokens < 1, a NULL q4_table (or q4_cache with n_q4_pages > 0), a misaligned
- * q4_cache; GC_ERR_UNSUPPORTED for tokens * Hq/Hkv > 16. */
+ * q4_cache; GC_ERR_UNSUPPORTED for tokens * Hq/Hkv > 16, softmax_scale > 8192,
+ * and sizes past 32-bit numbering. */
 GC_API size_t gc_paged_decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
                                                  int32_t max_blocks_per_seq, int32_t num_q_heads,
                                                  int32_t tokens);

@@ -81,21 +81,14 @@ __device__ __forceinline__ void kv_rows(Place* places, int block, int blocks, co
     const int64_t t = t0 + tl;
     const bool is_k = h < g.Hkv;
     if (!is_k) h -= g.Hkv;
-    uint4 x[GR], y[GR];
+    uint4 x[GR];
 #pragma unroll
-    for (int i = 0; i < GR; ++i) x[i] = y[i] = make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < GR; ++i) x[i] = make_uint4(0, 0, 0, 0);
+    const uint4* src =
+        (is_k ? k_new + t * g.k_stride : v_new + t * g.v_stride) + h * (4 * GR) + q;
     if (t < g.total_new) {
-      const uint4* src =
-          (is_k ? k_new + t * g.k_stride : v_new + t * g.v_stride) + h * (4 * GR) + q;
 #pragma unroll
       for (int i = 0; i < GR; ++i) x[i] = ld_plain(src + 4 * i);
-      if (is_k && !g.interleaved) {
-#pragma unroll
-        for (int i = 0; i < GR; ++i) {
-          const int c0 = 32 * i + 8 * q;
-          if (c0 < rot) y[i] = ld_plain(src + 4 * i + (c0 < half ? half : -half) / 8);
-        }
-      }
     }
     const int last = static_cast<int>(base - t0 * heads) + kRows - 1;
     look_up_all<kLanes>(places, t0, last / heads + 1, g, table, prefix_lens, cu_new_lens,
@@ -114,7 +107,8 @@ __device__ __forceinline__ void kv_rows(Place* places, int block, int blocks, co
         } else {
           const bool second = c0 >= half;
           const float4* c = reinterpret_cast<const float4*>(cs + c0 - (second ? half : 0));
-          halves8(x[i], y[i], second ? 1.f : -1.f, c, c + half / 4);
+          const uint4 y = ld_plain(src + 4 * i + (second ? -half : half) / 8);
+          halves8(x[i], y, second ? 1.f : -1.f, c, c + half / 4);
         }
       }
     }
@@ -193,8 +187,11 @@ __device__ __forceinline__ void q_units(Place* places, int block, int blocks, co
   }
 }
 
+// (Five blocks an SM: the registers that the rows of k and v would take otherwise leave
+// room for three, and too few loads of q are under way then: 8 x 1024 tokens of 64/8 heads
+// of 128 take 73 us, four blocks 62, five 57, six, with spills, 58.)
 template <int GR, int W>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kBlock, 5)
     append_q4_kernel(const uint4* q, uint4* q_out, const uint4* k_new, const uint4* v_new,
                      Q4Geom q4, const int32_t* table, const int32_t* prefix_lens,
                      const int32_t* cu_new_lens, const float* cos_sin, const int32_t* positions,
@@ -251,7 +248,7 @@ gc_status launch_append_q4(const gc_kv_pool* pool, const RopeArgs& a, const Q4Ca
                    static_cast<int64_t>(pool->num_sms) * 2048;
   const int W = few ? 1 : 2;
   g.threads = (g.Hq + W - 1) / W << g.head_shift;
-  const int64_t cap = static_cast<int64_t>(pool->num_sms) * 16;
+  const int64_t cap = static_cast<int64_t>(pool->num_sms) * 32;
   const int64_t kv = (static_cast<int64_t>(g.total_new) * 2 * g.Hkv + kRows - 1) / kRows;
   const int64_t qs = (static_cast<int64_t>(g.total_new) * g.threads + kBlock - 1) / kBlock;
   const int kv_blocks = static_cast<int>(kv < cap ? kv : cap);

@@ -43,13 +43,20 @@ struct Shape4 {
   static_assert(kPartBytes <= kRingBytes, "a warp's last part lies over its stages");
 };
 
+// What a warp's part is of: a pair (request, kv head; -1: no part), and the CTAs with keys of
+// the pair.
+struct Part {
+  int b, g, c0, c1;
+};
+
 // Shared memory: the warps' stages, over which the warps' last parts are kept, their first
-// parts, maxima and sums of both, the pairs they belong to, and the requests' first units.
+// parts, maxima and sums of both, what they are of, and the requests' first units and
+// lengths.
 template <typename S>
 size_t smem_bytes(int batch) {
   return S::kWarps * (S::kRingBytes + S::kPartBytes + 2 * S::kHeads * sizeof(float2) +
-                      2 * sizeof(int)) +
-         (static_cast<size_t>(batch) + 1) * sizeof(int);
+                      2 * sizeof(Part)) +
+         (2 * static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 
 template <int D, int NT>
@@ -60,8 +67,9 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
   extern __shared__ __align__(16) uint8_t smem[];
   float* first_parts = reinterpret_cast<float*>(smem + S::kWarps * S::kRingBytes);
   float2* mls = reinterpret_cast<float2*>(first_parts + S::kWarps * S::kHeads * S::kStride);
-  int* part_pairs = reinterpret_cast<int*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
-  int* start = part_pairs + 2 * S::kWarps;                                    // [batch + 1]
+  Part* parts = reinterpret_cast<Part*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
+  int* start = reinterpret_cast<int*>(parts + 2 * S::kWarps);              // [batch + 1]
+  int* lens = start + geo.batch + 1;                                       // [batch]
   __shared__ int scan[S::kWarps], merge_flag[2];
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -81,6 +89,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
           units = geo.Hkv * (kLead + ((T - 1) >> geo.unit_shift) + 1);
         else if (cta == 0)
           record_error(status, GC_ERR_OUT_OF_RANGE);
+        lens[b] = T;
       }
       int incl = units;
 #pragma unroll
@@ -100,7 +109,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
       __syncthreads();
     }
     if (tid == 0) start[geo.batch] = running;
-    if (tid < 2 * S::kWarps) part_pairs[tid] = -1;
+    if (tid < 2 * S::kWarps) parts[tid].b = -1;
     __syncthreads();
   }
   const int total = start[geo.batch];
@@ -119,7 +128,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
   for (int u = unit_of(mine); u < end;) {
     DecPiece w;
     w.b = dec::find_request(start, geo.batch, u);
-    const int T = ld_plain(seq_lens + w.b);
+    const int T = lens[w.b];
     const int local = u - start[w.b], nu = (start[w.b + 1] - start[w.b]) / geo.Hkv;
     w.g = local / nu;
     // units of the pair, counted from its first one with keys
@@ -144,7 +153,11 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
         w.part ? reinterpret_cast<float*>(smem + warp * S::kRingBytes)
                : first_parts + warp * S::kHeads * S::kStride,
         mls + (2 * warp + w.part) * S::kHeads);
-    if (lane == 0) part_pairs[2 * warp + w.part] = w.b * geo.Hkv + w.g;
+    if (lane == 0) {
+      const int pair0 = start[w.b] + w.g * nu;
+      parts[2 * warp + w.part] = Part{w.b, w.g, (pair0 + kLead) / (per * S::kWarps),
+                                      (pair0 + nu - 1) / (per * S::kWarps)};
+    }
   }
   __syncthreads();
 
@@ -152,32 +165,30 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
   // partials of CTAs: O, then (reference maximum, sum), two to a CTA: of a pair that began
   // before it, and of one that goes on after it
   float2* ws_ml = reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
-  int cut[2] = {-1, -1};
+  Part cut[2] = {{-1, 0, 0, 0}, {-1, 0, 0, 0}};
   for (int s0 = 0, s1; s0 < 2 * S::kWarps; s0 = s1) {
-    const int pair = part_pairs[s0];
+    const Part of = parts[s0];
     s1 = s0 + 1;
-    if (pair < 0) continue;
-    while (s1 < 2 * S::kWarps && (part_pairs[s1] == pair || part_pairs[s1] < 0)) ++s1;
-    const int b = pair / geo.Hkv, g = pair - b * geo.Hkv;
-    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
-    const int w0 = (pair0 + kLead) / per, w1 = (pair0 + nu - 1) / per;  // warps with its keys
-    const bool before = w0 < cta * S::kWarps, after = w1 >= (cta + 1) * S::kWarps;
+    if (of.b < 0) continue;
+    for (; s1 < 2 * S::kWarps; ++s1)
+      if (parts[s1].b >= 0 && (parts[s1].b != of.b || parts[s1].g != of.g)) break;
+    const bool before = of.c0 < cta, after = of.c1 > cta;
     const int part = before ? 0 : 1;
     if (before)
-      cut[0] = pair;
+      cut[0] = of;
     else if (after)
-      cut[1] = pair;
+      cut[1] = of;
     for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
       const int h = x / (D / 4), d = 4 * (x % (D / 4));
       Joined sum;
       for (int s = s0; s < s1; ++s) {
-        if (part_pairs[s] < 0) continue;
+        if (parts[s].b < 0) continue;
         const float* o = s & 1 ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
                                : first_parts + (s >> 1) * S::kHeads * S::kStride;
         sum.add(mls[s * S::kHeads + h], *reinterpret_cast<const float4*>(o + h * S::kStride + d));
       }
       if (!before && !after) {
-        sum.store(out + (first_row(b, g) + row(h)) * D + d);
+        sum.store(out + (first_row(of.b, of.g) + row(h)) * D + d);
       } else {
         const int64_t at = (static_cast<int64_t>(cta) * 2 + part) * S::kHeads + h;
         *reinterpret_cast<float4*>(ws + at * D + d) = sum.o;
@@ -186,32 +197,22 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
     }
   }
   // ---- the last CTA with keys of a cut pair joins the CTAs' parts
-  if (cut[0] < 0 && cut[1] < 0) return;  // (the same in every thread)
-  auto ctas_of = [&](int pair, int& c0, int& c1) {
-    const int b = pair / geo.Hkv, g = pair - b * geo.Hkv;
-    const int nu = (start[b + 1] - start[b]) / geo.Hkv, pair0 = start[b] + g * nu;
-    c0 = (pair0 + kLead) / per / S::kWarps;
-    c1 = (pair0 + nu - 1) / per / S::kWarps;
-  };
+  if (cut[0].b < 0 && cut[1].b < 0) return;  // (the same in every thread)
   __syncthreads();
   // (the barrier has the CTA's parts before the fence of the one thread that counts)
-  if ((tid == 0 && cut[0] >= 0) || (tid == 32 && cut[1] >= 0)) {
-    const int i = tid >> 5;
-    int c0, c1;
-    ctas_of(i ? cut[1] : cut[0], c0, c1);
+  if ((tid == 0 && cut[0].b >= 0) || (tid == 32 && cut[1].b >= 0)) {
+    const Part of = tid ? cut[1] : cut[0];
     __threadfence();
-    const int last = atomicAdd(merge_counters + c0, 1) == c1 - c0;
-    if (last) merge_counters[c0] = 0;
+    const int last = atomicAdd(merge_counters + of.c0, 1) == of.c1 - of.c0;
+    if (last) merge_counters[of.c0] = 0;
     __threadfence();
-    merge_flag[i] = last;
+    merge_flag[tid >> 5] = last;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (cut[i] < 0 || !merge_flag[i]) continue;
-    const int b = cut[i] / geo.Hkv, g = cut[i] - b * geo.Hkv;
-    int c0, c1;
-    ctas_of(cut[i], c0, c1);
+    if (cut[i].b < 0 || !merge_flag[i]) continue;
+    const int c0 = cut[i].c0, c1 = cut[i].c1;
     for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
       const int h = x / (D / 4), d = 4 * (x % (D / 4));
       Joined sum;
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum.add(ml[k], o[k]);
       }
-      sum.store(out + (first_row(b, g) + row(h)) * D + d);
+      sum.store(out + (first_row(cut[i].b, cut[i].g) + row(h)) * D + d);
     }
   }
 }
@@ -295,6 +296,9 @@ gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4
   geo.pool_k = pool->data + 2 * a.layer * geo.plane16;
   geo.q4_table = cache.table;
   geo.block_table = a.block_table;
+  if (geo.Hkv * head > UINT32_MAX)
+    return fail(GC_ERR_UNSUPPORTED, "%s: pages of %llu bytes", a.who,
+                static_cast<unsigned long long>(geo.Hkv * head));
   // units are numbered with 32-bit ints, with a margin for the shares' rounding
   const int64_t cap = static_cast<int64_t>(a.max_blocks) * cfg.page_size;
   const int64_t pairs = static_cast<int64_t>(a.batch) * geo.Hkv;

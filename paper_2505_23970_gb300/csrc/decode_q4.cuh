@@ -164,24 +164,31 @@ struct Keys4 {
     }
   }
 
-  __device__ __forceinline__ void load_q(const __nv_bfloat16* q_g, const Dec4Geom& geo) {
-    constexpr uint32_t all = 0xffffffffu;
+  // The columns as they are: 32 g + 8 c ... + 7 of column 8 t + r.
+  __device__ __forceinline__ void load_q(const __nv_bfloat16* q_g, const Dec4Geom& geo,
+                                         uint4 (&w)[NT][GR]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    const int cols = geo.G * geo.tokens;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int h = 8 * t + r;
-      uint4 w[GR];
-      uint32_t top = 0;
+      const int64_t row = (h >> geo.g_shift) * geo.Hq + (h & (geo.G - 1));
 #pragma unroll
       for (int g = 0; g < GR; ++g) {
-        w[g] = make_uint4(0, 0, 0, 0);
-        if (h < cols) {
-          const int64_t row = (h >> geo.g_shift) * geo.Hq + (h & (geo.G - 1));
-          w[g] = ld_plain(reinterpret_cast<const uint4*>(q_g + row * D) + 4 * g + c);
-        }
-        top = max(top, q4::abs_max8(w[g]));
+        w[t][g] = make_uint4(0, 0, 0, 0);
+        if (h < geo.G * geo.tokens)
+          w[t][g] = ld_plain(reinterpret_cast<const uint4*>(q_g + row * D) + 4 * g + c);
       }
+    }
+  }
+  __device__ __forceinline__ void set_q(const uint4 (&all_w)[NT][GR], const Dec4Geom& geo) {
+    constexpr uint32_t all = 0xffffffffu;
+    const int c = threadIdx.x & 3;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint4(&w)[GR] = all_w[t];
+      uint32_t top = 0;
+#pragma unroll
+      for (int g = 0; g < GR; ++g) top = max(top, q4::abs_max8(w[g]));
       top = max(top, __shfl_xor_sync(all, top, 1));
       top = max(top, __shfl_xor_sync(all, top, 2));
       // (a column of zeros, or with a NaN or infinity, stays as it is; 20 keeps the scale
@@ -491,15 +498,16 @@ struct Keys4 {
     // A window of 16 pairs is looked up at once, lane i a group of pair i / 2, and the next
     // one ahead of its use.
     const uint32_t key0 = static_cast<uint32_t>(w.k0), mine_in = static_cast<uint32_t>(lane) * kGroup;
+    uint4 q_words[NT][GR];
+    load_q(q_g, geo, q_words);
     int cur = look(key0 + mine_in);
-    int nxt = key0 + 16 * step < k1 ? look(key0 + 16 * step + mine_in) : -1;
     const Parts4<D> mine;
     // Pairs are copied kStages - 1 before their turn, into the stage whose reader of the round
     // before is done in every lane.  Bits 2 j, 2 j + 1 of `ready`: the groups of pair j from
     // now on are in 4 bits.
     const uint32_t end = ring + kStages * kStage;
     uint32_t to = ring, ahead = key0, ready = 0;
-    int ahead_i = 0;
+    int ahead_i = 0, nxt = -1;
     auto fetch = [&]() {
       ready >>= 2;
       if (ahead_i == 32) {
@@ -523,8 +531,10 @@ struct Keys4 {
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
     for (int i = 0; i < kStages - 1; ++i) fetch();
+    static_assert(kStages <= 16, "the first window has the first stages' pairs");
+    if (key0 + 16 * step < k1) nxt = look(key0 + 16 * step + mine_in);
     reset();
-    load_q(q_g, geo);
+    set_q(q_words, geo);
     uint32_t from = ring;
     // keys below this are seen by every column
     const uint32_t seen = min(k1, static_cast<uint32_t>(T - geo.tokens + 1));

@@ -932,6 +932,8 @@ gc_status gc_paged_decode_attn_q4(const void* q, const gc_kv_pool* pool,
   const int G = num_q_heads / hkv;
   if (G != 1 && G != 2 && G != 4 && G != 8 && G != 16)
     return fail(GC_ERR_UNSUPPORTED, "%s: q heads per kv head %d not in {1,2,4,8,16}", who, G);
+  if (softmax_scale > 8192.0f && softmax_scale < __builtin_inff())
+    return fail(GC_ERR_UNSUPPORTED, "%s: softmax_scale above 8192", who);
   if (tokens < 1) return fail(GC_ERR_INVALID_ARG, "%s: tokens %d < 1", who, tokens);
   if (tokens > 16 / G)
     return fail(GC_ERR_UNSUPPORTED, "%s: %d tokens of %d q heads per kv head (at most 16 rows)", who,

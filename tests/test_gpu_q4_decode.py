@@ -120,6 +120,33 @@ def test_sizes_of_values(size, q_size):
     assert ctx.pool.check() == gcb.GC_OK
 
 
+def test_columns_far_apart():
+    """Columns of q that differ by up to 2^30 within a head: each product is exact."""
+    ctx = _q4.Context([700, 40], 2, 128, 16, recent=1, seed=12)
+    bits = wl.normal_bf16(12, 71, (2, 1, 8, 128))
+    size = 2.0 ** -np.random.default_rng(12).integers(0, 31, (1, 1, 8, 128)).astype(np.float32)
+    bits = wl.f32_to_bf16_bits((_q4.f32(bits) * size * 8).astype(np.float32))
+    Decode(ctx, 8, q_bits=bits).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
+@pytest.mark.parametrize("q_exp,k_exp", [(100, 0), (-110, 0), (40, 58), (3, -60)])
+def test_the_ends_of_the_range(q_exp, k_exp):
+    """|q| up to 2^100, keys of 16-bit pages up to 2^60, with scales that bring the scores
+    back to the size of one (those of the other pages are then near 0 or one key's)."""
+    ctx = _q4.Context([90], 1, 64, 16, recent=100 if k_exp else 0, seed=13)
+    if k_exp:
+        import torch
+        k = _q4.f32(ctx.bits16[0, 0]) * np.float32(2.0 ** k_exp)
+        ctx.bits16[0, 0] = wl.f32_to_bf16_bits(k.astype(np.float32))
+        ctx.pool.planes().copy_(bf16_tensor(ctx.bits16))
+    q = _q4.f32(wl.normal_bf16(13, 71, (1, 1, 4, 64))) / 4
+    bits = wl.f32_to_bf16_bits((q * np.float32(2.0 ** q_exp)).astype(np.float32))
+    scale = float(np.float32(2.0 ** (-q_exp - k_exp)))
+    Decode(ctx, 4, q_bits=bits, scale=min(scale, 8192.0)).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
 def test_scores_that_keep_rising():
     """Each group of keys far above the ones before: the reference maximum is raised."""
     ctx = _q4.Context([640], 1, 128, 16, seed=3)
@@ -208,7 +235,7 @@ def test_refusals():
         refused(gcb.GC_ERR_INVALID_ARG, d, **change)
     refused(gcb.GC_ERR_OUT_OF_RANGE, d, layer=1)
     for change in (dict(tokens=5), dict(num_q_heads=24), dict(batch=8193),
-                   dict(max_blocks_per_seq=2 ** 28)):
+                   dict(max_blocks_per_seq=2 ** 28), dict(softmax_scale=8193.0)):
         refused(gcb.GC_ERR_UNSUPPORTED, d, **change)
     d.run(batch=0, workspace=None, workspace_bytes=0)
     assert ctx.pool.check() == gcb.GC_OK
