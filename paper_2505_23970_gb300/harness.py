@@ -469,3 +469,115 @@ class SharedContext:
 
     def close(self):
         self.pool.close()
+
+
+class FourBitContext:
+    """Serving with a context cache kept in 4 bits: every request's pages are in
+    the 4-bit cache, 16-bit pages only pass through the pool.
+
+    ``load`` brings cached 16-bit pages of a context in (gc_kv_restore into the
+    pool, gc_kv_pack_q4 from there); ``prefill`` takes one layer's q, k and v rows
+    of new tokens as the projection gives them (gc_kv_append_rope_q4, then
+    gc_prefix_prefill_attn_q4); ``step`` the same for one token of every request,
+    or a few drafted ones (gc_kv_append_rope_q4, gc_paged_decode_attn_q4).
+    ``advance`` says how many tokens each request keeps, on the stream of the last
+    call: drafted tokens that are not kept are overwritten by the next ones."""
+
+    def __init__(self, Hq, Hkv, d, ps, B, max_tokens, tokens: int = 1, rot_dim=None,
+                 base: float = 500000.0, L: int = 1, staging_pages: int = 1, seed: int = 0,
+                 device: str = "cuda"):
+        import torch
+        self.Hq, self.Hkv, self.d, self.ps, self.B, self.L = Hq, Hkv, d, ps, B, L
+        self.tokens, self.device = tokens, device
+        self.width = -(-max_tokens // ps)
+        self.pages = B * self.width
+        self.pool = gcb.KVPool.create(L, Hkv, d, ps, staging_pages, device=device)
+        self.cache = torch.empty(gcb.gc_kv_q4_bytes(self.pool.cfg, self.pages),
+                                 dtype=torch.uint8, device=device)
+        self.table_host = np.random.default_rng(seed).permutation(self.pages).astype(
+            np.int32).reshape(B, self.width)
+        self.table = _i32(self.table_host, device)
+        self.pool_table = _i32(np.full((B, self.width), -1), device)  # nothing stays in 16 bits
+        self.lens = _i32(np.zeros(B), device)                         # tokens that are kept
+        self.seq_lens = _i32(np.full(B, tokens), device)              # with a step's
+        self._cu = _i32(np.arange(B + 1) * tokens, device)
+        self.rot_dim = d if rot_dim is None else rot_dim
+        angle = np.arange(self.width * ps)[:, None] * \
+            base ** (-np.arange(0, max(self.rot_dim, 2), 2) / max(self.rot_dim, 2))
+        self.cos_sin = torch.from_numpy(
+            np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).to(device)
+        need = max(gcb.gc_paged_decode_q4_workspace_bytes(self.pool.handle, B, self.width, Hq,
+                                                          tokens),
+                   gcb.gc_prefix_prefill_q4_workspace_bytes(self.pool.handle, B, self.width,
+                                                            self.pages))
+        self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        self.q = torch.empty((B * tokens, Hq, d), dtype=torch.bfloat16, device=device)
+        self._stream, self._ids, self._new = None, [], None
+
+    def load(self, image, requests, blocks, stream=None):
+        """Pages [n][L][2][Hkv][ps][d] (device) into block blocks[i] of request
+        requests[i], as many at a time as the pool has pages."""
+        to = self.table_host[np.asarray(requests), np.asarray(blocks)]
+        for i in range(0, to.size, self.pool.cfg.num_pages):
+            part = to[i:i + self.pool.cfg.num_pages]
+            ids = (_i32(np.arange(part.size), self.device), _i32(part, self.device))
+            self._ids.append(ids)  # (kept: the stream reads them when it comes to it)
+            gcb.gc_kv_restore(self.pool.handle, image[i:i + part.size], ids[0], part.size, stream,
+                              None, gcb.GC_RESTORE_SRC_DEVICE)
+            gcb.gc_kv_pack_q4(self.pool.handle, ids[0], self.cache, self.pages, ids[1], part.size,
+                              0, self.L, stream)
+        self._stream = stream
+
+    def _append(self, qkv, q_out, cu, total, layer, stream):
+        Hq, Hkv, row = self.Hq, self.Hkv, qkv.stride(0)
+        gcb.gc_kv_append_rope_q4(
+            self.pool.handle, qkv[:, :Hq], row, q_out, qkv[:, Hq:Hq + Hkv], row, qkv[:, Hq + Hkv:],
+            row, self.cache, self.pages, self.table, self.lens, stream, layer, cu, self.B,
+            self.width, total, Hq, self.cos_sin, self.cos_sin.shape[0], self.rot_dim)
+        self._stream = stream
+
+    def begin(self, new_lens):
+        """The new tokens of every request for the prefill calls that follow."""
+        import torch
+        n = np.asarray(new_lens, np.int32)
+        cu = np.concatenate([[0], np.cumsum(n)])
+        self._new = (_i32(n, self.device), _i32(cu, self.device), int(cu[-1]),
+                     torch.empty((int(cu[-1]), self.Hq, self.d), dtype=torch.bfloat16,
+                                 device=self.device))
+
+    def prefill(self, qkv, out, layer: int = 0, stream=None):
+        """One layer of the new tokens: qkv [T_new][Hq + 2 Hkv][d] -> out [T_new][Hq][d]."""
+        n, cu, total, q = self._new
+        self._append(qkv, q, cu, total, layer, stream)
+        gcb.gc_prefix_prefill_attn_q4(
+            q, self.pool.handle, self.pool_table, self.lens, n, out, stream, layer, cu, self.B,
+            self.width, self.Hq, self.d ** -0.5, total, self.cache, self.table, self.pages,
+            self.workspace, self.workspace.numel())
+
+    def step(self, qkv, out, layer: int = 0, stream=None):
+        """One layer of the next tokens of every request: qkv [B * tokens][Hq + 2 Hkv][d]
+        -> out [B * tokens][Hq][d]."""
+        self._append(qkv, self.q, self._cu, self.B * self.tokens, layer, stream)
+        gcb.gc_paged_decode_attn_q4(
+            self.q, self.pool.handle, self.pool_table, self.seq_lens, out, stream, layer, self.B,
+            self.width, self.Hq, self.d ** -0.5, self.workspace, self.workspace.numel(),
+            self.cache, self.table, self.pages, self.tokens)
+
+    def advance(self, kept):
+        """Each request keeps kept[b] more tokens (an int32 tensor of the device, or one
+        number for all): behind the last call, on its stream."""
+        import torch
+        s = self._stream
+        if not s:
+            s = torch.cuda.default_stream(self.device)
+        elif isinstance(s, int):
+            s = torch.cuda.ExternalStream(s, self.device)
+        with torch.cuda.stream(s):
+            self.lens.add_(kept)
+            self.seq_lens.add_(kept)
+
+    def check(self, stream=None) -> int:
+        return self.pool.check(stream)
+
+    def close(self):
+        self.pool.close()

@@ -14,7 +14,7 @@ def f32(bits):
 
 def quantise(bits):
     """bf16 bits [..., d] -> (codes -7..7 [..., d/32, 32], scales [..., d/32] as bf16 bits)."""
-    x = f32(np.asarray(bits, np.uint16)).reshape(*np.shape(bits)[:-1], -1, 32)
+    x = f32(np.asarray(bits, np.uint16)).reshape(*np.shape(bits)[:-1], np.shape(bits)[-1] // 32, 32)
     with np.errstate(all="ignore"):
         amax = np.where(np.isfinite(x), np.abs(x), 0).max(-1).astype(np.float32)
         s_bits = wl.f32_to_bf16_bits(np.minimum(amax / np.float32(7), np.float32(2.0 ** 15)))
