@@ -445,16 +445,16 @@ struct Keys4 {
   }
 
   // Any group: in 16 bits, with keys that some column does not see, or none.
-  template <typename Look>
+  template <typename Entry, typename WideRow>
   __device__ __forceinline__ void one(uint32_t from, uint32_t key, int h, uint32_t ready, int T,
-                                      uint32_t k1, const Parts4<D>& mine, const Look& look,
-                                      const Dec4Geom& geo) {
+                                      uint32_t k1, const Parts4<D>& mine, const Entry& entry,
+                                      const WideRow& wide_row, const Dec4Geom& geo) {
     key += h * kGroup;
     from += h * Stage4<D>::kBytes;
     if (key >= k1) return;
     const bool four = ready >> h & 1;
     const uint8_t* kp = nullptr;
-    if (!four) look(key, &kp);
+    if (!four) kp = wide_row(key, entry(key));
     if (!four && kp == nullptr) return;
     const int n = T - static_cast<int>(key);
     float s[1][NT][4];
@@ -480,27 +480,29 @@ struct Keys4 {
     // (unsigned: look-ups run past a piece that may end near 2^31)
     const uint32_t k1 = static_cast<uint32_t>(w.k1), slots = static_cast<uint32_t>(geo.ps - 1);
     const uint8_t* q4_k = geo.q4_k + static_cast<uint64_t>(w.g) * q4_head_bytes(D, geo.ps);
-    // The 4-bit page of a key, -1: in 16 bits (wide: its row of K there), bad, or past the
-    // piece.
-    auto look = [&](uint32_t key, const uint8_t** wide = nullptr) -> int {
-      if (key >= k1) return -1;
-      const int64_t e = static_cast<int64_t>(w.b) * geo.max_blocks + (key >> geo.ps_shift);
-      const int p4 = ld_plain(geo.q4_table + e);
-      if (p4 >= 0 && p4 < geo.q4_pages) return p4;
-      const int page = p4 < 0 ? ld_plain(geo.block_table + e) : -1;
-      if (page < 0 || page >= geo.num_pages)
-        record_error(status, GC_ERR_OUT_OF_RANGE);
-      else if (wide)
-        *wide = geo.pool_k +
-                ((static_cast<int64_t>(page) * geo.Hkv + w.g) * geo.ps + (key & slots)) * D * 2;
-      return -1;
+    auto entry_of = [&](uint32_t key) {
+      return static_cast<int64_t>(w.b) * geo.max_blocks + (key >> geo.ps_shift);
     };
+    // The row of K of a key that is in no 4-bit page, null: in a bad one.
+    auto wide_row = [&](uint32_t key, int p4) -> const uint8_t* {
+      const int page = p4 < 0 ? ld_plain(geo.block_table + entry_of(key)) : -1;
+      if (page < 0 || page >= geo.num_pages) {
+        record_error(status, GC_ERR_OUT_OF_RANGE);
+        return nullptr;
+      }
+      return geo.pool_k +
+             ((static_cast<int64_t>(page) * geo.Hkv + w.g) * geo.ps + (key & slots)) * D * 2;
+    };
+    // A key's entry of the 4-bit table, -1 past the piece.  Nothing is asked of it yet: a
+    // window's entries are on their way while the window before is worked on.
+    auto entry = [&](uint32_t key) { return key < k1 ? ld_plain(geo.q4_table + entry_of(key)) : -1; };
+    auto in_4_bits = [&](int p4) { return p4 < geo.q4_pages ? p4 : -1; };
     // A window of 16 pairs is looked up at once, lane i a group of pair i / 2, and the next
     // one ahead of its use.
     const uint32_t key0 = static_cast<uint32_t>(w.k0), mine_in = static_cast<uint32_t>(lane) * kGroup;
     uint4 q_words[NT][GR];
     load_q(q_g, geo, q_words);
-    int cur = look(key0 + mine_in);
+    int cur = entry(key0 + mine_in);
     const Parts4<D> mine;
     // Pairs are copied kStages - 1 before their turn, into the stage whose reader of the round
     // before is done in every lane.  Bits 2 j, 2 j + 1 of `ready`: the groups of pair j from
@@ -512,8 +514,8 @@ struct Keys4 {
       ready >>= 2;
       if (ahead_i == 32) {
         ahead_i = 0;
-        cur = nxt;
-        nxt = ahead + 16 * step < k1 ? look(ahead + 16 * step + mine_in) : -1;
+        cur = in_4_bits(nxt);
+        nxt = entry(ahead + 16 * step + mine_in);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -530,9 +532,10 @@ struct Keys4 {
       to = to + kStage == end ? ring : to + kStage;
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    cur = in_4_bits(cur);
     for (int i = 0; i < kStages - 1; ++i) fetch();
     static_assert(kStages <= 16, "the first window has the first stages' pairs");
-    if (key0 + 16 * step < k1) nxt = look(key0 + 16 * step + mine_in);
+    nxt = entry(key0 + 16 * step + mine_in);
     reset();
     set_q(q_words, geo);
     uint32_t from = ring;
@@ -552,7 +555,7 @@ struct Keys4 {
         values<false>(from + Stage4<D>::kBytes, mine, kGroup, s[1]);
       } else {
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, look, geo);
+        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, entry, wide_row, geo);
       }
       from = from + kStage == end ? ring : from + kStage;
     }
