@@ -29,11 +29,12 @@ using dec::Keys4;
 constexpr int kLead = 4;      // units without keys in front of each pair's
 constexpr int kMinUnits = 2;  // of a warp's share, at least
 
-// Threads, resident CTAs and stages of shared memory of a variant.
+// Warps of an SM, in one CTA, and stages of shared memory of a variant.  (Two CTAs of half
+// the warps do not share the SM evenly: the one that came first is done with its equal
+// share 15 % earlier, 8 contexts of 65536 keys 124 us, now 119.)
 template <int D, int NT>
 struct Shape4 {
-  static constexpr int kWarps = 8;
-  static constexpr int kCtas = decode_ctas(D, 8 * NT);
+  static constexpr int kWarps = D * NT == 256 ? 8 : 16;
   static constexpr int kStages = 2;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kHeads = 8 * NT;
@@ -49,27 +50,44 @@ struct Part {
   int b, g, c0, c1;
 };
 
-// Shared memory: the warps' stages, over which the warps' last parts are kept, their first
-// parts, maxima and sums of both, what they are of, and the requests' first units and
-// lengths.
+// Shared memory: the warps' stages, over which the warps' last parts are kept, maxima and
+// sums of their first and last parts, what these are of, the requests' first units and
+// lengths, and the warps' first parts, as long as the batch leaves room for these (they are
+// in the workspace else).
+constexpr int kMostWithParts = 1024;  // requests
 template <typename S>
 size_t smem_bytes(int batch) {
-  return S::kWarps * (S::kRingBytes + S::kPartBytes + 2 * S::kHeads * sizeof(float2) +
-                      2 * sizeof(Part)) +
-         (2 * static_cast<size_t>(batch) + 1) * sizeof(int);
+  return S::kWarps * (S::kRingBytes + 2 * S::kHeads * sizeof(float2) + 2 * sizeof(Part) +
+                      (batch <= kMostWithParts ? S::kPartBytes : 0)) +
+         (2 * static_cast<size_t>(batch) + 4) / 4 * 4 * sizeof(int);
+}
+static_assert(16 * (9216 + 128 + 32 + 4224) + 2052 * 4 <= 227 * 1024, "shared memory");
+static_assert(16 * (9216 + 128 + 32) + 16388 * 4 <= 227 * 1024, "shared memory");
+
+// Workspace: the CTAs' parts (O, then maxima and sums; two to a CTA), then the warps' first
+// parts.
+template <typename S, int D>
+size_t workspace_bytes(int ctas, int batch) {
+  return ctas * (2 * S::kHeads * (D + 2) * sizeof(float) +
+                 (batch <= kMostWithParts ? 0 : S::kWarps * S::kPartBytes));
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
+__global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
     decode_q4_kernel(const __nv_bfloat16* q, const int32_t* seq_lens, __nv_bfloat16* out,
                      float* ws, Dec4Geom geo, int32_t* status, int* merge_counters) {
   using S = Shape4<D, NT>;
   extern __shared__ __align__(16) uint8_t smem[];
-  float* first_parts = reinterpret_cast<float*>(smem + S::kWarps * S::kRingBytes);
-  float2* mls = reinterpret_cast<float2*>(first_parts + S::kWarps * S::kHeads * S::kStride);
+  float2* mls = reinterpret_cast<float2*>(smem + S::kWarps * S::kRingBytes);
   Part* parts = reinterpret_cast<Part*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
   int* start = reinterpret_cast<int*>(parts + 2 * S::kWarps);              // [batch + 1]
   int* lens = start + geo.batch + 1;                                       // [batch]
+  float2* ws_ml = reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
+  float* first_parts =
+      geo.batch <= kMostWithParts
+          ? reinterpret_cast<float*>(start + (2 * geo.batch + 4) / 4 * 4)
+          : reinterpret_cast<float*>(ws_ml + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads) +
+                static_cast<int64_t>(blockIdx.x) * S::kWarps * S::kHeads * S::kStride;
   __shared__ int scan[S::kWarps], merge_flag[2];
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -162,9 +180,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, Shape4<D, NT>::kCtas)
   __syncthreads();
 
   // ---- the parts of this CTA's warps joined, pair after pair
-  // partials of CTAs: O, then (reference maximum, sum), two to a CTA: of a pair that began
-  // before it, and of one that goes on after it
-  float2* ws_ml = reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
+  // (two parts to a CTA: of a pair that began before it, and of one that goes on after it)
   Part cut[2] = {{-1, 0, 0, 0}, {-1, 0, 0, 0}};
   for (int s0 = 0, s1; s0 < 2 * S::kWarps; s0 = s1) {
     const Part of = parts[s0];
@@ -238,12 +254,17 @@ template <int D, int NT>
 gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const Dec4Geom& geo,
                  cudaStream_t stream) {
   using S = Shape4<D, NT>;
+  const int grid = min(pool->num_sms, kMergeCounters);
+  const size_t need = workspace_bytes<S, D>(grid, a.batch);
+  if (a.workspace == nullptr || a.workspace_bytes < need)
+    return fail(GC_ERR_INVALID_ARG,
+                "%s: workspace of %zu bytes needed (gc_paged_decode_q4_workspace_bytes), got %zu",
+                a.who, need, a.workspace_bytes);
   const size_t smem = smem_bytes<S>(a.batch);
   auto kernel = decode_q4_kernel<D, NT>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(smem));
   if (e != cudaSuccess) return cuda_fail(e, a.who);
-  const int grid = min(S::kCtas * pool->num_sms, kMergeCounters);
   e = launch_dependent(kernel, grid, S::kThreads, smem, stream,
                        static_cast<const __nv_bfloat16*>(a.q), a.seq_lens,
                        static_cast<__nv_bfloat16*>(a.out), static_cast<float*>(a.workspace), geo,
@@ -260,9 +281,15 @@ int ilog2(int x) {
 
 }  // namespace
 
-size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads, int32_t tokens) {
-  return decode_share_bytes(pool->cfg.head_dim, num_q_heads / pool->cfg.num_kv_heads * tokens,
-                            pool->num_sms, kMergeCounters);
+size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t num_q_heads,
+                                 int32_t tokens) {
+  const int ctas = min(pool->num_sms, kMergeCounters);
+  const bool narrow = num_q_heads / pool->cfg.num_kv_heads * tokens <= 8;
+  if (pool->cfg.head_dim == 128)
+    return narrow ? workspace_bytes<Shape4<128, 1>, 128>(ctas, batch)
+                  : workspace_bytes<Shape4<128, 2>, 128>(ctas, batch);
+  return narrow ? workspace_bytes<Shape4<64, 1>, 64>(ctas, batch)
+                : workspace_bytes<Shape4<64, 2>, 64>(ctas, batch);
 }
 
 gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4Cache& cache,
@@ -270,11 +297,6 @@ gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4
   const auto& cfg = pool->cfg;
   gc_status st = check_decode(pool, a);
   if (st != GC_OK) return st;
-  const size_t need = decode_q4_workspace_bytes(pool, a.num_q_heads, tokens);
-  if (a.workspace == nullptr || a.workspace_bytes < need)
-    return fail(GC_ERR_INVALID_ARG,
-                "%s: workspace of %zu bytes needed (gc_paged_decode_q4_workspace_bytes), got %zu",
-                a.who, need, a.workspace_bytes);
   Dec4Geom geo;
   geo.batch = a.batch;
   geo.Hq = a.num_q_heads;

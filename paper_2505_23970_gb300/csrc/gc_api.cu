@@ -906,7 +906,7 @@ size_t gc_paged_decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch,
       num_q_heads % pool->cfg.num_kv_heads ||
       static_cast<int64_t>(num_q_heads / pool->cfg.num_kv_heads) * tokens > 16)
     return 0;
-  return gc::decode_q4_workspace_bytes(pool, num_q_heads, tokens);
+  return gc::decode_q4_workspace_bytes(pool, batch, num_q_heads, tokens);
 }
 
 gc_status gc_paged_decode_attn_q4(const void* q, const gc_kv_pool* pool,

@@ -341,7 +341,8 @@ int64_t q4_scratch_pages(int32_t batch, int32_t max_blocks, int32_t q4_pages);
 gc_status launch_prefill_q4(const gc_kv_pool* pool, const AttnArgs& a, const Q4Cache& cache,
                             void* workspace, cudaStream_t stream);
 // Decode of `tokens` rows per request (decode_q4.cu).
-size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t num_q_heads, int32_t tokens);
+size_t decode_q4_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t num_q_heads,
+                                 int32_t tokens);
 gc_status launch_decode_q4(const gc_kv_pool* pool, const DecodeArgs& a, const Q4Cache& cache,
                            int32_t tokens, cudaStream_t stream);
 

@@ -39,10 +39,10 @@ class Decode:
         gcb.gc_paged_decode_attn_q4(**self.args(**change))
         return self
 
-    def check(self, skip=()):
+    def check(self, skip=(), only=None):
         c = self.ctx
         got = self.out.double().cpu().numpy()
-        for b in range(self.B):
+        for b in range(self.B) if only is None else only:
             if b in skip:
                 assert np.isnan(got[b]).all(), b
                 continue
@@ -246,3 +246,19 @@ def test_a_cache_without_pages():
     ctx = _q4.Context([100, 7], 2, 64, 16, recent=100)
     Decode(ctx, 4).run(q4_cache=None, n_q4_pages=0).check()
     assert ctx.pool.check() == gcb.GC_OK
+
+
+@pytest.mark.parametrize("B", [1024, 1025, 8192])
+@pytest.mark.parametrize("Hq,Hkv,d", [(1, 1, 64), (16, 1, 128), (8, 1, 128)])
+def test_batches_around_the_room_for_the_warps_parts(B, Hq, Hkv, d):
+    """Short contexts and a few long ones that are cut between warps and CTAs."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(1, 40, B)
+    lens[[3, B // 2, B - 1]] = [3000, 7000, 900]
+    ctx = _q4.Context(list(map(int, lens)), Hkv, d, 16, seed=B)
+    dec = Decode(ctx, Hq).run()
+    assert ctx.pool.check() == gcb.GC_OK
+    # (the long ones, their neighbours and some more)
+    keep = sorted({0, 2, 3, 4, B // 2 - 1, B // 2, B // 2 + 1, B - 2, B - 1, *range(7, B, B // 60)})
+    dec.check(skip=(), only=keep)
+    assert np.isfinite(dec.out.double().cpu().numpy()).all()
