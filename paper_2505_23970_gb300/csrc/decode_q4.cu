@@ -182,12 +182,17 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
   // ---- the parts of this CTA's warps joined, pair after pair
   // (two parts to a CTA: of a pair that began before it, and of one that goes on after it)
   Part cut[2] = {{-1, 0, 0, 0}, {-1, 0, 0, 0}};
-  for (int s0 = 0, s1; s0 < 2 * S::kWarps; s0 = s1) {
-    const Part of = parts[s0];
-    s1 = s0 + 1;
-    if (of.b < 0) continue;
-    for (; s1 < 2 * S::kWarps; ++s1)
-      if (parts[s1].b >= 0 && (parts[s1].b != of.b || parts[s1].g != of.g)) break;
+  // lane s has part s; the parts of a pair have the same key
+  static_assert(2 * S::kWarps <= 32, "a lane for every part");
+  Part of{-1, 0, 0, 0};
+  if (lane < 2 * S::kWarps) of = parts[lane];
+  const int key = of.b < 0 ? -1 - lane : of.b * geo.Hkv + of.g;
+  const uint32_t same = __match_any_sync(0xffffffffu, key);
+  uint32_t firsts = __ballot_sync(0xffffffffu, of.b >= 0 && (same & ((1u << lane) - 1)) == 0);
+  for (; firsts; firsts &= firsts - 1) {
+    const int s0 = __ffs(firsts) - 1;
+    const uint32_t all = __shfl_sync(0xffffffffu, same, s0);
+    of = parts[s0];
     const bool before = of.c0 < cta, after = of.c1 > cta;
     const int part = before ? 0 : 1;
     if (before)
@@ -197,11 +202,21 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
     for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
       const int h = x / (D / 4), d = 4 * (x % (D / 4));
       Joined sum;
-      for (int s = s0; s < s1; ++s) {
-        if (parts[s].b < 0) continue;
-        const float* o = s & 1 ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
-                               : first_parts + (s >> 1) * S::kHeads * S::kStride;
-        sum.add(mls[s * S::kHeads + h], *reinterpret_cast<const float4*>(o + h * S::kStride + d));
+      for (uint32_t left = all; left;) {
+        float2 ml[4];
+        float4 o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int s = left ? __ffs(left) - 1 : s0;
+          const float* from = s & 1
+                                  ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
+                                  : first_parts + (s >> 1) * S::kHeads * S::kStride;
+          ml[k] = left ? mls[s * S::kHeads + h] : make_float2(dec::kNone, 0.f);
+          o[k] = left ? *reinterpret_cast<const float4*>(from + h * S::kStride + d)
+                      : make_float4(0.f, 0.f, 0.f, 0.f);
+          left &= left - 1;
+        }
+        sum.add(ml, o);
       }
       if (!before && !after) {
         sum.store(out + (first_row(of.b, of.g) + row(h)) * D + d);
@@ -242,8 +257,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
           o[k] = c + k <= c1 ? __ldcg(reinterpret_cast<const float4*>(ws + at * D + d))
                              : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum.add(ml[k], o[k]);
+        sum.add(ml, o);
       }
       sum.store(out + (first_row(cut[i].b, cut[i].g) + row(h)) * D + d);
     }

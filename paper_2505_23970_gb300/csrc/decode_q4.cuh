@@ -619,17 +619,26 @@ struct Keys4 {
   }
 };
 
-// Parts joined one by one: O 2^(m - M) and sums, relative to the largest maximum yet.
+// Parts joined, N at a time: O 2^(m - M) and sums, relative to the largest maximum yet.
 struct Joined {
   float M = kNone, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  __device__ __forceinline__ void add(float2 ml, float4 v) {
-    const float top = fmaxf(M, ml.x);
-    const float a = ex2_approx(M - top), b = ex2_approx(ml.x - top);
+  template <int N>
+  __device__ __forceinline__ void add(const float2 (&ml)[N], const float4 (&v)[N]) {
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, ml[i].x);
+    const float a = ex2_approx(M - top);
     M = top;
-    L = fmaf(L, a, ml.y * b);
-    o.x = fmaf(o.x, a, v.x * b), o.y = fmaf(o.y, a, v.y * b);
-    o.z = fmaf(o.z, a, v.z * b), o.w = fmaf(o.w, a, v.w * b);
+    L *= a;
+    o.x *= a, o.y *= a, o.z *= a, o.w *= a;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float b = ex2_approx(ml[i].x - top);
+      L = fmaf(ml[i].y, b, L);
+      o.x = fmaf(v[i].x, b, o.x), o.y = fmaf(v[i].y, b, o.y);
+      o.z = fmaf(v[i].z, b, o.z), o.w = fmaf(v[i].w, b, o.w);
+    }
   }
   __device__ __forceinline__ void store(__nv_bfloat16* to) const {
     const float inv = 1.f / L;
