@@ -159,8 +159,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
     w.part = j0 == 0 && j1 == all ? -1 : j0 > 0 ? 0 : 1;
     Keys4<D, NT> keys;
     keys.template run<S::kStages>(
-        static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::kRingBytes, geo, w, T,
-        q + first_row(w.b, w.g) * D, status);
+        smem + warp * S::kRingBytes, geo, w, T, q + first_row(w.b, w.g) * D, status);
     if (w.part < 0) {
       keys.store(out + first_row(w.b, w.g) * D, cols, row);
       continue;

@@ -127,17 +127,19 @@ struct Parts4 {
   }
 };
 
+// (C++ loads, which the compiler may move between the barriers of the loop)
 template <int N>
-__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&r)[N]) {
+__device__ __forceinline__ void lds_words(const uint8_t* at, uint32_t (&r)[N]) {
   static_assert(N == 1 || N == 2 || N == 4, "a load");
-  if constexpr (N == 1)
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(at));
-  else if constexpr (N == 2)
-    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at));
-  else
-    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(at));
+  if constexpr (N == 1) {
+    r[0] = *reinterpret_cast<const uint32_t*>(at);
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(at);
+    r[0] = v.x, r[1] = v.y;
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
+  }
 }
 __device__ __forceinline__ float half_f32(uint32_t pair, int i) {  // of two bf16
   return __uint_as_float(i ? pair & 0xffff0000u : pair << 16);
@@ -239,7 +241,7 @@ struct Keys4 {
   }
 
   // S^T of a group of keys, times 2^(e - 133)
-  __device__ __forceinline__ void scores(uint32_t at, const Parts4<D>& mine,
+  __device__ __forceinline__ void scores(const uint8_t* at, const Parts4<D>& mine,
                                          float (&s)[NT][4]) const {
     uint32_t k[2][GR], sk[2][GR / 2];
 #pragma unroll
@@ -374,7 +376,7 @@ struct Keys4 {
 
   // O^T += V^T P^T; kTail: keys at or past n left out (their scale may be anything)
   template <bool kTail>
-  __device__ __forceinline__ void values(uint32_t at, const Parts4<D>& mine, int n,
+  __device__ __forceinline__ void values(const uint8_t* at, const Parts4<D>& mine, int n,
                                          const float (&p)[NT][4]) {
     uint32_t v[4][GR / 2], sv[2][GR / 2];
 #pragma unroll
@@ -446,7 +448,7 @@ struct Keys4 {
 
   // Any group: in 16 bits, with keys that some column does not see, or none.
   template <typename Entry, typename WideRow>
-  __device__ __forceinline__ void one(uint32_t from, uint32_t key, int h, uint32_t ready, int T,
+  __device__ __forceinline__ void one(const uint8_t* from, uint32_t key, int h, uint32_t ready, int T,
                                       uint32_t k1, const Parts4<D>& mine, const Entry& entry,
                                       const WideRow& wide_row, const Dec4Geom& geo) {
     key += h * kGroup;
@@ -473,7 +475,7 @@ struct Keys4 {
   // The keys of piece w of a request of T keys, two groups at a time, to O, reference
   // maxima and sums.  `ring`: the warp's kStages stages in shared memory, each for a pair.
   template <int kStages>
-  __device__ __forceinline__ void run(uint32_t ring, const Dec4Geom& geo, const DecPiece& w, int T,
+  __device__ __forceinline__ void run(const uint8_t* ring_at, const Dec4Geom& geo, const DecPiece& w, int T,
                                       const __nv_bfloat16* q_g, int32_t* status) {
     constexpr uint32_t kStage = 2 * Stage4<D>::kBytes, step = 2 * kGroup;
     const int lane = threadIdx.x & 31;
@@ -507,6 +509,7 @@ struct Keys4 {
     // Pairs are copied kStages - 1 before their turn, into the stage whose reader of the round
     // before is done in every lane.  Bits 2 j, 2 j + 1 of `ready`: the groups of pair j from
     // now on are in 4 bits.
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ring_at));
     const uint32_t end = ring + kStages * kStage;
     uint32_t to = ring, ahead = key0, ready = 0;
     int ahead_i = 0, nxt = -1;
@@ -538,7 +541,7 @@ struct Keys4 {
     nxt = entry(key0 + 16 * step + mine_in);
     reset();
     set_q(q_words, geo);
-    uint32_t from = ring;
+    uint32_t from = 0;
     // keys below this are seen by every column
     const uint32_t seen = min(k1, static_cast<uint32_t>(T - geo.tokens + 1));
     for (uint32_t key = key0; key < k1; key += step) {
@@ -548,16 +551,17 @@ struct Keys4 {
       // (the same in every lane; the vote says so)
       if (__all_sync(0xffffffffu, (ready & 3) == 3 && key + 2 * kGroup <= seen)) {
         float s[2][NT][4];
-        scores(from, mine, s[0]);
-        scores(from + Stage4<D>::kBytes, mine, s[1]);
+        const uint8_t* const at = ring_at + from;
+        scores(at, mine, s[0]);
+        scores(at + Stage4<D>::kBytes, mine, s[1]);
         softmax(s);
-        values<false>(from, mine, kGroup, s[0]);
-        values<false>(from + Stage4<D>::kBytes, mine, kGroup, s[1]);
+        values<false>(at, mine, kGroup, s[0]);
+        values<false>(at + Stage4<D>::kBytes, mine, kGroup, s[1]);
       } else {
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) one(from, key, h, ready, T, k1, mine, entry, wide_row, geo);
+        for (int h = 0; h < 2; ++h) one(ring_at + from, key, h, ready, T, k1, mine, entry, wide_row, geo);
       }
-      from = from + kStage == end ? ring : from + kStage;
+      from = from + kStage == kStages * kStage ? 0 : from + kStage;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     // the powers of two leave: 2^(kPBias - 133) of O, 16 of its rows r + 8, 2^kPBias of l
