@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
           ? reinterpret_cast<float*>(start + (2 * geo.batch + 4) / 4 * 4)
           : reinterpret_cast<float*>(ws_ml + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads) +
                 static_cast<int64_t>(blockIdx.x) * S::kWarps * S::kHeads * S::kStride;
-  __shared__ int scan[S::kWarps], merge_flag[2];
+  __shared__ int scan[S::kWarps], merge_flag[2], leader[32];
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = blockIdx.x, warps = static_cast<int>(gridDim.x) * S::kWarps;
@@ -178,88 +178,92 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
   }
   __syncthreads();
 
-  // ---- the parts of this CTA's warps joined, pair after pair
-  // (two parts to a CTA: of a pair that began before it, and of one that goes on after it)
-  Part cut[2] = {{-1, 0, 0, 0}, {-1, 0, 0, 0}};
-  // lane s has part s; the parts of a pair have the same key
+  // ---- the parts of this CTA's warps joined, pair by pair
+  // Lane s has part s; those of a pair have the same key, and the first of them speaks for
+  // the pair.  A pair with keys in other CTAs too leaves a part in the workspace, in the
+  // CTA's first place if it began before the CTA, else in its second.
   static_assert(2 * S::kWarps <= 32, "a lane for every part");
+  constexpr uint32_t kAll = 0xffffffffu;
   Part of{-1, 0, 0, 0};
   if (lane < 2 * S::kWarps) of = parts[lane];
-  const int key = of.b < 0 ? -1 - lane : of.b * geo.Hkv + of.g;
-  const uint32_t same = __match_any_sync(0xffffffffu, key);
-  uint32_t firsts = __ballot_sync(0xffffffffu, of.b >= 0 && (same & ((1u << lane) - 1)) == 0);
-  for (; firsts; firsts &= firsts - 1) {
-    const int s0 = __ffs(firsts) - 1;
-    const uint32_t all = __shfl_sync(0xffffffffu, same, s0);
-    of = parts[s0];
-    const bool before = of.c0 < cta, after = of.c1 > cta;
-    const int part = before ? 0 : 1;
-    if (before)
-      cut[0] = of;
-    else if (after)
-      cut[1] = of;
-    for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
-      const int h = x / (D / 4), d = 4 * (x % (D / 4));
-      Joined sum;
-      for (uint32_t left = all; left;) {
-        float2 ml[4];
-        float4 o[4];
+  const uint32_t same =
+      __match_any_sync(kAll, of.b < 0 ? -1 - lane : of.b * geo.Hkv + of.g);
+  const bool leads = of.b >= 0 && (same & ((1u << lane) - 1)) == 0;
+  const uint32_t leaders = __ballot_sync(kAll, leads);
+  const int pairs = __popc(leaders);
+  if (leads) leader[__popc(leaders & ((1u << lane) - 1))] = lane;  // (every warp the same)
+  __syncwarp();
+  const uint32_t cut_bits[2] = {
+      __ballot_sync(kAll, leads && of.c0 < cta),                   // (one lane at most)
+      __ballot_sync(kAll, leads && of.c0 >= cta && of.c1 > cta)};  // (as well)
+  const int quads = cols * (D / 4);  // four columns of a head each
+  for (int i0 = 0; i0 < pairs * quads; i0 += S::kThreads) {
+    const int i = i0 + tid, r = i / quads, x = i - r * quads;
+    // (whole warps: the parts of a pair are another lane's to tell)
+    const int s0 = r < pairs ? leader[r] : 0;
+    uint32_t left = __shfl_sync(kAll, same, s0);
+    if (r >= pairs) continue;
+    const int h = x / (D / 4), d = 4 * (x % (D / 4));
+    Joined sum;
+    while (left) {
+      float2 ml[4];
+      float4 o[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int s = left ? __ffs(left) - 1 : s0;
-          const float* from = s & 1
-                                  ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
-                                  : first_parts + (s >> 1) * S::kHeads * S::kStride;
-          ml[k] = left ? mls[s * S::kHeads + h] : make_float2(dec::kNone, 0.f);
-          o[k] = left ? *reinterpret_cast<const float4*>(from + h * S::kStride + d)
-                      : make_float4(0.f, 0.f, 0.f, 0.f);
-          left &= left - 1;
-        }
-        sum.add(ml, o);
+      for (int k = 0; k < 4; ++k) {
+        const int s = left ? __ffs(left) - 1 : s0;
+        const float* from = s & 1
+                                ? reinterpret_cast<const float*>(smem + (s >> 1) * S::kRingBytes)
+                                : first_parts + (s >> 1) * S::kHeads * S::kStride;
+        ml[k] = left ? mls[s * S::kHeads + h] : make_float2(dec::kNone, 0.f);
+        o[k] = left ? *reinterpret_cast<const float4*>(from + h * S::kStride + d)
+                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        left &= left - 1;
       }
-      if (!before && !after) {
-        sum.store(out + (first_row(of.b, of.g) + row(h)) * D + d);
-      } else {
-        const int64_t at = (static_cast<int64_t>(cta) * 2 + part) * S::kHeads + h;
-        *reinterpret_cast<float4*>(ws + at * D + d) = sum.o;
-        if (d == 0) ws_ml[at] = make_float2(sum.M, sum.L);
-      }
+      sum.add(ml, o);
+    }
+    if (((cut_bits[0] | cut_bits[1]) >> s0 & 1) == 0) {
+      sum.store(out + (first_row(parts[s0].b, parts[s0].g) + row(h)) * D + d);
+    } else {
+      const int64_t at = (static_cast<int64_t>(cta) * 2 + (cut_bits[1] >> s0 & 1)) * S::kHeads + h;
+      *reinterpret_cast<float4*>(ws + at * D + d) = sum.o;
+      if (d == 0) ws_ml[at] = make_float2(sum.M, sum.L);
     }
   }
   // ---- the last CTA with keys of a cut pair joins the CTAs' parts
-  if (cut[0].b < 0 && cut[1].b < 0) return;  // (the same in every thread)
+  if ((cut_bits[0] | cut_bits[1]) == 0) return;  // (the same in every thread)
   __syncthreads();
   // (the barrier has the CTA's parts before the fence of the one thread that counts)
-  if ((tid == 0 && cut[0].b >= 0) || (tid == 32 && cut[1].b >= 0)) {
-    const Part of = tid ? cut[1] : cut[0];
-    __threadfence();
-    const int last = atomicAdd(merge_counters + of.c0, 1) == of.c1 - of.c0;
-    if (last) merge_counters[of.c0] = 0;
-    __threadfence();
-    merge_flag[tid >> 5] = last;
+  if (tid < 2) {
+    int last = 0;
+    if (const uint32_t bits = tid ? cut_bits[1] : cut_bits[0]) {
+      const Part cut = parts[__ffs(bits) - 1];
+      __threadfence();
+      last = atomicAdd(merge_counters + cut.c0, 1) == cut.c1 - cut.c0;
+      if (last) merge_counters[cut.c0] = 0;
+      __threadfence();
+    }
+    merge_flag[tid] = last;
   }
   __syncthreads();
+  for (int i = tid; i < 2 * quads; i += S::kThreads) {
+    const int k0 = i >= quads, x = i - k0 * quads;
+    if (!merge_flag[k0]) continue;
+    const Part cut = parts[__ffs(k0 ? cut_bits[1] : cut_bits[0]) - 1];
+    const int h = x / (D / 4), d = 4 * (x % (D / 4));
+    Joined sum;
+    for (int c = cut.c0; c <= cut.c1; c += 8) {
+      float2 ml[8];
+      float4 o[8];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (cut[i].b < 0 || !merge_flag[i]) continue;
-    const int c0 = cut[i].c0, c1 = cut[i].c1;
-    for (int x = tid; x < cols * (D / 4); x += S::kThreads) {
-      const int h = x / (D / 4), d = 4 * (x % (D / 4));
-      Joined sum;
-      for (int c = c0; c <= c1; c += 8) {
-        float2 ml[8];
-        float4 o[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int64_t at = (static_cast<int64_t>(c + k) * 2 + (c + k == c0)) * S::kHeads + h;
-          ml[k] = c + k <= c1 ? __ldcg(ws_ml + at) : make_float2(dec::kNone, 0.f);
-          o[k] = c + k <= c1 ? __ldcg(reinterpret_cast<const float4*>(ws + at * D + d))
-                             : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        sum.add(ml, o);
+      for (int k = 0; k < 8; ++k) {
+        const int64_t at = (static_cast<int64_t>(c + k) * 2 + (c + k == cut.c0)) * S::kHeads + h;
+        ml[k] = c + k <= cut.c1 ? __ldcg(ws_ml + at) : make_float2(dec::kNone, 0.f);
+        o[k] = c + k <= cut.c1 ? __ldcg(reinterpret_cast<const float4*>(ws + at * D + d))
+                               : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      sum.store(out + (first_row(cut[i].b, cut[i].g) + row(h)) * D + d);
+      sum.add(ml, o);
     }
+    sum.store(out + (first_row(cut.b, cut.g) + row(h)) * D + d);
   }
 }
 
