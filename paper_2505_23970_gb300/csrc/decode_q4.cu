@@ -61,8 +61,8 @@ size_t smem_bytes(int batch) {
                       (batch <= kMostWithParts ? S::kPartBytes : 0)) +
          (2 * static_cast<size_t>(batch) + 4) / 4 * 4 * sizeof(int);
 }
-static_assert(16 * (9216 + 128 + 32 + 4224) + 2052 * 4 <= 227 * 1024, "shared memory");
-static_assert(16 * (9216 + 128 + 32) + 16388 * 4 <= 227 * 1024, "shared memory");
+static_assert(16 * (9216 + 128 + 32 + 4224 + 128) + 2052 * 4 + 256 <= 227 * 1024, "room");
+static_assert(16 * (9216 + 128 + 32 + 128) + 16388 * 4 + 256 <= 227 * 1024, "room");
 
 // Workspace: the CTAs' parts (O, then maxima and sums; two to a CTA), then the warps' first
 // parts.
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
           ? reinterpret_cast<float*>(start + (2 * geo.batch + 4) / 4 * 4)
           : reinterpret_cast<float*>(ws_ml + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads) +
                 static_cast<int64_t>(blockIdx.x) * S::kWarps * S::kHeads * S::kStride;
-  __shared__ int scan[S::kWarps], merge_flag[2], leader[32];
+  __shared__ int scan[S::kWarps], merge_flag[2], leaders_of[S::kWarps][32];
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = blockIdx.x, warps = static_cast<int>(gridDim.x) * S::kWarps;
@@ -191,7 +191,8 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
   const bool leads = of.b >= 0 && (same & ((1u << lane) - 1)) == 0;
   const uint32_t leaders = __ballot_sync(kAll, leads);
   const int pairs = __popc(leaders);
-  if (leads) leader[__popc(leaders & ((1u << lane) - 1))] = lane;  // (every warp the same)
+  int* leader = leaders_of[warp];
+  if (leads) leader[__popc(leaders & ((1u << lane) - 1))] = lane;
   __syncwarp();
   const uint32_t cut_bits[2] = {
       __ballot_sync(kAll, leads && of.c0 < cta),                   // (one lane at most)
