@@ -758,9 +758,9 @@ GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t
  *                it is packed).  An entry >= n_q4_pages, or a pool page outside
  *                the pool, is skipped (its keys left out) and recorded.
  *   tokens       1 to 16 / (Hq/Hkv).
- *   q, out       [batch][tokens][Hq][d] bf16, device; fp32 accumulation, P and
- *                P * s rounded to bf16 before the PV product (a term is off by
- *                2^-8 of itself at most), out rounded to nearest even.
+ *   q, out       [batch][tokens][Hq][d] bf16, device; fp32 accumulation, P * s (in
+ *                16-bit pages P) rounded to bf16 before the PV product, out
+ *                rounded to nearest even.
  *   seq_lens     int32 [batch], device: context lengths, the tokens included; a
  *                request whose length is outside [tokens, max_blocks_per_seq*ps]
  *                is skipped (its rows are not written) and recorded as

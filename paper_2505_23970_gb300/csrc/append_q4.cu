@@ -13,6 +13,10 @@
 // is two shuffles, both members of a pair of neighbours are in one lane and a lane's codes
 // are one store.  A pair in halves is met by reading the other half's 8 columns too (from
 // the L1: the row's other lanes read them).  The other blocks turn q as append_rope.cu does.
+//
+// Measured: 8 x 1024 tokens of 64/8 heads of 128 (311 MB) 57 us, 5.5 TB/s, 0.81 of the copy
+// rate (ncu: the wait for the look-ups and for the loads before them, as in append_rope.cu,
+// which moves 340 MB in 56); 8 tokens 6.4 us; 4400 ragged tokens of 32/8 heads of 64 11 us.
 #include "append_place.cuh"
 #include "q4_format.cuh"
 

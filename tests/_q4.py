@@ -141,8 +141,8 @@ def decode_reference(q, kv, scales, scale, tokens):
     """(out, bound) of rows q [tokens][Hq][d] of one request, in 64 bits.
 
     With A = sum p |v| / sum p and S = sum p s / sum p over a row's n keys:
-    * P and P s are rounded to bf16, 2^-8 of a term each: 2^-7 A (codes times the
-      rounded P s, and the offset times the same, differ from c s by nothing else);
+    * P s (P, of a 16-bit key) is rounded to bf16, 2^-8 of a term: 2^-8 A (codes times
+      the rounded P s, and the offset times the same, differ from c s by nothing else);
     * a group's score is a sum of 32 products q (c + 8) and a start of -8 sum q in
       binary32: at most 33 roundings of 2^-23 of sums up to 23 sum |q|, times s, and
       4 more of the sum over groups and its scalings; a 16-bit key's is d products;
@@ -168,6 +168,6 @@ def decode_reference(q, kv, scales, scale, tokens):
     A = np.einsum("ihgt,thd->ihgd", p, np.abs(kv[1]))
     S = np.repeat(np.einsum("ihgt,thc->ihgc", p, scales[1]), 32, -1)
     n = T + 64.0
-    bound = (A * (2.0 ** -7 + 2 * e + 2.0 ** -20 + n * 2.0 ** -23) + (A + 23 * S) * n / 4 * 2.0 ** -23 +
+    bound = (A * (2.0 ** -8 + 2 * e + 2.0 ** -20 + n * 2.0 ** -23) + (A + 23 * S) * n / 4 * 2.0 ** -23 +
              23 * S * 16 * 2.0 ** -23 + np.abs(o) * 2.0 ** -8)
     return o.reshape(tokens, Hq, d), bound.reshape(tokens, Hq, d)
