@@ -512,16 +512,24 @@ class FourBitContext:
                                                             self.pages))
         self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
         self.q = torch.empty((B * tokens, Hq, d), dtype=torch.bfloat16, device=device)
-        self._stream, self._ids, self._new = None, [], None
+        self._stream, self._new = None, None
+
+    def _torch_stream(self, stream):
+        import torch
+        if not stream:
+            return torch.cuda.default_stream(self.device)
+        return torch.cuda.ExternalStream(stream, self.device) if isinstance(stream, int) else stream
 
     def load(self, image, requests, blocks, stream=None):
         """Pages [n][L][2][Hkv][ps][d] (device) into block blocks[i] of request
         requests[i], as many at a time as the pool has pages."""
+        import torch
         to = self.table_host[np.asarray(requests), np.asarray(blocks)]
         for i in range(0, to.size, self.pool.cfg.num_pages):
             part = to[i:i + self.pool.cfg.num_pages]
-            ids = (_i32(np.arange(part.size), self.device), _i32(part, self.device))
-            self._ids.append(ids)  # (kept: the stream reads them when it comes to it)
+            # (of that stream: their memory is used again only behind the calls that read them)
+            with torch.cuda.stream(self._torch_stream(stream)):
+                ids = (_i32(np.arange(part.size), self.device), _i32(part, self.device))
             gcb.gc_kv_restore(self.pool.handle, image[i:i + part.size], ids[0], part.size, stream,
                               None, gcb.GC_RESTORE_SRC_DEVICE)
             gcb.gc_kv_pack_q4(self.pool.handle, ids[0], self.cache, self.pages, ids[1], part.size,
@@ -548,6 +556,8 @@ class FourBitContext:
     def prefill(self, qkv, out, layer: int = 0, stream=None):
         """One layer of the new tokens: qkv [T_new][Hq + 2 Hkv][d] -> out [T_new][Hq][d]."""
         n, cu, total, q = self._new
+        for x in (n, cu, q):  # (another begin() may come before this stream has passed)
+            x.record_stream(self._torch_stream(stream))
         self._append(qkv, q, cu, total, layer, stream)
         gcb.gc_prefix_prefill_attn_q4(
             q, self.pool.handle, self.pool_table, self.lens, n, out, stream, layer, cu, self.B,
@@ -567,12 +577,7 @@ class FourBitContext:
         """Each request keeps kept[b] more tokens (an int32 tensor of the device, or one
         number for all): behind the last call, on its stream."""
         import torch
-        s = self._stream
-        if not s:
-            s = torch.cuda.default_stream(self.device)
-        elif isinstance(s, int):
-            s = torch.cuda.ExternalStream(s, self.device)
-        with torch.cuda.stream(s):
+        with torch.cuda.stream(self._torch_stream(self._stream)):
             self.lens.add_(kept)
             self.seq_lens.add_(kept)
 

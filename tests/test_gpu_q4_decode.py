@@ -262,3 +262,23 @@ def test_batches_around_the_room_for_the_warps_parts(B, Hq, Hkv, d):
     keep = sorted({0, 2, 3, 4, B // 2 - 1, B // 2, B // 2 + 1, B - 2, B - 1, *range(7, B, B // 60)})
     dec.check(skip=(), only=keep)
     assert np.isfinite(dec.out.double().cpu().numpy()).all()
+
+
+def test_units_of_more_keys():
+    """A table so wide that its pairs' keys, 32 to a unit, could not be numbered in 32 bits."""
+    import torch
+    lens = [5000, 1, 40, 333] + [17 + i for i in range(60)]
+    ctx = _q4.Context(lens, 8, 64, 16, recent=1, seed=14)
+    d = Decode(ctx, 8)
+    wide = 2 ** 24
+    assert len(lens) * 8 * (wide * 16 // 32) > 2 ** 31
+    tables = []
+    for t in (ctx.dev4, ctx.dev16):
+        w = torch.full((len(lens), wide), -1, dtype=torch.int32, device="cuda")
+        w[:, :t.shape[1]] = t
+        tables.append(w)
+    need = gcb.gc_paged_decode_q4_workspace_bytes(ctx.pool.handle, len(lens), wide, 8, 1)
+    assert need == d.need
+    d.run(q4_table=tables[0], block_table=tables[1], max_blocks_per_seq=wide)
+    assert ctx.pool.check() == gcb.GC_OK
+    d.check()
