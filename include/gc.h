@@ -685,8 +685,9 @@ GC_API gc_status gc_shared_prefix_decode_attn(
  *     c = clamp(round_half_even(x * (1 / s)), -7, 7)
  *         (c = 0 for NaN x; every c = 0 when s = 0)
  * quotients rounded once in binary32, the product only to the whole number.  The
- * value that is held is c * s.  A head's rows of a page are its codes [ps][d/2] bytes, then
- * its scales [ps][d/32] bf16; c + 8 is a nibble (the lower one of a byte first):
+ * value that is held is c * s.  A head's rows of a page are its codes [ps][d/2]
+ * bytes, then its scales [ps][d/32] bf16; c + 8 is a nibble (the lower one of a byte
+ * first):
  *     K row: 32-bit word q*(d/32) + g has columns 32g + 8q + j (q < 4, j < 8),
  *            column j in nibble {0, 4, 2, 6, 1, 5, 3, 7}[j]
  *     V row: 16-bit word r*(d/32) + g has columns 32g + 4r + j (r < 8, j < 4),
@@ -756,7 +757,8 @@ GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t
  *   q4_table     an entry >= 0 is a 4-bit page; where it is -1 the block is pool
  *                page block_table[b][j] (a request's newest page, say, before
  *                it is packed).  An entry >= n_q4_pages, or a pool page outside
- *                the pool, is skipped (its keys left out) and recorded.
+ *                the pool, is skipped (its keys left out; a row with none left
+ *                becomes NaN) and recorded.
  *   tokens       1 to 16 / (Hq/Hkv).
  *   q, out       [batch][tokens][Hq][d] bf16, device; fp32 accumulation, P * s (in
  *                16-bit pages P) rounded to bf16 before the PV product, out
@@ -767,8 +769,9 @@ GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t
  *                GC_ERR_OUT_OF_RANGE.  Keys at or past it are never used.
  *   workspace    device scratch of gc_paged_decode_q4_workspace_bytes bytes for
  *                the same arguments, with the rules of gc_paged_decode_attn's.
- * Powers of two inside the kernel leave room for |q| up to 2^100 and, in 16-bit
- * pages, |K| up to 2^60; beyond that a row may become NaN.  Calls on one pool must not overlap on
+ * A key that a row does not see is not used for it, whatever it holds.  Powers of
+ * two inside the kernel leave room for |q| up to 2^100 and, in 16-bit pages, |K| up
+ * to 2^60; beyond that a row may become NaN.  Calls on one pool must not overlap on
  * the GPU with each other or with the other attention calls.  The same call gives
  * the same bits again; the order of its sums depends on the lengths in the call.
  * Errors: as gc_paged_decode_attn; GC_ERR_INVALID_ARG also for n_q4_pages < 0,

@@ -13,7 +13,7 @@
 //  * S is scaled group by group in binary32, S += s_g D_g; P is scaled by V's s_g before
 //    its product and P s_g rounded once to bf16, at most 2^-8 of a term.  (Rounding P alone,
 //    and scaling it after the transposition, is a rounding more for 30 instructions less of
-//    290 a group of keys: error against 64 bits 0.0026 instead of 0.0022, the output's own
+//    299 a group of keys: error against 64 bits 0.0026 instead of 0.0022, the output's own
 //    rounding being 0.0017.)
 // Powers of two keep everything in range: Q's columns are brought to 2^100 at the most, P
 // is 2^90 2^(x - m), and both leave again exactly.
@@ -80,7 +80,6 @@ struct Stage4 {
   static constexpr int GR = D / 32;
   static constexpr int kCodes = kGroup * D / 2, kScales = kGroup * D / 16;
   static constexpr int kBytes = 2 * (kCodes + kScales);
-
 };
 
 // (a predicate in place of a branch: branches are most of what a small loop adds)
@@ -159,8 +158,8 @@ struct Keys4 {
   static constexpr int GR = D / 32;
   float o[NT][D / 16][4];     // tile (g, t): columns 32 g + 4 r + 2 t (+ 1: rows r + 8)
   float m[NT][2], l[NT][2];
-  uint32_t q[NT][D / 16][2];  // Q^T: columns 32 g + 8 q ... + 7, the last four over 16
-  uint32_t off[NT][GR / 2];   // -8 2^-133 times the groups' sums of q (B operand, see load_q)
+  uint32_t q[NT][D / 16][2];  // Q^T: columns 32 g + 8 c ... + 7, the last four over 16
+  uint32_t off[NT][GR / 2];   // -8 2^-133 times the groups' sums of q (B operand, see set_q)
   float scale[NT][2];         // softmax_scale log2(e), and what undoes the powers of two
 
   __device__ __forceinline__ void reset() {
@@ -239,7 +238,8 @@ struct Keys4 {
         }
         off[t][i] = pack_bf16x2(v[0], v[1]);
       }
-      const float undo = times_pow2(geo.scale_log2, 133 - e);
+      // (never 0, which times the -infinity of a masked score would be NaN)
+      const float undo = fmaxf(times_pow2(geo.scale_log2, 133 - e), pow2(-126));
       // from the lanes of a column (r) to those of its scores (2 c, 2 c + 1)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -315,17 +315,19 @@ struct Keys4 {
       for (int e = 0; e < 4; ++e) s[t][e] = fmaf(b[t][e], 16.f, a[t][e]) * pow2(-73);
   }
 
-  // The column of token i of the request's last `tokens` sees the keys below
-  // n - (tokens - 1 - i).
+  // The token of the request's last `tokens` that column 2 c + x of tile t is of: token i sees
+  // the keys below n - (tokens - 1) + i.
+  __device__ __forceinline__ static int token(int t, int x, const Dec4Geom& geo) {
+    return (8 * t + 2 * static_cast<int>(threadIdx.x & 3) + x) >> geo.g_shift;
+  }
   __device__ __forceinline__ void mask(float (&s)[NT][4], const Parts4<D>& mine, int n,
                                        const Dec4Geom& geo) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int token = (8 * t + 2 * static_cast<int>(threadIdx.x & 3) + (e & 1)) >> geo.g_shift;
-        if (mine.row() + 8 * (e >> 1) + geo.tokens - 1 - token >= n) s[t][e] = -INFINITY;
-      }
+      for (int e = 0; e < 4; ++e)
+        if (mine.row() + 8 * (e >> 1) + geo.tokens - 1 - token(t, e & 1, geo) >= n)
+          s[t][e] = -INFINITY;
   }
 
   // scores of H groups -> P, times 2^kPBias
@@ -418,9 +420,12 @@ struct Keys4 {
     }
   }
 
-  // The same of rows of a 16-bit page.
-  __device__ __forceinline__ void values16(const uint8_t* vp, int n, const float (&p)[NT][4]) {
+  // The same of rows of a 16-bit page.  Keys that some column does not see are added one by
+  // one where they are seen: what a page holds may be infinite, and 0 times that is NaN.
+  __device__ __forceinline__ void values16(const uint8_t* vp, int n, const float (&p)[NT][4],
+                                           const Dec4Geom& geo) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    const int by_all = n - (geo.tokens - 1);
     uint32_t b[NT][2], b16[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -438,7 +443,7 @@ struct Keys4 {
       for (int x = 0; x < 4; ++x) {
         const int key = c + 4 * x;
         v[x][0] = v[x][1] = 0;
-        if (key < n) ldg(vp + (key * D + 32 * g + 4 * r) * 2, v[x]);
+        if (key < by_all) ldg(vp + (key * D + 32 * g + 4 * r) * 2, v[x]);
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -453,13 +458,41 @@ struct Keys4 {
         }
       }
     }
+#pragma unroll 1
+    for (int key = max(by_all, 0); key < min(n, kGroup); ++key) {
+      const int from = ((key & 3) * 2 + (key >> 2 & 1)) * 4 + c;  // the lane with its P
+      float w[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          w[t][x] = __shfl_sync(0xffffffffu, key < 8 ? p[t][x] : p[t][x + 2], from) * pow2(-65) *
+                    pow2(-68);
+#pragma unroll
+      for (int g = 0; g < GR; ++g) {
+        uint32_t v[2];
+        ldg(vp + (key * D + 32 * g + 4 * r) * 2, v);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (key >= by_all + token(t, x, geo)) continue;
+            const float y = w[t][x], y16 = 16.f * y;
+            o[t][2 * g][x] = fmaf(y, half_f32(v[0], 0), o[t][2 * g][x]);
+            o[t][2 * g][x + 2] = fmaf(y16, half_f32(v[0], 1), o[t][2 * g][x + 2]);
+            o[t][2 * g + 1][x] = fmaf(y, half_f32(v[1], 0), o[t][2 * g + 1][x]);
+            o[t][2 * g + 1][x + 2] = fmaf(y16, half_f32(v[1], 1), o[t][2 * g + 1][x + 2]);
+          }
+      }
+    }
   }
 
   // Any group: in 16 bits, with keys that some column does not see, or none.
   template <typename Entry, typename WideRow>
-  __device__ __forceinline__ void one(const uint8_t* from, uint32_t key, int h, uint32_t ready, int T,
-                                      uint32_t k1, const Parts4<D>& mine, const Entry& entry,
-                                      const WideRow& wide_row, const Dec4Geom& geo) {
+  __device__ __forceinline__ void one(const uint8_t* from, uint32_t key, int h, uint32_t ready,
+                                      int T, uint32_t k1, const Parts4<D>& mine,
+                                      const Entry& entry, const WideRow& wide_row,
+                                      const Dec4Geom& geo) {
     key += h * kGroup;
     from += h * Stage4<D>::kBytes;
     if (key >= k1) return;
@@ -478,14 +511,15 @@ struct Keys4 {
     if (four)
       values<true>(from, mine, n, s[0]);
     else
-      values16(kp + geo.plane16, n, s[0]);
+      values16(kp + geo.plane16, n, s[0], geo);
   }
 
   // The keys of piece w of a request of T keys, two groups at a time, to O, reference
   // maxima and sums.  `ring`: the warp's kStages stages in shared memory, each for a pair.
   template <int kStages>
-  __device__ __forceinline__ void run(const uint8_t* ring_at, const Dec4Geom& geo, const DecPiece& w, int T,
-                                      const __nv_bfloat16* q_g, int32_t* status) {
+  __device__ __forceinline__ void run(const uint8_t* ring_at, const Dec4Geom& geo,
+                                      const DecPiece& w, int T, const __nv_bfloat16* q_g,
+                                      int32_t* status) {
     constexpr uint32_t kStage = 2 * Stage4<D>::kBytes, step = 2 * kGroup;
     const int lane = threadIdx.x & 31;
     // (unsigned: look-ups run past a piece that may end near 2^31)
@@ -506,11 +540,14 @@ struct Keys4 {
     };
     // A key's entry of the 4-bit table, -1 past the piece.  Nothing is asked of it yet: a
     // window's entries are on their way while the window before is worked on.
-    auto entry = [&](uint32_t key) { return key < k1 ? ld_plain(geo.q4_table + entry_of(key)) : -1; };
+    auto entry = [&](uint32_t key) {
+      return key < k1 ? ld_plain(geo.q4_table + entry_of(key)) : -1;
+    };
     auto in_4_bits = [&](int p4) { return p4 < geo.q4_pages ? p4 : -1; };
     // A window of 16 pairs is looked up at once, lane i a group of pair i / 2, and the next
     // one ahead of its use.
-    const uint32_t key0 = static_cast<uint32_t>(w.k0), mine_in = static_cast<uint32_t>(lane) * kGroup;
+    const uint32_t key0 = static_cast<uint32_t>(w.k0);
+    const uint32_t mine_in = static_cast<uint32_t>(lane) * kGroup;
     uint4 q_words[NT][GR];
     load_q(q_g, geo, q_words);
     int cur = entry(key0 + mine_in);
@@ -568,7 +605,8 @@ struct Keys4 {
         values<false>(at + Stage4<D>::kBytes, mine, kGroup, s[1]);
       } else {
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) one(ring_at + from, key, h, ready, T, k1, mine, entry, wide_row, geo);
+        for (int h = 0; h < 2; ++h)
+          one(ring_at + from, key, h, ready, T, k1, mine, entry, wide_row, geo);
       }
       from = from + kStage == kStages * kStage ? 0 : from + kStage;
     }

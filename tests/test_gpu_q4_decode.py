@@ -177,6 +177,43 @@ def test_queries_of_zero_and_not_finite():
     assert (np.abs(got[keep] - want[0]) <= bound[0]).all()
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,tokens,lens", [
+    (4, 1, 64, 4, [4, 5, 16, 17, 18, 19, 20, 600]),
+    (32, 8, 128, 4, [4, 17, 33, 500]),
+    (16, 2, 128, 2, [2, 16, 17, 33]),
+    (8, 8, 128, 7, [7, 20, 23, 500]),
+    (8, 8, 64, 16, [16, 17, 32, 47]),
+])
+def test_drafted_tokens_that_are_not_finite(Hq, Hkv, d, tokens, lens):
+    """The newest token's K and V in a 16-bit page are NaN and infinities: only its own
+    row sees them."""
+    ctx = _q4.Context(lens, Hkv, d, 16, recent=1, seed=14)
+    for b, T in enumerate(lens):
+        page = ctx.table16[b, (T - 1) // 16]
+        ctx.bits16[0, 0, page, :, (T - 1) % 16] = 0x7FC0
+        ctx.bits16[0, 1, page, :, (T - 1) % 16] = 0x7F80 | (np.arange(d) % 2) << 15
+    ctx.pool.planes().copy_(bf16_tensor(ctx.bits16))
+    c = Decode(ctx, Hq, tokens).run()
+    assert ctx.pool.check() == gcb.GC_OK
+    got = c.out.double().cpu().numpy()
+    for b, T in enumerate(lens):
+        kv, s = ctx.keys(b)
+        kv[:, -1] = 0
+        want, bound = _q4.decode_reference(_q4.f32(c.q_bits[b]).astype(np.float64), kv, s, c.scale,
+                                           tokens)
+        assert np.isnan(got[b, -1]).all(), T
+        assert (np.abs(got[b, :-1] - want[:-1]) <= bound[:-1]).all(), T
+
+
+@pytest.mark.parametrize("recent", [0, 1])
+def test_the_smallest_queries_and_scale(recent):
+    """Scores that are all 0 in binary32: the mean of the values."""
+    ctx = _q4.Context([17, 300], 2, 64, 16, recent=recent, seed=15)
+    bits = np.full((2, 1, 4, 64), 1, np.uint16)
+    Decode(ctx, 4, q_bits=bits, scale=1e-30).run().check()
+    assert ctx.pool.check() == gcb.GC_OK
+
+
 def test_lengths_outside_the_table_are_skipped():
     ctx = _q4.Context([300, 40, 64, 20], 2, 64, 16, seed=5)
     cap = ctx.width * 16
@@ -202,6 +239,16 @@ def test_bad_pages_are_left_out():
     want, bound = _q4.decode_reference(_q4.f32(d.q_bits[0]).astype(np.float64), kv[:, left],
                                        s[:, left], d.scale, 1)
     assert (np.abs(d.out.double().cpu().numpy()[0] - want) <= bound).all()
+
+
+def test_a_request_without_a_page_that_is_left():
+    ctx = _q4.Context([300, 40], 2, 64, 16, seed=16)
+    t4 = ctx.table4.copy()
+    t4[0] = ctx.pages4
+    d = Decode(ctx, 4).run(q4_table=_i32(t4, "cuda"))
+    assert ctx.pool.check() == gcb.GC_ERR_OUT_OF_RANGE
+    assert np.isnan(d.out[0].double().cpu().numpy()).all()
+    d.check(only=[1])
 
 
 def test_the_same_call_gives_the_same_bits():
