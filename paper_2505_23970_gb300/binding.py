@@ -138,7 +138,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.gc_prefix_prefill_q4_workspace_bytes.restype = sz
         lib.gc_prefix_prefill_attn_q4.argtypes = attn + [vp, vp, i32, vp, sz]
         for f in ("gc_kv_append_rope_q4", "gc_kv_pack_q4", "gc_kv_unpack_q4",
-                  "gc_paged_decode_attn_q4", "gc_prefix_prefill_attn_q4", "gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
+                  "gc_paged_decode_attn_q4", "gc_prefix_prefill_attn_q4",
+                  "gc_kv_pool_create", "gc_kv_pool_destroy", "gc_kv_pool_data",
                   "gc_kv_pool_check", "gc_kv_restore", "gc_kv_save", "gc_kv_restore_layers",
                   "gc_kv_save_layers", "gc_kv_stage_layers", "gc_kv_save_q8", "gc_kv_restore_q8",
                   "gc_kv_append", "gc_kv_append_rope",

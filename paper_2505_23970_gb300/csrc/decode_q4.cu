@@ -24,8 +24,9 @@
 // of the copy rate; 4 tokens each of 16 contexts of up to 8192, 32/8 heads (84 MB) 38 us; 8 of
 // 65536 with heads of 64 68 us, 4.4 TB/s.  In the longer ones the loop runs at 60 % of the
 // issue slots, the ALU pipe (masks, shifts) at 52 %, the tensor pipe at 37 %; of the shorter
-// ones 9 us are the start (look-ups, first loads: 4) and the joins (5).  With 16 rows the
-// accumulators leave room for 8 warps an SM only, and their latencies are the bound.
+// ones 9 us are the start (look-ups, first loads: 4) and the joins (5).  With 16
+// columns a group takes 459 instead of 299 instructions and twice the products, by 8 warps an
+// SM (12, with Q in shared memory to make room, took 41 us for the 38).
 #include "decode_q4.cuh"
 
 namespace gc {
@@ -91,7 +92,8 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
   Part* parts = reinterpret_cast<Part*>(mls + 2 * S::kWarps * S::kHeads);  // [warps][2]
   int* start = reinterpret_cast<int*>(parts + 2 * S::kWarps);              // [batch + 1]
   int* lens = start + geo.batch + 1;                                       // [batch]
-  float2* ws_ml = reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
+  float2* ws_ml =
+      reinterpret_cast<float2*>(ws + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads * D);
   float* first_parts =
       geo.batch <= kMostWithParts
           ? reinterpret_cast<float*>(start + (2 * geo.batch + 4) / 4 * 4)

@@ -83,7 +83,8 @@ __global__ void __launch_bounds__(kThreads)
     if (!r.ok) continue;  // the whole warp
     uint4 x[GR];
 #pragma unroll
-    for (int i = 0; i < GR; ++i) x[i] = ld_plain(reinterpret_cast<const uint4*>(r.wide) + 4 * i + q);
+    for (int i = 0; i < GR; ++i)
+      x[i] = ld_plain(reinterpret_cast<const uint4*>(r.wide) + 4 * i + q);
     q4::store_row<GR>(x, is_k, r.codes, r.scales, true);
   }
 }
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(kThreads)
       r[u].ok = false;
       if (w0 + u * warps < parts)
         r[u] = part_of<GR>(g, w0 + u * warps, pool_ids, q4_ids, is_k[u], status);
-      if (r[u].ok) q4::load_row<GR>(r[u].codes, r[u].scales, is_k[u], c[u], s[u]);
+      if (r[u].ok) q4::load_row<GR>(r[u].codes, r[u].scales, c[u], s[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -140,7 +141,8 @@ __global__ void __launch_bounds__(kThreads)
       const int P = ld_plain(prefix_lens + b), n = ld_plain(new_lens + b);
       if (n > 0 && P >= 0) {
         const int64_t T = static_cast<int64_t>(P) + n;
-        pages = static_cast<int>(min(static_cast<int64_t>(max_blocks), (T + g.q4.ps - 1) >> g.q4.ps_shift));
+        pages = static_cast<int>(
+            min(static_cast<int64_t>(max_blocks), (T + g.q4.ps - 1) >> g.q4.ps_shift));
       }
     }
     int incl = pages;
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(kThreads)
       for (int u = 0; u < 2; ++u) {
         const int slot = slot0 + u * kWarpRows;
         q4::load_row<GR>(head + slot * (16 * GR),
-                         head + (g.q4.ps * (16 * GR) + slot * (2 * GR)), kv == 0, c[u], s[u]);
+                         head + (g.q4.ps * (16 * GR) + slot * (2 * GR)), c[u], s[u]);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {

@@ -4,9 +4,9 @@
 //     s = bf16_rne(min(amax / 7, 2^15)), 0 if that is below 2^-24
 //     c = clamp(rne(x * (1 / s)), -7, 7), every c = 0 when s = 0, c = 0 for NaN
 // (amax over the group's finite values; quotients rounded once in binary32, the product
-// only to the whole number), and c + 8 is stored in four bits.  The value is c s: 11 significant bits,
-// exact in binary32.  The rounding of s is a choice of the format: its 8 bits cost a
-// code at most 7 * 2^-9 of a step, and a scale takes two bytes.
+// only to the whole number), and c + 8 is stored in four bits.  The value is c s: 11
+// significant bits, exact in binary32.  The rounding of s is a choice of the format: its 8
+// bits cost a code at most 7 * 2^-8 of a step, and a scale takes two bytes.
 //
 // A (page, plane, kv head) has its rows' codes [ps][d/2] bytes, then their scales
 // [ps][d/32] bf16.  The order of a row's codes is the one in which the decode kernel's
@@ -202,7 +202,7 @@ __device__ __forceinline__ uint32_t whole_pair(uint32_t w) {
 // The inverse for the same four lanes: x[g] = bf16_rne(c s) of columns 32 g + 8 q ... + 7
 // (a product of bf16 values, rounded once).
 template <int GR>
-__device__ __forceinline__ void load_row(const uint8_t* codes, const uint8_t* scales, bool is_k,
+__device__ __forceinline__ void load_row(const uint8_t* codes, const uint8_t* scales,
                                          uint32_t (&w)[GR], uint32_t (&s)[GR / 2]) {
   const int q = threadIdx.x & 3;
   if constexpr (GR == 4) {
@@ -231,7 +231,8 @@ __device__ __forceinline__ void expand_row(const uint32_t (&w)[GR], const uint32
       // 16-bit word g of the units 2 q and 2 q + 1
       const uint32_t v = __byte_perm(w[g / 2], w[g / 2 + GR / 2], g & 1 ? 0x7632 : 0x5410);
       const uint32_t a = mul_bf16x2(whole_pair(v), s2), b = mul_bf16x2(whole_pair(v >> 4), s2);
-      const uint32_t c = mul_bf16x2(whole_pair(v >> 8), s2), d = mul_bf16x2(whole_pair(v >> 12), s2);
+      const uint32_t c = mul_bf16x2(whole_pair(v >> 8), s2);
+      const uint32_t d = mul_bf16x2(whole_pair(v >> 12), s2);
       x[g].x = __byte_perm(a, b, 0x5410);
       x[g].y = __byte_perm(c, d, 0x5410);
       x[g].z = __byte_perm(a, b, 0x7632);

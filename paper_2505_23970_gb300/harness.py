@@ -545,7 +545,8 @@ class FourBitContext:
         self._stream = stream
 
     def begin(self, new_lens):
-        """The new tokens of every request for the prefill calls that follow."""
+        """The new tokens of every request for the prefill calls that follow.  (A captured
+        prefill has them too: it may be replayed until the next begin().)"""
         import torch
         n = np.asarray(new_lens, np.int32)
         cu = np.concatenate([[0], np.cumsum(n)])
