@@ -1272,6 +1272,14 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 }
 
 template <int D>
+constexpr size_t smem_bytes(int batch, bool q8, bool span) {
+  using C = Cfg<D>;
+  return 1024 + 2 * C::kTileBytes + C::kStages * C::kTileBytes + sizeof(Barriers) +
+         (static_cast<size_t>(batch) + 1) * sizeof(int) + kSortMax * sizeof(int16_t) +
+         (q8 ? sizeof(Q8State) + 8 : 0) + (span ? kSortMax * sizeof(int) + kSpanHeldBytes : 0);
+}
+
+template <int D>
 gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                  int* work_counter, const Q8Pages* q8 = nullptr,
                  const UnpackedPages* unpacked = nullptr, const SpanGeom* span = nullptr,
@@ -1363,10 +1371,7 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
     if (r != CUDA_SUCCESS)
       return fail(GC_ERR_CUDA, "gc_prefix_prefill_attn_q8: image tensor map (CUresult %d)", (int)r);
   }
-  const size_t smem = 1024 + 2 * C::kTileBytes + C::kStages * C::kTileBytes + sizeof(Barriers) +
-                      (static_cast<size_t>(a.batch) + 1) * sizeof(int) +
-                      kSortMax * sizeof(int16_t) + (q8 ? sizeof(Q8State) + 8 : 0) +
-                      (span ? kSortMax * sizeof(int) + kSpanHeldBytes : 0);
+  const size_t smem = smem_bytes<D>(a.batch, q8 != nullptr, span != nullptr);
   static_assert(2 * kOwnBytes <= (2 + C::kStages) * C::kTileBytes, "own keys: shared memory");
   // (at d = 128 only the image variant is used: see below)
   constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
@@ -1386,8 +1391,9 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
                 : q8       ? attn_tc_kernel<D, Pages::kImage>
                 : unpacked ? attn_tc_kernel<D, kUnpacked>
                            : attn_tc_kernel<D, kPool>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  constexpr size_t kMostQ8 = smem_bytes<D>(kMaxBatch, true, false);
+  constexpr size_t kMostSpan = smem_bytes<D>(kMaxBatch, false, kSpan);
+  cudaError_t e = allow_shared<(kMostQ8 > kMostSpan ? kMostQ8 : kMostSpan)>(kernel);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   // items beyond one per CTA are claimed from a counter; a call that cannot
   // have any needs no counter, and only as many CTAs as it can have items

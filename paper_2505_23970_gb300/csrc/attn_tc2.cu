@@ -1315,7 +1315,7 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn2() {
   return fn;
 }
 
-size_t smem_bytes2(int batch, bool span = false) {
+constexpr size_t smem_bytes2(int batch, bool span = false) {
   return (span && batch <= kSortMax ? kSortMax * sizeof(int) + kSpanHeldBytes : 0) + 1024 +
          2 * kQBytes + static_cast<size_t>(2 * kRing) * kSlotBytes + sizeof(Bars2) +
          (static_cast<size_t>(batch) + 1) * sizeof(int) +
@@ -1337,9 +1337,9 @@ Kernel2 kernel2(int splits, bool img) {
   return splits > 1 ? attn_tc2_kernel<true, false, false> : attn_tc2_kernel<false, false, false>;
 }
 
-cudaError_t prepare_kernel(Kernel2 kernel, int splits, size_t smem) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+cudaError_t prepare_kernel(Kernel2 kernel, int splits) {
+  constexpr size_t kMostSorted = smem_bytes2(kSortMax, true), kMost = smem_bytes2(kMaxBatch, true);
+  cudaError_t e = allow_shared<(kMostSorted > kMost ? kMostSorted : kMost)>(kernel);
   if (e == cudaSuccess && splits > 4)
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   return e;
@@ -1358,7 +1358,7 @@ int clusters_that_fit(const gc_kv_pool* pool, int splits, size_t smem) {
     if (k > 0) return k - 1;
   }
   const Kernel2 kernel = kernel2(splits, false);
-  if (prepare_kernel(kernel, splits, smem) != cudaSuccess) {
+  if (prepare_kernel(kernel, splits) != cudaSuccess) {
     cudaGetLastError();
     return 0;
   }
@@ -1517,7 +1517,7 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   const Kernel2 kernel = own    ? attn_tc2_kernel<false, false, true, true>
                          : span ? attn_tc2_kernel<false, false, true>
                                 : kernel2(splits, unpacked != nullptr);
-  cudaError_t e = prepare_kernel(kernel, splits, smem);
+  cudaError_t e = prepare_kernel(kernel, splits);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   // (a join that follows leaves the counter at 0)
   if (geo.more_items && !geo.span.cuts) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);

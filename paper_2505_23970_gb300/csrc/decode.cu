@@ -121,7 +121,8 @@ size_t decode_workspace_bytes(const gc_kv_pool* pool, int32_t batch, int32_t max
 }
 
 gc_status check_decode(const gc_kv_pool* pool, const DecodeArgs& a) {
-  if (a.batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", a.who, a.batch);
+  if (a.batch > kMaxBatch)
+    return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > %d", a.who, a.batch, kMaxBatch);
   const int64_t cap = static_cast<int64_t>(a.max_blocks) * pool->cfg.page_size;
   if (cap > 2147483647LL)
     return fail(GC_ERR_UNSUPPORTED, "%s: %lld-token block table", a.who,

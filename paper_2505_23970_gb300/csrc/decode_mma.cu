@@ -84,9 +84,7 @@ gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const DecGeom& geo
   auto kernel = decode_mma_kernel<D, NT, kQ8, kParts, kTwo>;
   cudaError_t e = cudaSuccess;
   // a block gets 48 KB without asking, its static words (well below 1 KB) included
-  if (smem > 47 * 1024)
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(smem));
+  if (smem > 47 * 1024) e = allow_shared<decode_smem_bytes<S>(kMaxBatch, kTwo)>(kernel);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   e = launch_dependent(kernel, grid, S::kThreads, smem, stream,
                        static_cast<const __nv_bfloat16*>(a.q), a.block_table, a.seq_lens,

@@ -939,9 +939,9 @@ __device__ __forceinline__ void decode_cta(uint8_t* smem, Who who,
 }  // namespace
 
 template <typename S>
-size_t decode_smem_bytes(int batch, bool two = false) {
-  return (two ? 2 * static_cast<size_t>(batch) * sizeof(int) : 0) + S::kRedFloats * sizeof(float) + S::kWarps * S::kHeads * sizeof(float2) +
-         (static_cast<size_t>(batch) + 1) * sizeof(int);
+constexpr size_t decode_smem_bytes(int batch, bool two = false) {
+  return (two ? 2 * static_cast<size_t>(batch) * sizeof(int) : 0) + S::kRedFloats * sizeof(float) +
+         S::kWarps * S::kHeads * sizeof(float2) + (static_cast<size_t>(batch) + 1) * sizeof(int);
 }
 
 }  // namespace gc

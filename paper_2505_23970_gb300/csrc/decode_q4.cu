@@ -51,6 +51,7 @@ struct Shape4 {
   static constexpr int kStride = D + 4;                              // floats of a head
   static constexpr int kRingBytes = 2 * kStages * dec::Stage4<D>::kBytes;  // of a warp
   static constexpr int kPartBytes = kHeads * kStride * 4;
+  static constexpr int kStaticBytes = kWarps * (1 + 32) * 4 + 16;  // the kernel's own arrays
   static_assert(kPartBytes <= kRingBytes, "a warp's last part lies over its stages");
 };
 
@@ -66,13 +67,16 @@ struct Part {
 // in the workspace else).
 constexpr int kMostWithParts = 1024;  // requests
 template <typename S>
-size_t smem_bytes(int batch) {
+constexpr size_t smem_bytes(int batch) {
   return S::kWarps * (S::kRingBytes + 2 * S::kHeads * sizeof(float2) + 2 * sizeof(Part) +
                       (batch <= kMostWithParts ? S::kPartBytes : 0)) +
          (2 * static_cast<size_t>(batch) + 4) / 4 * 4 * sizeof(int);
 }
-static_assert(16 * (9216 + 128 + 32 + 4224 + 128) + 2052 * 4 + 256 <= 227 * 1024, "room");
-static_assert(16 * (9216 + 128 + 32 + 128) + 16388 * 4 + 256 <= 227 * 1024, "room");
+template <typename S>
+constexpr size_t most_smem_bytes() {
+  constexpr size_t few = smem_bytes<S>(kMostWithParts), many = smem_bytes<S>(kMaxBatch);
+  return few > many ? few : many;
+}
 
 // Workspace: the CTAs' parts (O, then maxima and sums; two to a CTA), then the warps' first
 // parts.
@@ -100,6 +104,7 @@ __global__ void __launch_bounds__(Shape4<D, NT>::kThreads, 1)
           : reinterpret_cast<float*>(ws_ml + static_cast<int64_t>(gridDim.x) * 2 * S::kHeads) +
                 static_cast<int64_t>(blockIdx.x) * S::kWarps * S::kHeads * S::kStride;
   __shared__ int scan[S::kWarps], merge_flag[2], leaders_of[S::kWarps][32];
+  static_assert(sizeof(scan) + sizeof(merge_flag) + sizeof(leaders_of) <= S::kStaticBytes, "room");
   dependent_begin();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = blockIdx.x, warps = static_cast<int>(gridDim.x) * S::kWarps;
@@ -291,8 +296,8 @@ gc_status launch(const gc_kv_pool* pool, const DecodeArgs& a, const Dec4Geom& ge
                 a.who, need, a.workspace_bytes);
   const size_t smem = smem_bytes<S>(a.batch);
   auto kernel = decode_q4_kernel<D, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  static_assert(most_smem_bytes<S>() + S::kStaticBytes <= 227 * 1024, "room");
+  cudaError_t e = allow_shared<most_smem_bytes<S>()>(kernel);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
   e = launch_dependent(kernel, grid, S::kThreads, smem, stream,
                        static_cast<const __nv_bfloat16*>(a.q), a.seq_lens,

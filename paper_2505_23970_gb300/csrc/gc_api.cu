@@ -677,7 +677,8 @@ static gc_status attn_common(const char* who, const void* q, const gc_kv_pool* p
     return fail(GC_ERR_UNSUPPORTED, "%s: q heads per kv head %d not in {1,2,4,8,16}", who, G);
   if (!(softmax_scale > 0.0f) || softmax_scale == __builtin_inff())
     return fail(GC_ERR_INVALID_ARG, "%s: softmax_scale must be positive and finite", who);
-  if (batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", who, batch);
+  if (batch > gc::kMaxBatch)
+    return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > %d", who, batch, gc::kMaxBatch);
   if (batch == 0 || total_new_tokens == 0) {
     *noop = true;
     return GC_OK;
@@ -972,7 +973,8 @@ static gc_status span_common(const char* who, const gc_kv_pool* pool, int32_t la
     return fail(GC_ERR_UNSUPPORTED, "%s: q heads per kv head %d not in {1,2,4,8,16}", who, G);
   if (!(softmax_scale > 0.0f) || softmax_scale == __builtin_inff())
     return fail(GC_ERR_INVALID_ARG, "%s: softmax_scale must be positive and finite", who);
-  if (batch > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > 8192", who, batch);
+  if (batch > gc::kMaxBatch)
+    return fail(GC_ERR_UNSUPPORTED, "%s: batch %d > %d", who, batch, gc::kMaxBatch);
   // positions in a block table are 32-bit ints
   if (static_cast<int64_t>(max_blocks_per_seq) * pool->cfg.page_size > 2147483647LL)
     return fail(GC_ERR_UNSUPPORTED, "%s: block table of %d pages", who, max_blocks_per_seq);
@@ -1042,7 +1044,8 @@ gc_status gc_shared_prefix_decode_attn(const void* q, const gc_kv_pool* pool,
   if (s != GC_OK) return s;
   if (num_groups < 0 || max_shared_blocks < 0)
     return fail(GC_ERR_INVALID_ARG, "%s: negative size", who);
-  if (num_groups > 8192) return fail(GC_ERR_UNSUPPORTED, "%s: %d groups > 8192", who, num_groups);
+  if (num_groups > gc::kMaxBatch)
+    return fail(GC_ERR_UNSUPPORTED, "%s: %d groups > %d", who, num_groups, gc::kMaxBatch);
   if (static_cast<int64_t>(max_shared_blocks) * pool->cfg.page_size > 2147483647LL)
     return fail(GC_ERR_UNSUPPORTED, "%s: shared block table of %d pages", who, max_shared_blocks);
   if (batch == 0) return GC_OK;

@@ -92,6 +92,21 @@ cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block
   return cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
 }
 
+// Requests (or groups) of a call at most: what is kept of each lies in shared memory.
+constexpr int kMaxBatch = 8192;
+
+// Dynamic shared memory past 48 KB has to be allowed first, and what is allowed belongs to
+// the kernel, for all host threads, not to a launch: where each call set its own size, one
+// thread's smaller call refused another's larger one that was about to be launched.  So it
+// is a constant, the most that any call of the kernel takes.  (Per context, and so set by
+// every call.)
+template <size_t kMost, typename... P>
+cudaError_t allow_shared(void (*kernel)(P...)) {
+  static_assert(kMost <= 227 * 1024, "shared memory of a block");
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(kMost));
+}
+
 // 16 8-bit codes (one 16-byte word, byte i = code i) -> 16 bf16 values
 // (lo: codes 0-7, hi: codes 8-15, in order), each c * s in binary32 rounded
 // to bf16 (nearest even).  The 8-bit restore and the attention over 8-bit
