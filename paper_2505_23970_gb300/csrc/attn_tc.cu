@@ -1322,6 +1322,30 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   if (pool_rows >= (1ull << 31))
     return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
                 static_cast<unsigned long long>(pool_rows));
+  // (at d = 128 only the image variant is used: see below)
+  constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
+  constexpr Pages kUnpacked = D == 128 ? Pages::kImage : Pages::kUnpacked;
+  // (and nothing is cut there)
+  constexpr bool kSpan = D == 64;
+  // Cross attention whose requests have one tile of rows: K and V by a warp each.  With
+  // pages of 16 one warp's copies are such a step's longest part (us, one warp | two; 8 kv
+  // heads: 40 requests of 120 rows over 4000 keys 98 | 86, 19 over 8192 83 | 71, 1 of 64
+  // over 60000 44 | 41, with pages of 64 85 | 85; of 240 rows over 4000 135 | 141).
+  const bool v_warp = span && !own && static_cast<long long>(a.total_new_tokens) * geo.G <=
+                                          static_cast<long long>(kTileM) * a.batch;
+  auto kernel = own && geo.G > 8 ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 2 : 0>
+                : own      ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 1 : 0>
+                : v_warp   ? attn_tc_kernel<D, kPool, kSpan, 0, kSpan>
+                : span     ? attn_tc_kernel<D, kPool, kSpan>
+                : q8       ? attn_tc_kernel<D, Pages::kImage>
+                : unpacked ? attn_tc_kernel<D, kUnpacked>
+                           : attn_tc_kernel<D, kPool>;
+  // (Before the maps: in a thread that has made no CUDA call yet this one makes a context
+  // current, and encoding a map wants one.)
+  constexpr size_t kMostQ8 = smem_bytes<D>(kMaxBatch, true, false);
+  constexpr size_t kMostSpan = smem_bytes<D>(kMaxBatch, false, kSpan);
+  cudaError_t e = allow_shared<(kMostQ8 > kMostSpan ? kMostQ8 : kMostSpan)>(kernel);
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   CUtensorMap map_q, map_kv;
   {
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(geo.Hq),
@@ -1373,28 +1397,6 @@ gc_status launch(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_t stream,
   }
   const size_t smem = smem_bytes<D>(a.batch, q8 != nullptr, span != nullptr);
   static_assert(2 * kOwnBytes <= (2 + C::kStages) * C::kTileBytes, "own keys: shared memory");
-  // (at d = 128 only the image variant is used: see below)
-  constexpr Pages kPool = D == 128 ? Pages::kImage : Pages::kPool;
-  constexpr Pages kUnpacked = D == 128 ? Pages::kImage : Pages::kUnpacked;
-  // (and nothing is cut there)
-  constexpr bool kSpan = D == 64;
-  // Cross attention whose requests have one tile of rows: K and V by a warp each.  With
-  // pages of 16 one warp's copies are such a step's longest part (us, one warp | two; 8 kv
-  // heads: 40 requests of 120 rows over 4000 keys 98 | 86, 19 over 8192 83 | 71, 1 of 64
-  // over 60000 44 | 41, with pages of 64 85 | 85; of 240 rows over 4000 135 | 141).
-  const bool v_warp = span && !own && static_cast<long long>(a.total_new_tokens) * geo.G <=
-                                          static_cast<long long>(kTileM) * a.batch;
-  auto kernel = own && geo.G > 8 ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 2 : 0>
-                : own      ? attn_tc_kernel<D, kPool, kSpan, kSpan ? 1 : 0>
-                : v_warp   ? attn_tc_kernel<D, kPool, kSpan, 0, kSpan>
-                : span     ? attn_tc_kernel<D, kPool, kSpan>
-                : q8       ? attn_tc_kernel<D, Pages::kImage>
-                : unpacked ? attn_tc_kernel<D, kUnpacked>
-                           : attn_tc_kernel<D, kPool>;
-  constexpr size_t kMostQ8 = smem_bytes<D>(kMaxBatch, true, false);
-  constexpr size_t kMostSpan = smem_bytes<D>(kMaxBatch, false, kSpan);
-  cudaError_t e = allow_shared<(kMostQ8 > kMostSpan ? kMostQ8 : kMostSpan)>(kernel);
-  if (e != cudaSuccess) return cuda_fail(e, a.who);
   // items beyond one per CTA are claimed from a counter; a call that cannot
   // have any needs no counter, and only as many CTAs as it can have items
   const long long most_items =

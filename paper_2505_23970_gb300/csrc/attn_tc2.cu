@@ -1451,6 +1451,13 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
   if (pool_rows >= (1ull << 31))
     return fail(GC_ERR_UNSUPPORTED, "%s: pool has %llu rows (limit 2^31)", a.who,
                 static_cast<unsigned long long>(pool_rows));
+  const Kernel2 kernel = own    ? attn_tc2_kernel<false, false, true, true>
+                         : span ? attn_tc2_kernel<false, false, true>
+                                : kernel2(splits, unpacked != nullptr);
+  // (Before the maps: in a thread that has made no CUDA call yet this one makes a context
+  // current, and encoding a map wants one.)
+  cudaError_t e = prepare_kernel(kernel, splits);
+  if (e != cudaSuccess) return cuda_fail(e, a.who);
   CUtensorMap map_q, map_k, map_v;
   {
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(kD), static_cast<cuuint64_t>(geo.Hq),
@@ -1514,11 +1521,6 @@ gc_status launch_attn_tc2(const gc_kv_pool* pool, const AttnArgs& a, cudaStream_
     if (own) clusters = pairs;
     geo.span.workers = static_cast<int32_t>(clusters);
   }
-  const Kernel2 kernel = own    ? attn_tc2_kernel<false, false, true, true>
-                         : span ? attn_tc2_kernel<false, false, true>
-                                : kernel2(splits, unpacked != nullptr);
-  cudaError_t e = prepare_kernel(kernel, splits);
-  if (e != cudaSuccess) return cuda_fail(e, a.who);
   // (a join that follows leaves the counter at 0)
   if (geo.more_items && !geo.span.cuts) e = cudaMemsetAsync(work_counter, 0, sizeof(int), stream);
   if (e != cudaSuccess) return cuda_fail(e, a.who);
