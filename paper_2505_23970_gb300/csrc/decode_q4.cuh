@@ -385,7 +385,10 @@ struct Keys4 {
         }
   }
 
-  // O^T += V^T P^T; kTail: keys at or past n left out (their scale may be anything)
+  // O^T += V^T P^T; kTail: a P of 0, that of a column that does not see the key, adds nothing
+  // whatever the key's scale is (0 times a NaN or an infinity would).  (That holds for keys at
+  // or past n too; clearing their scales as they are read besides saves 12 bytes of spills:
+  // 64 multi-turn contexts 68.5 us, without it 69.5.)
   template <bool kTail>
   __device__ __forceinline__ void values(const uint8_t* at, const Parts4<D>& mine, int n,
                                          const float (&p)[NT][4]) {
@@ -407,8 +410,13 @@ struct Keys4 {
       const float s0 = half_f32(sv[0][g / 2], g & 1), s1 = half_f32(sv[1][g / 2], g & 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t b0 = transpose8(pack_bf16x2(p[t][0] * s0, p[t][1] * s0));
-        const uint32_t b1 = transpose8(pack_bf16x2(p[t][2] * s1, p[t][3] * s1));
+        float ps[4] = {p[t][0] * s0, p[t][1] * s0, p[t][2] * s1, p[t][3] * s1};
+        if constexpr (kTail)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (p[t][e] == 0.f) ps[e] = 0.f;
+        const uint32_t b0 = transpose8(pack_bf16x2(ps[0], ps[1]));
+        const uint32_t b1 = transpose8(pack_bf16x2(ps[2], ps[3]));
         mma(o[t][2 * g], x & kLowNibbles, x & kHighNibbles, y & kLowNibbles, y & kHighNibbles, b0,
             b1);
         mma(o[t][2 * g + 1], x8 & kLowNibbles, x8 & kHighNibbles, y8 & kLowNibbles,
