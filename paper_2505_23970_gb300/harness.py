@@ -481,12 +481,16 @@ class FourBitContext:
     gc_prefix_prefill_attn_q4); ``step`` the same for one token of every request,
     or a few drafted ones (gc_kv_append_rope_q4, gc_paged_decode_attn_q4).
     ``advance`` says how many tokens each request keeps, on the stream of the last
-    call: drafted tokens that are not kept are overwritten by the next ones."""
+    call: drafted tokens that are not kept are overwritten by the next ones.
+    A step takes up to 16 / (Hq / Hkv) tokens of a request."""
 
     def __init__(self, Hq, Hkv, d, ps, B, max_tokens, tokens: int = 1, rot_dim=None,
                  base: float = 500000.0, L: int = 1, staging_pages: int = 1, seed: int = 0,
                  device: str = "cuda"):
         import torch
+        if tokens < 1 or tokens * (Hq // Hkv) > 16:
+            raise ValueError(f"steps of {tokens} tokens with {Hq // Hkv} q heads per kv head "
+                             "(1 to 16 rows)")
         self.Hq, self.Hkv, self.d, self.ps, self.B, self.L = Hq, Hkv, d, ps, B, L
         self.tokens, self.device = tokens, device
         self.width = -(-max_tokens // ps)
