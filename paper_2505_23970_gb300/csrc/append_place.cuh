@@ -16,7 +16,7 @@ struct RopeGeom {
   int32_t Hq, Hkv, ps_shift, num_pages, batch, max_blocks, layer, total_new;
   int32_t head_shift;    // units of a head, log2 (d / 16)
   int32_t rot_units;     // units of a head that are rotated (rot / 16)
-  int32_t heads;         // Hq + 2 Hkv
+  int32_t heads;         // Hq + 2 Hkv (16-bit pages)
   int32_t threads;       // of a token: ceil(heads / W) << head_shift
   int32_t interleaved, n_positions;
   int64_t q_stride, k_stride, v_stride;  // 16-byte words between tokens

@@ -229,7 +229,7 @@ Q4Geom q4_geom(const gc_kv_pool* pool, const Q4Cache& cache) {
 gc_status launch_append_q4(const gc_kv_pool* pool, const RopeArgs& a, const Q4Cache& cache,
                            cudaStream_t stream) {
   const auto& cfg = pool->cfg;
-  RopeGeom g;
+  RopeGeom g{};
   g.Hq = a.num_q_heads;
   g.Hkv = cfg.num_kv_heads;
   g.ps_shift = ilog2(cfg.page_size);
@@ -240,7 +240,6 @@ gc_status launch_append_q4(const gc_kv_pool* pool, const RopeArgs& a, const Q4Ca
   g.total_new = a.total_new_tokens;
   g.head_shift = ilog2(cfg.head_dim / 16);
   g.rot_units = a.rot_dim / 16;
-  g.heads = g.Hq;
   g.interleaved = a.interleaved ? 1 : 0;
   g.n_positions = a.n_positions;
   g.q_stride = a.q_stride / 8;

@@ -1479,8 +1479,6 @@ gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStr
 
 gc_status launch_attn_tc_unpacked(const gc_kv_pool* pool, const AttnArgs& a,
                                   const UnpackedPages& u, cudaStream_t stream) {
-  const gc_status st = check_item_bound(pool, a, pool->num_sms);
-  if (st != GC_OK) return st;
   return pool->cfg.head_dim == 128
              ? launch_attn_tc2(pool, a, stream, pool->work_counter, &u)
              : launch<64>(pool, a, stream, pool->work_counter, nullptr, &u);

@@ -278,7 +278,8 @@ gc_status launch_attn_tc_span(const gc_kv_pool* pool, const AttnArgs& a, cudaStr
 // GC_ERR_UNSUPPORTED before anything is launched when a call could pass it.
 gc_status check_item_bound(const gc_kv_pool* pool, const AttnArgs& a, int grid);
 
-// The same calls with image or 4-bit pages dequantised already (page numbers: see above).
+// The same calls with image or 4-bit pages dequantised already (page numbers: see above), by
+// a caller that has checked the item bound before it did so.
 gc_status launch_attn_tc_unpacked(const gc_kv_pool* pool, const AttnArgs& a,
                                   const UnpackedPages& unpacked, cudaStream_t stream);
 

@@ -8,7 +8,6 @@
 // Measured, 576 pages of 8 heads of 128 in 8 layers (302 MB in 16 bits, 85 in 4): packing 66
 // us (5.8 TB/s), reading back 62 (6.2); what a prefill of 8 x (8192 + 1024) tokens reads (one
 // layer, the same bytes) 61.
-#include "append_place.cuh"
 #include "q4_format.cuh"
 
 namespace gc {
