@@ -526,7 +526,9 @@ class FourBitContext:
 
     def load(self, image, requests, blocks, stream=None):
         """Pages [n][L][2][Hkv][ps][d] (device) into block blocks[i] of request
-        requests[i], as many at a time as the pool has pages."""
+        requests[i], as many at a time as the pool has pages (staging_pages).  Each time
+        their numbers are copied from the host, which waits for the stream: it cannot be
+        captured, and many pages want more than one at a time."""
         import torch
         to = self.table_host[np.asarray(requests), np.asarray(blocks)]
         for i in range(0, to.size, self.pool.cfg.num_pages):
@@ -550,10 +552,13 @@ class FourBitContext:
 
     def begin(self, new_lens):
         """The new tokens of every request for the prefill calls that follow.  (A captured
-        prefill has them too: it may be replayed until the next begin().)"""
+        prefill has them too: it may be replayed until the next begin().)  Waits for the
+        current stream."""
         import torch
         n = np.asarray(new_lens, np.int32)
         cu = np.concatenate([[0], np.cumsum(n)])
+        # (The copies from the host have waited for the current stream when q's memory is taken:
+        # nothing that used it before is still under way.)
         self._new = (_i32(n, self.device), _i32(cu, self.device), int(cu[-1]),
                      torch.empty((int(cu[-1]), self.Hq, self.d), dtype=torch.bfloat16,
                                  device=self.device))
