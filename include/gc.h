@@ -710,8 +710,8 @@ GC_API size_t gc_kv_q4_bytes(const gc_pool_config* cfg, int32_t n_q4_pages); /* 
  * gc_kv_append_rope, q4_table and n_q4_pages in the place of the pool's pages:
  * a token whose entry is not a 4-bit page (-1 included) has its q written and
  * its K and V skipped.  Two tokens may not have the same slot.
- * Errors: as gc_kv_append_rope; GC_ERR_INVALID_ARG also for n_q4_pages < 0 and
- * a misaligned or (with tokens to write) NULL q4_cache. */
+ * Errors: as gc_kv_append_rope; GC_ERR_INVALID_ARG also for n_q4_pages < 0 and,
+ * with tokens to write, a NULL or misaligned q4_cache. */
 GC_API gc_status gc_kv_append_rope_q4(gc_kv_pool* pool, const void* q, int64_t q_stride,
                                       void* q_out, const void* k_new, int64_t k_stride,
                                       const void* v_new, int64_t v_stride, void* q4_cache,
@@ -771,9 +771,11 @@ GC_API gc_status gc_kv_unpack_q4(gc_kv_pool* pool, const void* q4_cache, int32_t
  *                the same arguments, with the rules of gc_paged_decode_attn's.
  * A key that a row does not see is not used for it, whatever it holds.  Powers of
  * two inside the kernel leave room for |q| up to 2^100 and, in 16-bit pages, |K| up
- * to 2^60; beyond that a row may become NaN.  Calls on one pool must not overlap on
- * the GPU with each other or with the other attention calls.  The same call gives
- * the same bits again; the order of its sums depends on the lengths in the call.
+ * to 2^60; beyond that a row may become NaN.  K of a 16-bit page is taken to the
+ * nearest multiple of 2^-73 (exact from 2^-66 on), and results below 2^-80 may lose
+ * bits.  Calls on one pool must not overlap on the GPU with each other or with the
+ * other attention calls.  The same call gives the same bits again; the order of its
+ * sums depends on the lengths in the call.
  * Errors: as gc_paged_decode_attn; GC_ERR_INVALID_ARG also for n_q4_pages < 0,
  * tokens < 1, a NULL q4_table (or q4_cache with n_q4_pages > 0), a misaligned
  * q4_cache; GC_ERR_UNSUPPORTED for tokens * Hq/Hkv > 16, softmax_scale > 8192,
