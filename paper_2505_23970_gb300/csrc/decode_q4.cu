@@ -20,13 +20,19 @@
 //
 // Measured (one call, back to back), 64/8 heads of 128 unless stated: 8 contexts of 9216
 // keys (85 MB) 27 us; 64 multi-turn contexts, the newest page of each in 16 bits (307 MB) 68
-// us; 8 of 65536 (604 MB) 116 us; 32 documents of up to 65536 (1.23 GB) 225 us, 5.5 TB/s, 0.81
-// of the copy rate; 4 tokens each of 16 contexts of up to 8192, 32/8 heads (84 MB) 38 us; 8 of
-// 65536 with heads of 64 68 us, 4.4 TB/s.  In the longer ones the loop runs at 60 % of the
-// issue slots, the ALU pipe (masks, shifts) at 52 %, the tensor pipe at 37 %; of the shorter
-// ones 9 us are the start (look-ups, first loads: 4) and the joins (5).  With 16
-// columns a group takes 459 instead of 299 instructions and twice the products, by 8 warps an
-// SM (12, with Q in shared memory to make room, took 41 us for the 38).
+// us; 8 of 65536 (604 MB) 115 us; 32 documents of up to 65536 (1.23 GB) 219-223 us, 5.5-5.6
+// TB/s, 0.81-0.83 of the copy rate; 4 tokens each of 16 contexts of up to 8192, 32/8 heads
+// (84 MB) 39 us; 8 of 65536 with heads of 64 (302 MB) 69 us, 4.4 TB/s.
+// What holds it: copies of the kernel without its products | without its copies | whole, us:
+// 8 of 65536 111 | 98 | 115, so the copies; the same with heads of 64 58 | 60 | 69 and 8 of
+// 9216 17 | 22 | 26, neither alone; 16 columns over 94 MB 28 | 40 | 43, so the products.  No
+// unit is full: in the first of these issue slots 59 %, ALU pipe (masks, shifts) 52 %, tensor
+// pipe 38 %, DRAM 64 %.  Of the shorter calls 9 us are the start (look-ups, first loads: 4)
+// and the joins (5).  With 16 columns a group takes 459 instead of 299 instructions and twice
+// the products, by 8 warps an SM (12, with Q in shared memory to make room, took 41 us for 38).
+// Spills: none with heads of 64 and 8 columns; with heads of 128 a few words outside the loop
+// (7,000 of 78 million instructions); with heads of 64 and 16 columns in it, some 13 a pair of
+// groups, 1.6 % of the instructions.
 #include "decode_q4.cuh"
 
 namespace gc {
@@ -41,7 +47,8 @@ constexpr int kMinUnits = 2;  // of a warp's share, at least
 
 // Warps of an SM, in one CTA, and stages of shared memory of a variant.  (Two CTAs of half
 // the warps do not share the SM evenly: the one that came first is done with its equal
-// share 15 % earlier, 8 contexts of 65536 keys 124 us, now 119.)
+// share 15 % earlier, 8 contexts of 65536 keys 124 us for 119, both before the joins were
+// what they are.)
 template <int D, int NT>
 struct Shape4 {
   static constexpr int kWarps = D * NT == 256 ? 8 : 16;

@@ -19,8 +19,9 @@
 // is 2^90 2^(x - m), and both leave again exactly.
 //
 // Keys and scales come through shared memory, copied asynchronously a pair of groups ahead
-// (probe: random pieces of 1152 bytes 6.9 TB/s so, 5.7 by loads to registers, of which there
-// are too few for a group more).  Codes as e4m3 with m16n8k32 products would save half of K's
+// (a probe of nothing but copies: random pieces of 1152 bytes 6.9 TB/s so, 5.7 by loads to
+// registers, of which there are too few for a group more; this kernel without its products
+// copies 5.4 TB/s, and why not more is not known).  Codes as e4m3 with m16n8k32 products would save half of K's
 // masks, but that product is not native here (it is carried out as conversions and f16
 // products): 32 documents 366 us instead of 224.
 #pragma once
